@@ -64,7 +64,9 @@ typedef enum {
   FW_WARN_NONFINITE = 65    /* NaN/Inf seen in X, G or the state               */
 } fw_status;
 
-typedef enum { FW_F32 = 0, FW_BF16 = 1 } fw_dtype; /* element type of X */
+/* Element types.  The X of a layer is fp32 or bf16; e4m3 (8-bit floats, with a
+ * scale beside them) is a type of the norm's output and of the gated block. */
+typedef enum { FW_F32 = 0, FW_BF16 = 1, FW_E4M3 = 2 } fw_dtype;
 
 /* Engine of the two dense contractions (X^T X and G Q) and of the re-sync
  * products.  FP32: FFMA, matches an fp64 reference to ~1e-6.  TF32 / BF16:
@@ -292,6 +294,49 @@ fw_status fw_group_grad_transform_step(fw_layer* const* L, int32_t n, const floa
 #define FW_STATIC_MAX_M 256
 fw_status fw_cov_block_static(const float* X, int64_t rows, int64_t ldx, int32_t M, float* mu_out,
                               float* phix_out, void* cuda_stream);
+
+/* ---- Operators around the layers: what makes a layer's input and its gradient.
+ * They keep no state.  rows >= 1; ld* are leading dimensions in elements, at most
+ * 2^30.  Any alignment to whole elements is taken; where every matrix starts on 16
+ * bytes and its rows are a multiple of 16 bytes apart, 16 bytes move at a time.
+ * Sums are fp32 in a fixed order: the same call gives the same bits. ---- */
+
+/* Residual addition and root-mean-square norm, a transform of layer inputs like
+ * fw_whiten_forward / _backward that needs no statistics across rows:
+ *   s = x + res, rounded to `dtype` (s = x without res)
+ *   rstd = 1 / sqrt(mean(s^2) + eps),  y = s rstd w
+ * y is of `dtype`, or e4m3 with a scale for each row: y_scale = max|y| / 448 (at
+ * least 2^-120; 1 for a row of zeros), y held as e4m3(y / y_scale).
+ * x, res, sum: rows x M of `dtype`; w: M fp32; rstd, y_scale: rows fp32.
+ *   res      NULL: no addition          sum   NULL: s is not kept; needs res
+ *   y_scale  only, and always, with e4m3  rstd  NULL: not kept
+ * sum and y may be x or res themselves (same address, type and ld); any other overlap
+ * of outputs with inputs or with each other is FW_ERR_INVALID_ARG.
+ * 1 <= M <= 16384.  A NaN or infinity in a row makes that row's y, rstd and
+ * scale what the formulas give, and no other's. */
+typedef struct {
+  int32_t M;         /* features                                                 */
+  int32_t dtype;     /* fw_dtype of x, res, sum: FW_F32 or FW_BF16                */
+  int32_t y_dtype;   /* dtype, or FW_E4M3 (forward)                              */
+  float eps;         /* > 0                                                      */
+} fw_norm_desc;
+/* bf16 in and out, eps 1e-6 */
+void fw_norm_desc_default(fw_norm_desc* d, int32_t M);
+fw_status fw_rmsnorm_forward(const fw_norm_desc* d, int64_t rows, const void* x, int64_t ldx, const void* res,
+                             int64_t ldr, const float* w, void* sum, int64_t lds, void* y, int64_t ldy,
+                             float* y_scale, float* rstd, void* cuda_stream);
+/* From dy (the gradient of y), s and rstd of the forward call:
+ *   u = dy w,  n = s rstd,  dx = rstd (u - n mean(u n)) + dsum,  dw = sum over rows of dy n
+ * dx is the gradient of x and of res alike; dsum (NULL: none) is the gradient that
+ * reaches s by itself.  dy, s, dsum, dx: rows x M of `dtype` (y_dtype is not looked
+ * at: the gradient passes an e4m3 rounding unchanged).  dw: M fp32, overwritten;
+ * NULL: not wanted, and scratch may be NULL.  scratch: caller-owned, 256-byte aligned, at
+ * least fw_rmsnorm_scratch_bytes(d) bytes, free again when the call's work is done.
+ * dx may be dy, s or dsum itself. */
+size_t fw_rmsnorm_scratch_bytes(const fw_norm_desc* d);
+fw_status fw_rmsnorm_backward(const fw_norm_desc* d, int64_t rows, const void* dy, int64_t lddy, const void* s,
+                              int64_t lds, const void* dsum, int64_t ldds, const float* w, const float* rstd, void* dx,
+                              int64_t lddx, float* dw, void* scratch, size_t scratch_bytes, void* cuda_stream);
 
 /* State access (checkpointing, injecting a covariance, parity checks).
  * Matrices are M x M fp32 row-major, vectors M fp32, FW_F_LAMBDA_BAR one fp32.

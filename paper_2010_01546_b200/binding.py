@@ -18,7 +18,7 @@ FW_OK = 0
 FW_ERR_INVALID_ARG, FW_ERR_SHAPE, FW_ERR_STATE, FW_ERR_WORKSPACE = 1, 2, 3, 4
 FW_ERR_CUDA, FW_ERR_TIMEOUT, FW_ERR_UNSUPPORTED = 5, 6, 7
 FW_WARN_NO_SUBSPACE, FW_WARN_NONFINITE = 64, 65
-FW_F32, FW_BF16 = 0, 1
+FW_F32, FW_BF16, FW_E4M3 = 0, 1, 2
 FW_PREC_FP32, FW_PREC_TF32, FW_PREC_BF16 = 0, 1, 2
 FW_INIT_ALIGN, FW_INIT_MAXCOL = 0, 1
 FW_F_MU, FW_F_PHIX, FW_F_PHI_DIAG, FW_F_LAMBDA_BAR, FW_F_T, FW_F_Q, FW_F_QS, FW_F_PHIY, FW_F_ALIGN_W = range(9)
@@ -35,6 +35,7 @@ EXPORTS = [
     "fw_nhwc_scratch_bytes", "fw_cov_update_nhwc", "fw_group_cov_update_nhwc",
     "fw_whiten_forward", "fw_whiten_backward", "fw_step_momentum", "fw_whiteness",
     "fw_evd_scratch_bytes", "fw_evd_whiten", "fw_group_evd_whiten", "fw_spectrum",
+    "fw_norm_desc_default", "fw_rmsnorm_scratch_bytes", "fw_rmsnorm_forward", "fw_rmsnorm_backward",
 ]
 FW_STATIC_MAX_M = 256
 FW_PROF_NAMES = ["pilot", "gram", "moments", "resync", "recur_mv", "recur_upd", "smooth", "gq", "misc", "recur_chip"]
@@ -51,6 +52,10 @@ class fw_layer_desc(C.Structure):
     _fields_ = [("M", C.c_int32), ("N", C.c_int32), ("x_dtype", C.c_int32), ("prec", C.c_int32),
                 ("init", C.c_int32), ("alpha", C.c_float), ("beta", C.c_float), ("gamma", C.c_float),
                 ("delta", C.c_float), ("eps", C.c_float), ("c_rel", C.c_float), ("c_abs", C.c_float)]
+
+
+class fw_norm_desc(C.Structure):
+    _fields_ = [("M", C.c_int32), ("dtype", C.c_int32), ("y_dtype", C.c_int32), ("eps", C.c_float)]
 
 
 _LIB = None
@@ -106,6 +111,12 @@ def _lib():
     lib.fw_cov_block_static.argtypes = [vp, i64, i64, i32, vp, vp, vp]; lib.fw_cov_block_static.restype = i32
     lib.fw_debug_wait_probe.argtypes = [vp, C.c_uint32]; lib.fw_debug_wait_probe.restype = i32
     lib.fw_recursion_on_chip.argtypes = [P(fw_layer_desc)]; lib.fw_recursion_on_chip.restype = i32
+    lib.fw_norm_desc_default.argtypes = [P(fw_norm_desc), i32]; lib.fw_norm_desc_default.restype = None
+    lib.fw_rmsnorm_scratch_bytes.argtypes = [P(fw_norm_desc)]; lib.fw_rmsnorm_scratch_bytes.restype = sz
+    lib.fw_rmsnorm_forward.argtypes = [P(fw_norm_desc), i64, vp, i64, vp, i64, vp, vp, i64, vp, i64, vp, vp, vp]
+    lib.fw_rmsnorm_forward.restype = i32
+    lib.fw_rmsnorm_backward.argtypes = [P(fw_norm_desc), i64, vp, i64, vp, i64, vp, i64, vp, vp, vp, i64, vp, vp, sz, vp]
+    lib.fw_rmsnorm_backward.restype = i32
     _LIB = lib
     return lib
 
@@ -306,6 +317,96 @@ def fw_profile_end() -> dict:
 
 def fw_launch_count() -> int:
     return int(_lib().fw_launch_count())
+
+
+# ---- operators around the layers: tensors in, with their sizes, strides and types looked at ----
+def _torch_types():
+    import torch
+    return {torch.float32: FW_F32, torch.bfloat16: FW_BF16, torch.float8_e4m3fn: FW_E4M3}
+
+
+_TYPES = None
+
+
+def _matrix(t, rows, cols, dtype, name):
+    """(address, leading dimension) of a rows x cols CUDA tensor of one of this library's types, rows contiguous in themselves;
+    (None, 0) for None.  The device that the library launches on is the current one, so the tensor has to be there."""
+    global _TYPES
+    if t is None:
+        return None, 0
+    if _TYPES is None:
+        _TYPES = _torch_types()
+    if _TYPES.get(t.dtype) != dtype:
+        raise TypeError(f"{name}: {t.dtype} is not the type that its description says")
+    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols:
+        raise ValueError(f"{name}: expected {rows} x {cols}, got {tuple(t.shape)}")
+    ld = t.stride(0) if rows > 1 else max(t.stride(0), cols)
+    if cols > 1 and t.stride(1) != 1:
+        raise ValueError(f"{name}: the elements of a row have to be next to each other")
+    if rows > 1 and ld < cols:
+        raise ValueError(f"{name}: rows overlap")
+    _on_device(t, name)
+    return t.data_ptr(), ld
+
+
+def _vector(t, n, name, dtype=FW_F32):
+    """Address of a contiguous CUDA vector of n elements; None for None."""
+    global _TYPES
+    if t is None:
+        return None
+    if _TYPES is None:
+        _TYPES = _torch_types()
+    if _TYPES.get(t.dtype) != dtype:
+        raise TypeError(f"{name}: {t.dtype} is not the type that is expected")
+    if t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"{name}: expected {n} contiguous elements, got {tuple(t.shape)}")
+    _on_device(t, name)
+    return t.data_ptr()
+
+
+def _on_device(t, name):
+    import torch
+    if not t.is_cuda:
+        raise ValueError(f"{name}: not a CUDA tensor")
+    if t.get_device() != torch.cuda.current_device():
+        raise ValueError(f"{name}: on cuda:{t.get_device()}, but the current device is cuda:{torch.cuda.current_device()}")
+
+
+def fw_norm_desc_default(M: int, **overrides) -> fw_norm_desc:
+    d = fw_norm_desc()
+    _lib().fw_norm_desc_default(C.byref(d), M)
+    for k, v in overrides.items():
+        setattr(d, k, v)
+    return d
+
+
+def fw_rmsnorm_scratch_bytes(desc: fw_norm_desc) -> int:
+    return int(_lib().fw_rmsnorm_scratch_bytes(C.byref(desc)))
+
+
+def fw_rmsnorm_forward(desc: fw_norm_desc, x, w, y, res=None, sum_out=None, y_scale=None, rstd=None, stream: int = 0) -> None:
+    rows, M, t = x.shape[0], desc.M, desc.dtype
+    px, ldx = _matrix(x, rows, M, t, "x")
+    pr, ldr = _matrix(res, rows, M, t, "res")
+    ps, lds = _matrix(sum_out, rows, M, t, "sum_out")
+    py, ldy = _matrix(y, rows, M, desc.y_dtype, "y")
+    _check(_lib().fw_rmsnorm_forward(C.byref(desc), rows, px, ldx, pr, ldr, _vector(w, M, "w"), ps, lds, py, ldy,
+                                     _vector(y_scale, rows, "y_scale"), _vector(rstd, rows, "rstd"), stream), "fw_rmsnorm_forward")
+
+
+def fw_rmsnorm_backward(desc: fw_norm_desc, dy, s, w, rstd, dx, dw=None, dsum=None, scratch=None, stream: int = 0) -> None:
+    rows, M, t = dy.shape[0], desc.M, desc.dtype
+    pdy, lddy = _matrix(dy, rows, M, t, "dy")
+    ps, lds = _matrix(s, rows, M, t, "s")
+    pds, ldds = _matrix(dsum, rows, M, t, "dsum")
+    pdx, lddx = _matrix(dx, rows, M, t, "dx")
+    n = 0
+    if scratch is not None:
+        _on_device(scratch, "scratch")
+        n = scratch.numel() * scratch.element_size()
+    _check(_lib().fw_rmsnorm_backward(C.byref(desc), rows, pdy, lddy, ps, lds, pds, ldds, _vector(w, M, "w"),
+                                      _vector(rstd, rows, "rstd"), pdx, lddx, _vector(dw, M, "dw"), _ptr(scratch), n, stream),
+           "fw_rmsnorm_backward")
 
 
 # ---- convenience: a layer that owns its workspace tensor -------------------

@@ -1,0 +1,146 @@
+// Rows of a matrix as vectors of VEC elements: loads into and stores from fp32 registers, and sums over the threads that
+// share a row.  Used by the operators that pass over rows once (norm, distillation loss, gates of a gated block).
+#ifndef FW_ROWS_CUH_
+#define FW_ROWS_CUH_
+
+#include <cuda_bf16.h>
+#include <cuda_fp8.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+namespace fw {
+namespace rows {
+
+// Two bf16 of a 32-bit word, the lower address first.
+__device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {          // nearest even, a NaN stays one
+  const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+// Four fp32 to e4m3 (nearest even, beyond 448 to 448, a NaN stays one), the lowest address in the lowest byte.
+__device__ __forceinline__ uint32_t pack_e4m3(float a, float b, float c, float d) {
+  const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3);
+  const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(c, d), __NV_SATFINITE, __NV_E4M3);
+  return lo | (hi << 16);
+}
+
+__device__ __forceinline__ float to_f(float x) { return x; }
+__device__ __forceinline__ float to_f(__nv_bfloat16 x) { return __bfloat162float(x); }
+__device__ __forceinline__ void put(float* p, float v) { *p = v; }
+__device__ __forceinline__ void put(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
+__device__ __forceinline__ void put(__nv_fp8_storage_t* p, float v) { *p = __nv_cvt_float_to_fp8(v, __NV_SATFINITE, __NV_E4M3); }
+
+// n <= VEC elements from p on; those past n read as `none`.  With VEC > 1 a whole vector is aligned to its own size.
+template <int VEC>
+__device__ __forceinline__ void load(const float* p, int n, float none, float (&v)[VEC]) {
+  if (VEC == 4 && n >= 4) {
+    const float4 q = *reinterpret_cast<const float4*>(p);
+    v[0] = q.x; v[1 % VEC] = q.y; v[2 % VEC] = q.z; v[3 % VEC] = q.w;
+  } else if (VEC == 8 && n >= 8) {
+    const float4 q = reinterpret_cast<const float4*>(p)[0], r = reinterpret_cast<const float4*>(p)[1];
+    v[0] = q.x; v[1 % VEC] = q.y; v[2 % VEC] = q.z; v[3 % VEC] = q.w;
+    v[4 % VEC] = r.x; v[5 % VEC] = r.y; v[6 % VEC] = r.z; v[7 % VEC] = r.w;
+  } else {
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) v[e] = e < n ? p[e] : none;
+  }
+}
+template <int VEC>
+__device__ __forceinline__ void load(const __nv_bfloat16* p, int n, float none, float (&v)[VEC]) {
+  if (VEC == 8 && n >= 8) {
+    const uint4 q = *reinterpret_cast<const uint4*>(p);
+    v[0] = bf16_lo(q.x); v[1 % VEC] = bf16_hi(q.x); v[2 % VEC] = bf16_lo(q.y); v[3 % VEC] = bf16_hi(q.y);
+    v[4 % VEC] = bf16_lo(q.z); v[5 % VEC] = bf16_hi(q.z); v[6 % VEC] = bf16_lo(q.w); v[7 % VEC] = bf16_hi(q.w);
+  } else {
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) v[e] = e < n ? to_f(p[e]) : none;
+  }
+}
+template <int VEC>
+__device__ __forceinline__ void store(float* p, int n, const float (&v)[VEC]) {
+  if (VEC == 4 && n >= 4) {
+    *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1 % VEC], v[2 % VEC], v[3 % VEC]);
+  } else {
+#pragma unroll
+    for (int e = 0; e < VEC; ++e)
+      if (e < n) p[e] = v[e];
+  }
+}
+template <int VEC>
+__device__ __forceinline__ void store(__nv_bfloat16* p, int n, const float (&v)[VEC]) {
+  if (VEC == 8 && n >= 8) {
+    *reinterpret_cast<uint4*>(p) = make_uint4(pack_bf16(v[0], v[1 % VEC]), pack_bf16(v[2 % VEC], v[3 % VEC]),
+                                              pack_bf16(v[4 % VEC], v[5 % VEC]), pack_bf16(v[6 % VEC], v[7 % VEC]));
+  } else {
+#pragma unroll
+    for (int e = 0; e < VEC; ++e)
+      if (e < n) put(p + e, v[e]);
+  }
+}
+template <int VEC>
+__device__ __forceinline__ void store(__nv_fp8_storage_t* p, int n, const float (&v)[VEC]) {
+  if (VEC == 8 && n >= 8) {
+    *reinterpret_cast<uint2*>(p) = make_uint2(pack_e4m3(v[0], v[1 % VEC], v[2 % VEC], v[3 % VEC]),
+                                              pack_e4m3(v[4 % VEC], v[5 % VEC], v[6 % VEC], v[7 % VEC]));
+  } else if (VEC == 4 && n >= 4) {
+    *reinterpret_cast<uint32_t*>(p) = pack_e4m3(v[0], v[1 % VEC], v[2 % VEC], v[3 % VEC]);
+  } else {
+#pragma unroll
+    for (int e = 0; e < VEC; ++e)
+      if (e < n) put(p + e, v[e]);
+  }
+}
+
+// A value as its own type holds it.
+__device__ __forceinline__ float held(float v, const float*) { return v; }
+__device__ __forceinline__ float held(float v, const __nv_bfloat16*) { return __bfloat162float(__float2bfloat16_rn(v)); }
+
+// 2^x, relative error about 2^-22; 0 below 2^-126, infinity above the range, NaN for NaN.
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+// The larger of two non-negative numbers, a NaN if one of them is: as bit patterns NaN lies above infinity.
+__device__ __forceinline__ float max_keep_nan(float a, float b) {
+  return __uint_as_float(max(__float_as_uint(a), __float_as_uint(b)));
+}
+
+struct Sum { __device__ static float of(float a, float b) { return a + b; } };
+struct MaxAbs { __device__ static float of(float a, float b) { return max_keep_nan(a, b); } };
+
+// One value for each group of `width` threads (a power of two, 32 or more, within the CTA), the same bits in every thread: lanes
+// in pairs, then warps in order.  Every thread of the CTA comes here; buf: a float for each warp of the CTA, not used
+// again before another barrier of the CTA.
+template <class Op>
+__device__ __forceinline__ float over_group(float v, int width, float* buf) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v = Op::of(v, __shfl_xor_sync(0xffffffffu, v, o));
+  if (width == 32) return v;
+  const int w = threadIdx.x >> 5, per = width >> 5;
+  if ((threadIdx.x & 31) == 0) buf[w] = v;
+  __syncthreads();
+  const int first = w / per * per;
+  float r = buf[first];
+  for (int k = 1; k < per; ++k) r = Op::of(r, buf[first + k]);
+  return r;
+}
+
+}  // namespace rows
+
+// ---- host: argument checks shared by these operators ----
+inline bool aligned_to(const void* p, size_t bytes) { return (reinterpret_cast<uintptr_t>(p) % bytes) == 0; }
+// bytes from the first to the last element of a row-major matrix
+inline uint64_t matrix_span(int64_t rows, int64_t cols, int64_t ld, int elem) {
+  return ((uint64_t)(rows - 1) * (uint64_t)ld + (uint64_t)cols) * (uint64_t)elem;
+}
+inline bool overlap(const void* a, uint64_t na, const void* b, uint64_t nb) {
+  if (!a || !b) return false;
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return x < y + nb && y < x + na;
+}
+
+}  // namespace fw
+#endif
