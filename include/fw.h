@@ -338,6 +338,44 @@ fw_status fw_rmsnorm_backward(const fw_norm_desc* d, int64_t rows, const void* d
                               int64_t lds, const void* dsum, int64_t ldds, const float* w, const float* rstd, void* dx,
                               int64_t lddx, float* dw, void* scratch, size_t scratch_bytes, void* cuda_stream);
 
+/* Distillation loss against a teacher's top logits, and its gradient (what the weight
+ * gradient of a network's last layer is formed from).  With q = softmax(Z / tau) of a
+ * row and the K classes i_k that the teacher names, with its logits t_k:
+ *   t_lse NULL: p = softmax(t / tau) over the named classes, p_t = 0
+ *   t_lse     : p_k = exp(t_k / tau - t_lse), t_lse = the teacher's log sum exp(t / tau) over
+ *               all V classes; p_t = max(0, 1 - sum p) for all classes it does not name
+ *   loss = weight [sum_k p_k (log p_k - log q_ik) + p_t (log p_t - log q_t)]
+ * where q_t is the student's mass on the classes that are not named, and dZ = d loss / dZ.
+ * (Where a factor tau^2 is wanted it goes into weight, like the mean over rows.)
+ *   Z, dZ   rows x V, z_dtype; dZ may be Z (same address and ld), no other overlap
+ *   T, I    rows x K, dense: the teacher's logits (t_dtype), their classes (index_bits 32 or 64
+ *           bits, signed).  A class outside [0, V) marks an absent entry; a class named twice counts
+ *           once, with its first logit.
+ *   weight  rows; NULL: 1.  A row of weight 0 is not read: loss, stat and dZ are 0.
+ *   loss    rows;   stat  rows x 2: log sum exp(Z / tau) over all classes and over those not
+ *           named (-inf for none); NULL in the forward call: not kept
+ * forward: dZ NULL gives the loss alone; with dZ the gradient too, from the same pass over Z.
+ * backward: the gradient from the forward call's stat (weight may be another, but a row that the
+ * forward call left out has no stat to be read).
+ * Logits of -inf have no mass (a mask): gradient 0, infinite loss where p_k > 0.  A row in which no
+ * class has mass gives loss and gradient 0, and so does a row whose entries are all absent (t_lse
+ * NULL).  A NaN in a row, or +inf, makes that row's loss and gradient NaN.
+ * 1 <= K <= 1024, K <= V <= 2^20, rows < 2^28. */
+typedef struct {
+  int32_t V, K;
+  int32_t z_dtype, t_dtype;   /* FW_F32 or FW_BF16                               */
+  int32_t index_bits;         /* 32 or 64                                        */
+  float tau;                  /* 1e-6 to 1e6                                     */
+} fw_distill_desc;
+/* bf16 logits, 32-bit classes, tau 1 */
+void fw_distill_desc_default(fw_distill_desc* d, int32_t V, int32_t K);
+fw_status fw_distill_forward(const fw_distill_desc* d, const void* Z, int64_t rows, int64_t ldz, const void* T,
+                             const void* I, const float* t_lse, const float* weight, float* loss, float* stat,
+                             void* dZ, int64_t lddz, void* cuda_stream);
+fw_status fw_distill_backward(const fw_distill_desc* d, const void* Z, int64_t rows, int64_t ldz, const void* T,
+                              const void* I, const float* t_lse, const float* weight, const float* stat, void* dZ,
+                              int64_t lddz, void* cuda_stream);
+
 /* State access (checkpointing, injecting a covariance, parity checks).
  * Matrices are M x M fp32 row-major, vectors M fp32, FW_F_LAMBDA_BAR one fp32.
  * Copies run on the layer's stream.  Setting FW_F_PHIX marks Phi_y stale, sets

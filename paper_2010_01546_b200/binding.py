@@ -36,6 +36,7 @@ EXPORTS = [
     "fw_whiten_forward", "fw_whiten_backward", "fw_step_momentum", "fw_whiteness",
     "fw_evd_scratch_bytes", "fw_evd_whiten", "fw_group_evd_whiten", "fw_spectrum",
     "fw_norm_desc_default", "fw_rmsnorm_scratch_bytes", "fw_rmsnorm_forward", "fw_rmsnorm_backward",
+    "fw_distill_desc_default", "fw_distill_forward", "fw_distill_backward",
 ]
 FW_STATIC_MAX_M = 256
 FW_PROF_NAMES = ["pilot", "gram", "moments", "resync", "recur_mv", "recur_upd", "smooth", "gq", "misc", "recur_chip"]
@@ -56,6 +57,11 @@ class fw_layer_desc(C.Structure):
 
 class fw_norm_desc(C.Structure):
     _fields_ = [("M", C.c_int32), ("dtype", C.c_int32), ("y_dtype", C.c_int32), ("eps", C.c_float)]
+
+
+class fw_distill_desc(C.Structure):
+    _fields_ = [("V", C.c_int32), ("K", C.c_int32), ("z_dtype", C.c_int32), ("t_dtype", C.c_int32),
+                ("index_bits", C.c_int32), ("tau", C.c_float)]
 
 
 _LIB = None
@@ -117,6 +123,11 @@ def _lib():
     lib.fw_rmsnorm_forward.restype = i32
     lib.fw_rmsnorm_backward.argtypes = [P(fw_norm_desc), i64, vp, i64, vp, i64, vp, i64, vp, vp, vp, i64, vp, vp, sz, vp]
     lib.fw_rmsnorm_backward.restype = i32
+    lib.fw_distill_desc_default.argtypes = [P(fw_distill_desc), i32, i32]; lib.fw_distill_desc_default.restype = None
+    lib.fw_distill_forward.argtypes = [P(fw_distill_desc), vp, i64, i64, vp, vp, vp, vp, vp, vp, vp, i64, vp]
+    lib.fw_distill_forward.restype = i32
+    lib.fw_distill_backward.argtypes = [P(fw_distill_desc), vp, i64, i64, vp, vp, vp, vp, vp, vp, i64, vp]
+    lib.fw_distill_backward.restype = i32
     _LIB = lib
     return lib
 
@@ -322,7 +333,8 @@ def fw_launch_count() -> int:
 # ---- operators around the layers: tensors in, with their sizes, strides and types looked at ----
 def _torch_types():
     import torch
-    return {torch.float32: FW_F32, torch.bfloat16: FW_BF16, torch.float8_e4m3fn: FW_E4M3}
+    return {torch.float32: FW_F32, torch.bfloat16: FW_BF16, torch.float8_e4m3fn: FW_E4M3, torch.int32: "int32",
+            torch.int64: "int64"}
 
 
 _TYPES = None
@@ -407,6 +419,34 @@ def fw_rmsnorm_backward(desc: fw_norm_desc, dy, s, w, rstd, dx, dw=None, dsum=No
     _check(_lib().fw_rmsnorm_backward(C.byref(desc), rows, pdy, lddy, ps, lds, pds, ldds, _vector(w, M, "w"),
                                       _vector(rstd, rows, "rstd"), pdx, lddx, _vector(dw, M, "dw"), _ptr(scratch), n, stream),
            "fw_rmsnorm_backward")
+
+
+def fw_distill_desc_default(V: int, K: int, **overrides) -> fw_distill_desc:
+    d = fw_distill_desc()
+    _lib().fw_distill_desc_default(C.byref(d), V, K)
+    for k, v in overrides.items():
+        setattr(d, k, v)
+    return d
+
+
+def fw_distill_forward(desc: fw_distill_desc, Z, T, I, loss, stat=None, t_lse=None, weight=None, dZ=None, stream: int = 0) -> None:
+    rows, V, K = Z.shape[0], desc.V, desc.K
+    pz, ldz = _matrix(Z, rows, V, desc.z_dtype, "Z")
+    pd, lddz = _matrix(dZ, rows, V, desc.z_dtype, "dZ")
+    _check(_lib().fw_distill_forward(C.byref(desc), pz, rows, ldz, _vector(T, rows * K, "T", desc.t_dtype),
+                                     _vector(I, rows * K, "I", "int64" if desc.index_bits == 64 else "int32"),
+                                     _vector(t_lse, rows, "t_lse"), _vector(weight, rows, "weight"), _vector(loss, rows, "loss"),
+                                     _vector(stat, 2 * rows, "stat"), pd, lddz, stream), "fw_distill_forward")
+
+
+def fw_distill_backward(desc: fw_distill_desc, Z, T, I, stat, dZ, t_lse=None, weight=None, stream: int = 0) -> None:
+    rows, V, K = Z.shape[0], desc.V, desc.K
+    pz, ldz = _matrix(Z, rows, V, desc.z_dtype, "Z")
+    pd, lddz = _matrix(dZ, rows, V, desc.z_dtype, "dZ")
+    _check(_lib().fw_distill_backward(C.byref(desc), pz, rows, ldz, _vector(T, rows * K, "T", desc.t_dtype),
+                                      _vector(I, rows * K, "I", "int64" if desc.index_bits == 64 else "int32"),
+                                      _vector(t_lse, rows, "t_lse"), _vector(weight, rows, "weight"),
+                                      _vector(stat, 2 * rows, "stat"), pd, lddz, stream), "fw_distill_backward")
 
 
 # ---- convenience: a layer that owns its workspace tensor -------------------

@@ -1,0 +1,263 @@
+"""Distillation loss and gradient against the definition in 64 bits.
+
+Error bounds (u = 2^-24).  An exponential exp(-a) is computed with 2^-22 and 4 u a ln 2 of its argument; sums of exponentials
+have at most 32 x 8 + 5 + 16 + 8 steps for 2^20 classes (a thread's trips, lanes, warps, CTAs), 61 u up to 131072 of them: a
+probability is within E(a) = 2^-17 (1 + a / 8) of itself, 2^-15 (1 + a / 8) above that size.  Logarithms add 4 u (1 + |log|).
+"""
+import pytest
+import torch
+
+from optest_util import F64, HALF, captured, gen, matrix, put, surround_kept
+
+pytestmark = pytest.mark.gpu
+
+KINDS = {"f32": torch.float32, "bf16": torch.bfloat16}
+SIZES = [(3, 1, 1), (1, 2, 2), (5, 100, 10), (37, 1000, 10), (7, 1025, 33), (4, 2048, 1024), (3, 8191, 64), (2, 50021, 33),
+         (2, 131072, 64), (2, 131101, 100), (1, 300001, 7), (1, 1 << 20, 130)]
+
+
+@pytest.fixture(scope="module")
+def B():
+    from paper_2010_01546_b200 import binding, build
+    build.build_library()
+    return binding
+
+
+def desc(B, V, K, kind, t=torch.float32, bits=32, tau=1.0):
+    return B.fw_distill_desc_default(V, K, z_dtype=B.FW_F32 if kind == "f32" else B.FW_BF16,
+                                     t_dtype=B.FW_F32 if t == torch.float32 else B.FW_BF16, index_bits=bits, tau=tau)
+
+
+def inputs(rows, V, K, kind, seed, t=torch.float32, tau=1.0, **kw):
+    """Student's logits, the teacher's K largest and their classes, and the teacher's normaliser."""
+    g = gen(seed)
+    z = torch.randn(rows, V, generator=g, device="cuda") * 2
+    teacher = 0.7 * z + torch.randn(rows, V, generator=g, device="cuda")
+    top, at = teacher.topk(K, dim=1)
+    return put(z, KINDS[kind], **kw), top.to(t), at.to(torch.int32), torch.logsumexp(teacher.to(F64) / tau, 1).float()
+
+
+def column(v):
+    return v[:, None] if torch.is_tensor(v) else v
+
+
+def reference(z, T, I, tau, t_lse=None, weight=None):
+    """loss, stat, dZ, and bounds of the errors of loss and dZ."""
+    rows, V = z.shape
+    K = T.shape[1]
+    u = 2.0 ** -24
+    z, t, I = z.to(F64) / tau, T.to(F64) / tau, I.long()
+    w = torch.ones(rows, dtype=F64, device="cuda") if weight is None else weight.to(F64)
+    there = (I >= 0) & (I < V)
+    same = (I[:, :, None] == I[:, None, :]) & torch.ones(K, K, dtype=torch.bool, device="cuda").tril(-1)
+    there = there & ~(same & there[:, None, :]).any(2)
+    at = torch.where(there, I, 0)
+    named = torch.zeros(rows, V, device="cuda").scatter_add_(1, at, there.float()) > 0
+    lse = torch.logsumexp(z, 1)
+    rest = torch.logsumexp(z.masked_fill(named, float("-inf")), 1)
+    empty = lse == float("-inf")
+    t = t.masked_fill(~there, float("-inf"))
+    if t_lse is None:
+        norm = torch.logsumexp(t, 1, keepdim=True)
+        logp = torch.where(norm == float("-inf"), norm, t - norm)
+        pt = torch.zeros(rows, dtype=F64, device="cuda")
+        dpt = 0.0
+    else:
+        logp = t - t_lse.to(F64)[:, None]
+        pt = (1 - logp.exp().sum(1)).clamp(min=0)
+    p = logp.exp()
+    logq = z.gather(1, at) - lse[:, None]
+    qt = (rest - lse).exp()
+    kl = torch.where(p == 0, 0, p * (logp - logq)).sum(1) + torch.where(pt > 0, pt * (pt.log() - qt.log()), 0)
+    A = p.sum(1) + pt
+    q = (z - lse[:, None]).exp()
+    ratio = torch.where((pt > 0) & (qt > 0), pt / qt, 0)
+    dz = torch.where(named, A[:, None] * q, q * (A - ratio)[:, None]).scatter_add(1, at, torch.where(there, -p, 0))
+    live = (w != 0) & ~empty
+    loss = torch.where(live, w * kl, 0)
+    dz = torch.where(live[:, None], dz * (w / tau)[:, None], 0)
+    stat = torch.where((w != 0)[:, None], torch.stack((lse, rest), 1), 0)
+    # bounds: p within E and what rounds t / tau - t_lse, p_t what their sum is off, logarithms 4 u (1 + |log|)
+    E = 2.0 ** -17 if V <= 131072 else 2.0 ** -15
+    dp = p * E + 4 * u
+    if t_lse is not None:
+        dp = dp + p * 8 * u * (t.masked_fill(~there | torch.isinf(t), 0).abs() + t_lse.to(F64).abs()[:, None])
+        dpt = dp.sum(1)
+    mag = torch.where(p == 0, 0, logp.abs() + logq.abs())
+    lt = torch.where(pt > 0, pt.log().abs() + qt.log().abs(), 0)
+    dloss = w.abs() * ((dp * (1 + mag) + p * (E + 4 * u * (2 + mag))).sum(1) + dpt * (lt + 1) + pt * (E + 4 * u) * (2 + lt))
+    Ea = E * (1 + (z.amax(1, keepdim=True) - z).clamp(max=1e4) / 8)     # beyond that q is 0, and so is what it is multiplied by
+    dnamed = A[:, None] * q * Ea + column(dpt) * q + torch.zeros_like(q).scatter_add(1, at, torch.where(there, dp, 0))
+    dother = q * (2 * Ea * (A + ratio)[:, None] + column(dpt) * (1 + torch.where(qt > 0, 1 / qt, 0))[:, None])
+    return loss, stat, dz, dloss, torch.where(named, dnamed, dother) * (w.abs() / tau)[:, None]
+
+
+def check(got, want, bound, half=0.0):
+    got = got.to(F64)
+    fine = torch.isfinite(want)
+    assert torch.equal(torch.isnan(got), torch.isnan(want))
+    assert torch.equal(got[~fine & ~torch.isnan(want)], want[~fine & ~torch.isnan(want)])
+    off = (got - want).abs()[fine]
+    allowed = (bound + half * (want.abs() + bound))[fine] + 1e-37
+    assert bool((off <= allowed).all()), float((off / allowed).max())
+
+
+def check_stat(stat, want):
+    fine = torch.isfinite(want)
+    got = stat.to(F64)
+    assert torch.equal(got[~fine], want[~fine])
+    assert bool(((got - want).abs()[fine] <= 2.0 ** -15 + 8 * 2.0 ** -24 * want.abs()[fine]).all())
+
+
+def stat_bound(want):
+    """What the backward call's dZ may be off beyond the forward call's: its normalisers were rounded to fp32 and the student's
+    probabilities are relative to them (16 u |stat| of each term; the terms' size is the bound over E)."""
+    s = want[1].masked_fill(torch.isinf(want[1]), 0).abs().amax(1, keepdim=True)
+    return want[4] * (1 + 2.0 ** 17 * 16 * 2.0 ** -24 * (1 + s))
+
+
+@pytest.mark.parametrize("rows,V,K", SIZES)
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("rest", [False, True])
+def test_loss_and_gradient(B, rows, V, K, kind, rest):
+    for n, (pad, shift, t, bits, tau) in enumerate(((None, 0, torch.float32, 32, 1.0), (1, 1, torch.bfloat16, 64, 2.0))):
+        z, T, I, t_lse = inputs(rows, V, K, kind, V + K + n, t, tau, pad=pad, shift=shift)
+        if K > 2:
+            I[:, K // 2] = -1 if n == 0 else V + 5          # absent
+            I[0, K - 1] = I[0, 0]                           # twice: the first counts
+        if V > 50 and K < V // 2:
+            z[:, V // 3: V // 3 + 9] = float("-inf")        # masked classes
+            I[(I >= V // 3) & (I < V // 3 + 9)] = -1
+        idx = I.to(torch.int64) if bits == 64 else I
+        d = desc(B, V, K, kind, t, bits, tau)
+        weight = torch.rand(rows, generator=gen(V), device="cuda") + 0.5
+        tl = t_lse + 0.05 if rest else None                 # the rest keeps at least 1 - exp(-0.05)
+        loss, stat, dz = torch.empty(rows, device="cuda"), torch.empty(rows, 2, device="cuda"), matrix(rows, V, KINDS[kind], pad=pad, shift=shift)
+        B.fw_distill_forward(d, z, T, idx, loss, stat=stat, t_lse=tl, weight=weight, dZ=dz)
+        want = reference(z, T, I, tau, tl, weight)
+        check(loss, want[0], want[3])
+        check_stat(stat, want[1])
+        check(dz, want[2], want[4], HALF[KINDS[kind]])
+        assert surround_kept(dz)
+        # the loss alone is the same number; the backward call agrees with the definition on its own
+        loss2 = torch.empty(rows, device="cuda")
+        B.fw_distill_forward(d, z, T, idx, loss2, t_lse=tl, weight=weight)
+        assert torch.equal(loss, loss2)
+        dz2 = matrix(rows, V, KINDS[kind], pad=pad, shift=shift)
+        B.fw_distill_backward(d, z, T, idx, stat, dz2, t_lse=tl, weight=weight)
+        check(dz2, want[2], stat_bound(want), HALF[KINDS[kind]])
+        assert surround_kept(dz2)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("rest", [False, True])
+def test_special_rows(B, kind, rest):
+    """Rows of weight 0 that hold NaN, rows without entries, without any mass, with NaN, with +inf; the others as ever."""
+    V, K, rows = 3001, 20, 9
+    z, T, I, t_lse = inputs(rows, V, K, kind, 77)
+    weight = torch.full((rows,), 0.5, device="cuda")
+    z[1] = float("nan")
+    weight[1] = 0
+    I[2] = -1
+    z[3] = float("-inf")
+    z[4, 5] = float("nan")
+    z[5, 6] = float("inf")
+    T[6, 3:] = float("-inf")
+    z[7, I[7, 1].long()] = float("-inf")
+    tl = t_lse + 0.1 if rest else None
+    loss, stat, dz = torch.empty(rows, device="cuda"), torch.empty(rows, 2, device="cuda"), matrix(rows, V, KINDS[kind])
+    d = desc(B, V, K, kind)
+    B.fw_distill_forward(d, z, T, I, loss, stat=stat, t_lse=tl, weight=weight, dZ=dz)
+    rowsum = dz.to(F64).abs().sum(1)
+    for r in (1, 3) + (() if rest else (2,)):
+        assert float(loss[r]) == 0 and float(rowsum[r]) == 0
+    for r in (4, 5):
+        assert bool(torch.isnan(loss[r])) and bool(torch.isnan(dz[r].float()).all())
+    assert float(loss[7]) == float("inf") and bool(torch.isfinite(dz[7].float()).all())
+    keep = [0, 2, 6, 7, 8]
+    want = reference(z[keep], T[keep], I[keep], 1.0, None if tl is None else tl[keep], weight[keep])
+    check(loss[keep], want[0], want[3])
+    check(dz[keep], want[2], want[4], HALF[KINDS[kind]])
+    # the backward call, and in place
+    dz2 = matrix(rows, V, KINDS[kind])
+    B.fw_distill_backward(d, z, T, I, stat, dz2, t_lse=tl, weight=weight)
+    assert float(dz2.to(F64).abs().sum(1)[[1, 3]].sum()) == 0 and bool(torch.isnan(dz2[[4, 5]].float()).all())
+    zz = put(z, KINDS[kind])
+    B.fw_distill_backward(d, zz, T, I, stat, zz, t_lse=tl, weight=weight)
+    assert torch.equal(zz[keep], dz2[keep])
+    zz = put(z, KINDS[kind])
+    B.fw_distill_forward(d, zz, T, I, loss, t_lse=tl, weight=weight, dZ=zz)
+    assert torch.equal(zz[keep], dz[keep])
+
+
+@pytest.mark.parametrize("V", [40000, 200003])
+def test_in_place_long_rows(B, V):
+    """dZ over Z where several CTAs share a row, and where the row is read twice."""
+    for kind in ("f32", "bf16"):
+        z, T, I, t_lse = inputs(40, V, 50, kind, V, pad=None)
+        d = desc(B, V, 50, kind)
+        loss, stat, dz = torch.empty(40, device="cuda"), torch.empty(40, 2, device="cuda"), matrix(40, V, KINDS[kind], pad=None)
+        B.fw_distill_forward(d, z, T, I, loss, stat=stat, t_lse=t_lse, dZ=dz)
+        zz = put(z, KINDS[kind], pad=None)
+        B.fw_distill_forward(d, zz, T, I, loss, t_lse=t_lse, dZ=zz)
+        assert torch.equal(zz, dz)
+        B.fw_distill_backward(d, z, T, I, stat, dz, t_lse=t_lse)
+        zz = put(z, KINDS[kind], pad=None)
+        B.fw_distill_backward(d, zz, T, I, stat, zz, t_lse=t_lse)
+        assert torch.equal(zz, dz)
+
+
+def test_confident_student(B):
+    """Nearly all of the student's mass on a named class: the rest's mass (1e-12 of the whole) is what it is, not what is left
+    of a difference."""
+    V, K = 5000, 8
+    z, T, I, t_lse = inputs(4, V, K, "f32", 3)
+    z.scatter_(1, I[:, :1].long(), 40.0)
+    loss, stat, dz = torch.empty(4, device="cuda"), torch.empty(4, 2, device="cuda"), matrix(4, V, torch.float32)
+    B.fw_distill_forward(desc(B, V, K, "f32"), z, T, I, loss, stat=stat, t_lse=t_lse, dZ=dz)
+    want = reference(z, T, I, 1.0, t_lse)
+    check(loss, want[0], want[3])
+    check_stat(stat, want[1])
+    check(dz, want[2], want[4], HALF[torch.float32])
+
+
+def test_gradient_against_differences(B):
+    """Central differences of the loss in 64 bits, step 1e-5: truncation 1e-10 of the terms."""
+    V, K, tau, h = 30, 5, 2.0, 1e-5
+    z, T, I, t_lse = inputs(2, V, K, "f32", 8, tau=tau)
+    for tl in (None, t_lse):
+        dz, loss = matrix(2, V, torch.float32), torch.empty(2, device="cuda")
+        B.fw_distill_forward(desc(B, V, K, "f32", tau=tau), z, T, I, loss, t_lse=tl, dZ=dz)
+        z64 = z.to(F64).contiguous()
+        num = torch.empty_like(z64)
+        for i in range(V):
+            up, down = z64.clone(), z64.clone()
+            up[:, i] += h
+            down[:, i] -= h
+            num[:, i] = (reference(up, T, I, tau, tl)[0] - reference(down, T, I, tau, tl)[0]) / (2 * h)
+        assert float((dz.to(F64) - num).abs().max()) <= 2e-5 * float(num.abs().max())
+
+
+def test_repeated_other_stream_and_graph(B):
+    rows, V, K = 65, 33333, 40
+    z, T, I, t_lse = inputs(rows, V, K, "bf16", 13, pad=None)
+    d = desc(B, V, K, "bf16")
+    loss, stat, dz, dz2 = torch.empty(rows, device="cuda"), torch.empty(rows, 2, device="cuda"), matrix(rows, V, torch.bfloat16), matrix(rows, V, torch.bfloat16)
+
+    def call(stream):
+        B.fw_distill_forward(d, z, T, I, loss, stat=stat, t_lse=t_lse, dZ=dz, stream=stream)
+        B.fw_distill_backward(d, z, T, I, stat, dz2, t_lse=t_lse, stream=stream)
+
+    call(0)
+    torch.cuda.synchronize()
+    first = [t.clone() for t in (loss, stat, dz, dz2)]
+    call(0)
+    assert all(torch.equal(a, b) for a, b in zip(first, (loss, stat, dz, dz2)))
+    g = captured(call)
+    z.copy_(inputs(rows, V, K, "bf16", 14)[0])
+    g.replay()
+    torch.cuda.synchronize()
+    got = [t.clone() for t in (loss, stat, dz, dz2)]
+    assert not torch.equal(got[0], first[0])
+    call(0)
+    assert all(torch.equal(a, b) for a, b in zip(got, (loss, stat, dz, dz2)))

@@ -63,3 +63,30 @@ def test_tensors_are_looked_at():
         B.fw_rmsnorm_forward(d, x[:, :7], w, x)
     with pytest.raises(ValueError, match="next to each other"):
         B.fw_rmsnorm_forward(d, torch.zeros(8, 8, dtype=torch.bfloat16).T, w, x)
+
+
+def distill(lib, d, forward=True, rows=4, Z=A, ldz=104, T=2 * A, I=3 * A, tl=None, w=None, loss=4 * A, stat=5 * A, dZ=6 * A, lddz=104):
+    if forward:
+        return lib.fw_distill_forward(C.byref(d), Z, rows, ldz, T, I, tl, w, loss, stat, dZ, lddz, None)
+    return lib.fw_distill_backward(C.byref(d), Z, rows, ldz, T, I, tl, w, stat, dZ, lddz, None)
+
+
+def test_distill_refusals(lib):
+    inv, shape = B.FW_ERR_INVALID_ARG, B.FW_ERR_SHAPE
+    d = B.fw_distill_desc_default(100, 10)
+    assert (d.z_dtype, d.t_dtype, d.index_bits, d.tau) == (B.FW_BF16, B.FW_BF16, 32, 1.0)
+    assert lib.fw_distill_forward(None, A, 4, 104, 2 * A, 3 * A, None, None, 4 * A, None, None, 0, None) == inv
+    for kw in (dict(z_dtype=B.FW_E4M3), dict(t_dtype=5), dict(index_bits=16), dict(tau=0.0), dict(tau=-1.0), dict(tau=float("nan")),
+               dict(tau=1e7)):
+        assert distill(lib, B.fw_distill_desc_default(100, 10, **kw)) == inv, kw
+    for V, K in ((0, 1), (10, 0), (10, 11), ((1 << 20) + 1, 5), (5000, 1025)):
+        assert distill(lib, B.fw_distill_desc_default(V, K), ldz=1 << 21, lddz=1 << 21) == shape, (V, K)
+    for kw in (dict(Z=None), dict(T=None), dict(I=None), dict(loss=None), dict(Z=A + 1), dict(I=3 * A + 2), dict(T=2 * A + 1),
+               dict(loss=4 * A + 2), dict(stat=5 * A + 1), dict(dZ=A + 208), dict(dZ=A, lddz=112), dict(dZ=2 * A), dict(loss=3 * A),
+               dict(loss=A), dict(stat=4 * A + 8), dict(w=6 * A), dict(w=4 * A), dict(tl=5 * A), dict(tl=7 * A + 2)):
+        assert distill(lib, d, **kw) == inv, kw
+    for kw in (dict(rows=0), dict(rows=-1), dict(rows=1 << 28), dict(ldz=99), dict(lddz=99), dict(ldz=(1 << 30) + 1)):
+        assert distill(lib, d, **kw) == shape, kw
+    for kw in (dict(stat=None), dict(dZ=None), dict(stat=6 * A)):
+        assert distill(lib, d, forward=False, **kw) == inv, kw
+    assert distill(lib, B.fw_distill_desc_default(100, 10, index_bits=64), I=3 * A + 4) == inv
