@@ -338,6 +338,62 @@ fw_status fw_rmsnorm_backward(const fw_norm_desc* d, int64_t rows, const void* d
                               int64_t lds, const void* dsum, int64_t ldds, const float* w, const float* rstd, void* dx,
                               int64_t lddx, float* dw, void* scratch, size_t scratch_bytes, void* cuda_stream);
 
+/* Gated feed-forward block: two layers of the same input, one gating the other,
+ *   Zg = X Wg^T + bg,  Zu = X Wu^T + bu,  H = act(Zg) Zu (element by element)
+ * Both projections, the activation and the product are one kernel on the tensor
+ * cores (tcgen05, fp32 accumulation).  The backward call gives what fw_cov_update's companions take:
+ * dWg, dWu are the gradients G of the layers (Wg, bg) and (Wu, bu), dbg, dbu their g_b.
+ * X: rows x M, Wg, Wu: N x M, H, Zg, Zu: rows x N.
+ *   FW_BF16  X, weights, outputs bf16
+ *   FW_E4M3  X and weights e4m3 with a scale for each row of X (x_scale) and each row of
+ *            Wg, Wu (wg_scale, wu_scale); H, Zg, Zu bf16; forward only
+ * Scales and biases are fp32.  1 <= M, N <= 32768.  Every matrix but dWg, dWu starts on 16 bytes
+ * and has rows a multiple of 16 bytes apart (M and N may be any).
+ * Like a layer the block is a host object over caller-supplied device memory with a
+ * stream of its own: calls on one block are not for several threads at once, and its
+ * workspace belongs to the work in flight on its stream (two graphs that may run at
+ * the same time take two blocks). */
+typedef struct fw_gated fw_gated;
+typedef enum {
+  FW_ACT_SILU = 0,      /* a / (1 + exp(-a))                                      */
+  FW_ACT_GELU = 1,      /* a (1 + erf(a / sqrt 2)) / 2                            */
+  FW_ACT_GELU_TANH = 2, /* a (1 + tanh(sqrt(2 / pi) (a + 0.044715 a^3))) / 2      */
+  FW_ACT_RELU = 3       /* max(a, 0); derivative 0 at 0                           */
+} fw_act;
+typedef struct {
+  int32_t M, N;
+  int32_t x_dtype;      /* FW_BF16 or FW_E4M3                                     */
+  int32_t act;          /* fw_act                                                 */
+  int32_t grad;         /* 1: the workspace has room for backward calls (bf16)    */
+  int64_t max_rows;     /* grad: largest rows of a backward call                  */
+} fw_gated_desc;
+/* bf16, SiLU, no backward calls */
+void fw_gated_desc_default(fw_gated_desc* d, int32_t M, int32_t N);
+/* 0 if the description is invalid */
+size_t fw_gated_workspace_bytes(const fw_gated_desc* d);
+/* The workspace (256-byte aligned) outlives the block; on the current device. */
+fw_status fw_gated_create(const fw_gated_desc* d, void* dev_workspace, size_t bytes, void* cuda_stream, fw_gated** out);
+fw_status fw_gated_destroy(fw_gated* g);
+/* Zg, Zu: both or (where no backward call follows) neither.  bg, bu: both or neither.
+ * x_scale, wg_scale, wu_scale: with e4m3, and only then.  Outputs overlap nothing. */
+fw_status fw_gated_forward(fw_gated* g, const void* X, int64_t rows, int64_t ldx, const float* x_scale, const void* Wg,
+                           const void* Wu, int64_t ldw, const float* wg_scale, const float* wu_scale, const float* bg,
+                           const float* bu, void* H, int64_t ldh, void* Zg, void* Zu, int64_t ldz);
+/* From dH, the forward call's inputs and its Zg, Zu:
+ *   da = dH Zu act'(Zg), db = dH act(Zg) (both rounded to bf16 for the products)
+ *   dX = da Wg + db Wu (bf16; NULL: not wanted, and Wg, Wu may be NULL)
+ *   dWg = da^T X, dWu = db^T X (both or neither; dense N x M of dw_dtype, FW_F32 as the layers'
+ *   calls take them, or FW_BF16; X may be NULL without them)
+ *   dbg, dbu = sums of da, db over the rows before they are rounded (both or neither)
+ * Outputs are overwritten.  FW_ERR_WORKSPACE for a block made without grad, FW_ERR_SHAPE for more
+ * than max_rows. */
+fw_status fw_gated_backward(fw_gated* g, const void* dH, int64_t rows, int64_t lddh, const void* X, int64_t ldx,
+                            const void* Wg, const void* Wu, int64_t ldw, const void* Zg, const void* Zu, int64_t ldz,
+                            void* dX, int64_t lddx, void* dWg, void* dWu, int32_t dw_dtype, float* dbg, float* dbu);
+/* Waits for the block's stream; FW_ERR_TIMEOUT if a bounded device-side wait gave up since the last
+ * call (what the calls since then wrote is not to be used). */
+fw_status fw_gated_sync_status(fw_gated* g);
+
 /* Distillation loss against a teacher's top logits, and its gradient (what the weight
  * gradient of a network's last layer is formed from).  With q = softmax(Z / tau) of a
  * row and the K classes i_k that the teacher names, with its logits t_k:

@@ -37,8 +37,11 @@ EXPORTS = [
     "fw_evd_scratch_bytes", "fw_evd_whiten", "fw_group_evd_whiten", "fw_spectrum",
     "fw_norm_desc_default", "fw_rmsnorm_scratch_bytes", "fw_rmsnorm_forward", "fw_rmsnorm_backward",
     "fw_distill_desc_default", "fw_distill_forward", "fw_distill_backward",
+    "fw_gated_desc_default", "fw_gated_workspace_bytes", "fw_gated_create", "fw_gated_destroy", "fw_gated_forward",
+    "fw_gated_backward", "fw_gated_sync_status",
 ]
 FW_STATIC_MAX_M = 256
+FW_ACT_SILU, FW_ACT_GELU, FW_ACT_GELU_TANH, FW_ACT_RELU = range(4)
 FW_PROF_NAMES = ["pilot", "gram", "moments", "resync", "recur_mv", "recur_upd", "smooth", "gq", "misc", "recur_chip"]
 
 
@@ -62,6 +65,11 @@ class fw_norm_desc(C.Structure):
 class fw_distill_desc(C.Structure):
     _fields_ = [("V", C.c_int32), ("K", C.c_int32), ("z_dtype", C.c_int32), ("t_dtype", C.c_int32),
                 ("index_bits", C.c_int32), ("tau", C.c_float)]
+
+
+class fw_gated_desc(C.Structure):
+    _fields_ = [("M", C.c_int32), ("N", C.c_int32), ("x_dtype", C.c_int32), ("act", C.c_int32), ("grad", C.c_int32),
+                ("max_rows", C.c_int64)]
 
 
 _LIB = None
@@ -128,6 +136,15 @@ def _lib():
     lib.fw_distill_forward.restype = i32
     lib.fw_distill_backward.argtypes = [P(fw_distill_desc), vp, i64, i64, vp, vp, vp, vp, vp, vp, i64, vp]
     lib.fw_distill_backward.restype = i32
+    lib.fw_gated_desc_default.argtypes = [P(fw_gated_desc), i32, i32]; lib.fw_gated_desc_default.restype = None
+    lib.fw_gated_workspace_bytes.argtypes = [P(fw_gated_desc)]; lib.fw_gated_workspace_bytes.restype = sz
+    lib.fw_gated_create.argtypes = [P(fw_gated_desc), vp, sz, vp, P(vp)]; lib.fw_gated_create.restype = i32
+    lib.fw_gated_destroy.argtypes = [vp]; lib.fw_gated_destroy.restype = i32
+    lib.fw_gated_forward.argtypes = [vp, vp, i64, i64, vp, vp, vp, i64, vp, vp, vp, vp, vp, i64, vp, vp, i64]
+    lib.fw_gated_forward.restype = i32
+    lib.fw_gated_backward.argtypes = [vp, vp, i64, i64, vp, i64, vp, vp, i64, vp, vp, i64, vp, i64, vp, vp, i32, vp, vp]
+    lib.fw_gated_backward.restype = i32
+    lib.fw_gated_sync_status.argtypes = [vp]; lib.fw_gated_sync_status.restype = i32
     _LIB = lib
     return lib
 
@@ -376,6 +393,15 @@ def _vector(t, n, name, dtype=FW_F32):
     return t.data_ptr()
 
 
+def _pair(a, b, rows, cols, dtype, name):
+    """Two matrices with one leading dimension."""
+    pa, lda = _matrix(a, rows, cols, dtype, name)
+    pb, ldb = _matrix(b, rows, cols, dtype, name)
+    if a is not None and b is not None and lda != ldb:
+        raise ValueError(f"{name}: their rows have to be equally far apart")
+    return pa, pb, lda if a is not None else ldb
+
+
 def _on_device(t, name):
     import torch
     if not t.is_cuda:
@@ -513,3 +539,64 @@ class Layer:
 
     def sync_status(self):
         return fw_layer_sync_status(self.handle)
+
+
+class Gated:
+    """A gated feed-forward block over a workspace tensor of its own.  Methods take torch CUDA tensors, look at their sizes,
+    strides and types, and forward to the C entry points fw_gated_*."""
+
+    def __init__(self, M: int, N: int, max_rows: int = 0, device="cuda", stream: int = 0, **desc_overrides):
+        import torch
+        self.desc = fw_gated_desc()
+        _lib().fw_gated_desc_default(C.byref(self.desc), M, N)
+        self.desc.max_rows = max_rows
+        for k, v in desc_overrides.items():
+            setattr(self.desc, k, int(v))
+        self.M, self.N = M, N
+        self.nbytes = int(_lib().fw_gated_workspace_bytes(C.byref(self.desc)))
+        if self.nbytes == 0:
+            raise FwError(FW_ERR_INVALID_ARG, "fw_gated_workspace_bytes")
+        self.workspace = torch.empty(self.nbytes + 256, dtype=torch.uint8, device=device)
+        out = C.c_void_p()
+        _check(_lib().fw_gated_create(C.byref(self.desc), (self.workspace.data_ptr() + 255) // 256 * 256, self.nbytes, stream,
+                                      C.byref(out)), "fw_gated_create")
+        self.handle = out.value
+
+    def close(self):
+        if getattr(self, "handle", None):
+            _check(_lib().fw_gated_destroy(self.handle), "fw_gated_destroy")
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def forward(self, X, Wg, Wu, H, Zg=None, Zu=None, x_scale=None, wg_scale=None, wu_scale=None, bg=None, bu=None):
+        M, N, t, rows = self.M, self.N, self.desc.x_dtype, X.shape[0]
+        px, ldx = _matrix(X, rows, M, t, "X")
+        pg, pu, ldw = _pair(Wg, Wu, N, M, t, "Wg, Wu")
+        ph, ldh = _matrix(H, rows, N, FW_BF16, "H")
+        zg, zu, ldz = _pair(Zg, Zu, rows, N, FW_BF16, "Zg, Zu")
+        _check(_lib().fw_gated_forward(self.handle, px, rows, ldx, _vector(x_scale, rows, "x_scale"), pg, pu, ldw,
+                                       _vector(wg_scale, N, "wg_scale"), _vector(wu_scale, N, "wu_scale"), _vector(bg, N, "bg"),
+                                       _vector(bu, N, "bu"), ph, ldh, zg, zu, ldz), "fw_gated_forward")
+
+    def backward(self, dH, X, Wg, Wu, Zg, Zu, dX=None, dWg=None, dWu=None, dbg=None, dbu=None):
+        M, N, rows = self.M, self.N, dH.shape[0]
+        pd, lddh = _matrix(dH, rows, N, FW_BF16, "dH")
+        px, ldx = _matrix(X, rows, M, FW_BF16, "X")
+        pg, pu, ldw = _pair(Wg, Wu, N, M, FW_BF16, "Wg, Wu")
+        zg, zu, ldz = _pair(Zg, Zu, rows, N, FW_BF16, "Zg, Zu")
+        pdx, lddx = _matrix(dX, rows, M, FW_BF16, "dX")
+        kind = FW_F32
+        if dWg is not None:
+            import torch
+            kind = FW_BF16 if dWg.dtype == torch.bfloat16 else FW_F32
+        _check(_lib().fw_gated_backward(self.handle, pd, rows, lddh, px, ldx, pg, pu, ldw, zg, zu, ldz, pdx, lddx,
+                                        _vector(dWg, N * M, "dWg", kind), _vector(dWu, N * M, "dWu", kind), kind,
+                                        _vector(dbg, N, "dbg"), _vector(dbu, N, "dbu")), "fw_gated_backward")
+
+    def sync_status(self):
+        return _check(_lib().fw_gated_sync_status(self.handle), "fw_gated_sync_status")

@@ -10,6 +10,7 @@
 #include <cstring>
 #include <vector>
 
+#include "fw_gated.h"
 #include "fw_sm100.cuh"
 #include "fw_umma.h"
 
@@ -947,6 +948,14 @@ bool tmap_encode_kmajor_f32(CUtensorMap* m, const void* base, uint64_t inner, ui
                             uint32_t box_inner, uint32_t box_outer) {
   return encode_2d(m, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, base, inner, outer, ld, box_inner, box_outer,
                    CU_TENSOR_MAP_SWIZZLE_128B);
+}
+
+bool tmap_encode_rows128(CUtensorMap* m, int elem_bytes, const void* base, uint64_t inner, uint64_t outer, uint64_t ld,
+                         uint32_t box_outer) {
+  const CUtensorMapDataType dt = elem_bytes == 1   ? CU_TENSOR_MAP_DATA_TYPE_UINT8
+                                 : elem_bytes == 2 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16
+                                                   : CU_TENSOR_MAP_DATA_TYPE_FLOAT32;
+  return encode_2d(m, dt, elem_bytes, base, inner, outer, ld, 128u / (uint32_t)elem_bytes, box_outer, CU_TENSOR_MAP_SWIZZLE_128B);
 }
 
 // A wait that nothing ever satisfies, with a short poll limit: the bounded wait of every pipeline in this engine

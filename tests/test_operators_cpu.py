@@ -90,3 +90,32 @@ def test_distill_refusals(lib):
     for kw in (dict(stat=None), dict(dZ=None), dict(stat=6 * A)):
         assert distill(lib, d, forward=False, **kw) == inv, kw
     assert distill(lib, B.fw_distill_desc_default(100, 10, index_bits=64), I=3 * A + 4) == inv
+
+
+def test_gated_refusals(lib):
+    inv, shape, ws, no = B.FW_ERR_INVALID_ARG, B.FW_ERR_SHAPE, B.FW_ERR_WORKSPACE, B.FW_ERR_UNSUPPORTED
+
+    def make(M=64, N=32, at=A, n=1 << 30, **kw):
+        d = B.fw_gated_desc()
+        lib.fw_gated_desc_default(C.byref(d), M, N)
+        assert (d.x_dtype, d.act, d.grad, d.max_rows) == (B.FW_BF16, B.FW_ACT_SILU, 0, 0)
+        for k, v in kw.items():
+            setattr(d, k, v)
+        out = C.c_void_p()
+        st = lib.fw_gated_create(C.byref(d), at, n, None, C.byref(out))
+        assert out.value is None or st == B.FW_OK
+        return st, lib.fw_gated_workspace_bytes(C.byref(d))
+
+    for kw in (dict(x_dtype=9), dict(act=4), dict(act=-1), dict(grad=2)):
+        assert make(**kw) == (inv, 0), kw
+    for kw in (dict(M=0), dict(N=0), dict(M=32769), dict(N=40000), dict(grad=1), dict(grad=1, max_rows=-1)):
+        assert make(**kw) == (shape, 0), kw
+    assert make(x_dtype=B.FW_F32) == (no, 0) and make(x_dtype=B.FW_E4M3, grad=1, max_rows=4) == (no, 0)
+    assert make(at=A + 16)[0] == ws and make(n=100)[0] == ws and make(at=None)[0] == inv
+    st, n = make(grad=1, max_rows=1000)
+    assert n >= 2 * 1000 * 32 * 2 and make(grad=1, max_rows=1000, n=n - 1)[0] == ws
+    assert lib.fw_gated_create(None, A, 1 << 20, None, C.byref(C.c_void_p())) == inv
+    for f, k in ((lib.fw_gated_destroy, 0), (lib.fw_gated_sync_status, 0)):
+        assert f(None) == inv
+    assert lib.fw_gated_forward(None, A, 1, 64, None, A, A, 64, None, None, None, None, A, 64, None, None, 0) == inv
+    assert lib.fw_gated_backward(None, A, 1, 64, A, 64, A, A, 64, A, A, 64, A, 64, A, A, 0, A, A) == inv
