@@ -48,10 +48,12 @@ struct PairArgs {
   CUtensorMap out[3];                              // forward: H, Zg, Zu.  backward: dX, dWg, dWu
   PairProduct dx, dw;                              // forward: dx
   int32_t tiles;
-  int32_t M, N, act, keep, w_f32, w_direct;
+  int32_t M, N, act, keep, w_f32;
+  int32_t whole[3];                                // outputs: 1 rows are whole multiples of 16 bytes long and apart, 0 only apart, -1 neither
   int64_t rows;
   const float *xs, *wgs, *wus, *bg, *bu;
-  void* direct[2];                                 // dWg, dWu where their rows are not 16 bytes apart in multiples
+  void* to[3];                                     // the outputs of out[], as addresses
+  int64_t ld[3];
   int32_t* status;
 };
 
@@ -276,12 +278,34 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(GG_THREADS, 1) gated
       if (issuer) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
       sync_half();
     };
-    auto send = [&](const CUtensorMap* m, int x, int y, bool inside) {
-      fence_proxy_async_smem();
-      sync_half();
-      if (issuer && inside) {
-        tma_store_2d(m, room, x, y);
-        asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+    // the tile of results -> output o from (row y, column x) on; it has `height` x `width` elements, of 4 bytes with f32
+    auto send = [&](int o, int x, int y, int64_t height, int width, bool f32) {
+      if (x + (f32 ? 32 : 64) <= width ? g.whole[o] >= 0 : g.whole[o] > 0) {
+        fence_proxy_async_smem();
+        sync_half();
+        if (issuer && y < height && x < width) {
+          tma_store_2d(&g.out[o], room, x, y);
+          asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+        }
+        return;
+      }
+      // TMA writes whole 16 bytes: where a row ends inside of them, or rows start anywhere (a dense matrix of odd width), a warp
+      // copies its own 32 rows element by element
+      __syncwarp();
+      for (int i = 0; i < 32; ++i) {
+        const int rr = q * 32 + i;
+        if (y + rr >= height) break;
+        const uint32_t at = room + rr * 128 + ((uint32_t)((lane >> 2) ^ (rr & 7)) << 4) + (lane & 3) * 4;
+        uint32_t w;
+        asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w) : "r"(at) : "memory");
+        const int64_t row = (int64_t)(y + rr) * g.ld[o];
+        if (f32) {
+          if (x + lane < width) static_cast<float*>(g.to[o])[row + x + lane] = __uint_as_float(w);
+        } else {
+          uint16_t* d = static_cast<uint16_t*>(g.to[o]) + row + x + 2 * lane;
+          if (x + 2 * lane < width) d[0] = (uint16_t)w;
+          if (x + 2 * lane + 1 < width) d[1] = (uint16_t)(w >> 16);
+        }
       }
     };
     for (int t = pair; t < g.tiles; t += pairs) {
@@ -304,7 +328,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(GG_THREADS, 1) gated
       if (FWD) {
         const int n0 = 128 * tl.n + 64 * half;      // this half's 64 outputs
         const float xs = KIND == GG_FWD_E4M3 && row < g.rows ? g.xs[row] : 1.f;
-        const bool inside = m0 < g.rows && n0 < g.N;
         // 32 projections of one kind from accumulator column c on (output n0 + j): scaled, with their bias
         auto project = [&](float (&v)[32], int c, int j0, const float* ws, const float* bias) {
           tmem_ld32(acc + (uint32_t)c, reinterpret_cast<uint32_t(&)[32]>(v));
@@ -332,7 +355,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(GG_THREADS, 1) gated
               project(v, 128 * k + 64 * half + j0, j0, k ? g.wus : g.wgs, k ? g.bu : g.bg);
               put32(v, j0);
             }
-            send(&g.out[1 + k], n0, m0, inside);
+            send(1 + k, n0, m0, g.rows, g.N, false);
           }
         }
         room_free();
@@ -347,11 +370,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(GG_THREADS, 1) gated
             put32(v, j0);
           }
         });
-        send(&g.out[0], n0, m0, inside);
+        send(0, n0, m0, g.rows, g.N, false);
       } else {
         const int n0 = 256 * tl.n + 128 * half;     // this half's 128 columns
         const bool f32 = tl.kind == 1 && g.w_f32;
-        const bool direct = tl.kind == 1 && g.w_direct;
         const int64_t height = tl.kind == 1 ? g.N : g.rows;
         const int wide = f32 ? 32 : 64;             // columns of 128 bytes
         for (int c0 = 0; c0 < 128; c0 += wide) {
@@ -373,27 +395,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(GG_THREADS, 1) gated
             }
           }
           const int x = n0 + c0;
-          if (!direct) {
-            send(&g.out[tl.kind == 1 ? 1 + tl.which : 0], x, m0, m0 < height && x < g.M);
-            continue;
-          }
-          // rows of a dense matrix of odd width start anywhere: a warp copies its own 32 rows element by element
-          __syncwarp();
-          for (int i = 0; i < 32; ++i) {
-            const int rr = q * 32 + i;
-            if (m0 + rr >= height) break;
-            const uint32_t at = room + rr * 128 + ((uint32_t)((lane >> 2) ^ (rr & 7)) << 4) + (lane & 3) * 4;
-            uint32_t w;
-            asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w) : "r"(at) : "memory");
-            const int64_t o = (int64_t)(m0 + rr) * g.M;
-            if (f32) {
-              if (x + lane < g.M) static_cast<float*>(g.direct[tl.which])[o + x + lane] = __uint_as_float(w);
-            } else {
-              uint16_t* d = static_cast<uint16_t*>(g.direct[tl.which]) + o + x + 2 * lane;
-              if (x + 2 * lane < g.M) d[0] = (uint16_t)w;
-              if (x + 2 * lane + 1 < g.M) d[1] = (uint16_t)(w >> 16);
-            }
-          }
+          send(tl.kind == 1 ? 1 + tl.which : 0, x, m0, height, g.M, f32);
         }
       }
       b ^= 1;
@@ -440,6 +442,8 @@ fw_status launch_gated_pair_forward(const GatedForward& f, cudaStream_t s) {
   bool ok = tmap_encode_rows128(&g.a[0], es, f.X, f.M, f.rows, f.ldx, 128) && tmap_encode_rows128(&g.b[0], es, f.Wg, f.M, f.N, f.ldw, 128) &&
             tmap_encode_rows128(&g.b[1], es, f.Wu, f.M, f.N, f.ldw, 128) && tmap_encode_rows128(&g.out[0], 2, f.H, f.N, f.rows, f.ldh, 128);
   g.keep = f.Zg != nullptr;
+  g.to[0] = f.H; g.to[1] = f.Zg; g.to[2] = f.Zu; g.ld[0] = f.ldh; g.ld[1] = g.ld[2] = f.ldz;
+  g.whole[0] = g.whole[1] = g.whole[2] = f.N % 8 == 0;
   if (g.keep) ok = ok && tmap_encode_rows128(&g.out[1], 2, f.Zg, f.N, f.rows, f.ldz, 128) && tmap_encode_rows128(&g.out[2], 2, f.Zu, f.N, f.rows, f.ldz, 128);
   if (!ok) {
     fprintf(stderr, "[fw] tensor-map encoding failed (gated block, forward)\n");
@@ -462,6 +466,7 @@ fw_status launch_gated_pair_backward(const GatedBackward& b, cudaStream_t s) {
     ok = ok && tmap_encode_rows128(&g.a[0], 2, b.Da, b.N, b.rows, b.ldd, 128) && tmap_encode_rows128(&g.a[1], 2, b.Db, b.N, b.rows, b.ldd, 128) &&
          tmap_encode_rows128(&g.b[0], 2, b.Wg, b.M, b.N, b.ldw, 64) && tmap_encode_rows128(&g.b[1], 2, b.Wu, b.M, b.N, b.ldw, 64) &&
          tmap_encode_rows128(&g.out[0], 2, b.dX, b.M, b.rows, b.lddx, 128);
+    g.to[0] = b.dX; g.ld[0] = b.lddx; g.whole[0] = b.M % 8 == 0;
     g.dx.tiles_m = blocks(b.rows, 256); g.dx.tiles_n = blocks(b.M, 256);
     g.dx.seg_blocks = blocks(b.N, 64); g.dx.nk = 2 * g.dx.seg_blocks;
   }
@@ -469,11 +474,12 @@ fw_status launch_gated_pair_backward(const GatedBackward& b, cudaStream_t s) {
   if (b.dWg) {
     const int es = b.w_f32 ? 4 : 2;
     g.w_f32 = b.w_f32;
-    g.w_direct = ((int64_t)b.M * es) % 16 != 0 || reinterpret_cast<uintptr_t>(b.dWg) % 16 != 0 || reinterpret_cast<uintptr_t>(b.dWu) % 16 != 0;
-    g.direct[0] = b.dWg; g.direct[1] = b.dWu;
+    g.to[1] = b.dWg; g.to[2] = b.dWu; g.ld[1] = g.ld[2] = b.M;
+    const bool aligned = ((int64_t)b.M * es) % 16 == 0 && reinterpret_cast<uintptr_t>(b.dWg) % 16 == 0 && reinterpret_cast<uintptr_t>(b.dWu) % 16 == 0;
+    g.whole[1] = g.whole[2] = aligned ? 1 : -1;
     ok = ok && tmap_encode_rows128(&g.at[0], 2, b.Da, b.N, b.rows, b.ldd, 64) && tmap_encode_rows128(&g.at[1], 2, b.Db, b.N, b.rows, b.ldd, 64) &&
          tmap_encode_rows128(&g.bt, 2, b.X, b.M, b.rows, b.ldx, 64);
-    if (!g.w_direct)
+    if (aligned)
       ok = ok && tmap_encode_rows128(&g.out[1], es, b.dWg, b.M, b.N, b.M, 128) && tmap_encode_rows128(&g.out[2], es, b.dWu, b.M, b.N, b.M, 128);
     g.dw.tiles_m = 2 * blocks(b.N, 256); g.dw.tiles_n = blocks(b.M, 256);
     g.dw.nk = blocks(b.rows, 64);
