@@ -10,15 +10,21 @@
 //
 // The mass of the others is summed by itself, never as 1 - sum of the named: a trained student leaves little there.
 //
-// One pass: a row (2 to 4 bytes a class, read once) stays in the registers of a CTA, or of a cluster of up to 8 where it is
-// long, as exponentials relative to each thread's own largest logit; the sums go through shared memory of the cluster; then
-// the gradient is written.  HBM bandwidth bounds long rows.  Rows beyond what a cluster holds are read twice.
+// One pass: a row (2 to 4 bytes a class, read once) stays in the registers of a CTA, or of a cluster where it is long, as
+// exponentials relative to each thread's own largest logit; the sums go through shared memory of the cluster; then the
+// gradient is written.  HBM bandwidth bounds long rows.
+//
+//   distill_ring_kernel  long aligned rows of up to 256 entries: resident clusters walk the rows, two rows ahead of themselves
+//   distill_kernel       everything else: a CTA or cluster a row; rows beyond what a cluster holds are read twice
 #include <cstdio>
+#include <cstring>
+#include <mutex>
 
 #include <cooperative_groups.h>
 
 #include "fw_internal.h"
 #include "fw_rows.cuh"
+#include "fw_sm100.cuh"
 
 namespace fw {
 namespace {
@@ -297,6 +303,325 @@ __global__ void __launch_bounds__(512, 2) distill_kernel(const Distill p) {
   if (MODE != DIST_BACKWARD) cluster.sync();  // no CTA of the cluster leaves while its sum may still be read
 }
 
+// ---------------------------------------------------------------------------
+// Long rows.  A row is a chain of latencies (entries, their logits, the slice, an exchange over the cluster, stores), and with a
+// CTA for each slice of each row the chains and not the bytes took the time: 4096 x 131072 bf16 1708 us.  So clusters stay and
+// walk the rows, and everything is on its way before it is needed:
+//   - a thread copies its own classes of the next two rows to shared memory (cp.async: it reads back only what it wrote itself, so
+//     no barrier stands between), 96 KB in two CTAs a SM;
+//   - entry k of a row belongs to thread k: class, logits and weight are loaded three rows ahead, the student's logit two;
+//   - between its arrival at the cluster's barrier and its wait there a warp prepares the next row's entries (repeated classes,
+//     bit set, the teacher's and the named classes' sums);
+//   - what is written over the row's stores (named classes) or needs all warps (the loss) follows after the next row's barrier.
+// Two barriers a row: one of the CTA, one of the cluster.
+// ---------------------------------------------------------------------------
+constexpr int kRingThreads = 256, kRingWarps = 8, kRingSlots = 3, kRingMaxK = 256, kRingMaxCtas = 16;
+
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void st_cluster_pair(uint32_t addr, MaxSum v) {
+  asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(addr), "f"(v.m), "f"(v.l) : "memory");
+}
+__device__ __forceinline__ void unpack16(uint4 q, float (&v)[8]) {
+  v[0] = bf16_lo(q.x); v[1] = bf16_hi(q.x); v[2] = bf16_lo(q.y); v[3] = bf16_hi(q.y);
+  v[4] = bf16_lo(q.z); v[5] = bf16_hi(q.z); v[6] = bf16_lo(q.w); v[7] = bf16_hi(q.w);
+}
+__device__ __forceinline__ void unpack16(uint4 q, float (&v)[4]) {
+  v[0] = __uint_as_float(q.x); v[1] = __uint_as_float(q.y); v[2] = __uint_as_float(q.z); v[3] = __uint_as_float(q.w);
+}
+
+// What a thread knows of a row: its entry, and the row's numbers.
+struct RingRow {
+  float w, t_lse, s0, s1;    // weight (0 past the last row), teacher's normaliser, backward: stat
+  int c;                     // class of this thread's entry, -1: none
+  float t, z;                // teacher's and student's logit
+};
+
+template <class T, int NV, int MODE>
+__global__ void __launch_bounds__(kRingThreads, 2) distill_ring_kernel(const Distill p, int rows) {
+  constexpr int VEC = 16 / sizeof(T);
+  extern __shared__ __align__(16) uint8_t dyn8[];
+  __shared__ __align__(16) int s_cls[2][kRingMaxK];
+  __shared__ MaxSum s_teacher[2][kRingWarps], s_named[2][kRingWarps];
+  __shared__ MaxSum s_sum[2][kRingMaxCtas * kRingWarps];
+  __shared__ float s_kl[2][kRingWarps];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int C = (int)sm100::cluster_nctarank(), rank = (int)sm100::cluster_ctarank();
+  const int row0 = (int)blockIdx.x / C, step = (int)gridDim.x / C;
+  uint4* ring = reinterpret_cast<uint4*>(dyn8);                                  // [slot][k][thread]
+  constexpr int words = NV * kRingThreads * VEC / 32;
+  uint32_t* bits = reinterpret_cast<uint32_t*>(ring + kRingSlots * NV * kRingThreads);   // [3][words]
+  const float c2 = p.inv_tau * kLog2e;
+  const int first = rank * p.slice, last = min(p.V, first + p.slice);
+  const uint32_t ring_at = sm100::smem_u32(ring) + tid * 16;
+  const uint32_t push_at = sm100::mapa_shared(sm100::smem_u32(&s_sum[0][rank * kRingWarps + warp]), lane < C ? lane : 0);
+
+  auto zrow = [&](int row) { return static_cast<const T*>(p.Z) + (int64_t)row * p.ldz; };
+  auto load_row = [&](int row) {
+    RingRow r = {0.f, 0.f, 0.f, 0.f, -1, 0.f, 0.f};
+    if (row < rows) {
+      r.w = p.weight ? p.weight[row] : 1.f;
+      if (p.t_lse) r.t_lse = p.t_lse[row];
+      if (MODE == DIST_BACKWARD) { r.s0 = p.stat_in[2 * (int64_t)row]; r.s1 = p.stat_in[2 * (int64_t)row + 1]; }
+      if (tid < p.K) {
+        const int64_t at = (int64_t)row * p.K + tid;
+        const int64_t i = p.i64 ? static_cast<const int64_t*>(p.I)[at] : static_cast<const int32_t*>(p.I)[at];
+        r.c = i >= 0 && i < p.V ? (int)i : -1;
+        r.t = p.t_bf16 ? to_f(static_cast<const __nv_bfloat16*>(p.T)[at]) : static_cast<const float*>(p.T)[at];
+      }
+    }
+    return r;
+  };
+  // the student's logit of an entry; the backward pass needs those of its slice alone (dZ may be Z: others' are written over)
+  auto load_logit = [&](RingRow& r, int row) {
+    if (r.c >= 0 && r.w != 0.f && (MODE != DIST_BACKWARD || (r.c >= first && r.c < last))) r.z = to_f(zrow(row)[r.c]);
+  };
+  auto fetch = [&](const RingRow& r, int row, int it) {
+    if (r.w != 0.f) {
+      const T* z = zrow(row);
+      const uint32_t to = ring_at + (uint32_t)(it % kRingSlots) * (NV * kRingThreads * 16);
+#pragma unroll
+      for (int k = 0; k < NV; ++k) {
+        const int c = first + (k * kRingThreads + tid) * VEC;
+        if (c + VEC <= last) copy16(to + k * kRingThreads * 16, z + c);
+      }
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  auto teacher2 = [&](float t, float t_lse, float tm) { return p.t_lse ? fmaf(t, p.inv_tau, -t_lse) * kLog2e : (t - tm) * c2; };
+  // the entries of a row whose classes stand in s_cls[it & 1] (a barrier of the CTA ago): repeated ones out, bit set, sums
+  auto prepare = [&](RingRow& r, int it) {
+    if (warp * 32 >= p.K) return;
+    const unsigned same = __match_any_sync(0xffffffffu, r.c);
+    bool twice = (int)(__ffs(same) - 1) != lane;
+    const int4* before = reinterpret_cast<const int4*>(s_cls[it & 1]);
+    for (int j = 0; j < warp * 8; ++j) {
+      const int4 q = before[j];
+      twice |= q.x == r.c || q.y == r.c || q.z == r.c || q.w == r.c;
+    }
+    if (twice) r.c = -1;
+    if (r.c >= first && r.c < last) atomicOr(&bits[(it % 3) * words + ((r.c - first) >> 5)], 1u << ((r.c - first) & 31));
+    const bool in = r.c >= 0;
+    MaxSum t = {kLow, 0.f};
+    if (p.t_lse) {
+      t.l = in ? ex2(teacher2(r.t, r.t_lse, 0.f)) : 0.f;
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) t.l += __shfl_xor_sync(0xffffffffu, t.l, o);
+    } else {
+      if (in) t = {fmaxf(r.t, kLow), r.t == -INFINITY ? 0.f : r.t != r.t ? r.t : 1.f};
+      t = merge_lanes(t, c2);
+    }
+    MaxSum n = {kLow, 0.f};
+    if (MODE != DIST_BACKWARD) {
+      if (in) n = {fmaxf(r.z, kLow), r.z == -INFINITY ? 0.f : r.z != r.z ? r.z : 1.f};
+      n = merge_lanes(n, c2);
+    }
+    if (lane == 0) { s_teacher[it & 1][warp] = t; s_named[it & 1][warp] = n; }
+  };
+
+  dep_sync();
+  // ---- the first three rows ----
+  RingRow cur = load_row(row0), next = load_row(row0 + step), third = load_row(row0 + 2 * step);
+  fetch(cur, row0, 0);
+  fetch(next, row0 + step, 1);
+  load_logit(cur, row0);
+  load_logit(next, row0 + step);
+  for (int i = tid; i < 3 * words; i += kRingThreads) bits[i] = 0;
+  s_cls[0][tid] = cur.c;
+  s_cls[1][tid] = next.c;
+  __syncthreads();
+  prepare(cur, 0);
+  // what follows the next barrier: this thread's named class of the row before, and (one thread) its loss
+  T* late_at = nullptr;
+  float late = 0.f;
+  int late_row = -1;
+  float late_w = 0.f, late_rest = 0.f, late_lse = 0.f, late_other = 0.f;
+  auto finish = [&](int it) {
+    if (MODE != DIST_LOSS && late_at) put(late_at, late);
+    late_at = nullptr;
+    if (MODE != DIST_BACKWARD && late_row >= 0) {
+      float kl = 0.f;
+      for (int k = 0; k < kRingWarps; ++k) kl += s_kl[it & 1][k];
+      p.loss[late_row] = late_w * (kl + late_rest) * kLn2;
+      if (p.stat) { p.stat[2 * (int64_t)late_row] = late_lse; p.stat[2 * (int64_t)late_row + 1] = late_other; }
+      late_row = -1;
+    }
+  };
+
+  // no CTA writes into another's shared memory before that one has begun
+  sm100::cluster_arrive();
+  sm100::cluster_wait();
+  int it = 0;
+  int turn = 0;                 // place of the sums, by rows that count: two such rows are a cluster barrier apart
+  for (int row = row0; row < rows; row += step, ++it) {
+    const int b = it & 1;
+    asm volatile("cp.async.wait_group 1;" ::: "memory");        // this row's classes
+    __syncthreads();
+    finish(it ^ 1);
+    // ---- two and three rows ahead ----
+    s_cls[b][tid] = third.c;                                    // (the row's own have been used)
+    for (int i = tid; i < words; i += kRingThreads) bits[((it + 2) % 3) * words + i] = 0;
+    load_logit(third, row + 2 * step);
+    fetch(third, row + 2 * step, it + 2);
+    const RingRow fourth = load_row(row + 3 * step);
+
+    const bool live = cur.w != 0.f;                             // the same in all threads of the cluster
+    float e[NV][VEC];
+    MaxSum sum = {kLow, 0.f};
+    const T* z = zrow(row);
+    if (live) {
+      const uint4* slot = ring + (it % kRingSlots) * NV * kRingThreads + tid;
+      const uint32_t* set = bits + (it % 3) * words;
+#pragma unroll
+      for (int k = 0; k < NV; ++k) {
+        const int c = first + (k * kRingThreads + tid) * VEC;
+        if (c + VEC <= last) unpack16(slot[k * kRingThreads], e[k]);
+        else load<VEC>(z + c, last - c, -INFINITY, e[k]);        // the row's last few, and past them
+      }
+      if (MODE != DIST_BACKWARD) {
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+#pragma unroll
+          for (int v = 0; v < VEC; ++v) sum.m = fmaxf(sum.m, e[k][v]);
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+          const int at = (k * kRingThreads + tid) * VEC;
+          const uint32_t named = (set[at >> 5] >> (at & 31)) & ((1u << VEC) - 1u);
+          float part = 0.f;
+#pragma unroll
+          for (int v = 0; v < VEC; ++v) {
+            e[k][v] = ex2((e[k][v] - sum.m) * c2);
+            part += e[k][v];
+          }
+          if (named) {
+            part = 0.f;
+#pragma unroll
+            for (int v = 0; v < VEC; ++v)
+              if (!((named >> v) & 1u)) part += e[k][v];
+          }
+          sum.l += part;
+        }
+        const MaxSum s = merge_lanes(sum, c2);
+        if (lane < C) st_cluster_pair(push_at + (uint32_t)turn * (uint32_t)sizeof(s_sum[0]), s);
+        __syncwarp();
+        sm100::cluster_arrive();
+      }
+    }
+    prepare(next, it + 1);
+    __syncwarp();
+    if (live) {
+      if (MODE != DIST_BACKWARD) sm100::cluster_wait();
+      // ---- the teacher's mass, the student's normalisers: see distill_kernel ----
+      const int kw = (p.K + 31) / 32;
+      MaxSum t = lane < kw ? s_teacher[b][lane] : MaxSum{kLow, 0.f};
+      float ts;
+      if (p.t_lse) {
+        ts = t.l;
+#pragma unroll
+        for (int o = 4; o > 0; o >>= 1) ts += __shfl_xor_sync(0xffffffffu, ts, o);
+        ts = __shfl_sync(0xffffffffu, ts, 0);
+      } else {
+#pragma unroll
+        for (int o = 4; o > 0; o >>= 1) t = merge(t, {__shfl_xor_sync(0xffffffffu, t.m, o), __shfl_xor_sync(0xffffffffu, t.l, o)}, c2);
+        t.m = __shfl_sync(0xffffffffu, t.m, 0);
+        ts = __shfl_sync(0xffffffffu, t.l, 0);
+      }
+      const float tm = t.m;
+      const float scale_p = p.t_lse ? 1.f : (ts > 0.f ? 1.f / ts : (ts == 0.f ? 0.f : ts));
+      const float whole = ts * scale_p;
+      float pt = 0.f;
+      if (p.t_lse) pt = 1.f - whole < 0.f ? 0.f : 1.f - whole;
+      const float A = whole + pt;
+      float ref, inv, qt;
+      bool empty;
+      MaxSum all = {kLow, 0.f}, others = {kLow, 0.f};
+      if (MODE != DIST_BACKWARD) {
+        for (int i = lane; i < C * kRingWarps; i += 32) others = merge(others, s_sum[turn][i], c2);
+        others = merge_lanes(others, c2);
+        turn ^= 1;
+        MaxSum n = lane < kw ? s_named[b][lane] : MaxSum{kLow, 0.f};
+#pragma unroll
+        for (int o = 4; o > 0; o >>= 1) n = merge(n, {__shfl_xor_sync(0xffffffffu, n.m, o), __shfl_xor_sync(0xffffffffu, n.l, o)}, c2);
+        n.m = __shfl_sync(0xffffffffu, n.m, 0);
+        n.l = __shfl_sync(0xffffffffu, n.l, 0);
+        all = merge(others, n, c2);
+        empty = all.l == 0.f;
+        ref = all.m;
+        inv = 1.f / all.l;
+        qt = others.l * ex2((others.m - all.m) * c2) * inv;
+      } else {
+        ref = cur.s0;
+        inv = 1.f;
+        empty = ref == -INFINITY;
+        qt = ex2((cur.s1 - ref) * kLog2e);
+      }
+      auto student = [&](float v) { return ex2(MODE == DIST_BACKWARD ? fmaf(v, p.inv_tau, -ref) * kLog2e : (v - ref) * c2) * inv; };
+      const float ws = empty ? 0.f : cur.w * p.inv_tau;
+      if (MODE != DIST_LOSS) {
+        const float other = pt > 0.f && qt != 0.f ? A - pt / qt : A;
+        T* dz = static_cast<T*>(p.dZ) + (int64_t)row * p.lddz;
+        const float f = empty ? 0.f : MODE == DIST_BACKWARD ? ws * other : ws * other * ex2((sum.m - ref) * c2) * inv;
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+          const int c = first + (k * kRingThreads + tid) * VEC;
+          if (c >= last) continue;
+#pragma unroll
+          for (int v = 0; v < VEC; ++v) {
+            if (MODE == DIST_BACKWARD) e[k][v] = empty ? 0.f : f * student(e[k][v]);
+            else e[k][v] *= f;
+          }
+          store<VEC>(dz + c, last - c, e[k]);
+        }
+        if (cur.c >= first && cur.c < last) {
+          late_at = dz + cur.c;
+          late = empty ? 0.f : ws * (A * student(cur.z) - ex2(teacher2(cur.t, cur.t_lse, tm)) * scale_p);
+        }
+      }
+      if (MODE != DIST_BACKWARD && rank == 0) {
+        float kl = 0.f;
+        if (cur.c >= 0) {
+          const float lp = teacher2(cur.t, cur.t_lse, tm), pk = ex2(lp) * scale_p;
+          if (pk > 0.f || pk != pk) kl = pk * ((lp + log2f(scale_p)) - ((cur.z - all.m) * c2 - log2f(all.l)));
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) kl += __shfl_xor_sync(0xffffffffu, kl, o);
+        if (lane == 0) s_kl[b][warp] = kl;
+        if (tid == 0) {
+          late_row = row;
+          late_w = empty ? 0.f : cur.w;
+          late_rest = pt > 0.f ? pt * (log2f(pt) - log2f(qt)) : 0.f;
+          if (whole != whole) late_rest = whole;
+          late_lse = empty ? -INFINITY : fmaf(all.m, p.inv_tau, logf(all.l));
+          late_other = others.l == 0.f ? -INFINITY : fmaf(others.m, p.inv_tau, logf(others.l));
+          if (empty) late_rest = 0.f;
+        }
+        if (empty && lane == 0) s_kl[b][warp] = 0.f;
+      }
+    } else {
+      if (MODE != DIST_LOSS) {
+        const float zero[VEC] = {};
+        T* dz = static_cast<T*>(p.dZ) + (int64_t)row * p.lddz;
+        for (int c = first + tid * VEC; c < last; c += kRingThreads * VEC) store<VEC>(dz + c, last - c, zero);
+      }
+      if (MODE != DIST_BACKWARD && rank == 0 && tid == 0) {
+        p.loss[row] = 0.f;
+        if (p.stat) { p.stat[2 * (int64_t)row] = 0.f; p.stat[2 * (int64_t)row + 1] = 0.f; }
+      }
+    }
+    cur = next;
+    next = third;
+    third = fourth;
+  }
+  __syncthreads();
+  finish(it ^ 1);
+  __syncwarp();
+  asm volatile("cp.async.wait_group 0;" ::: "memory");
+  // no CTA leaves while its sums may still be written by another
+  sm100::cluster_arrive();
+  sm100::cluster_wait();
+}
+
 fw_status desc_check(const fw_distill_desc* d) {
   if (!d) return FW_ERR_INVALID_ARG;
   if (d->V < 1 || d->V > kMaxV || d->K < 1 || d->K > kMaxK || d->K > d->V) return FW_ERR_SHAPE;
@@ -312,8 +637,61 @@ cudaError_t launch(const Distill& p, int C, int threads, int64_t rows, cudaStrea
   return launch_dep_cluster(C, distill_kernel<T, VEC, NV, MODE, KEEP>, dim3((unsigned)(rows * C)), threads, smem, s, p);
 }
 
+template <class T, int NV, int MODE>
+cudaError_t launch_ring(const Distill& p, int C, int64_t rows, cudaStream_t s) {
+  static std::mutex mu;
+  static int resident[64][5];                               // clusters of 1, 2, 4, 8, 16 CTAs at once, per device
+  constexpr size_t smem = (size_t)kRingSlots * NV * kRingThreads * 16 + 3 * (NV * kRingThreads * (16 / sizeof(T)) / 8);
+  auto kernel = distill_ring_kernel<T, NV, MODE>;
+  int dev = 0, n = 0, lg = 0;
+  while ((1 << lg) < C) ++lg;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess || dev < 0 || dev >= 64) return e != cudaSuccess ? e : cudaErrorInvalidDevice;
+  {
+    std::lock_guard<std::mutex> lock(mu);
+    if (resident[dev][lg] == 0) {
+      e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+      if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+      if (e != cudaSuccess) return e;
+      cudaLaunchConfig_t cfg;
+      memset(&cfg, 0, sizeof(cfg));
+      cfg.gridDim = dim3((unsigned)(C * 1024)); cfg.blockDim = dim3(kRingThreads); cfg.dynamicSmemBytes = smem;
+      cudaLaunchAttribute at[1];
+      at[0].id = cudaLaunchAttributeClusterDimension;
+      at[0].val.clusterDim.x = C; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
+      cfg.attrs = at; cfg.numAttrs = 1;
+      if (cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess || n < 1) { cudaGetLastError(); n = 1; }
+      resident[dev][lg] = n;
+    }
+    n = resident[dev][lg];
+  }
+  if (n > rows) n = (int)rows;
+  return launch_dep_cluster(C, kernel, dim3((unsigned)(n * C)), kRingThreads, smem, s, p, (int)rows);
+}
+
+// Rows the ring takes: fewer than 2^28 of up to 16 slices; *C CTAs a row, *nv accesses a thread
+bool ring_shape(int V, int K, int vec, int* C, int* nv) {
+  if (K > kRingMaxK) return false;
+  const int cap = kRingThreads * 8 * vec;
+  int c = 1;
+  while (c <= kRingMaxCtas && c * cap < V) c *= 2;
+  if (c > kRingMaxCtas) return false;
+  *C = c;
+  const int per = (V + c * kRingThreads * vec - 1) / (c * kRingThreads * vec);
+  *nv = per <= 2 ? 2 : per <= 4 ? 4 : 8;
+  return true;
+}
+
 template <class T, int VEC, int MODE>
 cudaError_t launch_mode(Distill p, int64_t rows, cudaStream_t s) {
+  int ring_ctas = 0, ring_nv = 0;
+  if (VEC > 1 && p.V > 2048 && ring_shape(p.V, p.K, VEC, &ring_ctas, &ring_nv)) {
+    p.slice = (p.V + ring_ctas - 1) / ring_ctas;
+    p.slice = (p.slice + 31) / 32 * 32;
+    if (ring_nv == 2) return launch_ring<T, 2, MODE>(p, ring_ctas, rows, s);
+    if (ring_nv == 4) return launch_ring<T, 4, MODE>(p, ring_ctas, rows, s);
+    return launch_ring<T, 8, MODE>(p, ring_ctas, rows, s);
+  }
   constexpr int NV = VEC == 1 ? 16 : 32 / VEC;              // 32 classes of a thread in registers (16 single ones)
   constexpr int few = VEC == 1 ? 4 : 1;
   // threads and CTAs of a row: enough that the row is one trip, as far as 8 CTAs of 512 threads go

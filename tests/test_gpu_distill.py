@@ -13,7 +13,7 @@ pytestmark = pytest.mark.gpu
 
 KINDS = {"f32": torch.float32, "bf16": torch.bfloat16}
 SIZES = [(3, 1, 1), (1, 2, 2), (5, 100, 10), (37, 1000, 10), (7, 1025, 33), (4, 2048, 1024), (3, 8191, 64), (2, 50021, 33),
-         (2, 131072, 64), (2, 131101, 100), (1, 300001, 7), (1, 1 << 20, 130)]
+         (5, 3000, 256), (2, 9000, 257), (2, 131072, 64), (2, 131101, 100), (2, 250000, 256), (1, 300001, 7), (1, 1 << 20, 130)]
 
 
 @pytest.fixture(scope="module")
@@ -188,6 +188,27 @@ def test_special_rows(B, kind, rest):
     zz = put(z, KINDS[kind])
     B.fw_distill_forward(d, zz, T, I, loss, t_lse=tl, weight=weight, dZ=zz)
     assert torch.equal(zz[keep], dz[keep])
+
+
+@pytest.mark.parametrize("V,rows", [(9000, 700), (50000, 150), (131072, 90)])
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+def test_many_rows_with_gaps(B, V, rows, kind):
+    """Several rows for every cluster, some of weight 0 among them, in runs of one to three."""
+    z, T, I, t_lse = inputs(rows, V, 70, kind, V, pad=None)
+    I[::5, 60:] = I[::5, :10]                               # classes named twice
+    weight = torch.where(torch.rand(rows, generator=gen(4), device="cuda") < 0.4, 0.0, 1.5)
+    d = desc(B, V, 70, kind)
+    loss, stat, dz, dz2 = torch.empty(rows, device="cuda"), torch.empty(rows, 2, device="cuda"), matrix(rows, V, KINDS[kind], pad=None), matrix(rows, V, KINDS[kind], pad=None)
+    B.fw_distill_forward(d, z, T, I, loss, stat=stat, t_lse=t_lse + 0.05, weight=weight, dZ=dz)
+    B.fw_distill_backward(d, z, T, I, stat, dz2, t_lse=t_lse + 0.05, weight=weight)
+    for r0 in range(0, rows, 50):
+        r = slice(r0, r0 + 50)
+        want = reference(z[r], T[r], I[r], 1.0, t_lse[r] + 0.05, weight[r])
+        check(loss[r], want[0], want[3])
+        check_stat(stat[r], want[1])
+        check(dz[r], want[2], want[4], HALF[KINDS[kind]])
+        check(dz2[r], want[2], stat_bound(want), HALF[KINDS[kind]])
+    assert surround_kept(dz) and surround_kept(dz2)
 
 
 @pytest.mark.parametrize("V", [40000, 200003])
