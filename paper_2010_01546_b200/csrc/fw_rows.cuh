@@ -8,6 +8,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include "fw_lanes.cuh"
+
 namespace fw {
 namespace rows {
 
@@ -92,6 +94,100 @@ __device__ __forceinline__ void store(__nv_fp8_storage_t* p, int n, const float 
   }
 }
 
+// ---- element by element over a vector, two at a time where there are two (f32x2: half the issue slots) ----
+template <int VEC>
+__device__ __forceinline__ void vadd(float (&a)[VEC], const float (&b)[VEC]) {             // a += b
+  if (VEC == 1) a[0] += b[0];
+#pragma unroll
+  for (int e = 0; e + 1 < VEC; e += 2) unpack2(add2(pack2(a[e], a[e + 1]), pack2(b[e], b[e + 1])), a[e], a[e + 1]);
+}
+template <int VEC>
+__device__ __forceinline__ void vmul(float (&a)[VEC], const float (&b)[VEC]) {             // a *= b
+  if (VEC == 1) a[0] *= b[0];
+#pragma unroll
+  for (int e = 0; e + 1 < VEC; e += 2) unpack2(times2(pack2(a[e], a[e + 1]), pack2(b[e], b[e + 1])), a[e], a[e + 1]);
+}
+template <int VEC>
+__device__ __forceinline__ void vscale(float (&a)[VEC], float s) {                         // a *= s
+  if (VEC == 1) a[0] *= s;
+  const u64 ss = pack2(s, s);
+#pragma unroll
+  for (int e = 0; e + 1 < VEC; e += 2) unpack2(times2(pack2(a[e], a[e + 1]), ss), a[e], a[e + 1]);
+}
+template <int VEC>
+__device__ __forceinline__ void vfma(float (&c)[VEC], const float (&a)[VEC], const float (&b)[VEC]) {   // c += a b
+  if (VEC == 1) c[0] = fmaf(a[0], b[0], c[0]);
+#pragma unroll
+  for (int e = 0; e + 1 < VEC; e += 2)
+    unpack2(fmadd2(pack2(a[e], a[e + 1]), pack2(b[e], b[e + 1]), pack2(c[e], c[e + 1])), c[e], c[e + 1]);
+}
+template <int VEC>
+__device__ __forceinline__ void vfma(float (&c)[VEC], const float (&a)[VEC], float s) {    // c += a s
+  if (VEC == 1) c[0] = fmaf(a[0], s, c[0]);
+  const u64 ss = pack2(s, s);
+#pragma unroll
+  for (int e = 0; e + 1 < VEC; e += 2) unpack2(fmadd2(pack2(a[e], a[e + 1]), ss, pack2(c[e], c[e + 1])), c[e], c[e + 1]);
+}
+template <int VEC>
+__device__ __forceinline__ void vdot(float (&c)[2], const float (&a)[VEC], const float (&b)[VEC]) {     // c: two sums of products
+  if (VEC == 1) c[0] = fmaf(a[0], b[0], c[0]);
+  u64 acc = pack2(c[0], c[1]);
+#pragma unroll
+  for (int e = 0; e + 1 < VEC; e += 2) acc = fmadd2(pack2(a[e], a[e + 1]), pack2(b[e], b[e + 1]), acc);
+  if (VEC > 1) unpack2(acc, c[0], c[1]);
+}
+
+// ---- rows on their way to shared memory ahead of their use (cp.async) ----
+// Aligned rows (VEC > 1): a thread copies its own accesses of 16 bytes and reads back those alone, so that no barrier stands
+// between.  Other rows (VEC = 1): the threads of the row copy the aligned 16 bytes that it touches (the first of them may begin
+// with the end of the row before; past its end nothing is read), and read elements after a barrier.
+__device__ __forceinline__ void ahead16(uint32_t to, const void* from) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+}
+__device__ __forceinline__ void ahead16(uint32_t to, const void* from, int bytes) {         // the rest is filled with zeros
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory");
+}
+template <class T, int VEC, int NV>
+struct Ahead {
+  // bytes of one row of one tensor for `threads` threads of which `width` share a row
+  static __host__ __device__ __forceinline__ uint32_t row_bytes(int M, int threads, int width) {
+    if (VEC > 1) return (uint32_t)(NV * threads * 16);
+    return (uint32_t)((M * (int)sizeof(T) + 15) / 16 * 16 + 16) * (threads / width);
+  }
+  // room: shared address of this tensor's row
+  static __device__ __forceinline__ void fetch(uint32_t room, const T* row, int M, int width) {
+    const int tid = threadIdx.x, t = tid & (width - 1), nt = blockDim.x;
+    if (VEC > 1) {
+#pragma unroll
+      for (int k = 0; k < NV; ++k) {
+        const int c = (t + k * width) * VEC;
+        if (c + VEC <= M) ahead16(room + (k * nt + tid) * 16, row + c);
+      }
+    } else {
+      const uintptr_t a = reinterpret_cast<uintptr_t>(row), a0 = a & ~(uintptr_t)15, end = a + (uintptr_t)M * sizeof(T);
+      const uint32_t at = room + (tid / width) * row_bytes(M, 1, 1);
+      for (uintptr_t p = a0 + 16 * t; p < end; p += 16 * width) {
+        const int left = (int)(end - p < 16 ? end - p : 16);
+        ahead16(at + (uint32_t)(p - a0), reinterpret_cast<const void*>(p), left);
+      }
+    }
+  }
+  // this thread's k-th access, n > 0 elements of it valid
+  static __device__ __forceinline__ void get(const uint8_t* room, const T* row, int M, int width, int k, int c, int n, float (&o)[VEC]) {
+    const int tid = threadIdx.x;
+    if (VEC > 1) {
+      if (n >= VEC) load<VEC>(reinterpret_cast<const T*>(room + (k * (int)blockDim.x + tid) * 16), VEC, 0.f, o);
+      else load<VEC>(row + c, n, 0.f, o);
+    } else {
+      const uint8_t* at = room + (tid / width) * row_bytes(M, 1, 1) + (reinterpret_cast<uintptr_t>(row) & 15);
+      o[0] = n > 0 ? to_f(reinterpret_cast<const T*>(at)[c]) : 0.f;
+    }
+  }
+};
+__device__ __forceinline__ void ahead_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void ahead_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }   // all but the last N groups
+
 // A value as its own type holds it.
 __device__ __forceinline__ float held(float v, const float*) { return v; }
 __device__ __forceinline__ float held(float v, const __nv_bfloat16*) { return __bfloat162float(__float2bfloat16_rn(v)); }
@@ -103,9 +199,11 @@ __device__ __forceinline__ float ex2(float x) {
   return y;
 }
 
-// The larger of two non-negative numbers, a NaN if one of them is: as bit patterns NaN lies above infinity.
+// The larger of two numbers, a NaN if one of them is.
 __device__ __forceinline__ float max_keep_nan(float a, float b) {
-  return __uint_as_float(max(__float_as_uint(a), __float_as_uint(b)));
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
 }
 
 struct Sum { __device__ static float of(float a, float b) { return a + b; } };
