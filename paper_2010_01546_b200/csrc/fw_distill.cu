@@ -420,7 +420,7 @@ __global__ void __launch_bounds__(kRingThreads, 2) distill_ring_kernel(const Dis
     if (lane == 0) { s_teacher[it & 1][warp] = t; s_named[it & 1][warp] = n; }
   };
 
-  dep_sync();
+  dep_wait();
   // ---- the first three rows ----
   RingRow cur = load_row(row0), next = load_row(row0 + step), third = load_row(row0 + 2 * step);
   fetch(cur, row0, 0);
@@ -613,6 +613,7 @@ __global__ void __launch_bounds__(kRingThreads, 2) distill_ring_kernel(const Dis
     next = third;
     third = fourth;
   }
+  dep_trigger();
   __syncthreads();
   finish(it ^ 1);
   __syncwarp();

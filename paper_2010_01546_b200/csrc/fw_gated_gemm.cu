@@ -145,7 +145,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(GG_THREADS, 1) gated
     }
     mbar_fence_init();
   }
-  dep_sync();
+  rows::dep_wait();
   if (warp == 2) {
     tmem_alloc_pair(smem_u32(&tmem_base_sh), 512);
     tmem_relinquish_pair();
@@ -404,6 +404,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(GG_THREADS, 1) gated
     if (issuer) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");       // no CTA leaves before its copies have
   }
 #undef GG_ABORT
+  rows::dep_trigger();
   tc_fence_before();
   cluster_arrive();
   cluster_wait();

@@ -43,63 +43,63 @@ __device__ __forceinline__ void round_pairs(float (&v)[8], const __nv_bfloat16*)
   }
 }
 
-// T: type of x, r and s; Y: of y.  VEC elements an access, NV accesses a thread; SLOTS rows of a thread group on their way.
-// A CTA's groups of p.width threads walk the rows.  With a CTA a row the loads of a row waited for nothing but the sums, the
-// largest value and the stores of the rows before it: 8192 x 4096 bf16 to e4m3 71.5 us.
-template <class T, class Y, int VEC, int NV, int SLOTS, bool RES>
+// T: type of x, r and s; Y: of y.  VEC elements an access, NV accesses a thread; SLOTS rows of a CTA on their way.
+// A CTA walks the rows, one at a time.  With a CTA launched for each row its loads waited for nothing but the sums, the largest
+// value and the stores of the rows before it: 8192 x 4096 bf16 to e4m3 71.5 us.
+template <class T, class Y, int VEC, int NV, int SLOTS, bool RES, int FILL>
 __global__ void __launch_bounds__(512) norm_forward_kernel(const NormFwd p) {
-  typedef Ahead<T, VEC, NV> Ring;
+  typedef Ahead<T, VEC, NV, FILL> Ring;
   extern __shared__ __align__(16) uint8_t room[];            // [slot][x, res]
   __shared__ float buf[2][2][16];
-  const int tid = threadIdx.x, t = tid & (p.width - 1), nt = blockDim.x, per = nt / p.width, mine = tid / p.width;
-  const int64_t step = (int64_t)gridDim.x * per;
-  const uint32_t row_bytes = Ring::row_bytes(p.M, nt, p.width), slot_bytes = row_bytes * (RES ? 2 : 1);
+  const int t = threadIdx.x, width = blockDim.x;
+  const uint32_t row_bytes = Ring::row_bytes(p.M, width, width), slot_bytes = row_bytes * (RES ? 2 : 1);
   const uint32_t base = (uint32_t)__cvta_generic_to_shared(room);
   auto x_row = [&](int64_t row) { return static_cast<const T*>(p.x) + row * p.ldx; };
   auto r_row = [&](int64_t row) { return static_cast<const T*>(p.res) + row * p.ldr; };
   auto fetch = [&](int64_t row, int i) {
     if (row < p.rows) {
-      Ring::fetch(base + i * slot_bytes, x_row(row), p.M, p.width);
-      if (RES) Ring::fetch(base + i * slot_bytes + row_bytes, r_row(row), p.M, p.width);
+      Ring::fetch(base + i * slot_bytes, x_row(row), p.M, t, width);
+      if (RES) Ring::fetch(base + i * slot_bytes + row_bytes, r_row(row), p.M, t, width);
     }
     ahead_commit();
   };
-  dep_sync();
-  const int64_t first = (int64_t)blockIdx.x * per;
+  dep_wait();
 #pragma unroll
-  for (int i = 0; i < SLOTS; ++i) fetch(first + mine + i * step, i);
+  for (int i = 0; i < SLOTS; ++i) fetch((int64_t)blockIdx.x + (int64_t)i * gridDim.x, i);
   int i = 0, flip = 0;
-  for (int64_t row0 = first; row0 < p.rows; row0 += step, flip ^= 1) {
-    const int64_t row = row0 + mine;
-    const bool live = row < p.rows;
+  for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x, flip ^= 1) {
     const uint8_t* slot = room + i * slot_bytes;
     ahead_wait<SLOTS - 1>();
     if (VEC == 1) __syncthreads();
     float v[NV][VEC];
     float sq[2] = {0.f, 0.f};
+    const T* x = x_row(row);
+    const T* res = RES ? r_row(row) : nullptr;
+    T* sum = p.sum ? static_cast<T*>(p.sum) + row * p.lds : nullptr;
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
-      const int c = (t + k * p.width) * VEC, n = live ? p.M - c : 0;
-      Ring::get(slot, x_row(row), p.M, p.width, k, c, n, v[k]);
+      const uint32_t c = (uint32_t)(t + k * width) * VEC;
+      const int n = p.M - (int)c;
+      Ring::get(slot, x, p.M, width, k, c, n, v[k]);
       if (RES) {
         float r[VEC];
-        Ring::get(slot + row_bytes, r_row(row), p.M, p.width, k, c, n, r);
+        Ring::get(slot + row_bytes, res, p.M, width, k, c, n, r);
         vadd<VEC>(v[k], r);
         round_pairs(v[k], static_cast<const T*>(nullptr));
-        if (p.sum && live) store<VEC>(static_cast<T*>(p.sum) + row * p.lds + c, n, v[k]);
+        if (sum) Ring::keep(sum + c, n, v[k]);
       }
       vdot<VEC>(sq, v[k], v[k]);
     }
-    const float ss = over_group<Sum>(sq[0] + sq[1], p.width, buf[flip][0]);
-    fetch(row + SLOTS * step, i);                            // the slot has been read: the sum of the row's threads depends on it
+    const float ss = over_group<Sum>(sq[0] + sq[1], width, buf[flip][0]);
+    fetch(row + (int64_t)SLOTS * gridDim.x, i);              // the slot has been read: the sum of its threads depends on it
     const float rstd = rsqrtf(fmaf(ss, p.inv_M, p.eps));
-    if (t == 0 && live && p.rstd) p.rstd[row] = rstd;
+    if (t == 0 && p.rstd) p.rstd[row] = rstd;
     float top = 0.f;
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
-      const int c = (t + k * p.width) * VEC;
+      const uint32_t c = (uint32_t)(t + k * width) * VEC;
       float w[VEC];
-      load<VEC>(p.w + c, p.M - c, 0.f, w);
+      Ring::plain(p.w + c, p.M - (int)c, w);
       vscale<VEC>(v[k], rstd);
       vmul<VEC>(v[k], w);
       if (sizeof(Y) == 1) {
@@ -109,24 +109,24 @@ __global__ void __launch_bounds__(512) norm_forward_kernel(const NormFwd p) {
     }
     float inv = 1.f;
     if (sizeof(Y) == 1) {
-      top = over_group<MaxAbs>(top, p.width, buf[flip][1]);
+      top = over_group<MaxAbs>(top, width, buf[flip][1]);
       float scale = 1.f;
       if (top != 0.f) scale = top * (1.f / kE4m3Max);
       if (scale < kMinScale) scale = kMinScale;              // a NaN stays
-      if (t == 0 && live) p.y_scale[row] = scale;
+      if (t == 0) p.y_scale[row] = scale;
       inv = 1.f / scale;
     }
-    if (live) {
+    Y* y = static_cast<Y*>(p.y) + row * p.ldy;
 #pragma unroll
-      for (int k = 0; k < NV; ++k) {
-        const int c = (t + k * p.width) * VEC;
-        if (sizeof(Y) == 1) vscale<VEC>(v[k], inv);
-        store<VEC>(static_cast<Y*>(p.y) + row * p.ldy + c, p.M - c, v[k]);
-      }
+    for (int k = 0; k < NV; ++k) {
+      const uint32_t c = (uint32_t)(t + k * width) * VEC;
+      if (sizeof(Y) == 1) vscale<VEC>(v[k], inv);
+      Ring::keep(y + c, p.M - (int)c, v[k]);
     }
     if (++i == SLOTS) i = 0;
   }
   ahead_wait<0>();
+  dep_trigger();
 }
 
 struct NormBwd {
@@ -141,27 +141,29 @@ struct NormBwd {
 
 // A CTA takes every gridDim-th group of rows and keeps its columns' share of dw in registers, so that the sums over the rows have
 // a fixed order and cost one row of partial sums a CTA.  Rows are on their way as in the forward kernel.
-template <class T, int VEC, int NV, int SLOTS, bool DS>
+// SOLO: a row at a time (p.width is the CTA), else several.
+template <class T, int VEC, int NV, int SLOTS, bool DS, int FILL, bool SOLO>
 __global__ void __launch_bounds__(512) norm_backward_kernel(const NormBwd p) {
-  typedef Ahead<T, VEC, NV> Ring;
+  typedef Ahead<T, VEC, NV, FILL> Ring;
   extern __shared__ __align__(16) uint8_t room[];            // [slot][dy, s, ds], at the end the groups' sums
   __shared__ float buf[2][16];
-  const int tid = threadIdx.x, t = tid & (p.width - 1), nt = blockDim.x, per = nt / p.width, mine = tid / p.width;
+  const int tid = threadIdx.x, nt = blockDim.x, width = SOLO ? nt : p.width, t = SOLO ? tid : tid & (width - 1);
+  const int per = SOLO ? 1 : nt / width, mine = SOLO ? 0 : tid / width;
   const int64_t step = (int64_t)gridDim.x * per;
-  const uint32_t row_bytes = Ring::row_bytes(p.M, nt, p.width), slot_bytes = row_bytes * (DS ? 3 : 2);
+  const uint32_t row_bytes = Ring::row_bytes(p.M, nt, width), slot_bytes = row_bytes * (DS ? 3 : 2);
   const uint32_t base = (uint32_t)__cvta_generic_to_shared(room);
   auto u_row = [&](int64_t row) { return static_cast<const T*>(p.dy) + row * p.lddy; };
   auto s_row = [&](int64_t row) { return static_cast<const T*>(p.s) + row * p.lds; };
   auto d_row = [&](int64_t row) { return static_cast<const T*>(p.ds) + row * p.ldds; };
   auto fetch = [&](int64_t row, int i) {
     if (row < p.rows) {
-      Ring::fetch(base + i * slot_bytes, u_row(row), p.M, p.width);
-      Ring::fetch(base + i * slot_bytes + row_bytes, s_row(row), p.M, p.width);
-      if (DS) Ring::fetch(base + i * slot_bytes + 2 * row_bytes, d_row(row), p.M, p.width);
+      Ring::fetch(base + i * slot_bytes, u_row(row), p.M, t, width);
+      Ring::fetch(base + i * slot_bytes + row_bytes, s_row(row), p.M, t, width);
+      if (DS) Ring::fetch(base + i * slot_bytes + 2 * row_bytes, d_row(row), p.M, t, width);
     }
     ahead_commit();
   };
-  dep_sync();
+  dep_wait();
   float dw[NV][VEC];
 #pragma unroll
   for (int k = 0; k < NV; ++k)
@@ -174,37 +176,41 @@ __global__ void __launch_bounds__(512) norm_backward_kernel(const NormBwd p) {
   int i = 0, flip = 0;
   for (int64_t row0 = first; row0 < p.rows; row0 += step, flip ^= 1) {
     const int64_t row = row0 + mine;
-    const bool live = row < p.rows;
+    const bool live = SOLO || row < p.rows;
     const float rstd_next = row + step < p.rows ? p.rstd[row + step] : 0.f;
     const uint8_t* slot = room + i * slot_bytes;
     ahead_wait<SLOTS - 1>();
     if (VEC == 1) __syncthreads();
     float u[NV][VEC], n[NV][VEC];
+    const T *dy = u_row(row), *s = s_row(row), *ds = DS ? d_row(row) : nullptr;
+    T* dx = static_cast<T*>(p.dx) + row * p.lddx;
     float dots[2] = {0.f, 0.f};
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
-      const int c = (t + k * p.width) * VEC, left = live ? p.M - c : 0;
-      Ring::get(slot, u_row(row), p.M, p.width, k, c, left, u[k]);
-      Ring::get(slot + row_bytes, s_row(row), p.M, p.width, k, c, left, n[k]);
+      const uint32_t c = (uint32_t)(t + k * width) * VEC;
+      const int left = live ? p.M - (int)c : 0;
+      Ring::get(slot, dy, p.M, width, k, c, left, u[k]);
+      Ring::get(slot + row_bytes, s, p.M, width, k, c, left, n[k]);
       float w[VEC];
-      load<VEC>(p.w + c, p.M - c, 0.f, w);
+      Ring::plain(p.w + c, p.M - (int)c, w);
       vscale<VEC>(n[k], rstd);
       vfma<VEC>(dw[k], u[k], n[k]);
       vmul<VEC>(u[k], w);
       vdot<VEC>(dots, u[k], n[k]);
     }
-    const float dot = over_group<Sum>(dots[0] + dots[1], p.width, buf[flip]) * -p.inv_M;
+    const float dot = over_group<Sum>(dots[0] + dots[1], width, buf[flip]) * -p.inv_M;
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
-      const int c = (t + k * p.width) * VEC;
+      const uint32_t c = (uint32_t)(t + k * width) * VEC;
+      const int left = live ? p.M - (int)c : 0;
       vfma<VEC>(u[k], n[k], dot);
       vscale<VEC>(u[k], rstd);
       if (DS) {
         float add[VEC];
-        Ring::get(slot + 2 * row_bytes, d_row(row), p.M, p.width, k, c, live ? p.M - c : 0, add);
+        Ring::get(slot + 2 * row_bytes, ds, p.M, width, k, c, left, add);
         vadd<VEC>(u[k], add);
       }
-      if (live) store<VEC>(static_cast<T*>(p.dx) + row * p.lddx + c, p.M - c, u[k]);
+      if (live) Ring::keep(dx + c, p.M - (int)c, u[k]);
     }
     // the slot is given away when every thread that reads it has: itself, or (VEC = 1) the row's
     if (VEC == 1 && DS) __syncthreads();
@@ -213,13 +219,14 @@ __global__ void __launch_bounds__(512) norm_backward_kernel(const NormBwd p) {
     if (++i == SLOTS) i = 0;
   }
   ahead_wait<0>();
+  dep_trigger();
   if (!p.part) return;
   // the groups of the CTA in order, then the CTA's row of sums
   float* out = p.part + (int64_t)blockIdx.x * p.M;
-  if (per == 1) {
+  if (SOLO) {
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
-      const int c = (t + k * p.width) * VEC;
+      const int c = (t + k * width) * VEC;
 #pragma unroll
       for (int e = 0; e < VEC; ++e)
         if (c + e < p.M) out[c + e] = dw[k][e];
@@ -230,7 +237,7 @@ __global__ void __launch_bounds__(512) norm_backward_kernel(const NormBwd p) {
   __syncthreads();
 #pragma unroll
   for (int k = 0; k < NV; ++k) {
-    const int c = (t + k * p.width) * VEC;
+    const int c = (t + k * width) * VEC;
 #pragma unroll
     for (int e = 0; e < VEC; ++e)
       if (c + e < p.M) shared[mine * p.M + c + e] = dw[k][e];
@@ -318,23 +325,29 @@ cudaError_t fill(F* kernel, SmemAttrCache& cache, int threads, size_t smem, int6
   return cudaSuccess;
 }
 
-// Rows on their way: 128 bytes of them a thread, 1024 threads a SM.  Where they are not aligned two, or one of more than 8192
+// Rows on their way: 256 bytes of them a thread.  Where they are not aligned two, or one of more than 8192
 // elements (three tensors of 64 KB fit a SM once)
 constexpr int slots(int vec, int nv, int tensors) {
-  const int n = vec > 1 ? 128 / (16 * nv * tensors) : nv > 16 ? 1 : 2;
+  const int n = vec > 1 ? 256 / (16 * nv * tensors) : nv > 16 ? 1 : 2;
   return n < 1 ? 1 : n > 4 ? 4 : n;
 }
 
-template <class T, class Y, int VEC, int NV, bool RES>
+template <class T, class Y, int VEC, int NV, bool RES, int FILL>
 cudaError_t forward_launch(const NormFwd& p, cudaStream_t s) {
   constexpr int SLOTS = slots(VEC, NV, RES ? 2 : 1);
   static SmemAttrCache cache;
-  auto kernel = norm_forward_kernel<T, Y, VEC, NV, SLOTS, RES>;
-  const int threads = p.width < 128 ? 128 : p.width, per = threads / p.width;
-  const size_t smem = (size_t)SLOTS * (RES ? 2 : 1) * Ahead<T, VEC, NV>::row_bytes(p.M, threads, p.width);
+  auto kernel = norm_forward_kernel<T, Y, VEC, NV, SLOTS, RES, FILL>;
+  const size_t smem = (size_t)SLOTS * (RES ? 2 : 1) * Ahead<T, VEC, NV, FILL>::row_bytes(p.M, p.width, p.width);
   int ctas = 0;
-  const cudaError_t e = fill(kernel, cache, threads, smem, (p.rows + per - 1) / per, 1 << 30, &ctas);
-  return e != cudaSuccess ? e : launch_dep(kernel, ctas, threads, smem, s, p);
+  const cudaError_t e = fill(kernel, cache, p.width, smem, p.rows, 1 << 30, &ctas);
+  return e != cudaSuccess ? e : launch_dep(kernel, ctas, p.width, smem, s, p);
+}
+template <class T, class Y, int VEC, int NV, bool RES>
+cudaError_t forward_launch(const NormFwd& p, cudaStream_t s) {
+  constexpr int WHOLE = VEC > 1 ? ROW_WHOLE : ROW_PART, FULL = VEC > 1 ? ROW_FULL : ROW_PART;
+  if (VEC > 1 && p.M == NV * VEC * p.width) return forward_launch<T, Y, VEC, NV, RES, FULL>(p, s);
+  if (VEC > 1 && p.M % VEC == 0) return forward_launch<T, Y, VEC, NV, RES, WHOLE>(p, s);
+  return forward_launch<T, Y, VEC, NV, RES, ROW_PART>(p, s);
 }
 template <class T, class Y, int VEC, int NV>
 cudaError_t forward_launch(const NormFwd& p, cudaStream_t s) {
@@ -364,16 +377,26 @@ cudaError_t forward_vec(const NormFwd& p, bool vec, cudaStream_t s) {
 
 int backward_ctas() { return 4 * sm_count(); }
 
-template <class T, int VEC, int NV, bool DS>
+template <class T, int VEC, int NV, bool DS, int FILL, bool SOLO>
 cudaError_t backward_launch(const NormBwd& p, cudaStream_t s, int* ctas) {
-  constexpr int SLOTS = slots(VEC, NV, 2);
+  constexpr int SLOTS = slots(VEC, NV, DS ? 3 : 2);
   static SmemAttrCache cache;
-  auto kernel = norm_backward_kernel<T, VEC, NV, SLOTS, DS>;
-  const int threads = p.width < 128 ? 128 : p.width, per = threads / p.width;
-  size_t smem = (size_t)SLOTS * (DS ? 3 : 2) * Ahead<T, VEC, NV>::row_bytes(p.M, threads, p.width);
-  if (per > 1 && p.part && smem < (size_t)per * p.M * sizeof(float)) smem = (size_t)per * p.M * sizeof(float);
+  auto kernel = norm_backward_kernel<T, VEC, NV, SLOTS, DS, FILL, SOLO>;
+  const int threads = SOLO ? p.width : 128, per = threads / p.width;
+  size_t smem = (size_t)SLOTS * (DS ? 3 : 2) * Ahead<T, VEC, NV, FILL>::row_bytes(p.M, threads, p.width);
+  if (!SOLO && p.part && smem < (size_t)per * p.M * sizeof(float)) smem = (size_t)per * p.M * sizeof(float);
   const cudaError_t e = fill(kernel, cache, threads, smem, (p.rows + per - 1) / per, backward_ctas(), ctas);
   return e != cudaSuccess ? e : launch_dep(kernel, *ctas, threads, smem, s, p);
+}
+template <class T, int VEC, int NV, bool DS>
+cudaError_t backward_launch(const NormBwd& p, cudaStream_t s, int* ctas) {
+  constexpr int WHOLE = VEC > 1 ? ROW_WHOLE : ROW_PART, FULL = VEC > 1 ? ROW_FULL : ROW_PART;
+  if (p.width < 128)
+    return VEC > 1 && p.M % VEC == 0 ? backward_launch<T, VEC, NV, DS, WHOLE, false>(p, s, ctas)
+                                     : backward_launch<T, VEC, NV, DS, ROW_PART, false>(p, s, ctas);
+  if (VEC > 1 && p.M == NV * VEC * p.width) return backward_launch<T, VEC, NV, DS, FULL, true>(p, s, ctas);
+  if (VEC > 1 && p.M % VEC == 0) return backward_launch<T, VEC, NV, DS, WHOLE, true>(p, s, ctas);
+  return backward_launch<T, VEC, NV, DS, ROW_PART, true>(p, s, ctas);
 }
 template <class T, int VEC, int NV>
 cudaError_t backward_launch(const NormBwd& p, cudaStream_t s, int* ctas) {

@@ -13,6 +13,12 @@
 namespace fw {
 namespace rows {
 
+// The two halves of dep_sync (fw_internal.h) for kernels whose CTAs stay and walk over their work: the dependents of such a grid
+// come when its CTAs are through.  Earlier they take places beside those that still run, and the grid after next starts
+// where there is room, not where there is time: norm backward of 8192 x 4096 in a row of calls 97 us, this way PLACEHOLDER.
+__device__ __forceinline__ void dep_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void dep_trigger() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
 // Two bf16 of a 32-bit word, the lower address first.
 __device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
@@ -147,41 +153,53 @@ __device__ __forceinline__ void ahead16(uint32_t to, const void* from) {
 __device__ __forceinline__ void ahead16(uint32_t to, const void* from, int bytes) {         // the rest is filled with zeros
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory");
 }
-template <class T, int VEC, int NV>
+// How a row fills its threads' accesses: it ends inside one, with one, or it fills all of them
+enum { ROW_PART = 0, ROW_WHOLE = 1, ROW_FULL = 2 };
+template <class T, int VEC, int NV, int FILL>
 struct Ahead {
   // bytes of one row of one tensor for `threads` threads of which `width` share a row
   static __host__ __device__ __forceinline__ uint32_t row_bytes(int M, int threads, int width) {
     if (VEC > 1) return (uint32_t)(NV * threads * 16);
     return (uint32_t)((M * (int)sizeof(T) + 15) / 16 * 16 + 16) * (threads / width);
   }
-  // room: shared address of this tensor's row
-  static __device__ __forceinline__ void fetch(uint32_t room, const T* row, int M, int width) {
-    const int tid = threadIdx.x, t = tid & (width - 1), nt = blockDim.x;
+  // room: shared address of this tensor's row; t: the thread's place in its group
+  static __device__ __forceinline__ void fetch(uint32_t room, const T* row, int M, int t, int width) {
+    const int tid = threadIdx.x, nt = blockDim.x;
     if (VEC > 1) {
 #pragma unroll
       for (int k = 0; k < NV; ++k) {
         const int c = (t + k * width) * VEC;
-        if (c + VEC <= M) ahead16(room + (k * nt + tid) * 16, row + c);
+        if (FILL == ROW_FULL || c + VEC <= M) ahead16(room + (uint32_t)(k * nt + tid) * 16u, row + (uint32_t)c);
       }
     } else {
       const uintptr_t a = reinterpret_cast<uintptr_t>(row), a0 = a & ~(uintptr_t)15, end = a + (uintptr_t)M * sizeof(T);
-      const uint32_t at = room + (tid / width) * row_bytes(M, 1, 1);
+      const uint32_t at = room + (uint32_t)(tid / width) * row_bytes(M, 1, 1);
       for (uintptr_t p = a0 + 16 * t; p < end; p += 16 * width) {
         const int left = (int)(end - p < 16 ? end - p : 16);
         ahead16(at + (uint32_t)(p - a0), reinterpret_cast<const void*>(p), left);
       }
     }
   }
-  // this thread's k-th access, n > 0 elements of it valid
+  // this thread's k-th access, elements c .. c + VEC of the row, n of them valid (zeros in place of the others)
   static __device__ __forceinline__ void get(const uint8_t* room, const T* row, int M, int width, int k, int c, int n, float (&o)[VEC]) {
     const int tid = threadIdx.x;
     if (VEC > 1) {
-      if (n >= VEC) load<VEC>(reinterpret_cast<const T*>(room + (k * (int)blockDim.x + tid) * 16), VEC, 0.f, o);
-      else load<VEC>(row + c, n, 0.f, o);
+      if (FILL == ROW_FULL || (FILL == ROW_WHOLE ? n > 0 : n >= VEC)) load<VEC>(reinterpret_cast<const T*>(room + (k * (int)blockDim.x + tid) * 16), VEC, 0.f, o);
+      else load<VEC>(row + c, FILL == ROW_WHOLE ? 0 : n, 0.f, o);
     } else {
       const uint8_t* at = room + (tid / width) * row_bytes(M, 1, 1) + (reinterpret_cast<uintptr_t>(row) & 15);
       o[0] = n > 0 ? to_f(reinterpret_cast<const T*>(at)[c]) : 0.f;
     }
+  }
+  // n elements at most; a whole access or none where rows are whole
+  template <class Y>
+  static __device__ __forceinline__ void keep(Y* p, int n, const float (&v)[VEC]) {
+    if (FILL == ROW_FULL) store<VEC>(p, VEC, v);
+    else if (FILL == ROW_WHOLE) { if (n > 0) store<VEC>(p, VEC, v); }
+    else store<VEC>(p, n, v);
+  }
+  static __device__ __forceinline__ void plain(const float* p, int n, float (&v)[VEC]) {
+    load<VEC>(p, FILL == ROW_FULL ? VEC : FILL == ROW_WHOLE ? (n > 0 ? VEC : 0) : n, 0.f, v);
   }
 };
 __device__ __forceinline__ void ahead_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
@@ -210,20 +228,19 @@ struct Sum { __device__ static float of(float a, float b) { return a + b; } };
 struct MaxAbs { __device__ static float of(float a, float b) { return max_keep_nan(a, b); } };
 
 // One value for each group of `width` threads (a power of two, 32 or more, within the CTA), the same bits in every thread: lanes
-// in pairs, then warps in order.  Every thread of the CTA comes here; buf: a float for each warp of the CTA, not used
+// in pairs, then warps in pairs.  Every thread of the CTA comes here; buf: a float for each warp of the CTA, not used
 // again before another barrier of the CTA.
 template <class Op>
 __device__ __forceinline__ float over_group(float v, int width, float* buf) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) v = Op::of(v, __shfl_xor_sync(0xffffffffu, v, o));
   if (width == 32) return v;
-  const int w = threadIdx.x >> 5, per = width >> 5;
-  if ((threadIdx.x & 31) == 0) buf[w] = v;
+  const int w = threadIdx.x >> 5, per = width >> 5, lane = threadIdx.x & 31;
+  if (lane == 0) buf[w] = v;
   __syncthreads();
-  const int first = w / per * per;
-  float r = buf[first];
-  for (int k = 1; k < per; ++k) r = Op::of(r, buf[first + k]);
-  return r;
+  v = buf[(w & ~(per - 1)) + (lane & (per - 1))];
+  for (int o = per >> 1; o > 0; o >>= 1) v = Op::of(v, __shfl_xor_sync(0xffffffffu, v, o));
+  return v;
 }
 
 }  // namespace rows
