@@ -348,66 +348,67 @@ def fw_launch_count() -> int:
 
 
 # ---- operators around the layers: tensors in, with their sizes, strides and types looked at ----
-def _torch_types():
-    import torch
-    return {torch.float32: FW_F32, torch.bfloat16: FW_BF16, torch.float8_e4m3fn: FW_E4M3, torch.int32: "int32",
-            torch.int64: "int64"}
+_TYPES = None          # this library's types as torch has them (filled by the first call)
 
 
-_TYPES = None
-
-
-def _matrix(t, rows, cols, dtype, name):
-    """(address, leading dimension) of a rows x cols CUDA tensor of one of this library's types, rows contiguous in themselves;
-    (None, 0) for None.  The device that the library launches on is the current one, so the tensor has to be there."""
+def _here():
+    """The device that the library launches on: the current one.  Tensors have to be there."""
     global _TYPES
+    import torch
+    if _TYPES is None:
+        _TYPES = {FW_F32: torch.float32, FW_BF16: torch.bfloat16, FW_E4M3: torch.float8_e4m3fn, "int32": torch.int32,
+                  "int64": torch.int64}
+    return torch.cuda.current_device() if torch.cuda.is_initialized() or torch.cuda.is_available() else None
+
+
+def _refuse_device(t, dev, name):
+    if not t.is_cuda:
+        raise ValueError(f"{name}: not a CUDA tensor")
+    raise ValueError(f"{name}: on cuda:{t.get_device()}, but the current device is cuda:{dev}")
+
+
+def _matrix(t, rows, cols, dtype, name, dev):
+    """(address, leading dimension) of a rows x cols tensor of one of this library's types, the elements of a row next to each
+    other; (None, 0) for None."""
     if t is None:
         return None, 0
-    if _TYPES is None:
-        _TYPES = _torch_types()
-    if _TYPES.get(t.dtype) != dtype:
+    if t.dtype is not _TYPES[dtype]:
         raise TypeError(f"{name}: {t.dtype} is not the type that its description says")
-    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols:
-        raise ValueError(f"{name}: expected {rows} x {cols}, got {tuple(t.shape)}")
-    ld = t.stride(0) if rows > 1 else max(t.stride(0), cols)
-    if cols > 1 and t.stride(1) != 1:
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 2 or shape[0] != rows or shape[1] != cols:
+        raise ValueError(f"{name}: expected {rows} x {cols}, got {tuple(shape)}")
+    if stride[1] != 1 and cols > 1:
         raise ValueError(f"{name}: the elements of a row have to be next to each other")
-    if rows > 1 and ld < cols:
-        raise ValueError(f"{name}: rows overlap")
-    _on_device(t, name)
+    ld = stride[0]
+    if ld < cols:
+        if rows > 1:
+            raise ValueError(f"{name}: rows overlap")
+        ld = cols
+    if t.get_device() != dev:
+        _refuse_device(t, dev, name)
     return t.data_ptr(), ld
 
 
-def _vector(t, n, name, dtype=FW_F32):
-    """Address of a contiguous CUDA vector of n elements; None for None."""
-    global _TYPES
-    if t is None:
-        return None
-    if _TYPES is None:
-        _TYPES = _torch_types()
-    if _TYPES.get(t.dtype) != dtype:
-        raise TypeError(f"{name}: {t.dtype} is not the type that is expected")
-    if t.numel() != n or not t.is_contiguous():
-        raise ValueError(f"{name}: expected {n} contiguous elements, got {tuple(t.shape)}")
-    _on_device(t, name)
-    return t.data_ptr()
-
-
-def _pair(a, b, rows, cols, dtype, name):
+def _pair(a, b, rows, cols, dtype, name, dev):
     """Two matrices with one leading dimension."""
-    pa, lda = _matrix(a, rows, cols, dtype, name)
-    pb, ldb = _matrix(b, rows, cols, dtype, name)
+    pa, lda = _matrix(a, rows, cols, dtype, name, dev)
+    pb, ldb = _matrix(b, rows, cols, dtype, name, dev)
     if a is not None and b is not None and lda != ldb:
         raise ValueError(f"{name}: their rows have to be equally far apart")
     return pa, pb, lda if a is not None else ldb
 
 
-def _on_device(t, name):
-    import torch
-    if not t.is_cuda:
-        raise ValueError(f"{name}: not a CUDA tensor")
-    if t.get_device() != torch.cuda.current_device():
-        raise ValueError(f"{name}: on cuda:{t.get_device()}, but the current device is cuda:{torch.cuda.current_device()}")
+def _vector(t, n, name, dev, dtype=FW_F32):
+    """Address of a contiguous tensor of n elements; None for None."""
+    if t is None:
+        return None
+    if t.dtype is not _TYPES[dtype]:
+        raise TypeError(f"{name}: {t.dtype} is not the type that is expected")
+    if t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"{name}: expected {n} contiguous elements, got {tuple(t.shape)}")
+    if t.get_device() != dev:
+        _refuse_device(t, dev, name)
+    return t.data_ptr()
 
 
 def fw_norm_desc_default(M: int, **overrides) -> fw_norm_desc:
@@ -423,27 +424,28 @@ def fw_rmsnorm_scratch_bytes(desc: fw_norm_desc) -> int:
 
 
 def fw_rmsnorm_forward(desc: fw_norm_desc, x, w, y, res=None, sum_out=None, y_scale=None, rstd=None, stream: int = 0) -> None:
-    rows, M, t = x.shape[0], desc.M, desc.dtype
-    px, ldx = _matrix(x, rows, M, t, "x")
-    pr, ldr = _matrix(res, rows, M, t, "res")
-    ps, lds = _matrix(sum_out, rows, M, t, "sum_out")
-    py, ldy = _matrix(y, rows, M, desc.y_dtype, "y")
-    _check(_lib().fw_rmsnorm_forward(C.byref(desc), rows, px, ldx, pr, ldr, _vector(w, M, "w"), ps, lds, py, ldy,
-                                     _vector(y_scale, rows, "y_scale"), _vector(rstd, rows, "rstd"), stream), "fw_rmsnorm_forward")
+    rows, M, t, dev = x.shape[0], desc.M, desc.dtype, _here()
+    px, ldx = _matrix(x, rows, M, t, "x", dev)
+    pr, ldr = _matrix(res, rows, M, t, "res", dev)
+    ps, lds = _matrix(sum_out, rows, M, t, "sum_out", dev)
+    py, ldy = _matrix(y, rows, M, desc.y_dtype, "y", dev)
+    _check(_lib().fw_rmsnorm_forward(C.byref(desc), rows, px, ldx, pr, ldr, _vector(w, M, "w", dev), ps, lds, py, ldy,
+                                     _vector(y_scale, rows, "y_scale", dev), _vector(rstd, rows, "rstd", dev), stream), "fw_rmsnorm_forward")
 
 
 def fw_rmsnorm_backward(desc: fw_norm_desc, dy, s, w, rstd, dx, dw=None, dsum=None, scratch=None, stream: int = 0) -> None:
-    rows, M, t = dy.shape[0], desc.M, desc.dtype
-    pdy, lddy = _matrix(dy, rows, M, t, "dy")
-    ps, lds = _matrix(s, rows, M, t, "s")
-    pds, ldds = _matrix(dsum, rows, M, t, "dsum")
-    pdx, lddx = _matrix(dx, rows, M, t, "dx")
+    rows, M, t, dev = dy.shape[0], desc.M, desc.dtype, _here()
+    pdy, lddy = _matrix(dy, rows, M, t, "dy", dev)
+    ps, lds = _matrix(s, rows, M, t, "s", dev)
+    pds, ldds = _matrix(dsum, rows, M, t, "dsum", dev)
+    pdx, lddx = _matrix(dx, rows, M, t, "dx", dev)
     n = 0
     if scratch is not None:
-        _on_device(scratch, "scratch")
+        if scratch.get_device() != dev:
+            _refuse_device(scratch, dev, "scratch")
         n = scratch.numel() * scratch.element_size()
-    _check(_lib().fw_rmsnorm_backward(C.byref(desc), rows, pdy, lddy, ps, lds, pds, ldds, _vector(w, M, "w"),
-                                      _vector(rstd, rows, "rstd"), pdx, lddx, _vector(dw, M, "dw"), _ptr(scratch), n, stream),
+    _check(_lib().fw_rmsnorm_backward(C.byref(desc), rows, pdy, lddy, ps, lds, pds, ldds, _vector(w, M, "w", dev),
+                                      _vector(rstd, rows, "rstd", dev), pdx, lddx, _vector(dw, M, "dw", dev), _ptr(scratch), n, stream),
            "fw_rmsnorm_backward")
 
 
@@ -456,23 +458,23 @@ def fw_distill_desc_default(V: int, K: int, **overrides) -> fw_distill_desc:
 
 
 def fw_distill_forward(desc: fw_distill_desc, Z, T, I, loss, stat=None, t_lse=None, weight=None, dZ=None, stream: int = 0) -> None:
-    rows, V, K = Z.shape[0], desc.V, desc.K
-    pz, ldz = _matrix(Z, rows, V, desc.z_dtype, "Z")
-    pd, lddz = _matrix(dZ, rows, V, desc.z_dtype, "dZ")
-    _check(_lib().fw_distill_forward(C.byref(desc), pz, rows, ldz, _vector(T, rows * K, "T", desc.t_dtype),
-                                     _vector(I, rows * K, "I", "int64" if desc.index_bits == 64 else "int32"),
-                                     _vector(t_lse, rows, "t_lse"), _vector(weight, rows, "weight"), _vector(loss, rows, "loss"),
-                                     _vector(stat, 2 * rows, "stat"), pd, lddz, stream), "fw_distill_forward")
+    rows, V, K, dev = Z.shape[0], desc.V, desc.K, _here()
+    pz, ldz = _matrix(Z, rows, V, desc.z_dtype, "Z", dev)
+    pd, lddz = _matrix(dZ, rows, V, desc.z_dtype, "dZ", dev)
+    _check(_lib().fw_distill_forward(C.byref(desc), pz, rows, ldz, _vector(T, rows * K, "T", dev, desc.t_dtype),
+                                     _vector(I, rows * K, "I", dev, "int64" if desc.index_bits == 64 else "int32"),
+                                     _vector(t_lse, rows, "t_lse", dev), _vector(weight, rows, "weight", dev), _vector(loss, rows, "loss", dev),
+                                     _vector(stat, 2 * rows, "stat", dev), pd, lddz, stream), "fw_distill_forward")
 
 
 def fw_distill_backward(desc: fw_distill_desc, Z, T, I, stat, dZ, t_lse=None, weight=None, stream: int = 0) -> None:
-    rows, V, K = Z.shape[0], desc.V, desc.K
-    pz, ldz = _matrix(Z, rows, V, desc.z_dtype, "Z")
-    pd, lddz = _matrix(dZ, rows, V, desc.z_dtype, "dZ")
-    _check(_lib().fw_distill_backward(C.byref(desc), pz, rows, ldz, _vector(T, rows * K, "T", desc.t_dtype),
-                                      _vector(I, rows * K, "I", "int64" if desc.index_bits == 64 else "int32"),
-                                      _vector(t_lse, rows, "t_lse"), _vector(weight, rows, "weight"),
-                                      _vector(stat, 2 * rows, "stat"), pd, lddz, stream), "fw_distill_backward")
+    rows, V, K, dev = Z.shape[0], desc.V, desc.K, _here()
+    pz, ldz = _matrix(Z, rows, V, desc.z_dtype, "Z", dev)
+    pd, lddz = _matrix(dZ, rows, V, desc.z_dtype, "dZ", dev)
+    _check(_lib().fw_distill_backward(C.byref(desc), pz, rows, ldz, _vector(T, rows * K, "T", dev, desc.t_dtype),
+                                      _vector(I, rows * K, "I", dev, "int64" if desc.index_bits == 64 else "int32"),
+                                      _vector(t_lse, rows, "t_lse", dev), _vector(weight, rows, "weight", dev),
+                                      _vector(stat, 2 * rows, "stat", dev), pd, lddz, stream), "fw_distill_backward")
 
 
 # ---- convenience: a layer that owns its workspace tensor -------------------
@@ -574,29 +576,29 @@ class Gated:
             pass
 
     def forward(self, X, Wg, Wu, H, Zg=None, Zu=None, x_scale=None, wg_scale=None, wu_scale=None, bg=None, bu=None):
-        M, N, t, rows = self.M, self.N, self.desc.x_dtype, X.shape[0]
-        px, ldx = _matrix(X, rows, M, t, "X")
-        pg, pu, ldw = _pair(Wg, Wu, N, M, t, "Wg, Wu")
-        ph, ldh = _matrix(H, rows, N, FW_BF16, "H")
-        zg, zu, ldz = _pair(Zg, Zu, rows, N, FW_BF16, "Zg, Zu")
-        _check(_lib().fw_gated_forward(self.handle, px, rows, ldx, _vector(x_scale, rows, "x_scale"), pg, pu, ldw,
-                                       _vector(wg_scale, N, "wg_scale"), _vector(wu_scale, N, "wu_scale"), _vector(bg, N, "bg"),
-                                       _vector(bu, N, "bu"), ph, ldh, zg, zu, ldz), "fw_gated_forward")
+        M, N, t, rows, dev = self.M, self.N, self.desc.x_dtype, X.shape[0], _here()
+        px, ldx = _matrix(X, rows, M, t, "X", dev)
+        pg, pu, ldw = _pair(Wg, Wu, N, M, t, "Wg, Wu", dev)
+        ph, ldh = _matrix(H, rows, N, FW_BF16, "H", dev)
+        zg, zu, ldz = _pair(Zg, Zu, rows, N, FW_BF16, "Zg, Zu", dev)
+        _check(_lib().fw_gated_forward(self.handle, px, rows, ldx, _vector(x_scale, rows, "x_scale", dev), pg, pu, ldw,
+                                       _vector(wg_scale, N, "wg_scale", dev), _vector(wu_scale, N, "wu_scale", dev), _vector(bg, N, "bg", dev),
+                                       _vector(bu, N, "bu", dev), ph, ldh, zg, zu, ldz), "fw_gated_forward")
 
     def backward(self, dH, X, Wg, Wu, Zg, Zu, dX=None, dWg=None, dWu=None, dbg=None, dbu=None):
-        M, N, rows = self.M, self.N, dH.shape[0]
-        pd, lddh = _matrix(dH, rows, N, FW_BF16, "dH")
-        px, ldx = _matrix(X, rows, M, FW_BF16, "X")
-        pg, pu, ldw = _pair(Wg, Wu, N, M, FW_BF16, "Wg, Wu")
-        zg, zu, ldz = _pair(Zg, Zu, rows, N, FW_BF16, "Zg, Zu")
-        pdx, lddx = _matrix(dX, rows, M, FW_BF16, "dX")
+        M, N, rows, dev = self.M, self.N, dH.shape[0], _here()
+        pd, lddh = _matrix(dH, rows, N, FW_BF16, "dH", dev)
+        px, ldx = _matrix(X, rows, M, FW_BF16, "X", dev)
+        pg, pu, ldw = _pair(Wg, Wu, N, M, FW_BF16, "Wg, Wu", dev)
+        zg, zu, ldz = _pair(Zg, Zu, rows, N, FW_BF16, "Zg, Zu", dev)
+        pdx, lddx = _matrix(dX, rows, M, FW_BF16, "dX", dev)
         kind = FW_F32
         if dWg is not None:
             import torch
             kind = FW_BF16 if dWg.dtype == torch.bfloat16 else FW_F32
         _check(_lib().fw_gated_backward(self.handle, pd, rows, lddh, px, ldx, pg, pu, ldw, zg, zu, ldz, pdx, lddx,
-                                        _vector(dWg, N * M, "dWg", kind), _vector(dWu, N * M, "dWu", kind), kind,
-                                        _vector(dbg, N, "dbg"), _vector(dbu, N, "dbu")), "fw_gated_backward")
+                                        _vector(dWg, N * M, "dWg", dev, kind), _vector(dWu, N * M, "dWu", dev, kind), kind,
+                                        _vector(dbg, N, "dbg", dev), _vector(dbu, N, "dbu", dev)), "fw_gated_backward")
 
     def sync_status(self):
         return _check(_lib().fw_gated_sync_status(self.handle), "fw_gated_sync_status")

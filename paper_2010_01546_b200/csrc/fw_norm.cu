@@ -7,6 +7,7 @@
 // Both directions read each element once and write each result once: HBM bandwidth bounds them.  A row stays in the registers
 // of the threads that share it between its sum and its output.
 #include <cstdio>
+#include <mutex>
 
 #include "fw_internal.h"
 #include "fw_rows.cuh"
@@ -310,15 +311,34 @@ fw_status mat_check(const Mat& m, int M, int access, bool* vec) {
   return FW_OK;
 }
 
-// CTAs of one wave, or as many as there are groups of rows.  Per device, by shared memory.
+// What a kernel of one shape is launched with: found once for each device, number of threads and size of shared memory.
+struct FillCache {
+  std::mutex mu;
+  struct { int dev, threads, per_sm; size_t smem; } known[8] = {};
+  int n = 0;
+};
+// CTAs of one wave, or as many as there are groups of rows
 template <class F>
-cudaError_t fill(F* kernel, SmemAttrCache& cache, int threads, size_t smem, int64_t groups, int most, int* ctas) {
-  cudaError_t e = smem > 40 * 1024 ? ensure_dyn_smem(kernel, smem, cache) : cudaSuccess;
+cudaError_t fill(F* kernel, FillCache& cache, int threads, size_t smem, int64_t groups, int most, int* ctas) {
+  int dev = 0, per_sm = 0;
+  cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
-  int per_sm = 0;
-  e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, threads, smem);
-  if (e != cudaSuccess) return e;
-  int64_t n = (int64_t)(per_sm < 1 ? 1 : per_sm) * sm_count();
+  {
+    std::lock_guard<std::mutex> lock(cache.mu);
+    const int have = cache.n < 8 ? cache.n : 8;
+    for (int i = 0; i < have && !per_sm; ++i)
+      if (cache.known[i].dev == dev && cache.known[i].threads == threads && cache.known[i].smem == smem) per_sm = cache.known[i].per_sm;
+    if (!per_sm) {
+      // the most that any launch asks for: what is set late by one thread never undoes what another needs
+      e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024 - 1024);
+      if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, threads, smem);
+      if (e != cudaSuccess) return e;
+      if (per_sm < 1) return cudaErrorInvalidConfiguration;
+      cache.known[cache.n % 8] = {dev, threads, per_sm, smem};
+      if (++cache.n >= 16) cache.n = 8;
+    }
+  }
+  int64_t n = (int64_t)per_sm * sm_count();
   if (n > most) n = most;
   *ctas = (int)(groups < n ? groups : n);
   return cudaSuccess;
@@ -334,7 +354,7 @@ constexpr int slots(int vec, int nv, int tensors) {
 template <class T, class Y, int VEC, int NV, bool RES, int FILL>
 cudaError_t forward_launch(const NormFwd& p, cudaStream_t s) {
   constexpr int SLOTS = slots(VEC, NV, RES ? 2 : 1);
-  static SmemAttrCache cache;
+  static FillCache cache;
   auto kernel = norm_forward_kernel<T, Y, VEC, NV, SLOTS, RES, FILL>;
   const size_t smem = (size_t)SLOTS * (RES ? 2 : 1) * Ahead<T, VEC, NV, FILL>::row_bytes(p.M, p.width, p.width);
   int ctas = 0;
@@ -379,7 +399,7 @@ int backward_ctas() { return 4 * sm_count(); }
 template <class T, int VEC, int NV, bool DS, int FILL, bool SOLO>
 cudaError_t backward_launch(const NormBwd& p, cudaStream_t s, int* ctas) {
   constexpr int SLOTS = slots(VEC, NV, DS ? 3 : 2);
-  static SmemAttrCache cache;
+  static FillCache cache;
   auto kernel = norm_backward_kernel<T, VEC, NV, SLOTS, DS, FILL, SOLO>;
   const int threads = SOLO ? p.width : 128, per = threads / p.width;
   size_t smem = (size_t)SLOTS * (DS ? 3 : 2) * Ahead<T, VEC, NV, FILL>::row_bytes(p.M, threads, p.width);
