@@ -317,9 +317,6 @@ __global__ void __launch_bounds__(512, 2) distill_kernel(const Distill p) {
 // ---------------------------------------------------------------------------
 constexpr int kRingThreads = 256, kRingWarps = 8, kRingSlots = 3, kRingMaxK = 256, kRingMaxCtas = 16;
 
-__device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
-}
 __device__ __forceinline__ void st_cluster_pair(uint32_t addr, MaxSum v) {
   asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(addr), "f"(v.m), "f"(v.l) : "memory");
 }
@@ -338,8 +335,9 @@ struct RingRow {
   float t, z;                // teacher's and student's logit
 };
 
-template <class T, int NV, int MODE>
-__global__ void __launch_bounds__(kRingThreads, 2) distill_ring_kernel(const Distill p, int rows) {
+// FILL: the last CTA's slice ends inside an access of 16 bytes, with one, or all slices fill all accesses of their threads.
+template <class T, int NV, int MODE, int FILL>
+__global__ void __launch_bounds__(kRingThreads, 2) distill_ring_kernel(const Distill p, int rows, int C) {
   constexpr int VEC = 16 / sizeof(T);
   extern __shared__ __align__(16) uint8_t dyn8[];
   __shared__ __align__(16) int s_cls[2][kRingMaxK];
@@ -347,13 +345,16 @@ __global__ void __launch_bounds__(kRingThreads, 2) distill_ring_kernel(const Dis
   __shared__ MaxSum s_sum[2][kRingMaxCtas * kRingWarps];
   __shared__ float s_kl[2][kRingWarps];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int C = (int)sm100::cluster_nctarank(), rank = (int)sm100::cluster_ctarank();
-  const int row0 = (int)blockIdx.x / C, step = (int)gridDim.x / C;
+  const int rank = (int)blockIdx.x % C, row0 = (int)blockIdx.x / C, step = (int)gridDim.x / C;
   uint4* ring = reinterpret_cast<uint4*>(dyn8);                                  // [slot][k][thread]
   constexpr int words = NV * kRingThreads * VEC / 32;
   uint32_t* bits = reinterpret_cast<uint32_t*>(ring + kRingSlots * NV * kRingThreads);   // [3][words]
   const float c2 = p.inv_tau * kLog2e;
   const int first = rank * p.slice, last = min(p.V, first + p.slice);
+  const int mine = last - first - tid * VEC;      // classes of the slice from this thread's first on
+  // of its k-th access: whole (the ring has it), or at least begun
+  auto whole = [&](int k) { return FILL == ROW_FULL || (FILL == ROW_WHOLE ? mine > k * kRingThreads * VEC : mine >= (k * kRingThreads + 1) * VEC); };
+  auto begun = [&](int k) { return FILL == ROW_FULL || mine > k * kRingThreads * VEC; };
   const uint32_t ring_at = sm100::smem_u32(ring) + tid * 16;
   const uint32_t push_at = sm100::mapa_shared(sm100::smem_u32(&s_sum[0][rank * kRingWarps + warp]), lane < C ? lane : 0);
 
@@ -379,15 +380,13 @@ __global__ void __launch_bounds__(kRingThreads, 2) distill_ring_kernel(const Dis
   };
   auto fetch = [&](const RingRow& r, int row, int it) {
     if (r.w != 0.f) {
-      const T* z = zrow(row);
+      const T* z = zrow(row) + first;
       const uint32_t to = ring_at + (uint32_t)(it % kRingSlots) * (NV * kRingThreads * 16);
 #pragma unroll
-      for (int k = 0; k < NV; ++k) {
-        const int c = first + (k * kRingThreads + tid) * VEC;
-        if (c + VEC <= last) copy16(to + k * kRingThreads * 16, z + c);
-      }
+      for (int k = 0; k < NV; ++k)
+        if (whole(k)) ahead16(to + k * kRingThreads * 16, z + (uint32_t)((k * kRingThreads + tid) * VEC));
     }
-    asm volatile("cp.async.commit_group;" ::: "memory");
+    ahead_commit();
   };
   auto teacher2 = [&](float t, float t_lse, float tm) { return p.t_lse ? fmaf(t, p.inv_tau, -t_lse) * kLog2e : (t - tm) * c2; };
   // the entries of a row whose classes stand in s_cls[it & 1] (a barrier of the CTA ago): repeated ones out, bit set, sums
@@ -456,7 +455,7 @@ __global__ void __launch_bounds__(kRingThreads, 2) distill_ring_kernel(const Dis
   int turn = 0;                 // place of the sums, by rows that count: two such rows are a cluster barrier apart
   for (int row = row0; row < rows; row += step, ++it) {
     const int b = it & 1;
-    asm volatile("cp.async.wait_group 1;" ::: "memory");        // this row's classes
+    ahead_wait<1>();                                            // this row's classes
     __syncthreads();
     finish(it ^ 1);
     // ---- two and three rows ahead ----
@@ -469,39 +468,58 @@ __global__ void __launch_bounds__(kRingThreads, 2) distill_ring_kernel(const Dis
     const bool live = cur.w != 0.f;                             // the same in all threads of the cluster
     float e[NV][VEC];
     MaxSum sum = {kLow, 0.f};
-    const T* z = zrow(row);
+    const T* z = zrow(row) + first;
     if (live) {
       const uint4* slot = ring + (it % kRingSlots) * NV * kRingThreads + tid;
-      const uint32_t* set = bits + (it % 3) * words;
 #pragma unroll
       for (int k = 0; k < NV; ++k) {
-        const int c = first + (k * kRingThreads + tid) * VEC;
-        if (c + VEC <= last) unpack16(slot[k * kRingThreads], e[k]);
-        else load<VEC>(z + c, last - c, -INFINITY, e[k]);        // the row's last few, and past them
+        if (whole(k)) {
+          unpack16(slot[k * kRingThreads], e[k]);
+        } else if (FILL == ROW_PART) {                           // the row's last few, and past them
+          load<VEC>(z + (k * kRingThreads + tid) * VEC, mine - k * kRingThreads * VEC, -INFINITY, e[k]);
+        } else {
+#pragma unroll
+          for (int v = 0; v < VEC; ++v) e[k][v] = -INFINITY;
+        }
       }
       if (MODE != DIST_BACKWARD) {
+        float part[2] = {kLow, kLow};
 #pragma unroll
         for (int k = 0; k < NV; ++k)
 #pragma unroll
-          for (int v = 0; v < VEC; ++v) sum.m = fmaxf(sum.m, e[k][v]);
+          for (int v = 0; v < VEC; v += 2) {
+            part[0] = fmaxf(part[0], e[k][v]);
+            part[1] = fmaxf(part[1], e[k][v + 1]);
+          }
+        sum.m = fmaxf(part[0], part[1]);
+        part[0] = part[1] = 0.f;
+        const float less[2] = {-sum.m, -sum.m};
+        // a byte (bf16) or half of one of the bit set to an access
+        const uint32_t* set = bits + (it % 3) * words + tid * VEC / 32;
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
-          const int at = (k * kRingThreads + tid) * VEC;
-          const uint32_t named = (set[at >> 5] >> (at & 31)) & ((1u << VEC) - 1u);
-          float part = 0.f;
+          const uint32_t named = (set[k * kRingThreads * VEC / 32] >> (tid * VEC % 32)) & ((1u << VEC) - 1u);
 #pragma unroll
-          for (int v = 0; v < VEC; ++v) {
-            e[k][v] = ex2((e[k][v] - sum.m) * c2);
-            part += e[k][v];
+          for (int v = 0; v < VEC; v += 2) {
+            float two[2] = {e[k][v], e[k][v + 1]};
+            vadd<2>(two, less);
+            vscale<2>(two, c2);
+            e[k][v] = ex2(two[0]);
+            e[k][v + 1] = ex2(two[1]);
           }
-          if (named) {
-            part = 0.f;
+          if (!named) {
+#pragma unroll
+            for (int v = 0; v < VEC; v += 2) {
+              const float two[2] = {e[k][v], e[k][v + 1]};
+              vadd<2>(part, two);
+            }
+          } else {
 #pragma unroll
             for (int v = 0; v < VEC; ++v)
-              if (!((named >> v) & 1u)) part += e[k][v];
+              if (!((named >> v) & 1u)) part[v & 1] += e[k][v];
           }
-          sum.l += part;
         }
+        sum.l = part[0] + part[1];
         const MaxSum s = merge_lanes(sum, c2);
         if (lane < C) st_cluster_pair(push_at + (uint32_t)turn * (uint32_t)sizeof(s_sum[0]), s);
         __syncwarp();
@@ -562,16 +580,18 @@ __global__ void __launch_bounds__(kRingThreads, 2) distill_ring_kernel(const Dis
         const float other = pt > 0.f && qt != 0.f ? A - pt / qt : A;
         T* dz = static_cast<T*>(p.dZ) + (int64_t)row * p.lddz;
         const float f = empty ? 0.f : MODE == DIST_BACKWARD ? ws * other : ws * other * ex2((sum.m - ref) * c2) * inv;
+        T* mine_dz = dz + first;
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
-          const int c = first + (k * kRingThreads + tid) * VEC;
-          if (c >= last) continue;
+          if (!begun(k)) continue;
+          if (MODE == DIST_BACKWARD) {
 #pragma unroll
-          for (int v = 0; v < VEC; ++v) {
-            if (MODE == DIST_BACKWARD) e[k][v] = empty ? 0.f : f * student(e[k][v]);
-            else e[k][v] *= f;
+            for (int v = 0; v < VEC; ++v) e[k][v] = empty ? 0.f : f * student(e[k][v]);
+          } else {
+            vscale<VEC>(e[k], f);
           }
-          store<VEC>(dz + c, last - c, e[k]);
+          const uint32_t c = (uint32_t)((k * kRingThreads + tid) * VEC);
+          store<VEC>(mine_dz + c, FILL == ROW_PART ? mine - k * kRingThreads * VEC : VEC, e[k]);
         }
         if (cur.c >= first && cur.c < last) {
           late_at = dz + cur.c;
@@ -617,7 +637,7 @@ __global__ void __launch_bounds__(kRingThreads, 2) distill_ring_kernel(const Dis
   __syncthreads();
   finish(it ^ 1);
   __syncwarp();
-  asm volatile("cp.async.wait_group 0;" ::: "memory");
+  ahead_wait<0>();
   // no CTA leaves while its sums may still be written by another
   sm100::cluster_arrive();
   sm100::cluster_wait();
@@ -638,12 +658,12 @@ cudaError_t launch(const Distill& p, int C, int threads, int64_t rows, cudaStrea
   return launch_dep_cluster(C, distill_kernel<T, VEC, NV, MODE, KEEP>, dim3((unsigned)(rows * C)), threads, smem, s, p);
 }
 
-template <class T, int NV, int MODE>
+template <class T, int NV, int MODE, int FILL>
 cudaError_t launch_ring(const Distill& p, int C, int64_t rows, cudaStream_t s) {
   static std::mutex mu;
   static int resident[64][5];                               // clusters of 1, 2, 4, 8, 16 CTAs at once, per device
   constexpr size_t smem = (size_t)kRingSlots * NV * kRingThreads * 16 + 3 * (NV * kRingThreads * (16 / sizeof(T)) / 8);
-  auto kernel = distill_ring_kernel<T, NV, MODE>;
+  auto kernel = distill_ring_kernel<T, NV, MODE, FILL>;
   int dev = 0, n = 0, lg = 0;
   while ((1 << lg) < C) ++lg;
   cudaError_t e = cudaGetDevice(&dev);
@@ -667,7 +687,14 @@ cudaError_t launch_ring(const Distill& p, int C, int64_t rows, cudaStream_t s) {
     n = resident[dev][lg];
   }
   if (n > rows) n = (int)rows;
-  return launch_dep_cluster(C, kernel, dim3((unsigned)(n * C)), kRingThreads, smem, s, p, (int)rows);
+  return launch_dep_cluster(C, kernel, dim3((unsigned)(n * C)), kRingThreads, smem, s, p, (int)rows, C);
+}
+template <class T, int NV, int MODE>
+cudaError_t launch_ring(const Distill& p, int C, int64_t rows, cudaStream_t s) {
+  constexpr int VEC = 16 / sizeof(T);
+  if (p.slice == NV * kRingThreads * VEC && p.V == C * p.slice) return launch_ring<T, NV, MODE, ROW_FULL>(p, C, rows, s);
+  if (p.V % VEC == 0) return launch_ring<T, NV, MODE, ROW_WHOLE>(p, C, rows, s);
+  return launch_ring<T, NV, MODE, ROW_PART>(p, C, rows, s);
 }
 
 // Rows the ring takes: fewer than 2^28 of up to 16 slices; *C CTAs a row, *nv accesses a thread
