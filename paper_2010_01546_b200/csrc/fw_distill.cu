@@ -59,10 +59,46 @@ __device__ __forceinline__ MaxSum merge(MaxSum a, MaxSum b, float c2) {
   const float m = fmaxf(a.m, b.m);
   return {m, a.l * ex2((a.m - m) * c2) + b.l * ex2((b.m - m) * c2)};
 }
-__device__ __forceinline__ MaxSum merge_lanes(MaxSum s, float c2) {
+__device__ __forceinline__ float lanes_max(float v) {
+  float r;
+  asm("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
+  return r;
+}
+__device__ __forceinline__ float lanes_sum(float v) {
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) s = merge(s, {__shfl_xor_sync(0xffffffffu, s.m, o), __shfl_xor_sync(0xffffffffu, s.l, o)}, c2);
-  return s;
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return v;
+}
+// The whole warp's: its largest first, so that the chain is one exponential and five additions long (five merges took twice that)
+__device__ __forceinline__ MaxSum merge_lanes(MaxSum s, float c2) {
+  const float m = lanes_max(s.m);
+  return {m, lanes_sum(s.l * ex2((s.m - m) * c2))};
+}
+
+// Two and three of them at once: the chains run beside each other.
+__device__ __forceinline__ void merge_lanes2(MaxSum& a, MaxSum& b, float c2) {
+  const float ma = lanes_max(a.m), mb = lanes_max(b.m);
+  a = {ma, a.l * ex2((a.m - ma) * c2)};
+  b = {mb, b.l * ex2((b.m - mb) * c2)};
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    const float x = __shfl_xor_sync(0xffffffffu, a.l, o), y = __shfl_xor_sync(0xffffffffu, b.l, o);
+    a.l += x;
+    b.l += y;
+  }
+}
+__device__ __forceinline__ void merge_lanes3(MaxSum& a, MaxSum& b, MaxSum& c, float c2) {
+  const float ma = lanes_max(a.m), mb = lanes_max(b.m), mc = lanes_max(c.m);
+  a = {ma, a.l * ex2((a.m - ma) * c2)};
+  b = {mb, b.l * ex2((b.m - mb) * c2)};
+  c = {mc, c.l * ex2((c.m - mc) * c2)};
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    const float x = __shfl_xor_sync(0xffffffffu, a.l, o), y = __shfl_xor_sync(0xffffffffu, b.l, o), z = __shfl_xor_sync(0xffffffffu, c.l, o);
+    a.l += x;
+    b.l += y;
+    c.l += z;
+  }
 }
 
 // VEC classes an access, NV accesses a thread and trip.  KEEP: the CTA's slice is one trip, its exponentials stay in registers.
@@ -310,15 +346,18 @@ __global__ void __launch_bounds__(512, 2) distill_kernel(const Distill p) {
 //   - a thread copies its own classes of the next two rows to shared memory (cp.async: it reads back only what it wrote itself, so
 //     no barrier stands between), 96 KB in two CTAs a SM;
 //   - entry k of a row belongs to thread k: class, logits and weight are loaded three rows ahead, the student's logit two;
-//   - between its arrival at the cluster's barrier and its wait there a warp prepares the next row's entries (repeated classes,
-//     bit set, the teacher's and the named classes' sums);
+//   - while its sums are on their way to the cluster's other CTAs a warp prepares the next row's entries (repeated classes, bit
+//     set, the teacher's and the named classes' sums);
 //   - what is written over the row's stores (named classes) or needs all warps (the loss) follows after the next row's barrier.
-// Two barriers a row: one of the CTA, one of the cluster.
+// A row has one barrier of the CTA.  Sums go from each warp to each CTA of the cluster (st.async, counted in bytes there): a barrier of
+// the cluster would also wait for the stores of the row before.
 // ---------------------------------------------------------------------------
 constexpr int kRingThreads = 256, kRingWarps = 8, kRingSlots = 3, kRingMaxK = 256, kRingMaxCtas = 16;
 
-__device__ __forceinline__ void st_cluster_pair(uint32_t addr, MaxSum v) {
-  asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(addr), "f"(v.m), "f"(v.l) : "memory");
+// to a place in a CTA of the cluster, counted in bytes on that CTA's barrier
+__device__ __forceinline__ void send_pair(uint32_t addr, MaxSum v, uint32_t bar) {
+  asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 [%0], {%1, %2}, [%3];" ::"r"(addr), "f"(v.m), "f"(v.l), "r"(bar)
+               : "memory");
 }
 __device__ __forceinline__ void unpack16(uint4 q, float (&v)[8]) {
   v[0] = bf16_lo(q.x); v[1] = bf16_hi(q.x); v[2] = bf16_lo(q.y); v[3] = bf16_hi(q.y);
@@ -328,12 +367,17 @@ __device__ __forceinline__ void unpack16(uint4 q, float (&v)[4]) {
   v[0] = __uint_as_float(q.x); v[1] = __uint_as_float(q.y); v[2] = __uint_as_float(q.z); v[3] = __uint_as_float(q.w);
 }
 
-// What a thread knows of a row: its entry, and the row's numbers.
+// What a thread knows of a row: its entry, and the row's numbers.  Entries are kept as they were loaded until they are used: a
+// conversion next to the load waits for it (the loads queue behind the rows on their way: 2500 clocks).
 struct RingRow {
   float w, t_lse, s0, s1;    // weight (0 past the last row), teacher's normaliser, backward: stat
-  int c;                     // class of this thread's entry, -1: none
-  float t, z;                // teacher's and student's logit
+  int c, hi;                 // class of this thread's entry, -1: none; with 64 bits its upper half
+  uint32_t t, z;             // teacher's and student's logit, their bits
 };
+__device__ __forceinline__ uint32_t raw(const float* p) { return *reinterpret_cast<const uint32_t*>(p); }
+__device__ __forceinline__ uint32_t raw(const __nv_bfloat16* p) { return *reinterpret_cast<const uint16_t*>(p); }
+template <class T>
+__device__ __forceinline__ float from_raw(uint32_t v) { return __uint_as_float(sizeof(T) == 2 ? v << 16 : v); }
 
 // FILL: the last CTA's slice ends inside an access of 16 bytes, with one, or all slices fill all accesses of their threads.
 template <class T, int NV, int MODE, int FILL>
@@ -344,6 +388,8 @@ __global__ void __launch_bounds__(kRingThreads, 2) distill_ring_kernel(const Dis
   __shared__ MaxSum s_teacher[2][kRingWarps], s_named[2][kRingWarps];
   __shared__ MaxSum s_sum[2][kRingMaxCtas * kRingWarps];
   __shared__ float s_kl[2][kRingWarps];
+  __shared__ __align__(8) uint64_t s_bar[2];
+  __shared__ int s_lost;                     // a wait for the cluster's sums gave up
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int rank = (int)blockIdx.x % C, row0 = (int)blockIdx.x / C, step = (int)gridDim.x / C;
   uint4* ring = reinterpret_cast<uint4*>(dyn8);                                  // [slot][k][thread]
@@ -357,26 +403,38 @@ __global__ void __launch_bounds__(kRingThreads, 2) distill_ring_kernel(const Dis
   auto begun = [&](int k) { return FILL == ROW_FULL || mine > k * kRingThreads * VEC; };
   const uint32_t ring_at = sm100::smem_u32(ring) + tid * 16;
   const uint32_t push_at = sm100::mapa_shared(sm100::smem_u32(&s_sum[0][rank * kRingWarps + warp]), lane < C ? lane : 0);
+  const uint32_t push_bar = sm100::mapa_shared(sm100::smem_u32(&s_bar[0]), lane < C ? lane : 0);
 
   auto zrow = [&](int row) { return static_cast<const T*>(p.Z) + (int64_t)row * p.ldz; };
   auto load_row = [&](int row) {
-    RingRow r = {0.f, 0.f, 0.f, 0.f, -1, 0.f, 0.f};
+    RingRow r = {0.f, 0.f, 0.f, 0.f, -1, -1, 0u, 0u};
     if (row < rows) {
-      r.w = p.weight ? p.weight[row] : 1.f;
+      r.w = 1.f;
+      if (p.weight) r.w = p.weight[row];
       if (p.t_lse) r.t_lse = p.t_lse[row];
       if (MODE == DIST_BACKWARD) { r.s0 = p.stat_in[2 * (int64_t)row]; r.s1 = p.stat_in[2 * (int64_t)row + 1]; }
       if (tid < p.K) {
         const int64_t at = (int64_t)row * p.K + tid;
-        const int64_t i = p.i64 ? static_cast<const int64_t*>(p.I)[at] : static_cast<const int32_t*>(p.I)[at];
-        r.c = i >= 0 && i < p.V ? (int)i : -1;
-        r.t = p.t_bf16 ? to_f(static_cast<const __nv_bfloat16*>(p.T)[at]) : static_cast<const float*>(p.T)[at];
+        if (p.i64) {
+          const int2 i = static_cast<const int2*>(p.I)[at];
+          r.c = i.x;
+          r.hi = i.y;
+        } else {
+          r.c = static_cast<const int32_t*>(p.I)[at];
+        }
+        r.t = p.t_bf16 ? raw(static_cast<const __nv_bfloat16*>(p.T) + at) : raw(static_cast<const float*>(p.T) + at);
       }
     }
     return r;
   };
+  // the loads have had an iteration: class and logit of the entry
+  auto settle = [&](RingRow& r) {
+    if (r.c < 0 || r.c >= p.V || (p.i64 && r.hi != 0)) r.c = -1;
+    if (p.t_bf16) r.t <<= 16;
+  };
   // the student's logit of an entry; the backward pass needs those of its slice alone (dZ may be Z: others' are written over)
   auto load_logit = [&](RingRow& r, int row) {
-    if (r.c >= 0 && r.w != 0.f && (MODE != DIST_BACKWARD || (r.c >= first && r.c < last))) r.z = to_f(zrow(row)[r.c]);
+    if (r.c >= 0 && r.w != 0.f && (MODE != DIST_BACKWARD || (r.c >= first && r.c < last))) r.z = raw(zrow(row) + r.c);
   };
   auto fetch = [&](const RingRow& r, int row, int it) {
     if (r.w != 0.f) {
@@ -392,30 +450,29 @@ __global__ void __launch_bounds__(kRingThreads, 2) distill_ring_kernel(const Dis
   // the entries of a row whose classes stand in s_cls[it & 1] (a barrier of the CTA ago): repeated ones out, bit set, sums
   auto prepare = [&](RingRow& r, int it) {
     if (warp * 32 >= p.K) return;
-    const unsigned same = __match_any_sync(0xffffffffu, r.c);
-    bool twice = (int)(__ffs(same) - 1) != lane;
+    // the classes of the entries before this one, four at a time
+    bool twice = false;
     const int4* before = reinterpret_cast<const int4*>(s_cls[it & 1]);
     for (int j = 0; j < warp * 8; ++j) {
       const int4 q = before[j];
       twice |= q.x == r.c || q.y == r.c || q.z == r.c || q.w == r.c;
     }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int4 q = before[warp * 8 + j];
+      twice |= (4 * j < lane && q.x == r.c) || (4 * j + 1 < lane && q.y == r.c) || (4 * j + 2 < lane && q.z == r.c) || (4 * j + 3 < lane && q.w == r.c);
+    }
     if (twice) r.c = -1;
     if (r.c >= first && r.c < last) atomicOr(&bits[(it % 3) * words + ((r.c - first) >> 5)], 1u << ((r.c - first) & 31));
     const bool in = r.c >= 0;
-    MaxSum t = {kLow, 0.f};
-    if (p.t_lse) {
-      t.l = in ? ex2(teacher2(r.t, r.t_lse, 0.f)) : 0.f;
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) t.l += __shfl_xor_sync(0xffffffffu, t.l, o);
-    } else {
-      if (in) t = {fmaxf(r.t, kLow), r.t == -INFINITY ? 0.f : r.t != r.t ? r.t : 1.f};
-      t = merge_lanes(t, c2);
+    const float rt = __uint_as_float(r.t), rz = from_raw<T>(r.z);
+    MaxSum t = {kLow, 0.f}, n = {kLow, 0.f};
+    if (in) {
+      if (p.t_lse) t.l = ex2(teacher2(rt, r.t_lse, 0.f));
+      else t = {fmaxf(rt, kLow), rt == -INFINITY ? 0.f : rt != rt ? rt : 1.f};
+      if (MODE != DIST_BACKWARD) n = {fmaxf(rz, kLow), rz == -INFINITY ? 0.f : rz != rz ? rz : 1.f};
     }
-    MaxSum n = {kLow, 0.f};
-    if (MODE != DIST_BACKWARD) {
-      if (in) n = {fmaxf(r.z, kLow), r.z == -INFINITY ? 0.f : r.z != r.z ? r.z : 1.f};
-      n = merge_lanes(n, c2);
-    }
+    merge_lanes2(t, n, c2);
     if (lane == 0) { s_teacher[it & 1][warp] = t; s_named[it & 1][warp] = n; }
   };
 
@@ -424,9 +481,17 @@ __global__ void __launch_bounds__(kRingThreads, 2) distill_ring_kernel(const Dis
   RingRow cur = load_row(row0), next = load_row(row0 + step), third = load_row(row0 + 2 * step);
   fetch(cur, row0, 0);
   fetch(next, row0 + step, 1);
+  settle(cur);
+  settle(next);
   load_logit(cur, row0);
   load_logit(next, row0 + step);
   for (int i = tid; i < 3 * words; i += kRingThreads) bits[i] = 0;
+  if (tid == 0) {
+    s_lost = 0;
+    sm100::mbar_init(sm100::smem_u32(&s_bar[0]), 1);
+    sm100::mbar_init(sm100::smem_u32(&s_bar[1]), 1);
+    sm100::mbar_fence_init();
+  }
   s_cls[0][tid] = cur.c;
   s_cls[1][tid] = next.c;
   __syncthreads();
@@ -441,6 +506,7 @@ __global__ void __launch_bounds__(kRingThreads, 2) distill_ring_kernel(const Dis
     late_at = nullptr;
     if (MODE != DIST_BACKWARD && late_row >= 0) {
       float kl = 0.f;
+#pragma unroll
       for (int k = 0; k < kRingWarps; ++k) kl += s_kl[it & 1][k];
       p.loss[late_row] = late_w * (kl + late_rest) * kLn2;
       if (p.stat) { p.stat[2 * (int64_t)late_row] = late_lse; p.stat[2 * (int64_t)late_row + 1] = late_other; }
@@ -452,13 +518,17 @@ __global__ void __launch_bounds__(kRingThreads, 2) distill_ring_kernel(const Dis
   sm100::cluster_arrive();
   sm100::cluster_wait();
   int it = 0;
-  int turn = 0;                 // place of the sums, by rows that count: two such rows are a cluster barrier apart
+  // Place of the sums, by rows that count.  A CTA's place is written again two such rows on: by then every CTA has had all sums of
+  // the row between, which this CTA's warps sent after they had read the place.
+  int turn = 0;
+  uint32_t phase = 0;
   for (int row = row0; row < rows; row += step, ++it) {
     const int b = it & 1;
     ahead_wait<1>();                                            // this row's classes
     __syncthreads();
     finish(it ^ 1);
     // ---- two and three rows ahead ----
+    settle(third);
     s_cls[b][tid] = third.c;                                    // (the row's own have been used)
     for (int i = tid; i < words; i += kRingThreads) bits[((it + 2) % 3) * words + i] = 0;
     load_logit(third, row + 2 * step);
@@ -521,30 +591,36 @@ __global__ void __launch_bounds__(kRingThreads, 2) distill_ring_kernel(const Dis
         }
         sum.l = part[0] + part[1];
         const MaxSum s = merge_lanes(sum, c2);
-        if (lane < C) st_cluster_pair(push_at + (uint32_t)turn * (uint32_t)sizeof(s_sum[0]), s);
+        if (tid == 0) sm100::mbar_expect_tx(sm100::smem_u32(&s_bar[turn]), (uint32_t)(C * kRingWarps * sizeof(MaxSum)));
+        if (lane < C) send_pair(push_at + (uint32_t)turn * (uint32_t)sizeof(s_sum[0]), s, push_bar + (uint32_t)turn * 8u);
         __syncwarp();
-        sm100::cluster_arrive();
       }
     }
     prepare(next, it + 1);
     __syncwarp();
     if (live) {
-      if (MODE != DIST_BACKWARD) sm100::cluster_wait();
+      bool have = true;
+      if (MODE != DIST_BACKWARD) {
+        have = sm100::mbar_wait(sm100::smem_u32(&s_bar[turn]), phase, &s_lost, s_lost ? 1u : sm100::kSpinLimit);
+        if (!have) s_lost = 1;
+      }
       // ---- the teacher's mass, the student's normalisers: see distill_kernel ----
       const int kw = (p.K + 31) / 32;
       MaxSum t = lane < kw ? s_teacher[b][lane] : MaxSum{kLow, 0.f};
-      float ts;
-      if (p.t_lse) {
-        ts = t.l;
-#pragma unroll
-        for (int o = 4; o > 0; o >>= 1) ts += __shfl_xor_sync(0xffffffffu, ts, o);
-        ts = __shfl_sync(0xffffffffu, ts, 0);
+      MaxSum others = {kLow, 0.f}, n = {kLow, 0.f};
+      if (MODE != DIST_BACKWARD) {
+        const int sums = C * kRingWarps;
+        if (lane < sums) others = s_sum[turn][lane];
+        for (int i = lane + 32; i < sums; i += 32) others = merge(others, s_sum[turn][i], c2);
+        if (lane < kw) n = s_named[b][lane];
+        if (!have) others.l = NAN;               // the row's loss and gradient say so
+        merge_lanes3(t, others, n, c2);
+        turn ^= 1;
+        phase ^= (uint32_t)(turn == 0);
       } else {
-#pragma unroll
-        for (int o = 4; o > 0; o >>= 1) t = merge(t, {__shfl_xor_sync(0xffffffffu, t.m, o), __shfl_xor_sync(0xffffffffu, t.l, o)}, c2);
-        t.m = __shfl_sync(0xffffffffu, t.m, 0);
-        ts = __shfl_sync(0xffffffffu, t.l, 0);
+        t = merge_lanes(t, c2);
       }
+      const float ts = t.l;
       const float tm = t.m;
       const float scale_p = p.t_lse ? 1.f : (ts > 0.f ? 1.f / ts : (ts == 0.f ? 0.f : ts));
       const float whole = ts * scale_p;
@@ -553,16 +629,8 @@ __global__ void __launch_bounds__(kRingThreads, 2) distill_ring_kernel(const Dis
       const float A = whole + pt;
       float ref, inv, qt;
       bool empty;
-      MaxSum all = {kLow, 0.f}, others = {kLow, 0.f};
+      MaxSum all = {kLow, 0.f};
       if (MODE != DIST_BACKWARD) {
-        for (int i = lane; i < C * kRingWarps; i += 32) others = merge(others, s_sum[turn][i], c2);
-        others = merge_lanes(others, c2);
-        turn ^= 1;
-        MaxSum n = lane < kw ? s_named[b][lane] : MaxSum{kLow, 0.f};
-#pragma unroll
-        for (int o = 4; o > 0; o >>= 1) n = merge(n, {__shfl_xor_sync(0xffffffffu, n.m, o), __shfl_xor_sync(0xffffffffu, n.l, o)}, c2);
-        n.m = __shfl_sync(0xffffffffu, n.m, 0);
-        n.l = __shfl_sync(0xffffffffu, n.l, 0);
         all = merge(others, n, c2);
         empty = all.l == 0.f;
         ref = all.m;
@@ -595,19 +663,19 @@ __global__ void __launch_bounds__(kRingThreads, 2) distill_ring_kernel(const Dis
         }
         if (cur.c >= first && cur.c < last) {
           late_at = dz + cur.c;
-          late = empty ? 0.f : ws * (A * student(cur.z) - ex2(teacher2(cur.t, cur.t_lse, tm)) * scale_p);
+          late = empty ? 0.f : ws * (A * student(from_raw<T>(cur.z)) - ex2(teacher2(__uint_as_float(cur.t), cur.t_lse, tm)) * scale_p);
         }
       }
       if (MODE != DIST_BACKWARD && rank == 0) {
         float kl = 0.f;
         if (cur.c >= 0) {
-          const float lp = teacher2(cur.t, cur.t_lse, tm), pk = ex2(lp) * scale_p;
-          if (pk > 0.f || pk != pk) kl = pk * ((lp + log2f(scale_p)) - ((cur.z - all.m) * c2 - log2f(all.l)));
+          const float lp = teacher2(__uint_as_float(cur.t), cur.t_lse, tm), pk = ex2(lp) * scale_p;
+          if (pk > 0.f || pk != pk) kl = pk * ((lp + log2f(scale_p)) - ((from_raw<T>(cur.z) - all.m) * c2 - log2f(all.l)));
         }
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) kl += __shfl_xor_sync(0xffffffffu, kl, o);
         if (lane == 0) s_kl[b][warp] = kl;
-        if (tid == 0) {
+        if (tid == kRingThreads - 1) {          // of a warp that has entries last
           late_row = row;
           late_w = empty ? 0.f : cur.w;
           late_rest = pt > 0.f ? pt * (log2f(pt) - log2f(qt)) : 0.f;
