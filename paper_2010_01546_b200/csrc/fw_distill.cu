@@ -342,22 +342,28 @@ __global__ void __launch_bounds__(512, 2) distill_kernel(const Distill p) {
 // ---------------------------------------------------------------------------
 // Long rows.  A row is a chain of latencies (entries, their logits, the slice, an exchange over the cluster, stores), and with a
 // CTA for each slice of each row the chains and not the bytes took the time: 4096 x 131072 bf16 1708 us.  So clusters stay and
-// walk the rows, and everything is on its way before it is needed:
-//   - a thread copies its own classes of the next two rows to shared memory (cp.async: it reads back only what it wrote itself, so
-//     no barrier stands between), 96 KB in two CTAs a SM;
-//   - entry k of a row belongs to thread k: class, logits and weight are loaded three rows ahead, the student's logit two;
-//   - while its sums are on their way to the cluster's other CTAs a warp prepares the next row's entries (repeated classes, bit
-//     set, the teacher's and the named classes' sums);
-//   - what is written over the row's stores (named classes) or needs all warps (the loss) follows after the next row's barrier.
-// A row has one barrier of the CTA.  Sums go from each warp to each CTA of the cluster (st.async, counted in bytes there): a barrier of
-// the cluster would also wait for the stores of the row before.
+// walk the rows, everything is on its way before it is needed, and the entries have a warp of their own:
+//   eight warps   classes of the slice: cp.async two rows ahead (a thread reads back only what it copied: no barrier), exponentials
+//                 in registers, each warp's sum sent to every CTA of the cluster (st.async, counted in bytes there), the gradient
+//                 once the factor is known;
+//   one warp      entries: class, teacher's logit and row's numbers copied 2 kAheadRows + 1 rows ahead, the student's logit
+//                 kAheadRows + 1; repeated classes, bit set and the teacher's sums of the next row while the eight work on
+//                 this one; and the named classes' gradient of the row before over the eight warps' stores;
+//   one warp      all sums, the factor, the loss.
+// They meet on mbarriers, a CTA has no common barrier.  With the entries spread over the eight warps, a barrier a row and every
+// thread working out the factor, the fixed part of a row was 650 instructions a warp beside 320 for its classes: 690 us.
 // ---------------------------------------------------------------------------
-constexpr int kRingThreads = 256, kRingWarps = 8, kRingSlots = 3, kRingMaxK = 256, kRingMaxCtas = 16;
+constexpr int kRingWarps = 8, kRingThreads = 32 * kRingWarps, kRingSlots = 3, kRingMaxK = 256, kRingMaxCtas = 16;
+constexpr int kRingAll = kRingThreads + 64;
+constexpr int kAheadRows = 2, kEntrySlots = 2 * kAheadRows + 4;
 
 // to a place in a CTA of the cluster, counted in bytes on that CTA's barrier
 __device__ __forceinline__ void send_pair(uint32_t addr, MaxSum v, uint32_t bar) {
   asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 [%0], {%1, %2}, [%3];" ::"r"(addr), "f"(v.m), "f"(v.l), "r"(bar)
                : "memory");
+}
+__device__ __forceinline__ void ahead4(uint32_t to, const void* from) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to), "l"(from) : "memory");
 }
 __device__ __forceinline__ void unpack16(uint4 q, float (&v)[8]) {
   v[0] = bf16_lo(q.x); v[1] = bf16_hi(q.x); v[2] = bf16_lo(q.y); v[3] = bf16_hi(q.y);
@@ -366,347 +372,420 @@ __device__ __forceinline__ void unpack16(uint4 q, float (&v)[8]) {
 __device__ __forceinline__ void unpack16(uint4 q, float (&v)[4]) {
   v[0] = __uint_as_float(q.x); v[1] = __uint_as_float(q.y); v[2] = __uint_as_float(q.z); v[3] = __uint_as_float(q.w);
 }
+// A 16-bit element by itself cannot be copied ahead: the aligned word that holds it is, and this takes it out.
+template <class E>
+__device__ __forceinline__ float from_word(uint32_t w, const E* at) {
+  if (sizeof(E) == 4) return __uint_as_float(w);
+  return (reinterpret_cast<uintptr_t>(at) & 2) ? bf16_hi(w) : bf16_lo(w);
+}
+template <class E>
+__device__ __forceinline__ const void* word_of(const E* at) {
+  return reinterpret_cast<const void*>(reinterpret_cast<uintptr_t>(at) & ~(uintptr_t)3);
+}
 
-// What a thread knows of a row: its entry, and the row's numbers.  Entries are kept as they were loaded until they are used: a
-// conversion next to the load waits for it (the loads queue behind the rows on their way: 2500 clocks).
-struct RingRow {
-  float w, t_lse, s0, s1;    // weight (0 past the last row), teacher's normaliser, backward: stat
-  int c, hi;                 // class of this thread's entry, -1: none; with 64 bits its upper half
-  uint32_t t, z;             // teacher's and student's logit, their bits
-};
-__device__ __forceinline__ uint32_t raw(const float* p) { return *reinterpret_cast<const uint32_t*>(p); }
-__device__ __forceinline__ uint32_t raw(const __nv_bfloat16* p) { return *reinterpret_cast<const uint16_t*>(p); }
-template <class T>
-__device__ __forceinline__ float from_raw(uint32_t v) { return __uint_as_float(sizeof(T) == 2 ? v << 16 : v); }
+struct RingNumbers { float w, t_lse, s0, s1; };
+// What the sums' warp says of a row: of the classes that are not named, and for the gradient of those that are
+struct RingScale { float ref, factor, ws, A, inv, tm, scale_p; };
 
 // FILL: the last CTA's slice ends inside an access of 16 bytes, with one, or all slices fill all accesses of their threads.
 template <class T, int NV, int MODE, int FILL>
-__global__ void __launch_bounds__(kRingThreads, 2) distill_ring_kernel(const Distill p, int rows, int C) {
+__global__ void __launch_bounds__(kRingAll, 2) distill_ring_kernel(const Distill p, int rows, int C) {
   constexpr int VEC = 16 / sizeof(T);
+  constexpr int words = NV * kRingThreads * VEC / 32;
   extern __shared__ __align__(16) uint8_t dyn8[];
-  __shared__ __align__(16) int s_cls[2][kRingMaxK];
-  __shared__ MaxSum s_teacher[2][kRingWarps], s_named[2][kRingWarps];
   __shared__ MaxSum s_sum[2][kRingMaxCtas * kRingWarps];
-  __shared__ float s_kl[2][kRingWarps];
-  __shared__ __align__(8) uint64_t s_bar[2];
-  __shared__ int s_lost;                     // a wait for the cluster's sums gave up
+  __shared__ RingNumbers s_num[kEntrySlots];
+  __shared__ RingScale s_scale[2];
+  __shared__ MaxSum s_teacher[2], s_named[2];
+  __shared__ float s_w[kRingWarps][kRingSlots + 2];
+  __shared__ __align__(8) uint64_t bar_sums[2], bar_bits[2], bar_scale[2], bar_done[2];
+  __shared__ int s_lost;                          // a wait gave up
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int rank = (int)blockIdx.x % C, row0 = (int)blockIdx.x / C, step = (int)gridDim.x / C;
-  uint4* ring = reinterpret_cast<uint4*>(dyn8);                                  // [slot][k][thread]
-  constexpr int words = NV * kRingThreads * VEC / 32;
-  uint32_t* bits = reinterpret_cast<uint32_t*>(ring + kRingSlots * NV * kRingThreads);   // [3][words]
+  uint4* ring = reinterpret_cast<uint4*>(dyn8);                                             // [slot][k][thread]
+  uint32_t* bits = reinterpret_cast<uint32_t*>(ring + kRingSlots * NV * kRingThreads);      // [2][words]
+  // [slot][class, teacher's logit, student's logit, with 64 bits the class's upper half][K]
+  const int kp = (p.K + 3) & ~3, slot_words = kp * (p.i64 ? 4 : 3);
+  uint32_t* entries = bits + 2 * words;
   const float c2 = p.inv_tau * kLog2e;
   const int first = rank * p.slice, last = min(p.V, first + p.slice);
-  const int mine = last - first - tid * VEC;      // classes of the slice from this thread's first on
-  // of its k-th access: whole (the ring has it), or at least begun
-  auto whole = [&](int k) { return FILL == ROW_FULL || (FILL == ROW_WHOLE ? mine > k * kRingThreads * VEC : mine >= (k * kRingThreads + 1) * VEC); };
-  auto begun = [&](int k) { return FILL == ROW_FULL || mine > k * kRingThreads * VEC; };
-  const uint32_t ring_at = sm100::smem_u32(ring) + tid * 16;
-  const uint32_t push_at = sm100::mapa_shared(sm100::smem_u32(&s_sum[0][rank * kRingWarps + warp]), lane < C ? lane : 0);
-  const uint32_t push_bar = sm100::mapa_shared(sm100::smem_u32(&s_bar[0]), lane < C ? lane : 0);
-
+  auto bar = [](uint64_t& b) { return sm100::smem_u32(&b); };
+  // parity of the n-th wait on one of two barriers that take turns
+  auto wait = [&](uint64_t* two, int n) {
+    const bool ok = sm100::mbar_wait(bar(two[n & 1]), (uint32_t)(n >> 1) & 1u, &s_lost, s_lost ? 1u : sm100::kSpinLimit);
+    if (__all_sync(0xffffffffu, ok)) return true;              // one verdict a warp
+    s_lost = 1;
+    return false;
+  };
   auto zrow = [&](int row) { return static_cast<const T*>(p.Z) + (int64_t)row * p.ldz; };
-  auto load_row = [&](int row) {
-    RingRow r = {0.f, 0.f, 0.f, 0.f, -1, -1, 0u, 0u};
-    if (row < rows) {
-      r.w = 1.f;
-      if (p.weight) r.w = p.weight[row];
-      if (p.t_lse) r.t_lse = p.t_lse[row];
-      if (MODE == DIST_BACKWARD) { r.s0 = p.stat_in[2 * (int64_t)row]; r.s1 = p.stat_in[2 * (int64_t)row + 1]; }
-      if (tid < p.K) {
-        const int64_t at = (int64_t)row * p.K + tid;
-        if (p.i64) {
-          const int2 i = static_cast<const int2*>(p.I)[at];
-          r.c = i.x;
-          r.hi = i.y;
-        } else {
-          r.c = static_cast<const int32_t*>(p.I)[at];
-        }
-        r.t = p.t_bf16 ? raw(static_cast<const __nv_bfloat16*>(p.T) + at) : raw(static_cast<const float*>(p.T) + at);
-      }
-    }
-    return r;
-  };
-  // the loads have had an iteration: class and logit of the entry
-  auto settle = [&](RingRow& r) {
-    if (r.c < 0 || r.c >= p.V || (p.i64 && r.hi != 0)) r.c = -1;
-    if (p.t_bf16) r.t <<= 16;
-  };
-  // the student's logit of an entry; the backward pass needs those of its slice alone (dZ may be Z: others' are written over)
-  auto load_logit = [&](RingRow& r, int row) {
-    if (r.c >= 0 && r.w != 0.f && (MODE != DIST_BACKWARD || (r.c >= first && r.c < last))) r.z = raw(zrow(row) + r.c);
-  };
-  auto fetch = [&](const RingRow& r, int row, int it) {
-    if (r.w != 0.f) {
-      const T* z = zrow(row) + first;
-      const uint32_t to = ring_at + (uint32_t)(it % kRingSlots) * (NV * kRingThreads * 16);
-#pragma unroll
-      for (int k = 0; k < NV; ++k)
-        if (whole(k)) ahead16(to + k * kRingThreads * 16, z + (uint32_t)((k * kRingThreads + tid) * VEC));
-    }
-    ahead_commit();
-  };
-  auto teacher2 = [&](float t, float t_lse, float tm) { return p.t_lse ? fmaf(t, p.inv_tau, -t_lse) * kLog2e : (t - tm) * c2; };
-  // the entries of a row whose classes stand in s_cls[it & 1] (a barrier of the CTA ago): repeated ones out, bit set, sums
-  auto prepare = [&](RingRow& r, int it) {
-    if (warp * 32 >= p.K) return;
-    // the classes of the entries before this one, four at a time
-    bool twice = false;
-    const int4* before = reinterpret_cast<const int4*>(s_cls[it & 1]);
-    for (int j = 0; j < warp * 8; ++j) {
-      const int4 q = before[j];
-      twice |= q.x == r.c || q.y == r.c || q.z == r.c || q.w == r.c;
-    }
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const int4 q = before[warp * 8 + j];
-      twice |= (4 * j < lane && q.x == r.c) || (4 * j + 1 < lane && q.y == r.c) || (4 * j + 2 < lane && q.z == r.c) || (4 * j + 3 < lane && q.w == r.c);
-    }
-    if (twice) r.c = -1;
-    if (r.c >= first && r.c < last) atomicOr(&bits[(it % 3) * words + ((r.c - first) >> 5)], 1u << ((r.c - first) & 31));
-    const bool in = r.c >= 0;
-    const float rt = __uint_as_float(r.t), rz = from_raw<T>(r.z);
-    MaxSum t = {kLow, 0.f}, n = {kLow, 0.f};
-    if (in) {
-      if (p.t_lse) t.l = ex2(teacher2(rt, r.t_lse, 0.f));
-      else t = {fmaxf(rt, kLow), rt == -INFINITY ? 0.f : rt != rt ? rt : 1.f};
-      if (MODE != DIST_BACKWARD) n = {fmaxf(rz, kLow), rz == -INFINITY ? 0.f : rz != rz ? rz : 1.f};
-    }
-    merge_lanes2(t, n, c2);
-    if (lane == 0) { s_teacher[it & 1][warp] = t; s_named[it & 1][warp] = n; }
-  };
 
-  dep_wait();
-  // ---- the first three rows ----
-  RingRow cur = load_row(row0), next = load_row(row0 + step), third = load_row(row0 + 2 * step);
-  fetch(cur, row0, 0);
-  fetch(next, row0 + step, 1);
-  settle(cur);
-  settle(next);
-  load_logit(cur, row0);
-  load_logit(next, row0 + step);
-  for (int i = tid; i < 3 * words; i += kRingThreads) bits[i] = 0;
+  for (int i = tid; i < 2 * words; i += kRingAll) bits[i] = 0;
   if (tid == 0) {
     s_lost = 0;
-    sm100::mbar_init(sm100::smem_u32(&s_bar[0]), 1);
-    sm100::mbar_init(sm100::smem_u32(&s_bar[1]), 1);
+    for (int i = 0; i < 2; ++i) {
+      sm100::mbar_init(bar(bar_sums[i]), 1);
+      sm100::mbar_init(bar(bar_bits[i]), 1);
+      sm100::mbar_init(bar(bar_scale[i]), 1);
+      sm100::mbar_init(bar(bar_done[i]), kRingWarps);
+    }
     sm100::mbar_fence_init();
   }
-  s_cls[0][tid] = cur.c;
-  s_cls[1][tid] = next.c;
+  dep_wait();
   __syncthreads();
-  prepare(cur, 0);
-  // what follows the next barrier: this thread's named class of the row before, and (one thread) its loss
-  T* late_at = nullptr;
-  float late = 0.f;
-  int late_row = -1;
-  float late_w = 0.f, late_rest = 0.f, late_lse = 0.f, late_other = 0.f;
-  auto finish = [&](int it) {
-    if (MODE != DIST_LOSS && late_at) put(late_at, late);
-    late_at = nullptr;
-    if (MODE != DIST_BACKWARD && late_row >= 0) {
-      float kl = 0.f;
-#pragma unroll
-      for (int k = 0; k < kRingWarps; ++k) kl += s_kl[it & 1][k];
-      p.loss[late_row] = late_w * (kl + late_rest) * kLn2;
-      if (p.stat) { p.stat[2 * (int64_t)late_row] = late_lse; p.stat[2 * (int64_t)late_row + 1] = late_other; }
-      late_row = -1;
-    }
-  };
-
-  // no CTA writes into another's shared memory before that one has begun
+  // no CTA sends to another before that one has begun
   sm100::cluster_arrive();
   sm100::cluster_wait();
-  int it = 0;
-  // Place of the sums, by rows that count.  A CTA's place is written again two such rows on: by then every CTA has had all sums of
-  // the row between, which this CTA's warps sent after they had read the place.
-  int turn = 0;
-  uint32_t phase = 0;
-  for (int row = row0; row < rows; row += step, ++it) {
-    const int b = it & 1;
-    ahead_wait<1>();                                            // this row's classes
-    __syncthreads();
-    finish(it ^ 1);
-    // ---- two and three rows ahead ----
-    settle(third);
-    s_cls[b][tid] = third.c;                                    // (the row's own have been used)
-    for (int i = tid; i < words; i += kRingThreads) bits[((it + 2) % 3) * words + i] = 0;
-    load_logit(third, row + 2 * step);
-    fetch(third, row + 2 * step, it + 2);
-    const RingRow fourth = load_row(row + 3 * step);
 
-    const bool live = cur.w != 0.f;                             // the same in all threads of the cluster
-    float e[NV][VEC];
-    MaxSum sum = {kLow, 0.f};
-    const T* z = zrow(row) + first;
-    if (live) {
-      const uint4* slot = ring + (it % kRingSlots) * NV * kRingThreads + tid;
-#pragma unroll
-      for (int k = 0; k < NV; ++k) {
-        if (whole(k)) {
-          unpack16(slot[k * kRingThreads], e[k]);
-        } else if (FILL == ROW_PART) {                           // the row's last few, and past them
-          load<VEC>(z + (k * kRingThreads + tid) * VEC, mine - k * kRingThreads * VEC, -INFINITY, e[k]);
-        } else {
-#pragma unroll
-          for (int v = 0; v < VEC; ++v) e[k][v] = -INFINITY;
-        }
-      }
-      if (MODE != DIST_BACKWARD) {
-        float part[2] = {kLow, kLow};
+  if (warp < kRingWarps) {
+    // ---- classes ----
+    const int mine = last - first - tid * VEC;    // of the slice from this thread's first on
+    // its k-th access: whole (the ring has it), or at least begun
+    auto whole = [&](int k) { return FILL == ROW_FULL || (FILL == ROW_WHOLE ? mine > k * kRingThreads * VEC : mine >= (k * kRingThreads + 1) * VEC); };
+    auto begun = [&](int k) { return FILL == ROW_FULL || mine > k * kRingThreads * VEC; };
+    const uint32_t ring_at = sm100::smem_u32(ring) + tid * 16;
+    const uint32_t push_at = sm100::mapa_shared(sm100::smem_u32(&s_sum[0][rank * kRingWarps + warp]), lane < C ? lane : 0);
+    const uint32_t push_bar = sm100::mapa_shared(bar(bar_sums[0]), lane < C ? lane : 0);
+    auto fetch = [&](int row, int slot, bool live) {
+      if (live) {
+        const T* z = zrow(row) + first;
+        const uint32_t to = ring_at + (uint32_t)slot * (NV * kRingThreads * 16);
 #pragma unroll
         for (int k = 0; k < NV; ++k)
-#pragma unroll
-          for (int v = 0; v < VEC; v += 2) {
-            part[0] = fmaxf(part[0], e[k][v]);
-            part[1] = fmaxf(part[1], e[k][v + 1]);
-          }
-        sum.m = fmaxf(part[0], part[1]);
-        part[0] = part[1] = 0.f;
-        const float less[2] = {-sum.m, -sum.m};
-        // a byte (bf16) or half of one of the bit set to an access
-        const uint32_t* set = bits + (it % 3) * words + tid * VEC / 32;
+          if (whole(k)) ahead16(to + k * kRingThreads * 16, z + (uint32_t)((k * kRingThreads + tid) * VEC));
+      }
+    };
+    // weights, four rows ahead: a row of weight 0 is not fetched
+    auto fetch_weight = [&](int row, int it) {
+      if (lane == 0 && row < rows && p.weight) ahead4(sm100::smem_u32(&s_w[warp][it % (kRingSlots + 2)]), p.weight + row);
+    };
+    auto counts = [&](int row, int it) { return row < rows && (!p.weight || s_w[warp][it % (kRingSlots + 2)] != 0.f); };
+    for (int i = 0; i < 4; ++i) fetch_weight(row0 + i * step, i);
+    ahead_commit();
+    ahead_wait<0>();
+    __syncwarp();
+    bool live0 = counts(row0, 0), live1 = counts(row0 + step, 1);
+    fetch(row0, 0, live0);
+    ahead_commit();
+    fetch(row0 + step, 1, live1);
+    ahead_commit();
+    int turn = 0, slot = 0;
+    int it = 0;
+    for (int row = row0; row < rows; row += step, ++it) {
+      ahead_wait<1>();                            // this row's classes, the weight of the row after next
+      __syncwarp();
+      const bool live2 = counts(row + 2 * step, it + 2);
+      fetch(row + 2 * step, slot == 0 ? 2 : slot - 1, live2);       // (the slot of the row before)
+      fetch_weight(row + 4 * step, it + 4);
+      ahead_commit();
+      T* dz = MODE == DIST_LOSS ? nullptr : static_cast<T*>(p.dZ) + (int64_t)row * p.lddz + first;
+      // A row begins when its entries are ready and ends when its factor is there, whether it needs them or not: so no warp is a
+      // turn of a barrier ahead of another, and a place for sums has been read in every CTA before it is written again two such
+      // rows on (that takes all sums of the row between, which are sent after the factor of the row before).
+      if (!wait(bar_bits, it)) break;
+      if (live0) {                                // the same in all warps of the cluster
+        float e[NV][VEC];
+        float top = kLow;
+        const uint4* at = ring + slot * NV * kRingThreads + tid;
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
-          const uint32_t named = (set[k * kRingThreads * VEC / 32] >> (tid * VEC % 32)) & ((1u << VEC) - 1u);
+          if (whole(k)) {
+            unpack16(at[k * kRingThreads], e[k]);
+          } else if (FILL == ROW_PART) {          // the row's last few, and past them
+            load<VEC>(zrow(row) + first + (k * kRingThreads + tid) * VEC, mine - k * kRingThreads * VEC, -INFINITY, e[k]);
+          } else {
 #pragma unroll
-          for (int v = 0; v < VEC; v += 2) {
-            float two[2] = {e[k][v], e[k][v + 1]};
-            vadd<2>(two, less);
-            vscale<2>(two, c2);
-            e[k][v] = ex2(two[0]);
-            e[k][v + 1] = ex2(two[1]);
+            for (int v = 0; v < VEC; ++v) e[k][v] = -INFINITY;
           }
-          if (!named) {
+        }
+        if (MODE != DIST_BACKWARD) {
+          float part[2] = {kLow, kLow};
+#pragma unroll
+          for (int k = 0; k < NV; ++k)
 #pragma unroll
             for (int v = 0; v < VEC; v += 2) {
-              const float two[2] = {e[k][v], e[k][v + 1]};
-              vadd<2>(part, two);
+              part[0] = fmaxf(part[0], e[k][v]);
+              part[1] = fmaxf(part[1], e[k][v + 1]);
             }
-          } else {
+          top = fmaxf(part[0], part[1]);
+          part[0] = part[1] = 0.f;
+          const float less[2] = {-top, -top};
+          // a byte (bf16) or half of one of the bit set to an access
+          const uint32_t* set = bits + (it & 1) * words + tid * VEC / 32;
 #pragma unroll
-            for (int v = 0; v < VEC; ++v)
-              if (!((named >> v) & 1u)) part[v & 1] += e[k][v];
+          for (int k = 0; k < NV; ++k) {
+            const uint32_t named = (set[k * kRingThreads * VEC / 32] >> (tid * VEC % 32)) & ((1u << VEC) - 1u);
+#pragma unroll
+            for (int v = 0; v < VEC; v += 2) {
+              float two[2] = {e[k][v], e[k][v + 1]};
+              vadd<2>(two, less);
+              vscale<2>(two, c2);
+              e[k][v] = ex2(two[0]);
+              e[k][v + 1] = ex2(two[1]);
+            }
+            if (!named) {
+#pragma unroll
+              for (int v = 0; v < VEC; v += 2) {
+                const float two[2] = {e[k][v], e[k][v + 1]};
+                vadd<2>(part, two);
+              }
+            } else {
+#pragma unroll
+              for (int v = 0; v < VEC; ++v)
+                if (!((named >> v) & 1u)) part[v & 1] += e[k][v];
+            }
+          }
+          const MaxSum s = merge_lanes({top, part[0] + part[1]}, c2);
+          if (lane < C) send_pair(push_at + (uint32_t)turn * (uint32_t)sizeof(s_sum[0]), s, push_bar + (uint32_t)turn * 8u);
+          turn ^= 1;
+        }
+        if (MODE != DIST_LOSS) {
+          if (!wait(bar_scale, it)) break;
+          const RingScale& sc = s_scale[it & 1];
+          const float f = MODE == DIST_BACKWARD || sc.factor == 0.f ? sc.factor : sc.factor * ex2((top - sc.ref) * c2);
+#pragma unroll
+          for (int k = 0; k < NV; ++k) {
+            if (!begun(k)) continue;
+            if (MODE == DIST_BACKWARD) {
+#pragma unroll
+              for (int v = 0; v < VEC; ++v) e[k][v] = f == 0.f ? 0.f : f * ex2(fmaf(e[k][v], p.inv_tau, -sc.ref) * kLog2e);
+            } else {
+              vscale<VEC>(e[k], f);
+            }
+            store<VEC>(dz + (uint32_t)((k * kRingThreads + tid) * VEC), FILL == ROW_PART ? mine - k * kRingThreads * VEC : VEC, e[k]);
           }
         }
-        sum.l = part[0] + part[1];
-        const MaxSum s = merge_lanes(sum, c2);
-        if (tid == 0) sm100::mbar_expect_tx(sm100::smem_u32(&s_bar[turn]), (uint32_t)(C * kRingWarps * sizeof(MaxSum)));
-        if (lane < C) send_pair(push_at + (uint32_t)turn * (uint32_t)sizeof(s_sum[0]), s, push_bar + (uint32_t)turn * 8u);
-        __syncwarp();
-      }
-    }
-    prepare(next, it + 1);
-    __syncwarp();
-    if (live) {
-      bool have = true;
-      if (MODE != DIST_BACKWARD) {
-        have = sm100::mbar_wait(sm100::smem_u32(&s_bar[turn]), phase, &s_lost, s_lost ? 1u : sm100::kSpinLimit);
-        if (!have) s_lost = 1;
-      }
-      // ---- the teacher's mass, the student's normalisers: see distill_kernel ----
-      const int kw = (p.K + 31) / 32;
-      MaxSum t = lane < kw ? s_teacher[b][lane] : MaxSum{kLow, 0.f};
-      MaxSum others = {kLow, 0.f}, n = {kLow, 0.f};
-      if (MODE != DIST_BACKWARD) {
-        const int sums = C * kRingWarps;
-        if (lane < sums) others = s_sum[turn][lane];
-        for (int i = lane + 32; i < sums; i += 32) others = merge(others, s_sum[turn][i], c2);
-        if (lane < kw) n = s_named[b][lane];
-        if (!have) others.l = NAN;               // the row's loss and gradient say so
-        merge_lanes3(t, others, n, c2);
-        turn ^= 1;
-        phase ^= (uint32_t)(turn == 0);
-      } else {
-        t = merge_lanes(t, c2);
-      }
-      const float ts = t.l;
-      const float tm = t.m;
-      const float scale_p = p.t_lse ? 1.f : (ts > 0.f ? 1.f / ts : (ts == 0.f ? 0.f : ts));
-      const float whole = ts * scale_p;
-      float pt = 0.f;
-      if (p.t_lse) pt = 1.f - whole < 0.f ? 0.f : 1.f - whole;
-      const float A = whole + pt;
-      float ref, inv, qt;
-      bool empty;
-      MaxSum all = {kLow, 0.f};
-      if (MODE != DIST_BACKWARD) {
-        all = merge(others, n, c2);
-        empty = all.l == 0.f;
-        ref = all.m;
-        inv = 1.f / all.l;
-        qt = others.l * ex2((others.m - all.m) * c2) * inv;
-      } else {
-        ref = cur.s0;
-        inv = 1.f;
-        empty = ref == -INFINITY;
-        qt = ex2((cur.s1 - ref) * kLog2e);
-      }
-      auto student = [&](float v) { return ex2(MODE == DIST_BACKWARD ? fmaf(v, p.inv_tau, -ref) * kLog2e : (v - ref) * c2) * inv; };
-      const float ws = empty ? 0.f : cur.w * p.inv_tau;
-      if (MODE != DIST_LOSS) {
-        const float other = pt > 0.f && qt != 0.f ? A - pt / qt : A;
-        T* dz = static_cast<T*>(p.dZ) + (int64_t)row * p.lddz;
-        const float f = empty ? 0.f : MODE == DIST_BACKWARD ? ws * other : ws * other * ex2((sum.m - ref) * c2) * inv;
-        T* mine_dz = dz + first;
-#pragma unroll
-        for (int k = 0; k < NV; ++k) {
-          if (!begun(k)) continue;
-          if (MODE == DIST_BACKWARD) {
-#pragma unroll
-            for (int v = 0; v < VEC; ++v) e[k][v] = empty ? 0.f : f * student(e[k][v]);
-          } else {
-            vscale<VEC>(e[k], f);
-          }
-          const uint32_t c = (uint32_t)((k * kRingThreads + tid) * VEC);
-          store<VEC>(mine_dz + c, FILL == ROW_PART ? mine - k * kRingThreads * VEC : VEC, e[k]);
-        }
-        if (cur.c >= first && cur.c < last) {
-          late_at = dz + cur.c;
-          late = empty ? 0.f : ws * (A * student(from_raw<T>(cur.z)) - ex2(teacher2(__uint_as_float(cur.t), cur.t_lse, tm)) * scale_p);
-        }
-      }
-      if (MODE != DIST_BACKWARD && rank == 0) {
-        float kl = 0.f;
-        if (cur.c >= 0) {
-          const float lp = teacher2(__uint_as_float(cur.t), cur.t_lse, tm), pk = ex2(lp) * scale_p;
-          if (pk > 0.f || pk != pk) kl = pk * ((lp + log2f(scale_p)) - ((from_raw<T>(cur.z) - all.m) * c2 - log2f(all.l)));
-        }
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) kl += __shfl_xor_sync(0xffffffffu, kl, o);
-        if (lane == 0) s_kl[b][warp] = kl;
-        if (tid == kRingThreads - 1) {          // of a warp that has entries last
-          late_row = row;
-          late_w = empty ? 0.f : cur.w;
-          late_rest = pt > 0.f ? pt * (log2f(pt) - log2f(qt)) : 0.f;
-          if (whole != whole) late_rest = whole;
-          late_lse = empty ? -INFINITY : fmaf(all.m, p.inv_tau, logf(all.l));
-          late_other = others.l == 0.f ? -INFINITY : fmaf(others.m, p.inv_tau, logf(others.l));
-          if (empty) late_rest = 0.f;
-        }
-        if (empty && lane == 0) s_kl[b][warp] = 0.f;
-      }
-    } else {
-      if (MODE != DIST_LOSS) {
+      } else if (MODE != DIST_LOSS) {
         const float zero[VEC] = {};
-        T* dz = static_cast<T*>(p.dZ) + (int64_t)row * p.lddz;
-        for (int c = first + tid * VEC; c < last; c += kRingThreads * VEC) store<VEC>(dz + c, last - c, zero);
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+          if (begun(k)) store<VEC>(dz + (uint32_t)((k * kRingThreads + tid) * VEC), FILL == ROW_PART ? mine - k * kRingThreads * VEC : VEC, zero);
       }
-      if (MODE != DIST_BACKWARD && rank == 0 && tid == 0) {
-        p.loss[row] = 0.f;
-        if (p.stat) { p.stat[2 * (int64_t)row] = 0.f; p.stat[2 * (int64_t)row + 1] = 0.f; }
-      }
+      if (!wait(bar_scale, it)) break;
+      if (lane == 0) sm100::mbar_arrive(bar(bar_done[it & 1]));
+      live0 = live1;
+      live1 = live2;
+      if (++slot == kRingSlots) slot = 0;
     }
-    cur = next;
-    next = third;
-    third = fourth;
+    ahead_wait<0>();
+  } else {
+    const bool t16 = p.t_bf16 != 0;
+    auto slot_of = [](int it) { return it % kEntrySlots; };
+    auto cls = [&](int it) { return reinterpret_cast<int*>(entries + slot_of(it) * slot_words); };
+    auto weight = [&](int it) { return p.weight ? s_num[slot_of(it)].w : 1.f; };
+    auto t_lse_of = [&](int it) { return p.t_lse ? s_num[slot_of(it)].t_lse : 0.f; };
+    auto t_at = [&](int row, int k) { return static_cast<const char*>(p.T) + ((int64_t)row * p.K + k) * (t16 ? 2 : 4); };
+    auto t_of = [&](int it, int row, int k) {
+      const uint32_t w = entries[slot_of(it) * slot_words + kp + k];
+      return t16 ? from_word(w, reinterpret_cast<const __nv_bfloat16*>(t_at(row, k))) : __uint_as_float(w);
+    };
+    auto z_of = [&](int it, int row, int k, int c) { return from_word(entries[slot_of(it) * slot_words + 2 * kp + k], zrow(row) + c); };
+    auto teacher2 = [&](float t, float t_lse, float tm) { return p.t_lse ? fmaf(t, p.inv_tau, -t_lse) * kLog2e : (t - tm) * c2; };
+    if (warp == kRingWarps) {
+      // ---- entries ----
+      auto fetch_entries = [&](int row, int it) {
+        if (row >= rows) return;
+        RingNumbers& n = s_num[slot_of(it)];
+        const uint32_t to = sm100::smem_u32(entries + slot_of(it) * slot_words);
+        if (lane == 0 && p.weight) ahead4(sm100::smem_u32(&n.w), p.weight + row);
+        if (lane == 1 && p.t_lse) ahead4(sm100::smem_u32(&n.t_lse), p.t_lse + row);
+        if (MODE == DIST_BACKWARD && lane >= 2 && lane < 4) ahead4(sm100::smem_u32(&n.s0) + (lane - 2) * 4, p.stat_in + 2 * (int64_t)row + (lane - 2));
+        for (int k = lane; k < p.K; k += 32) {
+          const int64_t at = (int64_t)row * p.K + k;
+          const int32_t* i = static_cast<const int32_t*>(p.I) + (p.i64 ? 2 * at : at);
+          ahead4(to + k * 4, i);
+          if (p.i64) ahead4(to + (3 * kp + k) * 4, i + 1);
+          ahead4(to + (kp + k) * 4, word_of(t_at(row, k)));
+        }
+      };
+      // classes as they are used, and the student's logits on their way (the backward pass needs those of its slice alone: dZ may be
+      // Z, and other CTAs write over theirs)
+      auto fetch_logits = [&](int row, int it) {
+        if (row >= rows) return;
+        const bool live = weight(it) != 0.f;
+        int* c = cls(it);
+        const uint32_t to = sm100::smem_u32(c + 2 * kp);
+        for (int k = lane; k < p.K; k += 32) {
+          int i = c[k];
+          if (i >= p.V || (p.i64 && c[3 * kp + k] != 0)) i = -1;
+          if (i < 0) i = -1;
+          c[k] = i;
+          const bool wanted = MODE == DIST_BACKWARD ? i >= first && i < last : i >= 0;
+          if (live && wanted) ahead4(to + k * 4, word_of(zrow(row) + i));
+        }
+      };
+      // repeated classes out, bit set, sums of the teacher's and of the named classes' exponentials
+      auto prepare = [&](int row, int it) {
+        MaxSum t = {kLow, 0.f}, n = {kLow, 0.f};
+        if (weight(it) != 0.f) {
+          const float t_lse = t_lse_of(it);
+          int* c = cls(it);
+          for (int g = 0; g < p.K; g += 32) {
+            // a lane compares with the entries before its own, four at a time (a repeated class's first is not taken out)
+            const int k = g + lane, i = k < p.K ? c[k] : -1;
+            bool twice = false;
+            const int4* before = reinterpret_cast<const int4*>(c);
+#pragma unroll 4
+            for (int j = 0; j < g; j += 4) {
+              const int4 q = before[j >> 2];
+              twice |= q.x == i || q.y == i || q.z == i || q.w == i;
+            }
+#pragma unroll
+            for (int j = 0; j < 32; j += 4) {
+              if (g + j < p.K) {
+                const int4 q = before[(g + j) >> 2];
+                twice |= (j < lane && q.x == i) || (j + 1 < lane && q.y == i) || (j + 2 < lane && q.z == i) || (j + 3 < lane && q.w == i);
+              }
+            }
+            __syncwarp();
+            if (i >= 0 && twice) c[k] = -2;
+            if (i >= 0 && !twice) {
+              if (i >= first && i < last) atomicOr(&bits[(it & 1) * words + ((i - first) >> 5)], 1u << ((i - first) & 31));
+              const float rt = t_of(it, row, k);
+              if (p.t_lse) t.l += ex2(teacher2(rt, t_lse, 0.f));
+              else t = merge(t, {fmaxf(rt, kLow), rt == -INFINITY ? 0.f : rt != rt ? rt : 1.f}, c2);
+              if (MODE != DIST_BACKWARD) {
+                const float rz = z_of(it, row, k, i);
+                n = merge(n, {fmaxf(rz, kLow), rz == -INFINITY ? 0.f : rz != rz ? rz : 1.f}, c2);
+              }
+            }
+          }
+          merge_lanes2(t, n, c2);
+        }
+        if (lane == 0) { s_teacher[it & 1] = t; s_named[it & 1] = n; }
+        __syncwarp();
+        if (lane == 0) sm100::mbar_arrive(bar(bar_bits[it & 1]));
+      };
+      // a row whose stores are done: the named classes' gradient over them, its bits out
+      auto finish = [&](int row, int it) {
+        if (weight(it) == 0.f) return;
+        const RingScale sc = s_scale[it & 1];
+        const float t_lse = t_lse_of(it);
+        T* dz = MODE == DIST_LOSS ? nullptr : static_cast<T*>(p.dZ) + (int64_t)row * p.lddz;
+        const int* c = cls(it);
+        for (int k = lane; k < p.K; k += 32) {
+          const int i = c[k];
+          if (i < first || i >= last) continue;
+          bits[(it & 1) * words + ((i - first) >> 5)] = 0;
+          if (MODE != DIST_LOSS) {
+            const float z = z_of(it, row, k, i), pk = ex2(teacher2(t_of(it, row, k), t_lse, sc.tm)) * sc.scale_p;
+            const float q = ex2(MODE == DIST_BACKWARD ? fmaf(z, p.inv_tau, -sc.ref) * kLog2e : (z - sc.ref) * c2) * sc.inv;
+            put(dz + i, sc.ws == 0.f ? 0.f : sc.ws * (sc.A * q - pk));
+          }
+        }
+      };
+      for (int i = 0; i <= 2 * kAheadRows; ++i) fetch_entries(row0 + i * step, i);
+      ahead_commit();
+      ahead_wait<0>();
+      __syncwarp();
+      for (int i = 0; i <= kAheadRows; ++i) fetch_logits(row0 + i * step, i);
+      ahead_commit();
+      ahead_wait<0>();
+      __syncwarp();
+      prepare(row0, 0);
+      int it = 0;
+      bool lost = false;
+      for (int row = row0; row < rows; row += step, ++it) {
+        if (it > 0) {
+          lost = !wait(bar_done, it - 1);
+          if (lost) break;
+          finish(row - step, it - 1);
+          __syncwarp();
+        }
+        ahead_wait<kAheadRows - 1>();
+        __syncwarp();
+        if (row + step < rows) prepare(row + step, it + 1);
+        fetch_logits(row + (1 + kAheadRows) * step, it + 1 + kAheadRows);
+        fetch_entries(row + (1 + 2 * kAheadRows) * step, it + 1 + 2 * kAheadRows);
+        ahead_commit();
+      }
+      if (!lost && it > 0 && wait(bar_done, it - 1)) finish(row0 + (it - 1) * step, it - 1);
+      ahead_wait<0>();
+    } else {
+      // ---- sums ----
+      int sums = 0, it = 0, row = row0;            // rows that count; rows
+      bool lost = false;
+      for (; row < rows; row += step, ++it) {
+        lost = !wait(bar_bits, it);
+        if (lost) break;
+        const float w = weight(it);
+        if (w == 0.f) {
+          if (lane == 0) {
+            sm100::mbar_arrive(bar(bar_scale[it & 1]));
+            if (MODE != DIST_BACKWARD && rank == 0) {
+              p.loss[row] = 0.f;
+              if (p.stat) { p.stat[2 * (int64_t)row] = 0.f; p.stat[2 * (int64_t)row + 1] = 0.f; }
+            }
+          }
+          continue;
+        }
+        const MaxSum t = s_teacher[it & 1], n = s_named[it & 1];
+        const float t_lse = t_lse_of(it), tm = t.m, ts = t.l;
+        const float scale_p = p.t_lse ? 1.f : (ts > 0.f ? 1.f / ts : (ts == 0.f ? 0.f : ts));     // a NaN goes on
+        const float whole = ts * scale_p;
+        float pt = 0.f;
+        if (p.t_lse) pt = 1.f - whole < 0.f ? 0.f : 1.f - whole;
+        const float A = whole + pt;
+        float ref, inv, qt;
+        bool empty;
+        MaxSum all = {kLow, 0.f}, others = {kLow, 0.f};
+        if (MODE != DIST_BACKWARD) {
+          const int turn = sums & 1, count = C * kRingWarps;
+          if (lane == 0) sm100::mbar_expect_tx(bar(bar_sums[turn]), (uint32_t)(count * (int)sizeof(MaxSum)));
+          __syncwarp();
+          lost = !wait(bar_sums, sums);
+          if (lost) break;
+          ++sums;
+          if (lane < count) others = s_sum[turn][lane];
+          for (int i = lane + 32; i < count; i += 32) others = merge(others, s_sum[turn][i], c2);
+          others = merge_lanes(others, c2);
+          all = merge(others, n, c2);
+          empty = all.l == 0.f;
+          ref = all.m;
+          inv = 1.f / all.l;
+          qt = others.l * ex2((others.m - all.m) * c2) * inv;
+        } else {
+          ref = s_num[slot_of(it)].s0;
+          inv = 1.f;
+          empty = ref == -INFINITY;
+          qt = ex2((s_num[slot_of(it)].s1 - ref) * kLog2e);
+        }
+        const float ws = empty ? 0.f : w * p.inv_tau;
+        // q_j (A - p_t / q_t) of the others; where there are none, nothing stands at that factor
+        const float other = pt > 0.f && qt != 0.f ? A - pt / qt : A;
+        if (lane == 0) {
+          s_scale[it & 1] = {ref, ws == 0.f ? 0.f : ws * other * inv, ws, A, inv, tm, scale_p};
+          sm100::mbar_arrive(bar(bar_scale[it & 1]));
+        }
+        if (MODE != DIST_BACKWARD && rank == 0) {
+          float kl = 0.f;
+          const float log_all = log2f(all.l), log_p = log2f(scale_p);
+          const int* c = cls(it);
+          for (int k = lane; k < p.K; k += 32) {
+            const int i = c[k];
+            if (i < 0) continue;
+            const float lp = teacher2(t_of(it, row, k), t_lse, tm), pk = ex2(lp) * scale_p;
+            if (pk > 0.f || pk != pk) kl += pk * ((lp + log_p) - ((z_of(it, row, k, i) - all.m) * c2 - log_all));
+          }
+          kl = lanes_sum(kl);
+          if (lane == 0) {
+            if (pt > 0.f) kl += pt * (log2f(pt) - log2f(qt));
+            if (whole != whole) kl = whole;
+            p.loss[row] = empty ? 0.f : w * kl * kLn2;
+            if (p.stat) {
+              p.stat[2 * (int64_t)row] = empty ? -INFINITY : fmaf(all.m, p.inv_tau, logf(all.l));
+              p.stat[2 * (int64_t)row + 1] = others.l == 0.f ? -INFINITY : fmaf(others.m, p.inv_tau, logf(others.l));
+            }
+          }
+        }
+      }
+      // given up: no barrier is touched any more, and the losses of the rows that are left say so
+      if (lost && MODE != DIST_BACKWARD && rank == 0)
+        for (int r = row + lane * step; r < rows; r += 32 * step) p.loss[r] = NAN;
+    }
   }
   dep_trigger();
-  __syncthreads();
-  finish(it ^ 1);
-  __syncwarp();
-  ahead_wait<0>();
   // no CTA leaves while its sums may still be written by another
+  __syncwarp();
   sm100::cluster_arrive();
   sm100::cluster_wait();
 }
@@ -726,36 +805,47 @@ cudaError_t launch(const Distill& p, int C, int threads, int64_t rows, cudaStrea
   return launch_dep_cluster(C, distill_kernel<T, VEC, NV, MODE, KEEP>, dim3((unsigned)(rows * C)), threads, smem, s, p);
 }
 
+// Resident clusters of a kernel, found once for each device, cluster size and size of shared memory
+struct ClusterCache {
+  std::mutex mu;
+  struct { int dev, C, n; size_t smem; } known[16] = {};
+  int count = 0;
+};
+
 template <class T, int NV, int MODE, int FILL>
 cudaError_t launch_ring(const Distill& p, int C, int64_t rows, cudaStream_t s) {
-  static std::mutex mu;
-  static int resident[64][5];                               // clusters of 1, 2, 4, 8, 16 CTAs at once, per device
-  constexpr size_t smem = (size_t)kRingSlots * NV * kRingThreads * 16 + 3 * (NV * kRingThreads * (16 / sizeof(T)) / 8);
+  static ClusterCache cache;
+  constexpr int threads = kRingAll;
+  const size_t smem = (size_t)kRingSlots * NV * kRingThreads * 16 + 2 * (NV * kRingThreads * (16 / sizeof(T)) / 8) +
+                      (size_t)kEntrySlots * ((p.K + 3) & ~3) * (p.i64 ? 16 : 12);
   auto kernel = distill_ring_kernel<T, NV, MODE, FILL>;
-  int dev = 0, n = 0, lg = 0;
-  while ((1 << lg) < C) ++lg;
+  int dev = 0, n = 0;
   cudaError_t e = cudaGetDevice(&dev);
-  if (e != cudaSuccess || dev < 0 || dev >= 64) return e != cudaSuccess ? e : cudaErrorInvalidDevice;
+  if (e != cudaSuccess) return e;
   {
-    std::lock_guard<std::mutex> lock(mu);
-    if (resident[dev][lg] == 0) {
-      e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    std::lock_guard<std::mutex> lock(cache.mu);
+    const int have = cache.count < 16 ? cache.count : 16;
+    for (int i = 0; i < have && !n; ++i)
+      if (cache.known[i].dev == dev && cache.known[i].C == C && cache.known[i].smem == smem) n = cache.known[i].n;
+    if (!n) {
+      // as much as any launch asks for
+      e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 200 * 1024);
       if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
       if (e != cudaSuccess) return e;
       cudaLaunchConfig_t cfg;
       memset(&cfg, 0, sizeof(cfg));
-      cfg.gridDim = dim3((unsigned)(C * 1024)); cfg.blockDim = dim3(kRingThreads); cfg.dynamicSmemBytes = smem;
+      cfg.gridDim = dim3((unsigned)(C * 1024)); cfg.blockDim = dim3(threads); cfg.dynamicSmemBytes = smem;
       cudaLaunchAttribute at[1];
       at[0].id = cudaLaunchAttributeClusterDimension;
       at[0].val.clusterDim.x = C; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
       cfg.attrs = at; cfg.numAttrs = 1;
       if (cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess || n < 1) { cudaGetLastError(); n = 1; }
-      resident[dev][lg] = n;
+      cache.known[cache.count % 16] = {dev, C, n, smem};
+      if (++cache.count >= 32) cache.count = 16;
     }
-    n = resident[dev][lg];
   }
   if (n > rows) n = (int)rows;
-  return launch_dep_cluster(C, kernel, dim3((unsigned)(n * C)), kRingThreads, smem, s, p, (int)rows, C);
+  return launch_dep_cluster(C, kernel, dim3((unsigned)(n * C)), threads, smem, s, p, (int)rows, C);
 }
 template <class T, int NV, int MODE>
 cudaError_t launch_ring(const Distill& p, int C, int64_t rows, cudaStream_t s) {
