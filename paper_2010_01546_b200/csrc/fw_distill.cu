@@ -373,14 +373,7 @@ __device__ __forceinline__ void unpack16(uint4 q, float (&v)[8]) {
 __device__ __forceinline__ void unpack16(uint4 q, float (&v)[4]) {
   v[0] = __uint_as_float(q.x); v[1] = __uint_as_float(q.y); v[2] = __uint_as_float(q.z); v[3] = __uint_as_float(q.w);
 }
-// A 16-bit element by itself cannot be copied ahead: the aligned word that holds it is, and this takes it out.
-template <class E>
-__device__ __forceinline__ float from_word(uint32_t w, const E* at) {
-  if (sizeof(E) == 4) return __uint_as_float(w);
-  return (reinterpret_cast<uintptr_t>(at) & 2) ? bf16_hi(w) : bf16_lo(w);
-}
-template <class E>
-__device__ __forceinline__ const void* word_of(const E* at) {
+__device__ __forceinline__ const void* word_of(const void* at) {
   return reinterpret_cast<const void*>(reinterpret_cast<uintptr_t>(at) & ~(uintptr_t)3);
 }
 
@@ -576,12 +569,17 @@ __global__ void __launch_bounds__(kRingAll, 2) distill_ring_kernel(const Distill
     auto cls = [&](int it) { return reinterpret_cast<int*>(entries + slot_of(it) * slot_words); };
     auto weight = [&](int it) { return p.weight ? s_num[slot_of(it)].w : 1.f; };
     auto t_lse_of = [&](int it) { return p.t_lse ? s_num[slot_of(it)].t_lse : 0.f; };
-    auto t_at = [&](int row, int k) { return static_cast<const char*>(p.T) + ((int64_t)row * p.K + k) * (t16 ? 2 : 4); };
+    // A 16-bit element by itself cannot be copied ahead: the aligned word that holds it is; which half of it, from the element's number
+    const uint32_t t_odd = (uint32_t)(reinterpret_cast<uintptr_t>(p.T) >> 1), z_odd = (uint32_t)(reinterpret_cast<uintptr_t>(p.Z) >> 1);
+    auto half_of = [](uint32_t w, uint32_t n) { return (n & 1u) ? bf16_hi(w) : bf16_lo(w); };
     auto t_of = [&](int it, int row, int k) {
       const uint32_t w = entries[slot_of(it) * slot_words + kp + k];
-      return t16 ? from_word(w, reinterpret_cast<const __nv_bfloat16*>(t_at(row, k))) : __uint_as_float(w);
+      return t16 ? half_of(w, t_odd + (uint32_t)row * (uint32_t)p.K + (uint32_t)k) : __uint_as_float(w);
     };
-    auto z_of = [&](int it, int row, int k, int c) { return from_word(entries[slot_of(it) * slot_words + 2 * kp + k], zrow(row) + c); };
+    auto z_of = [&](int it, int row, int k, int c) {
+      const uint32_t w = entries[slot_of(it) * slot_words + 2 * kp + k];
+      return sizeof(T) == 2 ? half_of(w, z_odd + (uint32_t)row * (uint32_t)p.ldz + (uint32_t)c) : __uint_as_float(w);
+    };
     auto teacher2 = [&](float t, float t_lse, float tm) { return p.t_lse ? fmaf(t, p.inv_tau, -t_lse) * kLog2e : (t - tm) * c2; };
     if (warp == kRingWarps) {
       // ---- entries ----
@@ -592,12 +590,14 @@ __global__ void __launch_bounds__(kRingAll, 2) distill_ring_kernel(const Distill
         if (lane == 0 && p.weight) ahead4(sm100::smem_u32(&n.w), p.weight + row);
         if (lane == 1 && p.t_lse) ahead4(sm100::smem_u32(&n.t_lse), p.t_lse + row);
         if (MODE == DIST_BACKWARD && lane >= 2 && lane < 4) ahead4(sm100::smem_u32(&n.s0) + (lane - 2) * 4, p.stat_in + 2 * (int64_t)row + (lane - 2));
+        const int64_t at = (int64_t)row * p.K;
+        const int32_t* i = static_cast<const int32_t*>(p.I) + (p.i64 ? 2 * at : at);
+        const char* t = static_cast<const char*>(p.T) + (t16 ? 2 * at : 4 * at);
+#pragma unroll 2
         for (int k = lane; k < p.K; k += 32) {
-          const int64_t at = (int64_t)row * p.K + k;
-          const int32_t* i = static_cast<const int32_t*>(p.I) + (p.i64 ? 2 * at : at);
-          ahead4(to + k * 4, i);
-          if (p.i64) ahead4(to + (3 * kp + k) * 4, i + 1);
-          ahead4(to + (kp + k) * 4, word_of(t_at(row, k)));
+          ahead4(to + k * 4, i + (uint32_t)(p.i64 ? 2 * k : k));
+          if (p.i64) ahead4(to + (3 * kp + k) * 4, i + (uint32_t)(2 * k + 1));
+          ahead4(to + (kp + k) * 4, word_of(t + (uint32_t)(t16 ? 2 * k : 4 * k)));
         }
       };
       // classes as they are used, and the student's logits on their way (the backward pass needs those of its slice alone: dZ may be
@@ -607,13 +607,15 @@ __global__ void __launch_bounds__(kRingAll, 2) distill_ring_kernel(const Distill
         const bool live = weight(it) != 0.f;
         int* c = cls(it);
         const uint32_t to = sm100::smem_u32(c + 2 * kp);
+        const T* z = zrow(row);
+#pragma unroll 2
         for (int k = lane; k < p.K; k += 32) {
           int i = c[k];
           if (i >= p.V || (p.i64 && c[3 * kp + k] != 0)) i = -1;
           if (i < 0) i = -1;
           c[k] = i;
           const bool wanted = MODE == DIST_BACKWARD ? i >= first && i < last : i >= 0;
-          if (live && wanted) ahead4(to + k * 4, word_of(zrow(row) + i));
+          if (live && wanted) ahead4(to + k * 4, word_of(z + (uint32_t)i));
         }
       };
       // repeated classes out, bit set, sums of the teacher's and of the named classes' exponentials
@@ -625,14 +627,22 @@ __global__ void __launch_bounds__(kRingAll, 2) distill_ring_kernel(const Distill
           // Is a class there twice?  A bit for each, by its low bits, says no for most rows (K = 64: 9 of 10): comparing all with all
           // took 3500 of 4800 clocks.
           bool seen = false;
-#pragma unroll 2
-          for (int k = lane; k < p.K; k += 32) {
-            const int i = c[k];
-            if (i < 0) continue;
-            seen |= (atomicOr(&s_seen[(i & (kSeenBits - 1)) >> 5], 1u << (i & 31)) >> (i & 31)) & 1u;
-            if (i >= first && i < last) atomicOr(&bits[(it & 1) * words + ((i - first) >> 5)], 1u << ((i - first) & 31));
-            t.m = fmaxf(t.m, t_of(it, row, k));
-            if (MODE != DIST_BACKWARD) n.m = fmaxf(n.m, z_of(it, row, k, i));
+          for (int g = 0; g < p.K; g += 64) {          // two entries of a lane beside each other
+            const int k0 = g + lane, k1 = k0 + 32;
+            const int i0 = k0 < p.K ? c[k0] : -1, i1 = k1 < p.K ? c[k1] : -1;
+            const float t0 = i0 >= 0 ? t_of(it, row, k0) : kLow, t1 = i1 >= 0 ? t_of(it, row, k1) : kLow;
+            t.m = fmaxf(t.m, fmaxf(t0, t1));
+            if (MODE != DIST_BACKWARD) {
+              const float z0 = i0 >= 0 ? z_of(it, row, k0, i0) : kLow, z1 = i1 >= 0 ? z_of(it, row, k1, i1) : kLow;
+              n.m = fmaxf(n.m, fmaxf(z0, z1));
+            }
+            uint32_t was0 = 0, was1 = 0;
+            if (i0 >= 0) was0 = atomicOr(&s_seen[(i0 & (kSeenBits - 1)) >> 5], 1u << (i0 & 31));
+            if (i1 >= 0) was1 = atomicOr(&s_seen[(i1 & (kSeenBits - 1)) >> 5], 1u << (i1 & 31));
+            uint32_t* set = bits + (it & 1) * words;
+            if (i0 >= first && i0 < last) atomicOr(&set[(i0 - first) >> 5], 1u << ((i0 - first) & 31));
+            if (i1 >= first && i1 < last) atomicOr(&set[(i1 - first) >> 5], 1u << ((i1 - first) & 31));
+            seen |= ((was0 >> (i0 & 31)) & 1u) || ((was1 >> (i1 & 31)) & 1u);
           }
           __syncwarp();
           for (int k = lane; k < p.K; k += 32)
@@ -661,12 +671,15 @@ __global__ void __launch_bounds__(kRingAll, 2) distill_ring_kernel(const Distill
           }
           t.m = p.t_lse ? kLow : lanes_max(t.m);
           n.m = lanes_max(n.m);
-#pragma unroll 2
-          for (int k = lane; k < p.K; k += 32) {
-            const int i = c[k];
-            if (i < 0) continue;
-            t.l += ex2(teacher2(t_of(it, row, k), t_lse, t.m));
-            if (MODE != DIST_BACKWARD) n.l += ex2((z_of(it, row, k, i) - n.m) * c2);
+          for (int g = 0; g < p.K; g += 64) {
+            const int k0 = g + lane, k1 = k0 + 32;
+            const int i0 = k0 < p.K ? c[k0] : -1, i1 = k1 < p.K ? c[k1] : -1;
+            const float a0 = i0 >= 0 ? ex2(teacher2(t_of(it, row, k0), t_lse, t.m)) : 0.f, a1 = i1 >= 0 ? ex2(teacher2(t_of(it, row, k1), t_lse, t.m)) : 0.f;
+            t.l += a0 + a1;
+            if (MODE != DIST_BACKWARD) {
+              const float b0 = i0 >= 0 ? ex2((z_of(it, row, k0, i0) - n.m) * c2) : 0.f, b1 = i1 >= 0 ? ex2((z_of(it, row, k1, i1) - n.m) * c2) : 0.f;
+              n.l += b0 + b1;
+            }
           }
 #pragma unroll
           for (int o = 16; o > 0; o >>= 1) {
