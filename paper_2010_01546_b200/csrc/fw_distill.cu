@@ -346,10 +346,10 @@ __global__ void __launch_bounds__(512, 2) distill_kernel(const Distill p) {
 //   eight warps   classes of the slice: cp.async two rows ahead (a thread reads back only what it copied: no barrier), exponentials
 //                 in registers, each warp's sum sent to every CTA of the cluster (st.async, counted in bytes there), the gradient
 //                 once the factor is known;
-//   one warp      entries: class, teacher's logit and row's numbers copied 2 kAheadRows + 1 rows ahead, the student's logit
-//                 kAheadRows + 1; repeated classes, bit set and the teacher's sums of the next row while the eight work on
-//                 this one; and the named classes' gradient of the row before over the eight warps' stores;
-//   one warp      all sums, the factor, the loss.
+//   one warp      entries of the next row: repeated classes, bit set, sums of the teacher's and of the named classes; the loss of
+//                 the row before;
+//   one warp      all sums and the factor; the named classes' gradient of the row before over the eight warps' stores;
+//                 and entries copied ahead, class and teacher's logit 2 kAheadRows + 1 rows, the student's logit kAheadRows + 1.
 // They meet on mbarriers, a CTA has no common barrier.  With the entries spread over the eight warps, a barrier a row and every
 // thread working out the factor, the fixed part of a row was 650 instructions a warp beside 320 for its classes: 690 us.
 // ---------------------------------------------------------------------------
@@ -378,8 +378,8 @@ __device__ __forceinline__ const void* word_of(const void* at) {
 }
 
 struct RingNumbers { float w, t_lse, s0, s1; };
-// What the sums' warp says of a row: of the classes that are not named, and for the gradient of those that are
-struct RingScale { float ref, factor, ws, A, inv, tm, scale_p; };
+// What the sums' warp says of a row: to the classes that are not named, for the gradient of those that are, and for the loss
+struct RingScale { float ref, factor, ws, A, inv, tm, scale_p, whole, pt, qt, w; MaxSum all, others; };
 
 // FILL: the last CTA's slice ends inside an access of 16 bytes, with one, or all slices fill all accesses of their threads.
 template <class T, int NV, int MODE, int FILL>
@@ -389,11 +389,11 @@ __global__ void __launch_bounds__(kRingAll, 2) distill_ring_kernel(const Distill
   extern __shared__ __align__(16) uint8_t dyn8[];
   __shared__ MaxSum s_sum[2][kRingMaxCtas * kRingWarps];
   __shared__ RingNumbers s_num[kEntrySlots];
-  __shared__ RingScale s_scale[2];
+  __shared__ RingScale s_scale[4];
   __shared__ MaxSum s_teacher[2], s_named[2];
   __shared__ uint32_t s_seen[kSeenBits / 32];
   __shared__ float s_w[kRingWarps][kRingSlots + 2];
-  __shared__ __align__(8) uint64_t bar_sums[2], bar_bits[2], bar_scale[2], bar_done[2];
+  __shared__ __align__(8) uint64_t bar_sums[2], bar_bits[2], bar_scale[2], bar_done[2], bar_clear[2];
   __shared__ int s_lost;                          // a wait gave up
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int rank = (int)blockIdx.x % C, row0 = (int)blockIdx.x / C, step = (int)gridDim.x / C;
@@ -422,6 +422,7 @@ __global__ void __launch_bounds__(kRingAll, 2) distill_ring_kernel(const Distill
       sm100::mbar_init(bar(bar_sums[i]), 1);
       sm100::mbar_init(bar(bar_bits[i]), 1);
       sm100::mbar_init(bar(bar_scale[i]), 1);
+      sm100::mbar_init(bar(bar_clear[i]), 1);
       sm100::mbar_init(bar(bar_done[i]), kRingWarps);
     }
     sm100::mbar_fence_init();
@@ -536,7 +537,7 @@ __global__ void __launch_bounds__(kRingAll, 2) distill_ring_kernel(const Distill
         }
         if (MODE != DIST_LOSS) {
           if (!wait(bar_scale, it)) break;
-          const RingScale& sc = s_scale[it & 1];
+          const RingScale& sc = s_scale[it & 3];
           const float f = MODE == DIST_BACKWARD || sc.factor == 0.f ? sc.factor : sc.factor * ex2((top - sc.ref) * c2);
 #pragma unroll
           for (int k = 0; k < NV; ++k) {
@@ -581,43 +582,61 @@ __global__ void __launch_bounds__(kRingAll, 2) distill_ring_kernel(const Distill
       return sizeof(T) == 2 ? half_of(w, z_odd + (uint32_t)row * (uint32_t)p.ldz + (uint32_t)c) : __uint_as_float(w);
     };
     auto teacher2 = [&](float t, float t_lse, float tm) { return p.t_lse ? fmaf(t, p.inv_tau, -t_lse) * kLog2e : (t - tm) * c2; };
+    auto fetch_entries = [&](int row, int it) {
+      if (row >= rows) return;
+      RingNumbers& n = s_num[slot_of(it)];
+      const uint32_t to = sm100::smem_u32(entries + slot_of(it) * slot_words);
+      if (lane == 0 && p.weight) ahead4(sm100::smem_u32(&n.w), p.weight + row);
+      if (lane == 1 && p.t_lse) ahead4(sm100::smem_u32(&n.t_lse), p.t_lse + row);
+      if (MODE == DIST_BACKWARD && lane >= 2 && lane < 4) ahead4(sm100::smem_u32(&n.s0) + (lane - 2) * 4, p.stat_in + 2 * (int64_t)row + (lane - 2));
+      const int64_t at = (int64_t)row * p.K;
+      const int32_t* i = static_cast<const int32_t*>(p.I) + (p.i64 ? 2 * at : at);
+      const char* t = static_cast<const char*>(p.T) + (t16 ? 2 * at : 4 * at);
+#pragma unroll 2
+      for (int k = lane; k < p.K; k += 32) {
+        ahead4(to + k * 4, i + (uint32_t)(p.i64 ? 2 * k : k));
+        if (p.i64) ahead4(to + (3 * kp + k) * 4, i + (uint32_t)(2 * k + 1));
+        ahead4(to + (kp + k) * 4, word_of(t + (uint32_t)(t16 ? 2 * k : 4 * k)));
+      }
+    };
+    // classes as they are used, and the student's logits on their way (the backward pass needs those of its slice alone: dZ may be
+    // Z, and other CTAs write over theirs)
+    auto fetch_logits = [&](int row, int it) {
+      if (row >= rows) return;
+      const bool live = weight(it) != 0.f;
+      int* c = cls(it);
+      const uint32_t to = sm100::smem_u32(c + 2 * kp);
+      const T* z = zrow(row);
+#pragma unroll 2
+      for (int k = lane; k < p.K; k += 32) {
+        int i = c[k];
+        if (i >= p.V || (p.i64 && c[3 * kp + k] != 0)) i = -1;
+        if (i < 0) i = -1;
+        c[k] = i;
+        const bool wanted = MODE == DIST_BACKWARD ? i >= first && i < last : i >= 0;
+        if (live && wanted) ahead4(to + k * 4, word_of(z + (uint32_t)i));
+      }
+    };
+    // a row whose stores are done: the named classes' gradient over them, its bits out
+    auto finish = [&](int row, int it) {
+      if (weight(it) == 0.f) return;
+      const RingScale sc = s_scale[it & 3];
+      const float t_lse = t_lse_of(it);
+      T* dz = MODE == DIST_LOSS ? nullptr : static_cast<T*>(p.dZ) + (int64_t)row * p.lddz;
+      const int* c = cls(it);
+      for (int k = lane; k < p.K; k += 32) {
+        const int i = c[k];
+        if (i < first || i >= last) continue;
+        bits[(it & 1) * words + ((i - first) >> 5)] = 0;
+        if (MODE != DIST_LOSS) {
+          const float z = z_of(it, row, k, i), pk = ex2(teacher2(t_of(it, row, k), t_lse, sc.tm)) * sc.scale_p;
+          const float q = ex2(MODE == DIST_BACKWARD ? fmaf(z, p.inv_tau, -sc.ref) * kLog2e : (z - sc.ref) * c2) * sc.inv;
+          put(dz + i, sc.ws == 0.f ? 0.f : sc.ws * (sc.A * q - pk));
+        }
+      }
+    };
     if (warp == kRingWarps) {
-      // ---- entries ----
-      auto fetch_entries = [&](int row, int it) {
-        if (row >= rows) return;
-        RingNumbers& n = s_num[slot_of(it)];
-        const uint32_t to = sm100::smem_u32(entries + slot_of(it) * slot_words);
-        if (lane == 0 && p.weight) ahead4(sm100::smem_u32(&n.w), p.weight + row);
-        if (lane == 1 && p.t_lse) ahead4(sm100::smem_u32(&n.t_lse), p.t_lse + row);
-        if (MODE == DIST_BACKWARD && lane >= 2 && lane < 4) ahead4(sm100::smem_u32(&n.s0) + (lane - 2) * 4, p.stat_in + 2 * (int64_t)row + (lane - 2));
-        const int64_t at = (int64_t)row * p.K;
-        const int32_t* i = static_cast<const int32_t*>(p.I) + (p.i64 ? 2 * at : at);
-        const char* t = static_cast<const char*>(p.T) + (t16 ? 2 * at : 4 * at);
-#pragma unroll 2
-        for (int k = lane; k < p.K; k += 32) {
-          ahead4(to + k * 4, i + (uint32_t)(p.i64 ? 2 * k : k));
-          if (p.i64) ahead4(to + (3 * kp + k) * 4, i + (uint32_t)(2 * k + 1));
-          ahead4(to + (kp + k) * 4, word_of(t + (uint32_t)(t16 ? 2 * k : 4 * k)));
-        }
-      };
-      // classes as they are used, and the student's logits on their way (the backward pass needs those of its slice alone: dZ may be
-      // Z, and other CTAs write over theirs)
-      auto fetch_logits = [&](int row, int it) {
-        if (row >= rows) return;
-        const bool live = weight(it) != 0.f;
-        int* c = cls(it);
-        const uint32_t to = sm100::smem_u32(c + 2 * kp);
-        const T* z = zrow(row);
-#pragma unroll 2
-        for (int k = lane; k < p.K; k += 32) {
-          int i = c[k];
-          if (i >= p.V || (p.i64 && c[3 * kp + k] != 0)) i = -1;
-          if (i < 0) i = -1;
-          c[k] = i;
-          const bool wanted = MODE == DIST_BACKWARD ? i >= first && i < last : i >= 0;
-          if (live && wanted) ahead4(to + k * 4, word_of(z + (uint32_t)i));
-        }
-      };
+      // ---- entries of the next row ----
       // repeated classes out, bit set, sums of the teacher's and of the named classes' exponentials
       auto prepare = [&](int row, int it) {
         MaxSum t = {kLow, 0.f}, n = {kLow, 0.f};
@@ -692,24 +711,58 @@ __global__ void __launch_bounds__(kRingAll, 2) distill_ring_kernel(const Distill
         __syncwarp();
         if (lane == 0) sm100::mbar_arrive(bar(bar_bits[it & 1]));
       };
-      // a row whose stores are done: the named classes' gradient over them, its bits out
-      auto finish = [&](int row, int it) {
-        if (weight(it) == 0.f) return;
-        const RingScale sc = s_scale[it & 1];
-        const float t_lse = t_lse_of(it);
-        T* dz = MODE == DIST_LOSS ? nullptr : static_cast<T*>(p.dZ) + (int64_t)row * p.lddz;
+      // the loss of a row that is through, and its normalisers
+      auto write_loss = [&](int row, int it) {
+        if (MODE == DIST_BACKWARD || rank != 0) return;
+        if (weight(it) == 0.f) {
+          if (lane == 0) {
+            p.loss[row] = 0.f;
+            if (p.stat) { p.stat[2 * (int64_t)row] = 0.f; p.stat[2 * (int64_t)row + 1] = 0.f; }
+          }
+          return;
+        }
+        const RingScale sc = s_scale[it & 3];
+        const float t_lse = t_lse_of(it), log_all = log2f(sc.all.l), log_p = log2f(sc.scale_p);
+        const bool empty = sc.all.l == 0.f;
         const int* c = cls(it);
+        float kl = 0.f;
         for (int k = lane; k < p.K; k += 32) {
           const int i = c[k];
-          if (i < first || i >= last) continue;
-          bits[(it & 1) * words + ((i - first) >> 5)] = 0;
-          if (MODE != DIST_LOSS) {
-            const float z = z_of(it, row, k, i), pk = ex2(teacher2(t_of(it, row, k), t_lse, sc.tm)) * sc.scale_p;
-            const float q = ex2(MODE == DIST_BACKWARD ? fmaf(z, p.inv_tau, -sc.ref) * kLog2e : (z - sc.ref) * c2) * sc.inv;
-            put(dz + i, sc.ws == 0.f ? 0.f : sc.ws * (sc.A * q - pk));
+          if (i < 0) continue;
+          const float lp = teacher2(t_of(it, row, k), t_lse, sc.tm), pk = ex2(lp) * sc.scale_p;
+          if (pk > 0.f || pk != pk) kl += pk * ((lp + log_p) - ((z_of(it, row, k, i) - sc.all.m) * c2 - log_all));
+        }
+        kl = lanes_sum(kl);
+        if (lane == 0) {
+          if (sc.pt > 0.f) kl += sc.pt * (log2f(sc.pt) - log2f(sc.qt));
+          if (sc.whole != sc.whole) kl = sc.whole;
+          p.loss[row] = empty ? 0.f : sc.w * kl * kLn2;
+          if (p.stat) {
+            p.stat[2 * (int64_t)row] = empty ? -INFINITY : fmaf(sc.all.m, p.inv_tau, logf(sc.all.l));
+            p.stat[2 * (int64_t)row + 1] = sc.others.l == 0.f ? -INFINITY : fmaf(sc.others.m, p.inv_tau, logf(sc.others.l));
           }
         }
       };
+      asm volatile("bar.sync 1, 64;" ::: "memory");              // the first rows have landed
+      prepare(row0, 0);
+      int it = 0;
+      bool lost = false;
+      int row = row0;
+      for (; row < rows; row += step, ++it) {
+        if (it > 0) {
+          lost = !wait(bar_clear, it - 1);
+          if (lost) break;
+        }
+        if (row + step < rows) prepare(row + step, it + 1);
+        if (it > 0) write_loss(row - step, it - 1);
+      }
+      lost = lost || !wait(bar_clear, it - 1);
+      if (!lost) write_loss(row - step, it - 1);
+      // given up: no barrier is touched any more, and the losses of the rows that are left say so
+      if (lost && MODE != DIST_BACKWARD && rank == 0)
+        for (int r = max(row0, row - step) + lane * step; r < rows; r += 32 * step) p.loss[r] = NAN;
+    } else {
+      // ---- sums ----
       for (int i = 0; i <= 2 * kAheadRows; ++i) fetch_entries(row0 + i * step, i);
       ahead_commit();
       ahead_wait<0>();
@@ -717,107 +770,75 @@ __global__ void __launch_bounds__(kRingAll, 2) distill_ring_kernel(const Distill
       for (int i = 0; i <= kAheadRows; ++i) fetch_logits(row0 + i * step, i);
       ahead_commit();
       ahead_wait<0>();
-      __syncwarp();
-      prepare(row0, 0);
-      int it = 0;
+      asm volatile("bar.sync 1, 64;" ::: "memory");
+      int sums = 0, it = 0, row = row0;            // rows that count; rows
       bool lost = false;
-      for (int row = row0; row < rows; row += step, ++it) {
+      for (; row < rows; row += step, ++it) {
+        // the row before is through
         if (it > 0) {
           lost = !wait(bar_done, it - 1);
           if (lost) break;
           finish(row - step, it - 1);
+          ahead_wait<kAheadRows - 1>();
           __syncwarp();
+          if (lane == 0) sm100::mbar_arrive(bar(bar_clear[(it - 1) & 1]));
         }
-        ahead_wait<kAheadRows - 1>();
-        __syncwarp();
-        if (row + step < rows) prepare(row + step, it + 1);
-        fetch_logits(row + (1 + kAheadRows) * step, it + 1 + kAheadRows);
-        fetch_entries(row + (1 + 2 * kAheadRows) * step, it + 1 + 2 * kAheadRows);
-        ahead_commit();
-      }
-      if (!lost && it > 0 && wait(bar_done, it - 1)) finish(row0 + (it - 1) * step, it - 1);
-      ahead_wait<0>();
-    } else {
-      // ---- sums ----
-      int sums = 0, it = 0, row = row0;            // rows that count; rows
-      bool lost = false;
-      for (; row < rows; row += step, ++it) {
         lost = !wait(bar_bits, it);
         if (lost) break;
         const float w = weight(it);
         if (w == 0.f) {
-          if (lane == 0) {
-            sm100::mbar_arrive(bar(bar_scale[it & 1]));
-            if (MODE != DIST_BACKWARD && rank == 0) {
-              p.loss[row] = 0.f;
-              if (p.stat) { p.stat[2 * (int64_t)row] = 0.f; p.stat[2 * (int64_t)row + 1] = 0.f; }
-            }
-          }
-          continue;
-        }
-        const MaxSum t = s_teacher[it & 1], n = s_named[it & 1];
-        const float t_lse = t_lse_of(it), tm = t.m, ts = t.l;
-        const float scale_p = p.t_lse ? 1.f : (ts > 0.f ? 1.f / ts : (ts == 0.f ? 0.f : ts));     // a NaN goes on
-        const float whole = ts * scale_p;
-        float pt = 0.f;
-        if (p.t_lse) pt = 1.f - whole < 0.f ? 0.f : 1.f - whole;
-        const float A = whole + pt;
-        float ref, inv, qt;
-        bool empty;
-        MaxSum all = {kLow, 0.f}, others = {kLow, 0.f};
-        if (MODE != DIST_BACKWARD) {
-          const int turn = sums & 1, count = C * kRingWarps;
-          if (lane == 0) sm100::mbar_expect_tx(bar(bar_sums[turn]), (uint32_t)(count * (int)sizeof(MaxSum)));
-          __syncwarp();
-          lost = !wait(bar_sums, sums);
-          if (lost) break;
-          ++sums;
-          if (lane < count) others = s_sum[turn][lane];
-          for (int i = lane + 32; i < count; i += 32) others = merge(others, s_sum[turn][i], c2);
-          others = merge_lanes(others, c2);
-          all = merge(others, n, c2);
-          empty = all.l == 0.f;
-          ref = all.m;
-          inv = 1.f / all.l;
-          qt = others.l * ex2((others.m - all.m) * c2) * inv;
+          if (lane == 0) sm100::mbar_arrive(bar(bar_scale[it & 1]));
         } else {
-          ref = s_num[slot_of(it)].s0;
-          inv = 1.f;
-          empty = ref == -INFINITY;
-          qt = ex2((s_num[slot_of(it)].s1 - ref) * kLog2e);
-        }
-        const float ws = empty ? 0.f : w * p.inv_tau;
-        // q_j (A - p_t / q_t) of the others; where there are none, nothing stands at that factor
-        const float other = pt > 0.f && qt != 0.f ? A - pt / qt : A;
-        if (lane == 0) {
-          s_scale[it & 1] = {ref, ws == 0.f ? 0.f : ws * other * inv, ws, A, inv, tm, scale_p};
-          sm100::mbar_arrive(bar(bar_scale[it & 1]));
-        }
-        if (MODE != DIST_BACKWARD && rank == 0) {
-          float kl = 0.f;
-          const float log_all = log2f(all.l), log_p = log2f(scale_p);
-          const int* c = cls(it);
-          for (int k = lane; k < p.K; k += 32) {
-            const int i = c[k];
-            if (i < 0) continue;
-            const float lp = teacher2(t_of(it, row, k), t_lse, tm), pk = ex2(lp) * scale_p;
-            if (pk > 0.f || pk != pk) kl += pk * ((lp + log_p) - ((z_of(it, row, k, i) - all.m) * c2 - log_all));
+          const MaxSum t = s_teacher[it & 1], n = s_named[it & 1];
+          const float t_lse = t_lse_of(it), tm = t.m, ts = t.l;
+          const float scale_p = p.t_lse ? 1.f : (ts > 0.f ? 1.f / ts : (ts == 0.f ? 0.f : ts));     // a NaN goes on
+          const float whole = ts * scale_p;
+          float pt = 0.f;
+          if (p.t_lse) pt = 1.f - whole < 0.f ? 0.f : 1.f - whole;
+          const float A = whole + pt;
+          float ref, inv, qt;
+          bool empty;
+          MaxSum all = {kLow, 0.f}, others = {kLow, 0.f};
+          if (MODE != DIST_BACKWARD) {
+            const int turn = sums & 1, count = C * kRingWarps;
+            if (lane == 0) sm100::mbar_expect_tx(bar(bar_sums[turn]), (uint32_t)(count * (int)sizeof(MaxSum)));
+            __syncwarp();
+            lost = !wait(bar_sums, sums);
+            if (lost) break;
+            ++sums;
+            for (int i = lane; i < count; i += 32) others.m = fmaxf(others.m, s_sum[turn][i].m);
+            others.m = lanes_max(others.m);
+            for (int i = lane; i < count; i += 32) others.l += s_sum[turn][i].l * ex2((s_sum[turn][i].m - others.m) * c2);
+            others.l = lanes_sum(others.l);
+            all = merge(others, n, c2);
+            empty = all.l == 0.f;
+            ref = all.m;
+            inv = __fdividef(1.f, all.l);
+            qt = others.l * ex2((others.m - all.m) * c2) * inv;
+          } else {
+            ref = s_num[slot_of(it)].s0;
+            inv = 1.f;
+            empty = ref == -INFINITY;
+            qt = ex2((s_num[slot_of(it)].s1 - ref) * kLog2e);
           }
-          kl = lanes_sum(kl);
+          const float ws = empty ? 0.f : w * p.inv_tau;
+          // q_j (A - p_t / q_t) of the others; where there are none, nothing stands at that factor
+          const float other = pt > 0.f && qt != 0.f ? A - __fdividef(pt, qt) : A;
           if (lane == 0) {
-            if (pt > 0.f) kl += pt * (log2f(pt) - log2f(qt));
-            if (whole != whole) kl = whole;
-            p.loss[row] = empty ? 0.f : w * kl * kLn2;
-            if (p.stat) {
-              p.stat[2 * (int64_t)row] = empty ? -INFINITY : fmaf(all.m, p.inv_tau, logf(all.l));
-              p.stat[2 * (int64_t)row + 1] = others.l == 0.f ? -INFINITY : fmaf(others.m, p.inv_tau, logf(others.l));
-            }
+            s_scale[it & 3] = {ref, ws == 0.f ? 0.f : ws * other * inv, ws, A, inv, tm, scale_p, whole, pt, qt, w, all, others};
+            sm100::mbar_arrive(bar(bar_scale[it & 1]));
           }
         }
+        fetch_logits(row + (1 + kAheadRows) * step, it + 1 + kAheadRows);
+        fetch_entries(row + (1 + 2 * kAheadRows) * step, it + 1 + 2 * kAheadRows);
+        ahead_commit();
       }
-      // given up: no barrier is touched any more, and the losses of the rows that are left say so
-      if (lost && MODE != DIST_BACKWARD && rank == 0)
-        for (int r = row + lane * step; r < rows; r += 32 * step) p.loss[r] = NAN;
+      if (!lost && wait(bar_done, it - 1)) {
+        finish(row - step, it - 1);
+        __syncwarp();
+        if (lane == 0) sm100::mbar_arrive(bar(bar_clear[(it - 1) & 1]));
+      }
+      ahead_wait<0>();
     }
   }
   dep_trigger();
