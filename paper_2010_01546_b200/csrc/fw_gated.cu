@@ -153,6 +153,9 @@ bool disjoint(const View* out, int no, const View* in, int ni) {
   return true;
 }
 
+// A product whose tiles of 256 x 256 do not give every pair of SMs one goes to narrower tiles that share K
+bool few_tiles(int64_t tiles) { return tiles < sm_count() / 2; }
+
 fw_status here(const fw_gated* g) {
   int dev = -1;
   if (cudaGetDevice(&dev) != cudaSuccess) { cudaGetLastError(); return FW_ERR_CUDA; }
@@ -257,7 +260,7 @@ fw_status fw_gated_forward(fw_gated* g, const void* X, int64_t rows, int64_t ldx
   f.X = X; f.Wg = Wg; f.Wu = Wu; f.xs = x_scale; f.wgs = wg_scale; f.wus = wu_scale; f.bg = bg; f.bu = bu;
   f.H = H; f.Zg = Zg; f.Zu = Zu; f.rows = rows; f.ldx = ldx; f.ldw = ldw; f.ldh = ldh; f.ldz = ldz;
   f.M = M; f.N = N; f.e4m3 = q8; f.act = g->d.act; f.status = g->status;
-  return launch_gated_pair_forward(f, g->stream);
+  return few_tiles((rows + 255) / 256 * ((N + 127) / 128)) ? launch_gated_small_forward(f, g->stream) : launch_gated_pair_forward(f, g->stream);
 }
 
 fw_status fw_gated_backward(fw_gated* g, const void* dH, int64_t rows, int64_t lddh, const void* X, int64_t ldx, const void* Wg,
@@ -294,7 +297,16 @@ fw_status fw_gated_backward(fw_gated* g, const void* dH, int64_t rows, int64_t l
   GatedBackward b;
   b.X = X; b.Wg = Wg; b.Wu = Wu; b.Da = g->Da; b.Db = g->Db; b.dX = dX; b.dWg = dWg; b.dWu = dWu;
   b.rows = rows; b.ldx = ldx; b.ldw = ldw; b.ldd = g->ldd; b.lddx = lddx; b.M = M; b.N = N; b.w_f32 = dw_dtype == FW_F32; b.status = g->status;
-  return launch_gated_pair_backward(b, g->stream);
+  const int64_t mt = ((int64_t)M + 255) / 256;
+  if (dX && few_tiles((rows + 255) / 256 * mt)) {
+    if ((st = launch_gated_small_dx(b, g->stream)) != FW_OK) return st;
+    b.dX = nullptr;
+  }
+  if (dWg && few_tiles(2 * (((int64_t)N + 255) / 256) * mt)) {
+    if ((st = launch_gated_small_dw(b, g->stream)) != FW_OK) return st;
+    b.dWg = b.dWu = nullptr;
+  }
+  return b.dX || b.dWg ? launch_gated_pair_backward(b, g->stream) : FW_OK;
 }
 
 fw_status fw_gated_sync_status(fw_gated* g) {

@@ -40,8 +40,13 @@ struct GatedGates {
 int gated_gate_slabs(int64_t rows, int N);      // at most kGateSlabs
 constexpr int kGateSlabs = 64;
 cudaError_t launch_gated_gates(const GatedGates& g, cudaStream_t s);
+// tiles of 256 x 256 accumulators by CTA pairs (fw_gated_gemm.cu): products that fill the chip
 fw_status launch_gated_pair_forward(const GatedForward& f, cudaStream_t s);
 fw_status launch_gated_pair_backward(const GatedBackward& b, cudaStream_t s);
+// narrow tiles of 128 rows, K shared by clusters (fw_gated_small.cu): the others
+fw_status launch_gated_small_forward(const GatedForward& f, cudaStream_t s);
+fw_status launch_gated_small_dx(const GatedBackward& b, cudaStream_t s);
+fw_status launch_gated_small_dw(const GatedBackward& b, cudaStream_t s);
 
 }  // namespace fw
 #endif

@@ -16,7 +16,9 @@ pytestmark = pytest.mark.gpu
 BF16, E4M3 = torch.bfloat16, torch.float8_e4m3fn
 # rows, M, N
 SIZES = [(1, 1, 1), (1, 64, 128), (2, 7, 300), (3, 100, 8), (17, 1000, 257), (64, 72, 513), (128, 256, 128), (129, 65, 129),
-         (255, 300, 1367), (256, 128, 256), (300, 520, 640), (513, 129, 1000), (1000, 2304, 100), (33, 4000, 2050)]
+         (255, 300, 1367), (256, 128, 256), (300, 520, 640), (513, 129, 1000), (1000, 2304, 100), (33, 4000, 2050),
+         # products that fill the chip: forward; the weight gradients alone; all of them
+         (2600, 72, 1367), (200, 1400, 1700), (4000, 1100, 2050), (3000, 1024, 2304)]
 
 
 @pytest.fixture(scope="module")
