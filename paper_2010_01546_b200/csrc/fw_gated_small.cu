@@ -21,7 +21,7 @@ namespace {
 
 using namespace sm100;
 
-constexpr int GS_MAX_STAGES = 8;
+constexpr int GS_MAX_STAGES = 8, GS_MAX_SPLITS = 8;
 constexpr int GS_THREADS = 6 * 32;                 // producer, MMA, four epilogue warps
 enum { GS_FWD_BF16 = 0, GS_FWD_E4M3 = 1, GS_DX = 2, GS_DW = 3 };
 
@@ -59,7 +59,7 @@ __device__ __forceinline__ void sts4(uint32_t a, const uint32_t* v) {
 
 // F: outputs of a tile; the accumulator has NT columns.  Grid: (column tiles x splits, row tiles, matrices).
 template <int KIND, int F>
-__global__ void __launch_bounds__(GS_THREADS) gated_small_kernel(const __grid_constant__ SmallArgs g) {
+__global__ void __launch_bounds__(GS_THREADS, KIND <= GS_FWD_E4M3 && F == 32 ? 4 : 2) gated_small_kernel(const __grid_constant__ SmallArgs g) {
   constexpr bool FWD = KIND <= GS_FWD_E4M3;
   constexpr int NT = FWD ? 2 * F : F;
   constexpr int KB = KIND == GS_FWD_E4M3 ? 128 : 64;
@@ -205,13 +205,24 @@ __global__ void __launch_bounds__(GS_THREADS) gated_small_kernel(const __grid_co
       if (n <= 0) continue;
       const uint32_t at = base + (uint32_t)(r * PITCH + j) * 4u;
       float a[4] = {0.f, 0.f, 0.f, 0.f}, b[4] = {0.f, 0.f, 0.f, 0.f};
-      for (int s = 0; s < S; ++s) {
-        const uint32_t from = S > 1 ? mapa_shared(at, (uint32_t)s) : at;
-        const float4 x = ld_cluster4(from);
-        a[0] += x.x; a[1] += x.y; a[2] += x.z; a[3] += x.w;
-        if (FWD) {
-          const float4 y = ld_cluster4(from + F * 4);
-          b[0] += y.x; b[1] += y.y; b[2] += y.z; b[3] += y.w;
+      // four shares' loads before their sums: one by one the latency of another SM's shared memory was most of the kernel (333 x 1000 x
+      // 1367 in eight shares: 38 us; all eight at once take registers that cost a single token one of its four CTAs a SM)
+      for (int s0 = 0; s0 < S; s0 += 4) {
+        float4 x[4], y[4];
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+          if (s0 + s < S) {
+            const uint32_t from = mapa_shared(at, (uint32_t)(s0 + s));
+            x[s] = ld_cluster4(from);
+            if (FWD) y[s] = ld_cluster4(from + F * 4);
+          }
+        }
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+          if (s0 + s < S) {
+            a[0] += x[s].x; a[1] += x[s].y; a[2] += x[s].z; a[3] += x[s].w;
+            if (FWD) { b[0] += y[s].x; b[1] += y[s].y; b[2] += y[s].z; b[3] += y[s].w; }
+          }
         }
       }
       const int64_t row = m0 + r;
@@ -262,9 +273,12 @@ template <int KIND, int F>
 fw_status launch(SmallArgs& g, int matrices, cudaStream_t s, const char* what) {
   constexpr int NT = KIND <= GS_FWD_E4M3 ? 2 * F : F;
   const int mt = blocks(g.height, 128), nt = blocks(g.width, F);
-  // K shared by up to eight CTAs until every SM has two, a K block each at least
+  // K is shared by up to eight CTAs, four blocks of it each at least (the exchange of a cluster takes as long), until three SMs of
+  // four have one; where 16 blocks each are left, until there are 1.5 a SM, with few rows two: loads in flight are what counts
+  // there (64 rows, 4096 x 8192: 28.7 us against 34.7; 512 rows, 1024 x 2816, 8 blocks each: 22.7 against 16.9)
+  const int64_t tiles = (int64_t)mt * nt * matrices, sms = sm_count();
   int S = 1;
-  while (S < 8 && S * 2 <= g.nk && (int64_t)mt * nt * matrices * S < 2 * sm_count()) S *= 2;
+  while (S < GS_MAX_SPLITS && g.nk >= 8 * S && (4 * tiles * S < 3 * sms || (g.nk >= 32 * S && 2 * tiles * S < (g.height <= 32 ? 4 : 3) * sms))) S *= 2;
   g.splits = S;
   g.a_bytes = KIND == GS_DW ? 128 * 128 : g.a_rows * 128;
   g.stage_bytes = g.a_bytes + NT * 128;
