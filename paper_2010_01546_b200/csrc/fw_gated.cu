@@ -25,43 +25,73 @@ namespace {
 
 using namespace rows;
 
-// da = dh b act'(a), db = dh act(a), and partial sums of both over the rows.  A CTA has 256 columns and a slab of rows: a thread
-// eight neighbouring columns (16 bytes) of every eighth row.  Reads 6 bytes an element and writes 4: HBM bound.
-__global__ void __launch_bounds__(256) gated_gates_kernel(const GatedGates g) {
-  __shared__ float acc[8][256];
+__device__ __forceinline__ void unpack8(uint4 q, float (&v)[8]) {
+  v[0] = bf16_lo(q.x); v[1] = bf16_hi(q.x); v[2] = bf16_lo(q.y); v[3] = bf16_hi(q.y);
+  v[4] = bf16_lo(q.z); v[5] = bf16_hi(q.z); v[6] = bf16_lo(q.w); v[7] = bf16_hi(q.w);
+}
+
+// da = dh b act'(a), db = dh act(a), and with SUMS partial sums of both over the rows.  A CTA has 256 columns and a slab of rows: a
+// thread eight neighbouring columns (16 bytes) of every eighth row, two rows' loads in flight.  Reads 6 bytes an element and writes 4:
+// HBM bound.  (One kernel for all activations took 98 registers and two CTAs a SM: 8192 x 8192 184 us.)
+template <int ACT, bool SUMS>
+__global__ void __launch_bounds__(256, SUMS ? 3 : 4) gated_gates_kernel(const GatedGates g) {
+  __shared__ float acc[SUMS ? 8 : 1][256];
   const int lane = threadIdx.x & 31, ty = threadIdx.x >> 5;
   const int col = blockIdx.x * 256 + lane * 8, n = g.N - col;
   const int64_t per = (g.rows + g.slabs - 1) / g.slabs;
   const int64_t r0 = blockIdx.y * per, r1 = min(g.rows, r0 + per);
   dep_sync();
   float sa[8], sb[8];
+  if (SUMS) {
 #pragma unroll
-  for (int e = 0; e < 8; ++e) sa[e] = sb[e] = 0.f;
+    for (int e = 0; e < 8; ++e) sa[e] = sb[e] = 0.f;
+  }
   typedef const __nv_bfloat16* In;
   typedef __nv_bfloat16* Out;
-  if (n > 0) {
-    with_act(g.act, [&](auto act) {
-#pragma unroll 2
-      for (int64_t r = r0 + ty; r < r1; r += 8) {
-        float h[8], a[8], b[8];
-        load<8>(static_cast<In>(g.dH) + r * g.lddh + col, n, 0.f, h);
-        load<8>(static_cast<In>(g.Zg) + r * g.ldz + col, n, 0.f, a);
-        load<8>(static_cast<In>(g.Zu) + r * g.ldz + col, n, 0.f, b);
+  In dh = static_cast<In>(g.dH) + col, zg = static_cast<In>(g.Zg) + col, zu = static_cast<In>(g.Zu) + col;
+  Out oa = static_cast<Out>(g.Da) + col, ob = static_cast<Out>(g.Db) + col;
+  auto one = [&](int64_t r, float (&h)[8], float (&a)[8], float (&b)[8]) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          float f, df;
-          act.both(a[e], f, df);
-          a[e] = h[e] * b[e] * df;
-          b[e] = h[e] * f;
-          sa[e] += a[e];
-          sb[e] += b[e];
-        }
-        store<8>(static_cast<Out>(g.Da) + r * g.ldd + col, n, a);
-        store<8>(static_cast<Out>(g.Db) + r * g.ldd + col, n, b);
+    for (int e = 0; e < 8; ++e) {
+      float f, df;
+      Act<ACT>::both(a[e], f, df);
+      a[e] = h[e] * b[e] * df;
+      b[e] = h[e] * f;
+      if (SUMS) { sa[e] += a[e]; sb[e] += b[e]; }
+    }
+    store<8>(oa + r * g.ldd, n, a);
+    store<8>(ob + r * g.ldd, n, b);
+  };
+  int64_t r = r0 + ty;
+  if (n >= 8) {
+    for (; r + 8 < r1; r += 16) {
+      uint4 q[6];
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        q[3 * k] = *reinterpret_cast<const uint4*>(dh + (r + 8 * k) * g.lddh);
+        q[3 * k + 1] = *reinterpret_cast<const uint4*>(zg + (r + 8 * k) * g.ldz);
+        q[3 * k + 2] = *reinterpret_cast<const uint4*>(zu + (r + 8 * k) * g.ldz);
       }
-    });
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        float h[8], a[8], b[8];
+        unpack8(q[3 * k], h);
+        unpack8(q[3 * k + 1], a);
+        unpack8(q[3 * k + 2], b);
+        one(r + 8 * k, h, a, b);
+      }
+    }
   }
-  if (!g.part) return;
+  if (n > 0) {
+    for (; r < r1; r += 8) {
+      float h[8], a[8], b[8];
+      load<8>(dh + r * g.lddh, n, 0.f, h);
+      load<8>(zg + r * g.ldz, n, 0.f, a);
+      load<8>(zu + r * g.ldz, n, 0.f, b);
+      one(r, h, a, b);
+    }
+  }
+  if (!SUMS) return;
   for (int k = 0; k < 2; ++k) {
     __syncthreads();
 #pragma unroll
@@ -176,7 +206,12 @@ cudaError_t launch_gated_gates(const GatedGates& g, cudaStream_t s) {
   cudaError_t e;
   {
     ProfScope ps(FW_PROF_MISC, s);
-    e = launch_dep(gated_gates_kernel, dim3((g.N + 255) / 256, g.slabs), 256, 0, s, g);
+    const dim3 grid((g.N + 255) / 256, g.slabs);
+    auto go = [&](auto with, auto without) { return launch_dep(g.part ? with : without, grid, 256, 0, s, g); };
+    if (g.act == FW_ACT_SILU) e = go(gated_gates_kernel<FW_ACT_SILU, true>, gated_gates_kernel<FW_ACT_SILU, false>);
+    else if (g.act == FW_ACT_GELU) e = go(gated_gates_kernel<FW_ACT_GELU, true>, gated_gates_kernel<FW_ACT_GELU, false>);
+    else if (g.act == FW_ACT_GELU_TANH) e = go(gated_gates_kernel<FW_ACT_GELU_TANH, true>, gated_gates_kernel<FW_ACT_GELU_TANH, false>);
+    else e = go(gated_gates_kernel<FW_ACT_RELU, true>, gated_gates_kernel<FW_ACT_RELU, false>);
   }
   if (e == cudaSuccess && g.part) {
     ProfScope ps(FW_PROF_MISC, s);

@@ -57,6 +57,57 @@ __device__ __forceinline__ void sts4(uint32_t a, const uint32_t* v) {
   asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(a), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
 }
 
+// n neighbouring values of a row, as many as the matrix has, in one access where that may be
+template <int n>
+__device__ __forceinline__ void put_row(const SmallArgs& g, int o, int64_t row, int col, const float (&v)[n], bool f32) {
+  const int left = g.width - col;
+  const int64_t at = row * g.ld[o] + col;
+  if (f32) {
+    float* p = static_cast<float*>(g.out[o]) + at;
+    if (g.vec && left >= n) {
+#pragma unroll
+      for (int e = 0; e < n; e += 4) *reinterpret_cast<float4*>(p + e) = make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
+    } else {
+#pragma unroll
+      for (int e = 0; e < n; ++e)
+        if (e < left) p[e] = v[e];
+    }
+  } else {
+    __nv_bfloat16* p = static_cast<__nv_bfloat16*>(g.out[o]) + at;
+    if (g.vec && left >= n) {
+#pragma unroll
+      for (int e = 0; e < n; e += 4) *reinterpret_cast<uint2*>(p + e) = make_uint2(rows::pack_bf16(v[e], v[e + 1]), rows::pack_bf16(v[e + 2], v[e + 3]));
+    } else {
+#pragma unroll
+      for (int e = 0; e < n; ++e)
+        if (e < left) p[e] = __float2bfloat16_rn(v[e]);
+    }
+  }
+}
+// n neighbouring outputs from their sums: of one matrix, or of both projections
+template <int KIND, int n>
+__device__ __forceinline__ void finish(const SmallArgs& g, int which, int64_t row, int col, float (&a)[n], float (&b)[n]) {
+  if (KIND > GS_FWD_E4M3) {
+    put_row<n>(g, KIND == GS_DW ? which : 0, row, col, a, KIND == GS_DW && g.f32);
+    return;
+  }
+  const int left = g.width - col;
+  const float xs = KIND == GS_FWD_E4M3 ? g.xs[row] : 1.f;
+#pragma unroll
+  for (int e = 0; e < n; ++e) {
+    if (e < left) {
+      if (KIND == GS_FWD_E4M3) { a[e] *= xs * g.wgs[col + e]; b[e] *= xs * g.wus[col + e]; }
+      if (g.bg) { a[e] += g.bg[col + e]; b[e] += g.bu[col + e]; }
+    }
+  }
+  if (g.out[1]) { put_row<n>(g, 1, row, col, a, false); put_row<n>(g, 2, row, col, b, false); }
+  with_act(g.act, [&](auto act) {
+#pragma unroll
+    for (int e = 0; e < n; ++e) a[e] = act.value(a[e]) * b[e];
+  });
+  put_row<n>(g, 0, row, col, a, false);
+}
+
 // F: outputs of a tile; the accumulator has NT columns.  Grid: (column tiles x splits, row tiles, matrices).
 template <int KIND, int F>
 __global__ void __launch_bounds__(GS_THREADS, KIND <= GS_FWD_E4M3 && F == 32 ? 4 : 2) gated_small_kernel(const __grid_constant__ SmallArgs g) {
@@ -76,6 +127,7 @@ __global__ void __launch_bounds__(GS_THREADS, KIND <= GS_FWD_E4M3 && F == 32 ? 4
   const int k0 = (int)((int64_t)g.nk * rank / S), nk = (int)((int64_t)g.nk * (rank + 1) / S) - k0;
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   const int stages = g.stages;
+  const bool direct = S == 1 && !(FWD && g.out[1]);
 
   if (threadIdx.x == 0) {
     abort_flag = never = 0;
@@ -168,7 +220,9 @@ __global__ void __launch_bounds__(GS_THREADS, KIND <= GS_FWD_E4M3 && F == 32 ? 4
     }
     __syncwarp();
   } else {
-    // ---- this CTA's share to shared memory, a row a thread (every product has read its operands) ----
+    // ---- epilogue, a row a thread: the results themselves where the tile is this CTA's alone, else its share to shared memory
+    //      (every product has read its operands).  With both projections kept they go through shared memory too: three outputs
+    //      of 32 bytes a row are more stores than the way around (512 rows, 1024 x 2816: 20.9 us against 16.8). ----
     const int q = warp & 3, r = q * 32 + lane;
     const int64_t left = g.height - m0;
     if (q * 32 < left) {
@@ -177,15 +231,26 @@ __global__ void __launch_bounds__(GS_THREADS, KIND <= GS_FWD_E4M3 && F == 32 ? 4
         if (lane == 0) GS_ABORT(413);
       } else {
         tc_fence_after();
-        const uint32_t row = base + (uint32_t)(r * PITCH) * 4u;
+        const uint32_t row = base + (uint32_t)(r * PITCH) * 4u, lanes = tmem_base + ((uint32_t)(q * 32) << 16);
+        if (!direct) {
 #pragma unroll
-        for (int c = 0; c < NT; c += 16) {
-          uint32_t v[16];
-          tmem_ld16(tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)c, v);
-          tmem_ld_wait();
-          if (r < left) {
+          for (int c = 0; c < NT; c += 16) {
+            uint32_t v[16];
+            tmem_ld16(lanes + (uint32_t)c, v);
+            tmem_ld_wait();
+            if (r < left) {
 #pragma unroll
-            for (int j = 0; j < 16; j += 4) sts4(row + (uint32_t)(c + j) * 4u, v + j);
+              for (int j = 0; j < 16; j += 4) sts4(row + (uint32_t)(c + j) * 4u, v + j);
+            }
+          }
+        } else {
+#pragma unroll 1
+          for (int c = 0; c < F; c += 16) {
+            float a[16], b[16];
+            tmem_ld16(lanes + (uint32_t)c, reinterpret_cast<uint32_t(&)[16]>(a));
+            if (FWD) tmem_ld16(lanes + (uint32_t)(F + c), reinterpret_cast<uint32_t(&)[16]>(b));
+            tmem_ld_wait();
+            if (r < left && n0 + c < g.width) finish<KIND, 16>(g, which, m0 + r, n0 + c, a, b);
           }
         }
       }
@@ -197,12 +262,12 @@ __global__ void __launch_bounds__(GS_THREADS, KIND <= GS_FWD_E4M3 && F == 32 ? 4
   if (S > 1) { cluster_arrive(); cluster_wait(); }
 
   // ---- four neighbouring outputs a thread, of this CTA's part of the columns: all shares in order ----
-  if (!abort_flag) {
+  if (!direct && !abort_flag) {
     const int part = F / S, quads = part / 4;       // a power of two
     const int have = (int)(g.height - m0 < 128 ? g.height - m0 : 128);
     for (int i = threadIdx.x; i < have * quads; i += GS_THREADS) {
-      const int r = i / quads, j = rank * part + (i - r * quads) * 4, col = n0 + j, n = g.width - col;
-      if (n <= 0) continue;
+      const int r = i / quads, j = rank * part + (i - r * quads) * 4, col = n0 + j;
+      if (col >= g.width) continue;
       const uint32_t at = base + (uint32_t)(r * PITCH + j) * 4u;
       float a[4] = {0.f, 0.f, 0.f, 0.f}, b[4] = {0.f, 0.f, 0.f, 0.f};
       // four shares' loads before their sums: one by one the latency of another SM's shared memory was most of the kernel (333 x 1000 x
@@ -225,37 +290,7 @@ __global__ void __launch_bounds__(GS_THREADS, KIND <= GS_FWD_E4M3 && F == 32 ? 4
           }
         }
       }
-      const int64_t row = m0 + r;
-      auto put4 = [&](int o, const float (&v)[4]) {
-        if (KIND == GS_DW && g.f32) {
-          float* p = static_cast<float*>(g.out[o]) + row * g.ld[o] + col;
-          if (g.vec && n >= 4) *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
-          else
-            for (int e = 0; e < 4 && e < n; ++e) p[e] = v[e];
-        } else {
-          __nv_bfloat16* p = static_cast<__nv_bfloat16*>(g.out[o]) + row * g.ld[o] + col;
-          if (g.vec && n >= 4) *reinterpret_cast<uint2*>(p) = make_uint2(rows::pack_bf16(v[0], v[1]), rows::pack_bf16(v[2], v[3]));
-          else
-            for (int e = 0; e < 4 && e < n; ++e) p[e] = __float2bfloat16_rn(v[e]);
-        }
-      };
-      if (FWD) {
-        const float xs = KIND == GS_FWD_E4M3 ? g.xs[row] : 1.f;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          if (e >= n) break;
-          if (KIND == GS_FWD_E4M3) { a[e] *= xs * g.wgs[col + e]; b[e] *= xs * g.wus[col + e]; }
-          if (g.bg) { a[e] += g.bg[col + e]; b[e] += g.bu[col + e]; }
-        }
-        if (g.out[1]) { put4(1, a); put4(2, b); }
-        with_act(g.act, [&](auto act) {
-#pragma unroll
-          for (int e = 0; e < 4; ++e) a[e] = act.value(a[e]) * b[e];
-        });
-        put4(0, a);
-      } else {
-        put4(KIND == GS_DW ? which : 0, a);
-      }
+      finish<KIND, 4>(g, which, m0 + r, col, a, b);
     }
   }
   // no CTA leaves while its shares are being read
