@@ -101,6 +101,15 @@ __device__ __forceinline__ void merge_lanes3(MaxSum& a, MaxSum& b, MaxSum& c, fl
   }
 }
 
+// With P of the teacher's mass and Q of the student's on the named classes: log p_t - log q_t (base 2), and A - p_t / q_t, from the masses
+// that are small.  Where both lie almost wholly on the other classes the loss is what is left of two logarithms near 0.
+__device__ __forceinline__ float log_rest(float pt, float qt, float P, float Q) {
+  return P < 0.5f && Q < 0.5f ? (log1pf(-P) - log1pf(-Q)) * kLog2e : log2f(pt) - log2f(qt);
+}
+__device__ __forceinline__ float factor_rest(float A, float pt, float qt, float P, float Q) {
+  return P < 0.5f && Q < 0.5f ? __fdividef(P - Q, qt) : A - __fdividef(pt, qt);
+}
+
 // VEC classes an access, NV accesses a thread and trip.  KEEP: the CTA's slice is one trip, its exponentials stay in registers.
 template <class T, int VEC, int NV, int MODE, bool KEEP>
 __global__ void __launch_bounds__(512, 2) distill_kernel(const Distill p) {
@@ -245,7 +254,7 @@ __global__ void __launch_bounds__(512, 2) distill_kernel(const Distill p) {
 
   // ---- the student's normalisers: the others' over the cluster in order, then the named classes ----
   // q_j = exp((z_j - ref) / tau) inv, or, from what the forward call left, exp(z_j / tau - ref)
-  float ref, inv, qt;                         // qt: the mass of the classes that are not named
+  float ref, inv, qt, Q = 1.f;                // qt: the mass of the classes that are not named, Q: of those that are (forward)
   bool empty;                                 // no class has any
   MaxSum all = {kLow, 0.f}, others = {kLow, 0.f};
   if (MODE != DIST_BACKWARD) {
@@ -258,12 +267,14 @@ __global__ void __launch_bounds__(512, 2) distill_kernel(const Distill p) {
     __syncthreads();                          // red_m, red_l have been read
     if (lane == 0) { red_m[warp] = n.m; red_l[warp] = n.l; }
     __syncthreads();
-    all = others;
-    for (int k = 0; k < nw; ++k) all = merge(all, {red_m[k], red_l[k]}, c2);
+    MaxSum named = {red_m[0], red_l[0]};
+    for (int k = 1; k < nw; ++k) named = merge(named, {red_m[k], red_l[k]}, c2);
+    all = merge(others, named, c2);
     empty = all.l == 0.f;
     ref = all.m;
     inv = 1.f / all.l;
     qt = others.l * ex2((others.m - all.m) * c2) * inv;
+    Q = named.l * ex2((named.m - all.m) * c2) * inv;
   } else {
     ref = p.stat_in[2 * row];
     inv = 1.f;
@@ -288,7 +299,7 @@ __global__ void __launch_bounds__(512, 2) distill_kernel(const Distill p) {
       if (tid == 0) {
         kl = 0.f;
         for (int k = 0; k < nw; ++k) kl += red_x[k];
-        if (pt > 0.f) kl += pt * (log2f(pt) - log2f(qt));
+        if (pt > 0.f) kl += pt * log_rest(pt, qt, whole, Q);
         if (whole != whole) kl = whole;
         p.loss[row] = empty ? 0.f : wt * kl * kLn2;
         if (p.stat) {
@@ -302,7 +313,7 @@ __global__ void __launch_bounds__(512, 2) distill_kernel(const Distill p) {
   if (MODE != DIST_LOSS) {
     const float ws = empty ? 0.f : wt * p.inv_tau;
     // q_j (A - p_t / q_t) of the others; where there are none, nothing stands at that factor
-    const float other = pt > 0.f && qt != 0.f ? A - pt / qt : A;
+    const float other = pt > 0.f && qt != 0.f ? factor_rest(A, pt, qt, whole, Q) : A;
     if (KEEP && MODE == DIST_BOTH) {
       const float f = empty ? 0.f : ws * other * ex2((sum.m - ref) * c2) * inv;
 #pragma unroll
@@ -379,7 +390,7 @@ __device__ __forceinline__ const void* word_of(const void* at) {
 
 struct RingNumbers { float w, t_lse, s0, s1; };
 // What the sums' warp says of a row: to the classes that are not named, for the gradient of those that are, and for the loss
-struct RingScale { float ref, factor, ws, A, inv, tm, scale_p, whole, pt, qt, w; MaxSum all, others; };
+struct RingScale { float ref, factor, ws, A, inv, tm, scale_p, whole, pt, qt, Q, w; MaxSum all, others; };
 
 // FILL: the last CTA's slice ends inside an access of 16 bytes, with one, or all slices fill all accesses of their threads.
 template <class T, int NV, int MODE, int FILL>
@@ -734,7 +745,7 @@ __global__ void __launch_bounds__(kRingAll, 2) distill_ring_kernel(const Distill
         }
         kl = lanes_sum(kl);
         if (lane == 0) {
-          if (sc.pt > 0.f) kl += sc.pt * (log2f(sc.pt) - log2f(sc.qt));
+          if (sc.pt > 0.f) kl += sc.pt * log_rest(sc.pt, sc.qt, sc.whole, sc.Q);
           if (sc.whole != sc.whole) kl = sc.whole;
           p.loss[row] = empty ? 0.f : sc.w * kl * kLn2;
           if (p.stat) {
@@ -796,7 +807,7 @@ __global__ void __launch_bounds__(kRingAll, 2) distill_ring_kernel(const Distill
           float pt = 0.f;
           if (p.t_lse) pt = 1.f - whole < 0.f ? 0.f : 1.f - whole;
           const float A = whole + pt;
-          float ref, inv, qt;
+          float ref, inv, qt, Q = 1.f;
           bool empty;
           MaxSum all = {kLow, 0.f}, others = {kLow, 0.f};
           if (MODE != DIST_BACKWARD) {
@@ -815,6 +826,7 @@ __global__ void __launch_bounds__(kRingAll, 2) distill_ring_kernel(const Distill
             ref = all.m;
             inv = __fdividef(1.f, all.l);
             qt = others.l * ex2((others.m - all.m) * c2) * inv;
+            Q = n.l * ex2((n.m - all.m) * c2) * inv;
           } else {
             ref = s_num[slot_of(it)].s0;
             inv = 1.f;
@@ -823,9 +835,9 @@ __global__ void __launch_bounds__(kRingAll, 2) distill_ring_kernel(const Distill
           }
           const float ws = empty ? 0.f : w * p.inv_tau;
           // q_j (A - p_t / q_t) of the others; where there are none, nothing stands at that factor
-          const float other = pt > 0.f && qt != 0.f ? A - __fdividef(pt, qt) : A;
+          const float other = pt > 0.f && qt != 0.f ? factor_rest(A, pt, qt, whole, Q) : A;
           if (lane == 0) {
-            s_scale[it & 3] = {ref, ws == 0.f ? 0.f : ws * other * inv, ws, A, inv, tm, scale_p, whole, pt, qt, w, all, others};
+            s_scale[it & 3] = {ref, ws == 0.f ? 0.f : ws * other * inv, ws, A, inv, tm, scale_p, whole, pt, qt, Q, w, all, others};
             sm100::mbar_arrive(bar(bar_scale[it & 1]));
           }
         }

@@ -242,6 +242,24 @@ def test_confident_student(B):
     check(dz, want[2], want[4], HALF[torch.float32])
 
 
+@pytest.mark.parametrize("V,K", [(1500, 2), (42440, 45)])
+def test_little_named_mass(B, V, K):
+    """A flat teacher: nearly all mass, its and the student's, on the classes that are not named (P, Q of 1e-4 to 1e-2).  The loss is
+    then of the size of P: its terms p log(p / q) within E, and p_t (log(1 - P) - log(1 - Q)) within 4 E (P + Q)."""
+    tau = 4.0
+    z, T, I, t_lse = inputs(20, V, K, "f32", V, tau=tau)
+    loss, dz = torch.empty(20, device="cuda"), matrix(20, V, torch.float32)
+    B.fw_distill_forward(desc(B, V, K, "f32", tau=tau), z, T, I, loss, t_lse=t_lse, dZ=dz)
+    want = reference(z, T, I, tau, t_lse)
+    logp = T.to(F64) / tau - t_lse.to(F64)[:, None]
+    p = logp.exp()
+    logq = z.to(F64).gather(1, I.long()) / tau - torch.logsumexp(z.to(F64) / tau, 1, keepdim=True)
+    E = 2.0 ** -17 + 16 * 2.0 ** -24 * t_lse.to(F64).abs()          # t / tau - t_lse is rounded at the size of t_lse
+    bound = (p * (logp.abs() + logq.abs() + 1)).sum(1) * E + 4 * E * (p.sum(1) + logq.exp().sum(1))
+    assert bool(((loss.to(F64) - want[0]).abs() <= bound).all())
+    check(dz, want[2], want[4], HALF[torch.float32])
+
+
 def test_gradient_against_differences(B):
     """Central differences of the loss in 64 bits, step 1e-5: truncation 1e-10 of the terms."""
     V, K, tau, h = 30, 5, 2.0, 1e-5
