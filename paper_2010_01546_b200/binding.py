@@ -348,17 +348,18 @@ def fw_launch_count() -> int:
 
 
 # ---- operators around the layers: tensors in, with their sizes, strides and types looked at ----
-_TYPES = None          # this library's types as torch has them (filled by the first call)
+_TYPES = _torch = None  # this library's types as torch has them, and torch (both with the first call)
 
 
 def _here():
     """The device that the library launches on: the current one.  Tensors have to be there."""
-    global _TYPES
-    import torch
+    global _TYPES, _torch
     if _TYPES is None:
+        import torch
+        _torch = torch
         _TYPES = {FW_F32: torch.float32, FW_BF16: torch.bfloat16, FW_E4M3: torch.float8_e4m3fn, "int32": torch.int32,
                   "int64": torch.int64}
-    return torch.cuda.current_device() if torch.cuda.is_initialized() or torch.cuda.is_available() else None
+    return _torch.cuda.current_device() if _torch.cuda.is_initialized() or _torch.cuda.is_available() else None
 
 
 def _refuse_device(t, dev, name):

@@ -105,24 +105,27 @@ __global__ void __launch_bounds__(256, SUMS ? 3 : 4) gated_gates_kernel(const Ga
   }
 }
 
-// dbg, dbu: the slabs' sums in order
-__global__ void __launch_bounds__(128) gated_bias_kernel(const float* part, int slabs, int N, float* dbg, float* dbu) {
-  const int c = blockIdx.x * 128 + threadIdx.x;
+// dbg, dbu: sums over the slabs, 32 columns a CTA: eight warps take every eighth slab, all of them in flight, and are added in order
+// (a thread for each column took 9 us for the 64 slabs of N = 8192)
+__global__ void __launch_bounds__(256) gated_bias_kernel(const float* part, int slabs, int N, float* dbg, float* dbu) {
+  __shared__ float acc[8][32];
+  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
   dep_sync();
   float* out = blockIdx.y ? dbu : dbg;
-  if (c >= N || !out) return;
   const float* p = part + (int64_t)blockIdx.y * slabs * N + c;
-  float s = 0.f;
-  int k = 0;
-  for (; k + 8 <= slabs; k += 8) {
-    float v[8];
+  float v[kGateSlabs / 8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = p[(int64_t)(k + j) * N];
+  for (int k = 0; k < kGateSlabs / 8; ++k) v[k] = c < N && w + 8 * k < slabs ? p[(int64_t)(w + 8 * k) * N] : 0.f;
+  float s = v[0];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) s += v[j];
+  for (int k = 1; k < kGateSlabs / 8; ++k) s += v[k];
+  acc[w][lane] = s;
+  __syncthreads();
+  if (w == 0 && c < N) {
+#pragma unroll
+    for (int k = 1; k < 8; ++k) s += acc[k][lane];
+    out[c] = s;
   }
-  for (; k < slabs; ++k) s += p[(int64_t)k * N];
-  out[c] = s;
 }
 
 constexpr int kGatedMaxDim = 32768;
@@ -215,7 +218,7 @@ cudaError_t launch_gated_gates(const GatedGates& g, cudaStream_t s) {
   }
   if (e == cudaSuccess && g.part) {
     ProfScope ps(FW_PROF_MISC, s);
-    e = launch_dep(gated_bias_kernel, dim3((g.N + 127) / 128, 2), 128, 0, s, g.part, g.slabs, g.N, g.dbg, g.dbu);
+    e = launch_dep(gated_bias_kernel, dim3((g.N + 31) / 32, 2), 256, 0, s, g.part, g.slabs, g.N, g.dbg, g.dbu);
   }
   return e;
 }

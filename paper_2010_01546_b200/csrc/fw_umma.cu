@@ -42,7 +42,8 @@ EncodeTiledFn encode_fn() {
 
 // 2-D row-major tensor [outer][inner] with leading dimension ld (elements); box = box_inner x box_outer.
 bool encode_2d(CUtensorMap* m, CUtensorMapDataType dt, int elem_bytes, const void* base, uint64_t inner,
-               uint64_t outer, uint64_t ld, uint32_t box_inner, uint32_t box_outer, CUtensorMapSwizzle sw) {
+               uint64_t outer, uint64_t ld, uint32_t box_inner, uint32_t box_outer, CUtensorMapSwizzle sw,
+               CUtensorMapL2promotion l2 = CU_TENSOR_MAP_L2_PROMOTION_L2_128B) {
   EncodeTiledFn fn = encode_fn();
   if (!fn) return false;
   cuuint64_t dims[2] = {inner, outer};
@@ -50,7 +51,7 @@ bool encode_2d(CUtensorMap* m, CUtensorMapDataType dt, int elem_bytes, const voi
   cuuint32_t box[2] = {box_inner, box_outer};
   cuuint32_t estr[2] = {1, 1};
   CUresult r = fn(m, dt, 2, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, sw,
-                  CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+                  l2, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   return r == CUDA_SUCCESS;
 }
 
@@ -955,7 +956,9 @@ bool tmap_encode_rows128(CUtensorMap* m, int elem_bytes, const void* base, uint6
   const CUtensorMapDataType dt = elem_bytes == 1   ? CU_TENSOR_MAP_DATA_TYPE_UINT8
                                  : elem_bytes == 2 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16
                                                    : CU_TENSOR_MAP_DATA_TYPE_FLOAT32;
-  return encode_2d(m, dt, elem_bytes, base, inner, outer, ld, 128u / (uint32_t)elem_bytes, box_outer, CU_TENSOR_MAP_SWIZZLE_128B);
+  // a row's next 128 bytes are the next K block's: fetched with these (2048 x 4096 x 8192 e4m3 135 -> 106 us, one token 27.6 -> 26.0)
+  return encode_2d(m, dt, elem_bytes, base, inner, outer, ld, 128u / (uint32_t)elem_bytes, box_outer, CU_TENSOR_MAP_SWIZZLE_128B,
+                   CU_TENSOR_MAP_L2_PROMOTION_L2_256B);
 }
 
 // A wait that nothing ever satisfies, with a short poll limit: the bounded wait of every pipeline in this engine
