@@ -347,7 +347,7 @@ fw_status fw_rmsnorm_backward(const fw_norm_desc* d, int64_t rows, const void* d
  *   FW_BF16  X, weights, outputs bf16
  *   FW_E4M3  X and weights e4m3 with a scale for each row of X (x_scale) and each row of
  *            Wg, Wu (wg_scale, wu_scale); H, Zg, Zu bf16; forward only
- * Scales and biases are fp32.  1 <= M, N <= 32768.  Every matrix but dWg, dWu starts on 16 bytes
+ * Scales and biases are fp32.  1 <= M, N <= 32768, 1 <= rows <= 2^26.  Every matrix but dWg, dWu starts on 16 bytes
  * and has rows a multiple of 16 bytes apart (M and N may be any).
  * Like a layer the block is a host object over caller-supplied device memory with a
  * stream of its own: calls on one block are not for several threads at once, and its

@@ -129,6 +129,7 @@ __global__ void __launch_bounds__(256) gated_bias_kernel(const float* part, int 
 }
 
 constexpr int kGatedMaxDim = 32768;
+constexpr int64_t kGatedMaxRows = 1 << 26;        // tiles are counted in 32 bits
 constexpr size_t kAlign = 256;
 size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
 
@@ -139,7 +140,7 @@ fw_status desc_check(const fw_gated_desc* d) {
   if (d->act < FW_ACT_SILU || d->act > FW_ACT_RELU) return FW_ERR_INVALID_ARG;
   if (d->grad != 0 && d->grad != 1) return FW_ERR_INVALID_ARG;
   if (d->grad && d->x_dtype == FW_E4M3) return FW_ERR_UNSUPPORTED;
-  if (d->grad && (d->max_rows < 1 || d->max_rows > 0x7fffffff)) return FW_ERR_SHAPE;
+  if (d->grad && (d->max_rows < 1 || d->max_rows > kGatedMaxRows)) return FW_ERR_SHAPE;
   return FW_OK;
 }
 
@@ -279,7 +280,7 @@ fw_status fw_gated_forward(fw_gated* g, const void* X, int64_t rows, int64_t ldx
   if (!g || !X || !Wg || !Wu || !H || (Zg == nullptr) != (Zu == nullptr) || (bg == nullptr) != (bu == nullptr)) return FW_ERR_INVALID_ARG;
   const bool q8 = g->d.x_dtype == FW_E4M3;
   if (q8 != (x_scale != nullptr) || q8 != (wg_scale != nullptr) || q8 != (wu_scale != nullptr)) return FW_ERR_INVALID_ARG;
-  if (rows < 1 || rows > 0x7fffff00) return FW_ERR_SHAPE;
+  if (rows < 1 || rows > kGatedMaxRows) return FW_ERR_SHAPE;
   const int M = g->d.M, N = g->d.N, es = q8 ? 1 : 2;
   ldx = pitch(rows, M, ldx, es); ldw = pitch(N, M, ldw, es); ldh = pitch(rows, N, ldh, 2); ldz = pitch(rows, N, ldz, 2);
   const View in[8] = {{X, rows, M, ldx, es}, {Wg, N, M, ldw, es}, {Wu, N, M, ldw, es}, {x_scale, 1, rows, rows, 4},
@@ -309,7 +310,7 @@ fw_status fw_gated_backward(fw_gated* g, const void* dH, int64_t rows, int64_t l
   if ((dX && (!Wg || !Wu)) || (dWg && !X)) return FW_ERR_INVALID_ARG;
   if (dWg && dw_dtype != FW_F32 && dw_dtype != FW_BF16) return FW_ERR_INVALID_ARG;
   if (!g->d.grad) return FW_ERR_WORKSPACE;
-  if (rows < 1 || rows > g->d.max_rows || rows > 0x7fffff00) return FW_ERR_SHAPE;
+  if (rows < 1 || rows > g->d.max_rows) return FW_ERR_SHAPE;
   const int M = g->d.M, N = g->d.N, ws = dw_dtype == FW_F32 ? 4 : 2;
   lddh = pitch(rows, N, lddh, 2); ldx = pitch(rows, M, ldx, 2); ldw = pitch(N, M, ldw, 2); ldz = pitch(rows, N, ldz, 2);
   lddx = pitch(rows, M, lddx, 2);

@@ -489,6 +489,13 @@ fw_status fw_rmsnorm_forward(const fw_norm_desc* d, int64_t rows, const void* x,
     const uint64_t n = o.p ? matrix_span(rows, d->M, o.ld, o.elem) : 0;
     if (overlap(o.p, n, w, (uint64_t)d->M * 4) || overlap(o.p, n, y_scale, nvec) || overlap(o.p, n, rstd, nvec)) return FW_ERR_INVALID_ARG;
   }
+  const void* rows_out[2] = {y_scale, rstd};
+  for (const void* v : rows_out) {
+    if (overlap(v, nvec, w, (uint64_t)d->M * 4)) return FW_ERR_INVALID_ARG;
+    for (const Mat& i : in)
+      if (overlap(v, nvec, i.p, i.p ? matrix_span(rows, d->M, i.ld, i.elem) : 0)) return FW_ERR_INVALID_ARG;
+  }
+  if (overlap(y_scale, nvec, rstd, nvec)) return FW_ERR_INVALID_ARG;
   NormFwd p;
   p.x = x; p.res = res; p.w = w; p.sum = sum; p.y = y; p.y_scale = y_scale; p.rstd = rstd;
   p.rows = rows; p.ldx = ldx; p.ldr = ldr; p.lds = lds; p.ldy = ldy; p.M = d->M; p.width = 0;
@@ -527,6 +534,18 @@ fw_status fw_rmsnorm_backward(const fw_norm_desc* d, int64_t rows, const void* d
   if (overlap(dx, nout, w, (uint64_t)d->M * 4) || overlap(dx, nout, rstd, (uint64_t)rows * 4) ||
       overlap(dx, nout, dw, (uint64_t)d->M * 4))
     return FW_ERR_INVALID_ARG;
+  if (dw) {
+    const uint64_t nw = (uint64_t)d->M * 4, ns = fw_rmsnorm_scratch_bytes(d);
+    const void* others[2] = {w, rstd};
+    const uint64_t no[2] = {nw, (uint64_t)rows * 4};
+    for (int k = 0; k < 2; ++k)
+      if (overlap(dw, nw, others[k], no[k]) || overlap(scratch, ns, others[k], no[k])) return FW_ERR_INVALID_ARG;
+    for (const Mat& i : in) {
+      const uint64_t n = i.p ? matrix_span(rows, d->M, i.ld, es) : 0;
+      if (overlap(dw, nw, i.p, n) || overlap(scratch, ns, i.p, n)) return FW_ERR_INVALID_ARG;
+    }
+    if (overlap(scratch, ns, dx, nout) || overlap(scratch, ns, dw, nw)) return FW_ERR_INVALID_ARG;
+  }
   NormBwd p;
   p.dy = dy; p.s = s; p.ds = dsum; p.w = w; p.rstd = rstd; p.dx = dx; p.part = dw ? static_cast<float*>(scratch) : nullptr;
   p.rows = rows; p.lddy = lddy; p.lds = lds; p.ldds = ldds; p.lddx = lddx; p.M = d->M; p.width = 0; p.inv_M = 1.f / (float)d->M;

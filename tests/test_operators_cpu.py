@@ -38,14 +38,14 @@ def test_norm_refusals(lib):
         assert norm_forward(lib, B.fw_norm_desc_default(M)) == shape
     for kw in (dict(x=None), dict(w=None), dict(y=None), dict(s=4 * A, lds=64), dict(scale=4 * A), dict(x=A + 1), dict(w=2 * A + 2),
                dict(rstd=A + 2), dict(y=A + 2), dict(y=A, ldy=72), dict(res=4 * A, ldr=64, s=3 * A, lds=64),
-               dict(y=2 * A), dict(rstd=3 * A)):
+               dict(y=2 * A), dict(rstd=3 * A), dict(rstd=A), dict(rstd=2 * A + 64)):
         assert norm_forward(lib, d, **kw) == inv, kw
     for kw in (dict(rows=0), dict(rows=-3), dict(rows=1 << 31), dict(ldx=63), dict(ldy=0), dict(ldx=(1 << 30) + 1)):
         assert norm_forward(lib, d, **kw) == shape, kw
     assert norm_forward(lib, ok(y_dtype=B.FW_E4M3)) == inv                  # no place for the scales
     assert norm_forward(lib, ok(y_dtype=B.FW_E4M3), y=A, scale=4 * A) == inv   # bytes over the bf16 rows they are made from
     for kw in (dict(dy=None), dict(s=None), dict(w=None), dict(rstd=None), dict(dx=None), dict(scratch=None), dict(dx=A + 64),
-               dict(dx=3 * A)):
+               dict(dx=3 * A), dict(dw=A), dict(dw=3 * A), dict(dw=7 * A + 64), dict(scratch=2 * A), dict(scratch=4 * A), dict(scratch=5 * A)):
         assert norm_backward(lib, d, **kw) == inv, kw
     assert norm_backward(lib, d, rows=0) == shape and norm_backward(lib, d, lddx=60) == shape
     assert norm_backward(lib, d, n=100) == ws and norm_backward(lib, d, scratch=7 * A + 8) == ws
@@ -108,7 +108,7 @@ def test_gated_refusals(lib):
 
     for kw in (dict(x_dtype=9), dict(act=4), dict(act=-1), dict(grad=2)):
         assert make(**kw) == (inv, 0), kw
-    for kw in (dict(M=0), dict(N=0), dict(M=32769), dict(N=40000), dict(grad=1), dict(grad=1, max_rows=-1)):
+    for kw in (dict(M=0), dict(N=0), dict(M=32769), dict(N=40000), dict(grad=1), dict(grad=1, max_rows=-1), dict(grad=1, max_rows=(1 << 26) + 1)):
         assert make(**kw) == (shape, 0), kw
     assert make(x_dtype=B.FW_F32) == (no, 0) and make(x_dtype=B.FW_E4M3, grad=1, max_rows=4) == (no, 0)
     assert make(at=A + 16)[0] == ws and make(n=100)[0] == ws and make(at=None)[0] == inv
