@@ -12,7 +12,7 @@ from optest_util import F64, HALF, captured, gen, matrix, put, surround_kept
 pytestmark = pytest.mark.gpu
 
 KINDS = {"f32": torch.float32, "bf16": torch.bfloat16}
-SIZES = [(3, 1, 1), (1, 2, 2), (5, 100, 10), (37, 1000, 10), (7, 1025, 33), (4, 2048, 1024), (3, 8191, 64), (2, 50021, 33),
+SIZES = [(3, 1, 1), (1, 2, 2), (5, 100, 10), (37, 1000, 10), (9, 300, 81), (6, 512, 128), (5, 1024, 129), (7, 2047, 64), (7, 1025, 33), (4, 2048, 1024), (3, 8191, 64), (2, 50021, 33),
          (5, 3000, 256), (2, 9000, 257), (2, 131072, 64), (2, 131101, 100), (2, 250000, 256), (1, 300001, 7), (1, 1 << 20, 130)]
 
 
