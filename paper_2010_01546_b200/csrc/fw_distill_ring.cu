@@ -16,16 +16,15 @@ namespace {
 //   eight warps   classes of the slice: cp.async two rows ahead (a thread reads back only what it copied: no barrier), exponentials
 //                 in registers, each warp's sum sent to every CTA of the cluster (st.async, counted in bytes there), the gradient
 //                 once the factor is known;
-//   one warp      entries of the next row: repeated classes, bit set, sums of the teacher's and of the named classes; the loss of
-//                 the row before;
-//   one warp      all sums and the factor; the named classes' gradient of the row before over the eight warps' stores;
+//   one warp      entries of the next row: repeated classes, bit set, sums of the teacher's and of the named classes;
+//   one warp      all sums, the factor and the loss; the named classes' gradient of the row before over the eight warps' stores;
 //                 and entries copied ahead, class and teacher's logit 2 kAheadRows + 1 rows, the student's logit kAheadRows + 1.
 // They meet on mbarriers, a CTA has no common barrier.  With the entries spread over the eight warps, a barrier a row and every
 // thread working out the factor, the fixed part of a row was 650 instructions a warp beside 320 for its classes: 690 us.
 // ---------------------------------------------------------------------------
 constexpr int kRingWarps = 8, kRingThreads = 32 * kRingWarps, kRingSlots = 3, kRingMaxK = 256, kRingMaxCtas = 16;
 constexpr int kRingAll = kRingThreads + 64;
-constexpr int kAheadRows = 2, kEntrySlots = 2 * kAheadRows + 4;
+constexpr int kAheadRows = 1, kEntrySlots = 2 * kAheadRows + 4;
 constexpr int kSeenBits = 16384;
 
 // to a place in a CTA of the cluster, counted in bytes on that CTA's barrier
@@ -49,7 +48,10 @@ __device__ __forceinline__ const void* word_of(const void* at) {
 
 struct RingNumbers { float w, t_lse, s0, s1; };
 // What the sums' warp says of a row: to the classes that are not named, for the gradient of those that are, and for the loss
-struct RingScale { float ref, factor, ws, A, inv, tm, scale_p, whole, pt, qt, Q, w; MaxSum all, others; };
+struct RingScale { float ref, factor, ws, A, inv, scale_p; };
+// Of a row's entries: the teacher's exponentials and the named classes', each relative to its largest; with w the teacher's exponentials
+// and a their exponents (base 2), sum w a and sum w (z - named.m)
+struct RingEntries { MaxSum teacher, named; float wa, wz; };
 
 // FILL: the last CTA's slice ends inside an access of 16 bytes, with one, or all slices fill all accesses of their threads.
 template <class T, int NV, int MODE, int FILL>
@@ -57,10 +59,9 @@ __global__ void __launch_bounds__(kRingAll, 2) distill_ring_kernel(const Distill
   constexpr int VEC = 16 / sizeof(T);
   constexpr int words = NV * kRingThreads * VEC / 32;
   extern __shared__ __align__(16) uint8_t dyn8[];
-  __shared__ MaxSum s_sum[2][kRingMaxCtas * kRingWarps];
   __shared__ RingNumbers s_num[kEntrySlots];
-  __shared__ RingScale s_scale[4];
-  __shared__ MaxSum s_teacher[2], s_named[2];
+  __shared__ RingScale s_scale[2];
+  __shared__ RingEntries s_entries[2];
   __shared__ uint32_t s_seen[kSeenBits / 32];
   __shared__ float s_w[kRingWarps][kRingSlots + 2];
   __shared__ __align__(8) uint64_t bar_sums[2], bar_bits[2], bar_scale[2], bar_done[2], bar_clear[2];
@@ -72,6 +73,9 @@ __global__ void __launch_bounds__(kRingAll, 2) distill_ring_kernel(const Distill
   // [slot][class, teacher's logit, student's logit, with 64 bits the class's upper half][K]
   const int kp = (p.K + 3) & ~3, slot_words = kp * (p.i64 ? 4 : 3);
   uint32_t* entries = bits + 2 * words;
+  // sums of every warp of the cluster, in two places that take turns
+  MaxSum* s_sum = reinterpret_cast<MaxSum*>(entries + kEntrySlots * slot_words);
+  const int place = C * kRingWarps;
   const float c2 = p.inv_tau * kLog2e;
   const int first = rank * p.slice, last = min(p.V, first + p.slice);
   auto bar = [](uint64_t& b) { return sm100::smem_u32(&b); };
@@ -110,7 +114,7 @@ __global__ void __launch_bounds__(kRingAll, 2) distill_ring_kernel(const Distill
     auto whole = [&](int k) { return FILL == ROW_FULL || (FILL == ROW_WHOLE ? mine > k * kRingThreads * VEC : mine >= (k * kRingThreads + 1) * VEC); };
     auto begun = [&](int k) { return FILL == ROW_FULL || mine > k * kRingThreads * VEC; };
     const uint32_t ring_at = sm100::smem_u32(ring) + tid * 16;
-    const uint32_t push_at = sm100::mapa_shared(sm100::smem_u32(&s_sum[0][rank * kRingWarps + warp]), lane < C ? lane : 0);
+    const uint32_t push_at = sm100::mapa_shared(sm100::smem_u32(&s_sum[rank * kRingWarps + warp]), lane < C ? lane : 0);
     const uint32_t push_bar = sm100::mapa_shared(bar(bar_sums[0]), lane < C ? lane : 0);
     auto fetch = [&](int row, int slot, bool live) {
       if (live) {
@@ -202,12 +206,12 @@ __global__ void __launch_bounds__(kRingAll, 2) distill_ring_kernel(const Distill
             }
           }
           const MaxSum s = merge_lanes({top, part[0] + part[1]}, c2);
-          if (lane < C) send_pair(push_at + (uint32_t)turn * (uint32_t)sizeof(s_sum[0]), s, push_bar + (uint32_t)turn * 8u);
+          if (lane < C) send_pair(push_at + (uint32_t)(turn * place) * (uint32_t)sizeof(MaxSum), s, push_bar + (uint32_t)turn * 8u);
           turn ^= 1;
         }
         if (MODE != DIST_LOSS) {
           if (!wait(bar_scale, it)) break;
-          const RingScale& sc = s_scale[it & 3];
+          const RingScale& sc = s_scale[it & 1];
           const float f = MODE == DIST_BACKWARD || sc.factor == 0.f ? sc.factor : sc.factor * ex2((top - sc.ref) * c2);
 #pragma unroll
           for (int k = 0; k < NV; ++k) {
@@ -290,16 +294,16 @@ __global__ void __launch_bounds__(kRingAll, 2) distill_ring_kernel(const Distill
     // a row whose stores are done: the named classes' gradient over them, its bits out
     auto finish = [&](int row, int it) {
       if (weight(it) == 0.f) return;
-      const RingScale sc = s_scale[it & 3];
-      const float t_lse = t_lse_of(it);
+      const RingScale sc = s_scale[it & 1];
       T* dz = MODE == DIST_LOSS ? nullptr : static_cast<T*>(p.dZ) + (int64_t)row * p.lddz;
       const int* c = cls(it);
+      const uint32_t* values = entries + slot_of(it) * slot_words + kp;      // as prepare left them
       for (int k = lane; k < p.K; k += 32) {
         const int i = c[k];
         if (i < first || i >= last) continue;
         bits[(it & 1) * words + ((i - first) >> 5)] = 0;
         if (MODE != DIST_LOSS) {
-          const float z = z_of(it, row, k, i), pk = ex2(teacher2(t_of(it, row, k), t_lse, sc.tm)) * sc.scale_p;
+          const float z = __uint_as_float(values[kp + k]), pk = ex2(__uint_as_float(values[k])) * sc.scale_p;
           const float q = ex2(MODE == DIST_BACKWARD ? fmaf(z, p.inv_tau, -sc.ref) * kLog2e : (z - sc.ref) * c2) * sc.inv;
           put(dz + i, sc.ws == 0.f ? 0.f : sc.ws * (sc.A * q - pk));
         }
@@ -310,6 +314,7 @@ __global__ void __launch_bounds__(kRingAll, 2) distill_ring_kernel(const Distill
       // repeated classes out, bit set, sums of the teacher's and of the named classes' exponentials
       auto prepare = [&](int row, int it) {
         MaxSum t = {kLow, 0.f}, n = {kLow, 0.f};
+        float wa = 0.f, wz = 0.f;
         if (weight(it) != 0.f) {
           const float t_lse = t_lse_of(it);
           int* c = cls(it);
@@ -360,77 +365,45 @@ __global__ void __launch_bounds__(kRingAll, 2) distill_ring_kernel(const Distill
           }
           t.m = p.t_lse ? kLow : lanes_max(t.m);
           n.m = lanes_max(n.m);
+          uint32_t* values = entries + slot_of(it) * slot_words + kp;
           for (int g = 0; g < p.K; g += 64) {
             const int k0 = g + lane, k1 = k0 + 32;
             const int i0 = k0 < p.K ? c[k0] : -1, i1 = k1 < p.K ? c[k1] : -1;
-            const float a0 = i0 >= 0 ? ex2(teacher2(t_of(it, row, k0), t_lse, t.m)) : 0.f, a1 = i1 >= 0 ? ex2(teacher2(t_of(it, row, k1), t_lse, t.m)) : 0.f;
-            t.l += a0 + a1;
+            const float a0 = i0 >= 0 ? teacher2(t_of(it, row, k0), t_lse, t.m) : -INFINITY, a1 = i1 >= 0 ? teacher2(t_of(it, row, k1), t_lse, t.m) : -INFINITY;
+            const float z0 = i0 >= 0 ? z_of(it, row, k0, i0) : 0.f, z1 = i1 >= 0 ? z_of(it, row, k1, i1) : 0.f;
+            const float w0 = ex2(a0), w1 = ex2(a1);
+            t.l += w0 + w1;
             if (MODE != DIST_BACKWARD) {
-              const float b0 = i0 >= 0 ? ex2((z_of(it, row, k0, i0) - n.m) * c2) : 0.f, b1 = i1 >= 0 ? ex2((z_of(it, row, k1, i1) - n.m) * c2) : 0.f;
-              n.l += b0 + b1;
+              const float d0 = z0 - n.m, d1 = z1 - n.m;
+              n.l += (i0 >= 0 ? ex2(d0 * c2) : 0.f) + (i1 >= 0 ? ex2(d1 * c2) : 0.f);
+              if (w0 > 0.f) { wa = fmaf(w0, a0, wa); wz = fmaf(w0, d0, wz); }
+              if (w1 > 0.f) { wa = fmaf(w1, a1, wa); wz = fmaf(w1, d1, wz); }
             }
+            // the loss and the gradient take them from here
+            if (i0 >= 0) { values[k0] = __float_as_uint(a0); values[kp + k0] = __float_as_uint(z0); }
+            if (i1 >= 0) { values[k1] = __float_as_uint(a1); values[kp + k1] = __float_as_uint(z1); }
           }
 #pragma unroll
           for (int o = 16; o > 0; o >>= 1) {
-            const float x = __shfl_xor_sync(0xffffffffu, t.l, o), y = __shfl_xor_sync(0xffffffffu, n.l, o);
-            t.l += x;
-            n.l += y;
+            t.l += __shfl_xor_sync(0xffffffffu, t.l, o);
+            if (MODE != DIST_BACKWARD) {
+              n.l += __shfl_xor_sync(0xffffffffu, n.l, o);
+              wa += __shfl_xor_sync(0xffffffffu, wa, o);
+              wz += __shfl_xor_sync(0xffffffffu, wz, o);
+            }
           }
         }
-        if (lane == 0) { s_teacher[it & 1] = t; s_named[it & 1] = n; }
+        if (lane == 0) s_entries[it & 1] = {t, n, wa, wz};
         __syncwarp();
         if (lane == 0) sm100::mbar_arrive(bar(bar_bits[it & 1]));
-      };
-      // the loss of a row that is through, and its normalisers
-      auto write_loss = [&](int row, int it) {
-        if (MODE == DIST_BACKWARD || rank != 0) return;
-        if (weight(it) == 0.f) {
-          if (lane == 0) {
-            p.loss[row] = 0.f;
-            if (p.stat) { p.stat[2 * (int64_t)row] = 0.f; p.stat[2 * (int64_t)row + 1] = 0.f; }
-          }
-          return;
-        }
-        const RingScale sc = s_scale[it & 3];
-        const float t_lse = t_lse_of(it), log_all = log2f(sc.all.l), log_p = log2f(sc.scale_p);
-        const bool empty = sc.all.l == 0.f;
-        const int* c = cls(it);
-        float kl = 0.f;
-        for (int k = lane; k < p.K; k += 32) {
-          const int i = c[k];
-          if (i < 0) continue;
-          const float lp = teacher2(t_of(it, row, k), t_lse, sc.tm), pk = ex2(lp) * sc.scale_p;
-          if (pk > 0.f || pk != pk) kl += pk * ((lp + log_p) - ((z_of(it, row, k, i) - sc.all.m) * c2 - log_all));
-        }
-        kl = lanes_sum(kl);
-        if (lane == 0) {
-          if (sc.pt > 0.f) kl += sc.pt * log_rest(sc.pt, sc.qt, sc.whole, sc.Q);
-          if (sc.whole != sc.whole) kl = sc.whole;
-          p.loss[row] = empty ? 0.f : sc.w * kl * kLn2;
-          if (p.stat) {
-            p.stat[2 * (int64_t)row] = empty ? -INFINITY : fmaf(sc.all.m, p.inv_tau, logf(sc.all.l));
-            p.stat[2 * (int64_t)row + 1] = sc.others.l == 0.f ? -INFINITY : fmaf(sc.others.m, p.inv_tau, logf(sc.others.l));
-          }
-        }
       };
       asm volatile("bar.sync 1, 64;" ::: "memory");              // the first rows have landed
       prepare(row0, 0);
       int it = 0;
-      bool lost = false;
-      int row = row0;
-      for (; row < rows; row += step, ++it) {
-        if (it > 0) {
-          lost = !wait(bar_clear, it - 1);
-          if (lost) break;
-        }
-        if (row + step < rows) prepare(row + step, it + 1);
-        if (it > 0) write_loss(row - step, it - 1);
+      for (int row = row0; row + step < rows; row += step, ++it) {
+        if (it > 0 && !wait(bar_clear, it - 1)) break;
+        prepare(row + step, it + 1);
       }
-      lost = lost || !wait(bar_clear, it - 1);
-      if (!lost) write_loss(row - step, it - 1);
-      // given up: no barrier is touched any more, and the losses of the rows that are left say so
-      if (lost && MODE != DIST_BACKWARD && rank == 0)
-        for (int r = max(row0, row - step) + lane * step; r < rows; r += 32 * step) p.loss[r] = NAN;
     } else {
       // ---- sums ----
       for (int i = 0; i <= 2 * kAheadRows; ++i) fetch_entries(row0 + i * step, i);
@@ -457,10 +430,17 @@ __global__ void __launch_bounds__(kRingAll, 2) distill_ring_kernel(const Distill
         if (lost) break;
         const float w = weight(it);
         if (w == 0.f) {
-          if (lane == 0) sm100::mbar_arrive(bar(bar_scale[it & 1]));
+          if (lane == 0) {
+            sm100::mbar_arrive(bar(bar_scale[it & 1]));
+            if (MODE != DIST_BACKWARD && rank == 0) {
+              p.loss[row] = 0.f;
+              if (p.stat) { p.stat[2 * (int64_t)row] = 0.f; p.stat[2 * (int64_t)row + 1] = 0.f; }
+            }
+          }
         } else {
-          const MaxSum t = s_teacher[it & 1], n = s_named[it & 1];
-          const float t_lse = t_lse_of(it), tm = t.m, ts = t.l;
+          const RingEntries en = s_entries[it & 1];
+          const MaxSum n = en.named;
+          const float ts = en.teacher.l;
           const float scale_p = p.t_lse ? 1.f : (ts > 0.f ? 1.f / ts : (ts == 0.f ? 0.f : ts));     // a NaN goes on
           const float whole = ts * scale_p;
           float pt = 0.f;
@@ -470,15 +450,16 @@ __global__ void __launch_bounds__(kRingAll, 2) distill_ring_kernel(const Distill
           bool empty;
           MaxSum all = {kLow, 0.f}, others = {kLow, 0.f};
           if (MODE != DIST_BACKWARD) {
-            const int turn = sums & 1, count = C * kRingWarps;
-            if (lane == 0) sm100::mbar_expect_tx(bar(bar_sums[turn]), (uint32_t)(count * (int)sizeof(MaxSum)));
+            const int count = place;
+            const MaxSum* sent = s_sum + (sums & 1) * place;
+            if (lane == 0) sm100::mbar_expect_tx(bar(bar_sums[sums & 1]), (uint32_t)(count * (int)sizeof(MaxSum)));
             __syncwarp();
             lost = !wait(bar_sums, sums);
             if (lost) break;
             ++sums;
-            for (int i = lane; i < count; i += 32) others.m = fmaxf(others.m, s_sum[turn][i].m);
+            for (int i = lane; i < count; i += 32) others.m = fmaxf(others.m, sent[i].m);
             others.m = lanes_max(others.m);
-            for (int i = lane; i < count; i += 32) others.l += s_sum[turn][i].l * ex2((s_sum[turn][i].m - others.m) * c2);
+            for (int i = lane; i < count; i += 32) others.l += sent[i].l * ex2((sent[i].m - others.m) * c2);
             others.l = lanes_sum(others.l);
             all = merge(others, n, c2);
             empty = all.l == 0.f;
@@ -496,20 +477,32 @@ __global__ void __launch_bounds__(kRingAll, 2) distill_ring_kernel(const Distill
           // q_j (A - p_t / q_t) of the others; where there are none, nothing stands at that factor
           const float other = pt > 0.f && qt != 0.f ? factor_rest(A, pt, qt, whole, Q) : A;
           if (lane == 0) {
-            s_scale[it & 3] = {ref, ws == 0.f ? 0.f : ws * other * inv, ws, A, inv, tm, scale_p, whole, pt, qt, Q, w, all, others};
+            s_scale[it & 1] = {ref, ws == 0.f ? 0.f : ws * other * inv, ws, A, inv, scale_p};
             sm100::mbar_arrive(bar(bar_scale[it & 1]));
+            if (MODE != DIST_BACKWARD && rank == 0) {
+              // sum p (log p - log q), p = w scale_p: from the entries' sums, relative to the named classes' largest logit
+              float kl = 0.f;
+              if (ts != 0.f)
+                kl = scale_p * (en.wa + ts * log2f(scale_p) - (c2 * fmaf(n.m - all.m, ts, en.wz) - ts * log2f(all.l)));
+              if (pt > 0.f) kl += pt * log_rest(pt, qt, whole, Q);
+              if (whole != whole) kl = whole;
+              p.loss[row] = empty ? 0.f : w * kl * kLn2;
+              if (p.stat) {
+                p.stat[2 * (int64_t)row] = empty ? -INFINITY : fmaf(all.m, p.inv_tau, logf(all.l));
+                p.stat[2 * (int64_t)row + 1] = others.l == 0.f ? -INFINITY : fmaf(others.m, p.inv_tau, logf(others.l));
+              }
+            }
           }
         }
         fetch_logits(row + (1 + kAheadRows) * step, it + 1 + kAheadRows);
         fetch_entries(row + (1 + 2 * kAheadRows) * step, it + 1 + 2 * kAheadRows);
         ahead_commit();
       }
-      if (!lost && wait(bar_done, it - 1)) {
-        finish(row - step, it - 1);
-        __syncwarp();
-        if (lane == 0) sm100::mbar_arrive(bar(bar_clear[(it - 1) & 1]));
-      }
+      if (!lost && wait(bar_done, it - 1)) finish(row - step, it - 1);
       ahead_wait<0>();
+      // given up: no barrier is touched any more, and the losses of the rows that are left say so
+      if (lost && MODE != DIST_BACKWARD && rank == 0)
+        for (int r = row + lane * step; r < rows; r += 32 * step) p.loss[r] = NAN;
     }
   }
   dep_trigger();
@@ -531,7 +524,7 @@ cudaError_t launch_clusters(const Distill& p, int C, int64_t rows, cudaStream_t 
   static ClusterCache cache;
   constexpr int threads = kRingAll;
   const size_t smem = (size_t)kRingSlots * NV * kRingThreads * 16 + 2 * (NV * kRingThreads * (16 / sizeof(T)) / 8) +
-                      (size_t)kEntrySlots * ((p.K + 3) & ~3) * (p.i64 ? 16 : 12);
+                      (size_t)kEntrySlots * ((p.K + 3) & ~3) * (p.i64 ? 16 : 12) + 2 * (size_t)C * kRingWarps * sizeof(MaxSum);
   auto kernel = distill_ring_kernel<T, NV, MODE, FILL>;
   int dev = 0, n = 0;
   cudaError_t e = cudaGetDevice(&dev);
@@ -578,7 +571,7 @@ bool ring_shape(int V, int K, int vec, int* C, int* nv) {
   if (c > kRingMaxCtas) return false;
   *C = c;
   const int per = (V + c * kRingThreads * vec - 1) / (c * kRingThreads * vec);
-  *nv = per <= 2 ? 2 : per <= 4 ? 4 : 8;
+  *nv = per <= 2 ? 2 : per <= 4 ? 4 : per <= 6 ? 6 : 8;
   return true;
 }
 
@@ -593,6 +586,7 @@ cudaError_t launch_ring(const Distill& p0, int64_t rows, cudaStream_t s, bool* t
   p.slice = ((p.V + C - 1) / C + 31) / 32 * 32;
   if (nv == 2) return launch_fill<T, 2, MODE>(p, C, rows, s);
   if (nv == 4) return launch_fill<T, 4, MODE>(p, C, rows, s);
+  if (nv == 6) return launch_fill<T, 6, MODE>(p, C, rows, s);
   return launch_fill<T, 8, MODE>(p, C, rows, s);
 }
 
