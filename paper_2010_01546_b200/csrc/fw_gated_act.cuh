@@ -8,9 +8,7 @@ namespace fw {
 
 // 1 / (1 + exp(-x)): 0 and 1 at the ends, NaN for NaN
 __device__ __forceinline__ float logistic(float x) {
-  float r;
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + rows::ex2(-1.4426950408889634f * x)));
-  return r;
+  return rows::rcp(1.f + rows::ex2(-1.4426950408889634f * x));
 }
 
 template <int ACT>

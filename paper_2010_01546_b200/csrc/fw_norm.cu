@@ -101,7 +101,7 @@ __global__ void __launch_bounds__(512) norm_forward_kernel(const NormFwd p) {
       const uint32_t c = (uint32_t)(t + k * width) * VEC;
       float w[VEC];
       Ring::plain(p.w + c, p.M - (int)c, w);
-      vscale<VEC>(v[k], rstd);
+      if (sizeof(Y) != 1) vscale<VEC>(v[k], rstd);           // the scale takes rstd out of an 8-bit y again: y / c = 448 s w / max |s w|
       vmul<VEC>(v[k], w);
       if (sizeof(Y) == 1) {
 #pragma unroll
@@ -111,11 +111,15 @@ __global__ void __launch_bounds__(512) norm_forward_kernel(const NormFwd p) {
     float inv = 1.f;
     if (sizeof(Y) == 1) {
       top = over_group<MaxAbs>(top, width, buf[flip][1]);
-      float scale = 1.f;
-      if (top != 0.f) scale = top * (1.f / kE4m3Max);
-      if (scale < kMinScale) scale = kMinScale;              // a NaN stays
-      if (t == 0) p.y_scale[row] = scale;
-      inv = 1.f / scale;
+      const float size = top * rstd;                         // max |y|; NaN where the row has a NaN or an infinity
+      const bool tiny = size < kMinScale * kE4m3Max;
+      if (t == 0) p.y_scale[row] = top == 0.f ? 1.f : tiny ? kMinScale : size / kE4m3Max;
+      const bool by_size = tiny || top < 1e-36f;              // 448 / top may be beyond fp32
+      inv = tiny ? 1.f / kMinScale : size != size ? size : kE4m3Max * rcp(by_size ? size : top);
+      if (by_size) {
+#pragma unroll
+        for (int k = 0; k < NV; ++k) vscale<VEC>(v[k], rstd);
+      }
     }
     Y* y = static_cast<Y*>(p.y) + row * p.ldy;
 #pragma unroll

@@ -217,6 +217,13 @@ __device__ __forceinline__ float ex2(float x) {
   return y;
 }
 
+// 1 / x within one unit in the last place
+__device__ __forceinline__ float rcp(float x) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+
 // The larger of two numbers, a NaN if one of them is.
 __device__ __forceinline__ float max_keep_nan(float a, float b) {
   float r;
