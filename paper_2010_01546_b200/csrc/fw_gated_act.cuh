@@ -25,7 +25,8 @@ struct Act {
       df = fmaf(a * 0.3989422804014327f, rows::ex2(-0.72134752044448170f * a * a), cdf);
     } else if (ACT == FW_ACT_GELU_TANH) {
       // (1 + tanh(x)) / 2 = logistic(2 x)
-      const float k = 1.5957691216057308f, a2 = a * a;
+      // (the square is kept finite: p is 0 or 1 long before, and 0 times infinity is no derivative; a NaN goes on through f)
+      const float k = 1.5957691216057308f, a2 = fminf(a * a, 1e30f);
       const float p = logistic(k * a * fmaf(0.044715f, a2, 1.f));
       f = a * p;
       df = fmaf(f * (1.f - p), k * fmaf(0.134145f, a2, 1.f), p);

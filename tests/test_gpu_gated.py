@@ -285,3 +285,19 @@ def test_more_rows_than_room(B):
     with pytest.raises(B.FwError) as e:
         blk.backward(t[0], t[1], W, W, t[2], t[3], dX=bf(11, 64))
     assert e.value.status == B.FW_ERR_WORKSPACE
+
+
+@pytest.mark.parametrize("act", ACTS)
+def test_activations_at_the_ends(B, act):
+    """Far from 0 the derivative is 1 or 0 and the value a or 0, up to the largest finite bf16, whose square is beyond fp32.
+    At most a reciprocal (one unit, 2 u) and a product (u) are rounded: 4 u."""
+    big = torch.tensor([1e6, 1e10, 1.8e19, 1.9e19, 1e25, 1e30, 1e38, torch.finfo(BF16).max])
+    a = torch.cat([big, -big]).cuda()
+    N = a.numel()
+    Zg, Zu, dH = (put(v[None], BF16, pad=None) for v in (a, torch.ones_like(a), torch.ones_like(a)))
+    blk = block(B, 64, N, 1, act=ACTS.index(act), grad=1)
+    dbg, dbu = torch.empty(N, device="cuda"), torch.empty(N, device="cuda")
+    blk.backward(dH, None, None, None, Zg, Zu, dbg=dbg, dbu=dbu)
+    want = Zg[0].to(F64)
+    assert bool(((dbg.to(F64) - (want > 0).to(F64)).abs() <= 4 * U).all()), dbg
+    assert bool(((dbu.to(F64) - want.clamp(min=0)).abs() <= 4 * U * want.clamp(min=0)).all()), dbu
