@@ -140,8 +140,8 @@ __global__ void __launch_bounds__(kRingAll, 2) distill_ring_kernel(const Distill
     fetch(row0 + step, 1, live1);
     ahead_commit();
     int turn = 0, slot = 0;
-    int it = 0;
-    for (int row = row0; row < rows; row += step, ++it) {
+    int it = 0, row = row0;
+    for (; row < rows; row += step, ++it) {
       ahead_wait<1>();                            // this row's classes, the weight of the row after next
       __syncwarp();
       const bool live2 = counts(row + 2 * step, it + 2);
@@ -238,6 +238,10 @@ __global__ void __launch_bounds__(kRingAll, 2) distill_ring_kernel(const Distill
       if (++slot == kRingSlots) slot = 0;
     }
     ahead_wait<0>();
+    // given up: no row that is left is taken for a gradient
+    if (MODE != DIST_LOSS)
+      for (; row < rows; row += step)
+        for (int c = first + tid; c < last; c += kRingThreads) put(static_cast<T*>(p.dZ) + (int64_t)row * p.lddz + c, NAN);
   } else {
     const bool t16 = p.t_bf16 != 0;
     auto slot_of = [](int it) { return it % kEntrySlots; };
@@ -498,11 +502,16 @@ __global__ void __launch_bounds__(kRingAll, 2) distill_ring_kernel(const Distill
         fetch_entries(row + (1 + 2 * kAheadRows) * step, it + 1 + 2 * kAheadRows);
         ahead_commit();
       }
-      if (!lost && wait(bar_done, it - 1)) finish(row - step, it - 1);
+      lost = lost || !wait(bar_done, it - 1);
+      if (!lost) finish(row - step, it - 1);
       ahead_wait<0>();
-      // given up: no barrier is touched any more, and the losses of the rows that are left say so
-      if (lost && MODE != DIST_BACKWARD && rank == 0)
-        for (int r = row + lane * step; r < rows; r += 32 * step) p.loss[r] = NAN;
+      // given up: no barrier is touched any more, and the rows that are left say so, with the one before, whose named classes'
+      // gradient may be missing
+      if (lost)
+        for (int r = (it > 0 ? row - step : row) + lane * step; r < rows; r += 32 * step) {
+          if (MODE != DIST_BACKWARD && rank == 0) p.loss[r] = NAN;
+          if (MODE != DIST_LOSS && first < last) put(static_cast<T*>(p.dZ) + (int64_t)r * p.lddz + first, NAN);
+        }
     }
   }
   dep_trigger();
