@@ -6,7 +6,7 @@
 //
 //   loss = w [sum_k p_k (log p_k - log q_ik) + p_t (log p_t - log q_t)]
 //   dZ_j = w / tau (A q_j - p_j)            named classes,  A = sum p + p_t
-//        = w / tau (A q_j - p_t q_j / q_t)  the others
+//        = w / tau (A q_t - p_t) q_j / q_t  the others
 //
 // The mass of the others is summed by itself, never as 1 - sum of the named: a trained student leaves little there.
 //
@@ -108,26 +108,26 @@ __global__ void __launch_bounds__(512, 2) distill_kernel(const Distill p) {
       }
 #pragma unroll
       for (int k = 0; k < NV; ++k) {
-#pragma unroll
-        for (int v = 0; v < VEC; ++v) now.m = fmaxf(now.m, e[k][v]);
-      }
-#pragma unroll
-      for (int k = 0; k < NV; ++k) {
         const int c = base + (k * nt + tid) * VEC - first;
         uint32_t named = 0;
         if (c + first < last) {
           named = bits[c >> 5] >> (c & 31);
           if (VEC < 32) named &= (1u << VEC) - 1u;
         }
-#pragma unroll
-        for (int v = 0; v < VEC; ++v) {
-          e[k][v] = ex2((e[k][v] - now.m) * c2);
-          if (!named) now.l += e[k][v];
-        }
         if (named) {
 #pragma unroll
           for (int v = 0; v < VEC; ++v)
-            if (!((named >> v) & 1u)) now.l += e[k][v];
+            if ((named >> v) & 1u) e[k][v] = -INFINITY;
+        }
+#pragma unroll
+        for (int v = 0; v < VEC; ++v) now.m = fmaxf(now.m, e[k][v]);
+      }
+#pragma unroll
+      for (int k = 0; k < NV; ++k) {
+#pragma unroll
+        for (int v = 0; v < VEC; ++v) {
+          e[k][v] = ex2((e[k][v] - now.m) * c2);
+          now.l += e[k][v];
         }
       }
       sum = KEEP ? now : merge(sum, now, c2);
@@ -217,7 +217,7 @@ __global__ void __launch_bounds__(512, 2) distill_kernel(const Distill p) {
       if (tid == 0) {
         kl = 0.f;
         for (int k = 0; k < nw; ++k) kl += red_x[k];
-        if (pt > 0.f) kl += pt * log_rest(pt, qt, whole, Q);
+        if (pt > 0.f) kl += pt * log_rest(pt, others, all, c2, whole, Q);
         if (whole != whole) kl = whole;
         p.loss[row] = empty ? 0.f : wt * kl * kLn2;
         if (p.stat) {
@@ -230,10 +230,11 @@ __global__ void __launch_bounds__(512, 2) distill_kernel(const Distill p) {
   // ---- gradient ----
   if (MODE != DIST_LOSS) {
     const float ws = empty ? 0.f : wt * p.inv_tau;
-    // q_j (A - p_t / q_t) of the others; where there are none, nothing stands at that factor
-    const float other = pt > 0.f && qt != 0.f ? factor_rest(A, pt, qt, whole, Q) : A;
+    // (A q_t - p_t) q_j / q_t of the others: the first factor, and q_j / q_t relative to the others' largest or their normaliser
+    const float other = ws == 0.f ? 0.f : ws * excess_rest(A, pt, qt, whole, Q);
+    const float other_ref = MODE == DIST_BACKWARD ? p.stat_in[2 * row + 1] : others.m;
     if (KEEP && MODE == DIST_BOTH) {
-      const float f = empty ? 0.f : ws * other * ex2((sum.m - ref) * c2) * inv;
+      const float f = others.l == 0.f ? 0.f : other * ex2((sum.m - others.m) * c2) / others.l;
 #pragma unroll
       for (int k = 0; k < NV; ++k) {
         const int c = first + (k * nt + tid) * VEC;
@@ -242,7 +243,7 @@ __global__ void __launch_bounds__(512, 2) distill_kernel(const Distill p) {
         if (c < last) store<VEC>(dz + c, last - c, e[k]);
       }
     } else {
-      const float f = ws * other;
+      const float f = MODE == DIST_BACKWARD ? (other_ref == -INFINITY ? 0.f : other) : (others.l == 0.f ? 0.f : other / others.l);
       for (int base = first; base < last; base += nt * NV * VEC) {
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
@@ -253,7 +254,8 @@ __global__ void __launch_bounds__(512, 2) distill_kernel(const Distill p) {
         for (int k = 0; k < NV; ++k) {
           const int c = base + (k * nt + tid) * VEC;
 #pragma unroll
-          for (int v = 0; v < VEC; ++v) e[k][v] = empty ? 0.f : f * student(e[k][v]);
+          for (int v = 0; v < VEC; ++v)
+            e[k][v] = f == 0.f ? 0.f : f * ex2(MODE == DIST_BACKWARD ? fmaf(e[k][v], p.inv_tau, -other_ref) * kLog2e : (e[k][v] - other_ref) * c2);
           if (c < last) store<VEC>(dz + c, last - c, e[k]);
         }
       }

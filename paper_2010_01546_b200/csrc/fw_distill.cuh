@@ -33,10 +33,11 @@ struct Distill {
 
 // Largest logit m and the sum of exp((z - m) / tau).  Differences of logits are scaled, not logits: near the largest, where the
 // mass is, their rounding is small.  c2 = log2(e) / tau.
+// (The roundings are written out: the loss alone and the loss with the gradient are the same number.)
 struct MaxSum { float m, l; };
 __device__ __forceinline__ MaxSum merge(MaxSum a, MaxSum b, float c2) {
   const float m = fmaxf(a.m, b.m);
-  return {m, a.l * ex2((a.m - m) * c2) + b.l * ex2((b.m - m) * c2)};
+  return {m, fmaf(a.l, ex2((a.m - m) * c2), __fmul_rn(b.l, ex2((b.m - m) * c2)))};
 }
 __device__ __forceinline__ float lanes_max(float v) {
   float r;
@@ -80,13 +81,16 @@ __device__ __forceinline__ void merge_lanes3(MaxSum& a, MaxSum& b, MaxSum& c, fl
   }
 }
 
-// With P of the teacher's mass and Q of the student's on the named classes: log p_t - log q_t (base 2), and A - p_t / q_t, from the masses
+// With P of the teacher's mass and Q of the student's on the named classes: log p_t - log q_t (base 2), and A q_t - p_t, from the masses
 // that are small.  Where both lie almost wholly on the other classes the loss is what is left of two logarithms near 0.
-__device__ __forceinline__ float log_rest(float pt, float qt, float P, float Q) {
-  return P < 0.5f && Q < 0.5f ? (log1pf(-P) - log1pf(-Q)) * kLog2e : log2f(pt) - log2f(qt);
+// log q_t comes from logarithms, and the others' exponentials are relative to the largest of the others: a named class 90 tau ahead
+// takes their mass out of fp32, not the loss nor their gradient (A q_t - p_t times their shares of q_t).
+__device__ __forceinline__ float log_rest(float pt, MaxSum others, MaxSum all, float c2, float P, float Q) {
+  if (P < 0.5f && Q < 0.5f) return (log1pf(-P) - log1pf(-Q)) * kLog2e;
+  return log2f(pt) - fmaf(others.m - all.m, c2, log2f(others.l) - log2f(all.l));
 }
-__device__ __forceinline__ float factor_rest(float A, float pt, float qt, float P, float Q) {
-  return P < 0.5f && Q < 0.5f ? __fdividef(P - Q, qt) : A - __fdividef(pt, qt);
+__device__ __forceinline__ float excess_rest(float A, float pt, float qt, float P, float Q) {
+  return pt > 0.f ? (P < 0.5f && Q < 0.5f ? P - Q : fmaf(A, qt, -pt)) : A * qt;
 }
 
 // Launchers of a kernel for rows of one kind; *taken: the shape is one of its own

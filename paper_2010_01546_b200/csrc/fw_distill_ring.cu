@@ -48,7 +48,7 @@ __device__ __forceinline__ const void* word_of(const void* at) {
 
 struct RingNumbers { float w, t_lse, s0, s1; };
 // What the sums' warp says of a row: to the classes that are not named, for the gradient of those that are, and for the loss
-struct RingScale { float ref, factor, ws, A, inv, scale_p; };
+struct RingScale { float ref, other_ref, factor, ws, A, inv, scale_p; };
 // Of a row's entries: the teacher's exponentials and the named classes', each relative to its largest; with w the teacher's exponentials
 // and a their exponents (base 2), sum w a and sum w (z - named.m)
 struct RingEntries { MaxSum teacher, named; float wa, wz; };
@@ -170,21 +170,27 @@ __global__ void __launch_bounds__(kRingAll, 2) distill_ring_kernel(const Distill
         }
         if (MODE != DIST_BACKWARD) {
           float part[2] = {kLow, kLow};
-#pragma unroll
-          for (int k = 0; k < NV; ++k)
-#pragma unroll
-            for (int v = 0; v < VEC; v += 2) {
-              part[0] = fmaxf(part[0], e[k][v]);
-              part[1] = fmaxf(part[1], e[k][v + 1]);
-            }
-          top = fmaxf(part[0], part[1]);
-          part[0] = part[1] = 0.f;
-          const float less[2] = {-top, -top};
           // a byte (bf16) or half of one of the bit set to an access
           const uint32_t* set = bits + (it & 1) * words + tid * VEC / 32;
 #pragma unroll
           for (int k = 0; k < NV; ++k) {
             const uint32_t named = (set[k * kRingThreads * VEC / 32] >> (tid * VEC % 32)) & ((1u << VEC) - 1u);
+            if (named) {
+#pragma unroll
+              for (int v = 0; v < VEC; ++v)
+                if ((named >> v) & 1u) e[k][v] = -INFINITY;
+            }
+#pragma unroll
+            for (int v = 0; v < VEC; v += 2) {
+              part[0] = fmaxf(part[0], e[k][v]);
+              part[1] = fmaxf(part[1], e[k][v + 1]);
+            }
+          }
+          top = fmaxf(part[0], part[1]);
+          part[0] = part[1] = 0.f;
+          const float less[2] = {-top, -top};
+#pragma unroll
+          for (int k = 0; k < NV; ++k) {
 #pragma unroll
             for (int v = 0; v < VEC; v += 2) {
               float two[2] = {e[k][v], e[k][v + 1]};
@@ -192,17 +198,8 @@ __global__ void __launch_bounds__(kRingAll, 2) distill_ring_kernel(const Distill
               vscale<2>(two, c2);
               e[k][v] = ex2(two[0]);
               e[k][v + 1] = ex2(two[1]);
-            }
-            if (!named) {
-#pragma unroll
-              for (int v = 0; v < VEC; v += 2) {
-                const float two[2] = {e[k][v], e[k][v + 1]};
-                vadd<2>(part, two);
-              }
-            } else {
-#pragma unroll
-              for (int v = 0; v < VEC; ++v)
-                if (!((named >> v) & 1u)) part[v & 1] += e[k][v];
+              const float ex[2] = {e[k][v], e[k][v + 1]};
+              vadd<2>(part, ex);
             }
           }
           const MaxSum s = merge_lanes({top, part[0] + part[1]}, c2);
@@ -212,13 +209,13 @@ __global__ void __launch_bounds__(kRingAll, 2) distill_ring_kernel(const Distill
         if (MODE != DIST_LOSS) {
           if (!wait(bar_scale, it)) break;
           const RingScale& sc = s_scale[it & 1];
-          const float f = MODE == DIST_BACKWARD || sc.factor == 0.f ? sc.factor : sc.factor * ex2((top - sc.ref) * c2);
+          const float f = MODE == DIST_BACKWARD || sc.factor == 0.f ? sc.factor : sc.factor * ex2((top - sc.other_ref) * c2);
 #pragma unroll
           for (int k = 0; k < NV; ++k) {
             if (!begun(k)) continue;
             if (MODE == DIST_BACKWARD) {
 #pragma unroll
-              for (int v = 0; v < VEC; ++v) e[k][v] = f == 0.f ? 0.f : f * ex2(fmaf(e[k][v], p.inv_tau, -sc.ref) * kLog2e);
+              for (int v = 0; v < VEC; ++v) e[k][v] = f == 0.f ? 0.f : f * ex2(fmaf(e[k][v], p.inv_tau, -sc.other_ref) * kLog2e);
             } else {
               vscale<VEC>(e[k], f);
             }
@@ -478,17 +475,19 @@ __global__ void __launch_bounds__(kRingAll, 2) distill_ring_kernel(const Distill
             qt = ex2((s_num[slot_of(it)].s1 - ref) * kLog2e);
           }
           const float ws = empty ? 0.f : w * p.inv_tau;
-          // q_j (A - p_t / q_t) of the others; where there are none, nothing stands at that factor
-          const float other = pt > 0.f && qt != 0.f ? factor_rest(A, pt, qt, whole, Q) : A;
+          // (A q_t - p_t) q_j / q_t of the others: the first factor, and q_j / q_t relative to the others' largest or their normaliser
+          const float other = ws == 0.f ? 0.f : ws * excess_rest(A, pt, qt, whole, Q);
+          const float other_ref = MODE == DIST_BACKWARD ? s_num[slot_of(it)].s1 : others.m;
+          const bool none = MODE == DIST_BACKWARD ? other_ref == -INFINITY : others.l == 0.f;
           if (lane == 0) {
-            s_scale[it & 1] = {ref, ws == 0.f ? 0.f : ws * other * inv, ws, A, inv, scale_p};
+            s_scale[it & 1] = {ref, other_ref, none ? 0.f : MODE == DIST_BACKWARD ? other : __fdividef(other, others.l), ws, A, inv, scale_p};
             sm100::mbar_arrive(bar(bar_scale[it & 1]));
             if (MODE != DIST_BACKWARD && rank == 0) {
               // sum p (log p - log q), p = w scale_p: from the entries' sums, relative to the named classes' largest logit
               float kl = 0.f;
               if (ts != 0.f)
                 kl = scale_p * (en.wa + ts * log2f(scale_p) - (c2 * fmaf(n.m - all.m, ts, en.wz) - ts * log2f(all.l)));
-              if (pt > 0.f) kl += pt * log_rest(pt, qt, whole, Q);
+              if (pt > 0.f) kl += pt * log_rest(pt, others, all, c2, whole, Q);
               if (whole != whole) kl = whole;
               p.loss[row] = empty ? 0.f : w * kl * kLn2;
               if (p.stat) {

@@ -84,18 +84,22 @@ __global__ void __launch_bounds__(32 * kWarpRows) distill_warp_kernel(const Dist
   if (MODE != DIST_BACKWARD) {
     named.m = lanes_max(named.m);
 #pragma unroll
-    for (int k = 0; k < NV; ++k)
-#pragma unroll
-      for (int v = 0; v < VEC; ++v) sum.m = fmaxf(sum.m, e[k][v]);
-    sum.m = lanes_max(sum.m);                 // the row's largest: one reference for all lanes
-#pragma unroll
     for (int k = 0; k < NV; ++k) {
       const int c = (k * 32 + lane) * VEC;
       const uint32_t is = c < p.V ? (bits[c >> 5] >> (c & 31)) & (VEC < 32 ? (1u << VEC) - 1u : ~0u) : 0u;
 #pragma unroll
       for (int v = 0; v < VEC; ++v) {
+        if ((is >> v) & 1u) e[k][v] = -INFINITY;
+        sum.m = fmaxf(sum.m, e[k][v]);
+      }
+    }
+    sum.m = lanes_max(sum.m);                 // the others' largest: one reference for all lanes
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+#pragma unroll
+      for (int v = 0; v < VEC; ++v) {
         e[k][v] = ex2((e[k][v] - sum.m) * c2);
-        if (!((is >> v) & 1u)) sum.l += e[k][v];
+        sum.l += e[k][v];
       }
     }
   }
@@ -149,7 +153,7 @@ __global__ void __launch_bounds__(32 * kWarpRows) distill_warp_kernel(const Dist
     }
     kl = lanes_sum(kl);
     if (lane == 0) {
-      if (pt > 0.f) kl += pt * log_rest(pt, qt, whole, Q);
+      if (pt > 0.f) kl += pt * log_rest(pt, others, all, c2, whole, Q);
       if (whole != whole) kl = whole;
       p.loss[row] = empty ? 0.f : wt * kl * kLn2;
       if (p.stat) {
@@ -160,14 +164,15 @@ __global__ void __launch_bounds__(32 * kWarpRows) distill_warp_kernel(const Dist
   }
   if (MODE != DIST_LOSS) {
     const float ws = empty ? 0.f : wt * p.inv_tau;
-    const float other = pt > 0.f && qt != 0.f ? factor_rest(A, pt, qt, whole, Q) : A;
-    const float f = ws == 0.f ? 0.f : MODE == DIST_BACKWARD ? ws * other : ws * other * ex2((sum.m - ref) * c2) * inv;
+    const float other = ws == 0.f ? 0.f : ws * excess_rest(A, pt, qt, whole, Q);
+    const float other_ref = MODE == DIST_BACKWARD ? p.stat_in[2 * (int64_t)row + 1] : others.m;
+    const float f = MODE == DIST_BACKWARD ? (other_ref == -INFINITY ? 0.f : other) : (others.l == 0.f ? 0.f : other / others.l);
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
       const int c = (k * 32 + lane) * VEC;
       if (c >= p.V) continue;
 #pragma unroll
-      for (int v = 0; v < VEC; ++v) e[k][v] = MODE != DIST_BACKWARD ? e[k][v] * f : ws == 0.f ? 0.f : f * student(e[k][v]);
+      for (int v = 0; v < VEC; ++v) e[k][v] = MODE != DIST_BACKWARD ? e[k][v] * f : f == 0.f ? 0.f : f * ex2(fmaf(e[k][v], p.inv_tau, -other_ref) * kLog2e);
       store<VEC>(dz + c, p.V - c, e[k]);
     }
     __syncwarp();                             // the named classes are written over

@@ -300,3 +300,52 @@ def test_repeated_other_stream_and_graph(B):
     assert not torch.equal(got[0], first[0])
     call(0)
     assert all(torch.equal(a, b) for a, b in zip(got, (loss, stat, dz, dz2)))
+
+
+@pytest.mark.parametrize("rows,V,K", [(5, 300, 4), (4, 2048, 100), (3, 9000, 64), (3, 50021, 33), (2, 131072, 64), (3, 3000, 300), (1, 300001, 7)])
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("gap,tau", [(60.0, 1.0), (150.0, 1.0), (900.0, 1.0), (30.0, 0.0625)])
+def test_one_named_class_far_ahead(B, rows, V, K, kind, gap, tau):
+    """A student sure of a class that the teacher names: the others' mass q_t is beyond fp32, their loss and gradient are not.
+
+    In 64 bits with logarithms, so that no gap is too wide.  Bounds beyond those of the file's head, relative to an element:
+    the forward call's share of the others E (1 + a / 8), a its distance from their largest; the backward call's E and, for an
+    exponential of z / tau - stat in fp32, 2 u |stat| (stat's roundings), 2 u |z / tau| and 4 u of the difference.  q_t itself
+    is below e^-40 of p_t here."""
+    u, E, half = 2.0 ** -24, 2.0 ** -17 if V <= 131072 else 2.0 ** -15, HALF[KINDS[kind]]
+    z, T, I, t_lse = inputs(rows, V, K, kind, V + K, tau=tau, pad=None)
+    z.scatter_add_(1, I[:, :1].long(), torch.full((rows, 1), gap, device="cuda").to(z.dtype))
+    tl = t_lse + 0.05
+    weight = torch.rand(rows, generator=gen(V), device="cuda") + 0.5
+    d = desc(B, V, K, kind, tau=tau)
+    loss, stat = torch.empty(rows, device="cuda"), torch.empty(rows, 2, device="cuda")
+    fwd, bwd = matrix(rows, V, KINDS[kind]), matrix(rows, V, KINDS[kind])
+    B.fw_distill_forward(d, z, T, I, loss, stat=stat, t_lse=tl, weight=weight, dZ=fwd)
+    B.fw_distill_backward(d, z, T, I, stat, bwd, t_lse=tl, weight=weight)
+
+    at, w = I.long(), weight.to(F64)[:, None]
+    zz, t, tl = z.to(F64) / tau, T.to(F64) / tau, tl.to(F64)[:, None]
+    lse = torch.logsumexp(zz, 1, keepdim=True)
+    rest = torch.logsumexp(zz.scatter(1, at, float("-inf")), 1, keepdim=True)
+    logp, logq, log_qt = t - tl, zz.gather(1, at) - lse, rest - lse
+    assert float(log_qt.max()) < -40
+    p = logp.exp()
+    pt = 1 - p.sum(1, keepdim=True)
+    dp = p * (E + 8 * u * (t.abs() + tl.abs()))
+    dpt = dp.sum(1, keepdim=True) + 4 * u
+    mag, lt = logp.abs() + logq.abs(), pt.log().abs() + log_qt.abs()
+    want = w * ((p * (logp - logq)).sum(1, keepdim=True) + pt * (pt.log() - log_qt))
+    bound = w * ((dp * (1 + mag) + p * (E + 4 * u * (2 + mag))).sum(1, keepdim=True) + dpt * (lt + 1) + pt * (E + 4 * u) * (2 + lt))
+    check(loss, want[:, 0], bound[:, 0])
+    check_stat(stat, torch.cat((lse, rest), 1))
+
+    share = (zz - rest).exp()
+    others = w / tau * (log_qt.exp() - pt) * share
+    named = w / tau * (logq.exp() - p)
+    far = zz.scatter(1, at, float("-inf")).amax(1, keepdim=True) - zz
+    of_stat = lambda v, s: E + 2 ** -21 + u * (2 * s.abs() + 2 * v.abs() + 4 * (v - s).abs())  # noqa: E731
+    for got, rel, rel_named in ((fwd, E * (1 + far / 8), E * (1 + (zz.amax(1, keepdim=True) - zz.gather(1, at)) / 8)),
+                                (bwd, of_stat(zz, rest), of_stat(zz.gather(1, at), lse))):
+        dz = others.scatter(1, at, named)
+        allowed = (others.abs() * (rel + dpt / pt)).scatter(1, at, w / tau * (logq.exp() * rel_named + dp))
+        check(got, dz, allowed, half)
