@@ -141,11 +141,11 @@ __global__ void __launch_bounds__(GS_THREADS, KIND <= GS_FWD_E4M3 && F == 32 ? 4
     tma_prefetch_desc(&g.b[0]);
     if (FWD) tma_prefetch_desc(&g.b[1]);
   }
-  if (warp == 1) {
+  dep_sync();
+  if (warp == 1) {                                 // after the wait: a grid before this one may still need columns (see dep_sync)
     tmem_alloc(smem_u32(&tmem_base_sh), NT < 32 ? 32 : NT);
     tmem_relinquish();
   }
-  dep_sync();
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
