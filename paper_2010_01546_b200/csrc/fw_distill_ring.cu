@@ -229,6 +229,7 @@ __global__ void __launch_bounds__(kRingAll, 2) distill_ring_kernel(const Distill
           if (begun(k)) store<VEC>(dz + (uint32_t)((k * kRingThreads + tid) * VEC), FILL == ROW_PART ? mine - k * kRingThreads * VEC : VEC, zero);
       }
       if (!wait(bar_scale, it)) break;
+      __syncwarp();                               // lane 0 speaks for the stores of all lanes
       if (lane == 0) sm100::mbar_arrive(bar(bar_done[it & 1]));
       live0 = live1;
       live1 = live2;

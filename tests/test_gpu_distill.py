@@ -349,3 +349,25 @@ def test_one_named_class_far_ahead(B, rows, V, K, kind, gap, tau):
         dz = others.scatter(1, at, named)
         allowed = (others.abs() * (rel + dpt / pt)).scatter(1, at, w / tau * (logq.exp() * rel_named + dp))
         check(got, dz, allowed, half)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [9000, 50021, 131072])
+def test_named_classes_over_their_neighbours(B, V, kind):
+    """256 named classes a row, spread over every warp's stores: each holds its own gradient, forward and backward, row after row."""
+    rows, K = 300, 256
+    g = gen(V)
+    z = put(torch.randn(rows, V, generator=g, device="cuda") * 2, KINDS[kind], pad=None)
+    I = torch.stack([torch.randperm(V, generator=g, device="cuda")[:K] for _ in range(rows)]).to(torch.int32)
+    T = torch.randn(rows, K, generator=g, device="cuda")
+    d = desc(B, V, K, kind)
+    loss, stat = torch.empty(rows, device="cuda"), torch.empty(rows, 2, device="cuda")
+    for _ in range(3):
+        dz, dz2 = matrix(rows, V, KINDS[kind], pad=None), matrix(rows, V, KINDS[kind], pad=None)
+        B.fw_distill_forward(d, z, T, I, loss, stat=stat, dZ=dz)
+        B.fw_distill_backward(d, z, T, I, stat, dz2)
+        for r0 in range(0, rows, 50):
+            r = slice(r0, r0 + 50)
+            want = reference(z[r], T[r], I[r], 1.0)
+            check(dz[r], want[2], want[4], HALF[KINDS[kind]])
+            check(dz2[r], want[2], stat_bound(want), HALF[KINDS[kind]])

@@ -29,3 +29,15 @@ def test_tensor_memory_is_taken_after_the_wait(name, body):
 
 def test_every_kernel_with_tensor_memory_was_looked_at():
     assert sum("tmem_alloc" in body for _, body in kernels()) == 6
+
+
+@pytest.mark.parametrize("bar", ["bar_done", "bar_clear", "bar_bits"])
+def test_one_lane_speaks_for_its_warp_after_a_warp_barrier(bar):
+    """Long rows of the distillation loss: lane 0 arrives for what all lanes of its warp have stored or cleared.  Its release covers
+    the others' accesses through a __syncwarp (a vote or shuffle orders no memory), else the named classes' gradient, which
+    another warp writes over these stores, may come first."""
+    with open(os.path.join(CSRC, "fw_distill_ring.cu")) as f:
+        text = re.sub(r"//[^\n]*", "", f.read())
+    arrivals = re.findall(rf"([^;{{}}]*;)\s*if \(lane == 0\) sm100::mbar_arrive\(bar\({bar}\[", text)
+    assert len(arrivals) == text.count(f"mbar_arrive(bar({bar}[") == 1
+    assert arrivals[0].strip() == "__syncwarp();"
