@@ -344,6 +344,7 @@ __global__ void __launch_bounds__(kRingAll, 2) distill_ring_kernel(const Distill
           for (int k = lane; k < p.K; k += 32)
             if (c[k] >= 0) s_seen[(c[k] & (kSeenBits - 1)) >> 5] = 0;
           if (__any_sync(0xffffffffu, seen)) {
+            bool out = false;
             for (int g = 0; g < p.K; g += 32) {
               // a lane compares with the entries before its own, four at a time (a repeated class's first is not taken out)
               const int k = g + lane, i = k < p.K ? c[k] : -1;
@@ -362,7 +363,16 @@ __global__ void __launch_bounds__(kRingAll, 2) distill_ring_kernel(const Distill
                 }
               }
               __syncwarp();
-              if (i >= 0 && twice) c[k] = -2;
+              if (i >= 0 && twice) {
+                c[k] = -2;
+                out = true;
+              }
+            }
+            // the teacher's largest of what counts: an ignored logit far ahead would leave no exponential of the others
+            if (__any_sync(0xffffffffu, out)) {
+              t.m = kLow;
+              for (int k = lane; k < p.K; k += 32)
+                if (c[k] >= 0) t.m = fmaxf(t.m, t_of(it, row, k));
             }
           }
           t.m = p.t_lse ? kLow : lanes_max(t.m);

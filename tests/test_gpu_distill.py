@@ -371,3 +371,32 @@ def test_named_classes_over_their_neighbours(B, V, kind):
             want = reference(z[r], T[r], I[r], 1.0)
             check(dz[r], want[2], want[4], HALF[KINDS[kind]])
             check(dz2[r], want[2], stat_bound(want), HALF[KINDS[kind]])
+
+
+@pytest.mark.parametrize("rows,V,K,shift", [(5, 1000, 20, 0), (7, 5000, 20, 0), (6, 131072, 256, 0), (4, 5000, 300, 0), (3, 5000, 20, 1)])
+@pytest.mark.parametrize("ignored", [8.0, 200.0, float("inf"), float("nan")])
+@pytest.mark.parametrize("tau", [1.0, 0.0625])
+def test_the_ignored_logit_of_a_repeated_class(B, rows, V, K, shift, ignored, tau):
+    """A class named twice counts with its first logit, however large the second one is: the rest of the row is relative to the
+    largest logit that counts."""
+    z, T, I, t_lse = inputs(rows, V, K, "f32", V + K, tau=tau, pad=shift or None, shift=shift)
+    z.mul_(tau)                                             # a student as flat as the teacher is at tau
+    T.mul_(tau)
+    I[:, K - 1] = I[:, 0]
+    I[1:, K // 2] = I[1:, 3]
+    T[:, K - 1] = T[:, 0] + ignored
+    T[1:, K // 2] = T[1:, 3] + 2 * ignored
+    T, I = T.contiguous(), I.contiguous()
+    d = desc(B, V, K, "f32", tau=tau)
+    loss, stat = torch.empty(rows, device="cuda"), torch.empty(rows, 2, device="cuda")
+    dz, dz2 = (matrix(rows, V, torch.float32, pad=shift or None, shift=shift) for _ in range(2))
+    B.fw_distill_forward(d, z, T, I, loss, stat=stat, dZ=dz)
+    B.fw_distill_backward(d, z, T, I, stat, dz2)
+    counted = T.clone()
+    counted[:, K - 1] = 0                                   # what the definition leaves out anyway
+    counted[1:, K // 2] = 0
+    want = reference(z, counted, I, tau)
+    assert float(want[0].min()) > 0
+    check(loss, want[0], want[3])
+    check(dz, want[2], want[4], HALF[torch.float32])
+    check(dz2, want[2], stat_bound(want), HALF[torch.float32])
