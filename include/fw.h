@@ -416,7 +416,8 @@ fw_status fw_gated_sync_status(fw_gated* g);
  * forward call left out has no stat to be read).
  * Logits of -inf have no mass (a mask): gradient 0, infinite loss where p_k > 0.  A row in which no
  * class has mass gives loss and gradient 0, and so does a row whose entries are all absent (t_lse
- * NULL).  A NaN in a row, or +inf, makes that row's loss and gradient NaN.
+ * NULL).  The lowest finite value is a logit like any other: a row of it alone is flat.  A NaN in a
+ * row, or +inf, makes that row's loss and gradient NaN.
  * Nothing keeps a status: where a bounded device-side wait gave up, rows that may not
  * be finished have NaN in their loss and among the elements of their gradient.
  * 1 <= K <= 1024, K <= V <= 2^20, rows < 2^28. */

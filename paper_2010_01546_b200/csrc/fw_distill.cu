@@ -208,7 +208,7 @@ __global__ void __launch_bounds__(512, 2) distill_kernel(const Distill p) {
       for (int k = tid; k < p.K; k += nt) {
         if (cls[k] < 0) continue;
         const float lp = teacher2(tv[k]), pk = ex2(lp) * scale_p;
-        if (pk > 0.f || pk != pk) kl += pk * ((lp + log2f(scale_p)) - ((zv[k] - all.m) * c2 - log2f(all.l)));
+        if (pk > 0.f || pk != pk) kl += pk * (kDown * (lp + log2f(scale_p)) - fmaf(zv[k] - all.m, c2 * kDown, -kDown * log2f(all.l)));
       }
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) kl += __shfl_xor_sync(0xffffffffu, kl, o);
@@ -219,7 +219,7 @@ __global__ void __launch_bounds__(512, 2) distill_kernel(const Distill p) {
         for (int k = 0; k < nw; ++k) kl += red_x[k];
         if (pt > 0.f) kl += pt * log_rest(pt, others, all, c2, whole, Q);
         if (whole != whole) kl = whole;
-        p.loss[row] = empty ? 0.f : wt * kl * kLn2;
+        p.loss[row] = empty ? 0.f : wt * kl * kUp;
         if (p.stat) {
           p.stat[2 * row] = empty ? -INFINITY : fmaf(all.m, p.inv_tau, logf(all.l));
           p.stat[2 * row + 1] = others.l == 0.f ? -INFINITY : fmaf(others.m, p.inv_tau, logf(others.l));

@@ -13,7 +13,10 @@ using namespace rows;
 constexpr int kMaxK = 1024;
 constexpr int kMaxV = 1 << 20;             // a cluster's bit sets and entries stay below 48 KB of shared memory a CTA
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-constexpr float kLow = -3.0e38f;           // below every finite logit that matters: the largest of nothing
+constexpr float kLow = -3.402823466e38f;   // the lowest finite value: the largest of nothing, beside a sum of 0
+// Logarithms are summed times 2^-21 (exact), so that a logit at the lowest finite value (a mask) times log2(e) / tau stays in
+// fp32 for every tau; kUp = 2^21 ln 2 makes the loss of them.
+constexpr float kDown = 4.76837158203125e-07f, kUp = 2097152.f * kLn2;
 enum { DIST_LOSS = 0, DIST_BOTH = 1, DIST_BACKWARD = 2 };
 
 struct Distill {
@@ -81,13 +84,13 @@ __device__ __forceinline__ void merge_lanes3(MaxSum& a, MaxSum& b, MaxSum& c, fl
   }
 }
 
-// With P of the teacher's mass and Q of the student's on the named classes: log p_t - log q_t (base 2), and A q_t - p_t, from the masses
+// With P of the teacher's mass and Q of the student's on the named classes: log p_t - log q_t (base 2, times kDown), and A q_t - p_t, from the masses
 // that are small.  Where both lie almost wholly on the other classes the loss is what is left of two logarithms near 0.
 // log q_t comes from logarithms, and the others' exponentials are relative to the largest of the others: a named class 90 tau ahead
 // takes their mass out of fp32, not the loss nor their gradient (A q_t - p_t times their shares of q_t).
 __device__ __forceinline__ float log_rest(float pt, MaxSum others, MaxSum all, float c2, float P, float Q) {
-  if (P < 0.5f && Q < 0.5f) return (log1pf(-P) - log1pf(-Q)) * kLog2e;
-  return log2f(pt) - fmaf(others.m - all.m, c2, log2f(others.l) - log2f(all.l));
+  if (P < 0.5f && Q < 0.5f) return (log1pf(-P) - log1pf(-Q)) * (kLog2e * kDown);
+  return kDown * log2f(pt) - fmaf(others.m - all.m, c2 * kDown, kDown * (log2f(others.l) - log2f(all.l)));
 }
 __device__ __forceinline__ float excess_rest(float A, float pt, float qt, float P, float Q) {
   return pt > 0.f ? (P < 0.5f && Q < 0.5f ? P - Q : fmaf(A, qt, -pt)) : A * qt;

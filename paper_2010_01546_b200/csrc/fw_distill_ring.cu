@@ -50,7 +50,7 @@ struct RingNumbers { float w, t_lse, s0, s1; };
 // What the sums' warp says of a row: to the classes that are not named, for the gradient of those that are, and for the loss
 struct RingScale { float ref, other_ref, factor, ws, A, inv, scale_p; };
 // Of a row's entries: the teacher's exponentials and the named classes', each relative to its largest; with w the teacher's exponentials
-// and a their exponents (base 2), sum w a and sum w (z - named.m)
+// and a their exponents (base 2), sum w a and sum w (z - named.m) kDown
 struct RingEntries { MaxSum teacher, named; float wa, wz; };
 
 // FILL: the last CTA's slice ends inside an access of 16 bytes, with one, or all slices fill all accesses of their threads.
@@ -388,8 +388,8 @@ __global__ void __launch_bounds__(kRingAll, 2) distill_ring_kernel(const Distill
             if (MODE != DIST_BACKWARD) {
               const float d0 = z0 - n.m, d1 = z1 - n.m;
               n.l += (i0 >= 0 ? ex2(d0 * c2) : 0.f) + (i1 >= 0 ? ex2(d1 * c2) : 0.f);
-              if (w0 > 0.f) { wa = fmaf(w0, a0, wa); wz = fmaf(w0, d0, wz); }
-              if (w1 > 0.f) { wa = fmaf(w1, a1, wa); wz = fmaf(w1, d1, wz); }
+              if (w0 > 0.f) { wa = fmaf(w0, a0, wa); wz = fmaf(w0 * kDown, d0, wz); }
+              if (w1 > 0.f) { wa = fmaf(w1, a1, wa); wz = fmaf(w1 * kDown, d1, wz); }
             }
             // the loss and the gradient take them from here
             if (i0 >= 0) { values[k0] = __float_as_uint(a0); values[kp + k0] = __float_as_uint(z0); }
@@ -497,10 +497,10 @@ __global__ void __launch_bounds__(kRingAll, 2) distill_ring_kernel(const Distill
               // sum p (log p - log q), p = w scale_p: from the entries' sums, relative to the named classes' largest logit
               float kl = 0.f;
               if (ts != 0.f)
-                kl = scale_p * (en.wa + ts * log2f(scale_p) - (c2 * fmaf(n.m - all.m, ts, en.wz) - ts * log2f(all.l)));
+                kl = scale_p * (kDown * fmaf(ts, log2f(scale_p), en.wa) - fmaf(c2, fmaf((n.m - all.m) * kDown, ts, en.wz), -kDown * (ts * log2f(all.l))));
               if (pt > 0.f) kl += pt * log_rest(pt, others, all, c2, whole, Q);
               if (whole != whole) kl = whole;
-              p.loss[row] = empty ? 0.f : w * kl * kLn2;
+              p.loss[row] = empty ? 0.f : w * kl * kUp;
               if (p.stat) {
                 p.stat[2 * (int64_t)row] = empty ? -INFINITY : fmaf(all.m, p.inv_tau, logf(all.l));
                 p.stat[2 * (int64_t)row + 1] = others.l == 0.f ? -INFINITY : fmaf(others.m, p.inv_tau, logf(others.l));

@@ -149,13 +149,13 @@ __global__ void __launch_bounds__(32 * kWarpRows) distill_warp_kernel(const Dist
     for (int j = 0; j < EPL; ++j) {
       if (cls[j] < 0) continue;
       const float lp = teacher2(tv[j]), pk = ex2(lp) * scale_p;
-      if (pk > 0.f || pk != pk) kl += pk * ((lp + log_p) - ((zv[j] - all.m) * c2 - log_all));
+      if (pk > 0.f || pk != pk) kl += pk * (kDown * (lp + log_p) - fmaf(zv[j] - all.m, c2 * kDown, -kDown * log_all));
     }
     kl = lanes_sum(kl);
     if (lane == 0) {
       if (pt > 0.f) kl += pt * log_rest(pt, others, all, c2, whole, Q);
       if (whole != whole) kl = whole;
-      p.loss[row] = empty ? 0.f : wt * kl * kLn2;
+      p.loss[row] = empty ? 0.f : wt * kl * kUp;
       if (p.stat) {
         p.stat[2 * (int64_t)row] = empty ? -INFINITY : fmaf(all.m, p.inv_tau, logf(all.l));
         p.stat[2 * (int64_t)row + 1] = others.l == 0.f ? -INFINITY : fmaf(others.m, p.inv_tau, logf(others.l));

@@ -400,3 +400,95 @@ def test_the_ignored_logit_of_a_repeated_class(B, rows, V, K, shift, ignored, ta
     check(loss, want[0], want[3])
     check(dz, want[2], want[4], HALF[torch.float32])
     check(dz2, want[2], stat_bound(want), HALF[torch.float32])
+
+
+def by_logs(z, T, I, tau, t_lse=None, weight=None):
+    """loss and dZ in 64 bits with their bounds, every logarithm relative to the largest logit that it is about: for logits so far
+    apart, or so far from 0, that 64 bits do not hold them beside each other.  Entries are present and not repeated; some class
+    is not named, and some logit of a row is finite."""
+    rows, V = z.shape
+    u, E = 2.0 ** -24, 2.0 ** -17 if V <= 131072 else 2.0 ** -15
+    zz, t, at = z.to(F64) / tau, T.to(F64) / tau, I.long()
+    w = torch.ones(rows, 1, dtype=F64, device="cuda") if weight is None else weight.to(F64)[:, None]
+    m = zz.amax(1, keepdim=True)
+    lse = (zz - m).exp().sum(1, keepdim=True).log()                      # relative to m
+    hidden = zz.scatter(1, at, float("-inf"))
+    om = hidden.amax(1, keepdim=True)
+    om = torch.where(om == float("-inf"), m, om)                         # nobody there: no share, whatever it is relative to
+    share = (hidden - om).exp()
+    mass = share.sum(1, keepdim=True)
+    log_qt = om - m + mass.log() - lse
+    share = torch.where(mass > 0, share / mass, 0)
+    logq = zz.gather(1, at) - m - lse
+    if t_lse is None:
+        logp, pt = torch.log_softmax(t, 1), torch.zeros(rows, 1, dtype=F64, device="cuda")
+        dp = logp.exp() * E + 4 * u
+        dpt = 0 * pt
+    else:
+        tl = t_lse.to(F64)[:, None]
+        logp = t - tl
+        pt = (1 - logp.exp().sum(1, keepdim=True)).clamp(min=0)
+        dp = logp.exp() * (E + 8 * u * (t.abs() + tl.abs())) + 4 * u
+        dpt = dp.sum(1, keepdim=True) + 4 * u
+    p = logp.exp()
+    mag, lt = logp.abs() + logq.abs(), torch.where(pt > 0, pt.log().abs() + log_qt.abs(), 0)
+    loss = w * ((p * (logp - logq)).sum(1, keepdim=True) + torch.where(pt > 0, pt * (pt.log() - log_qt), 0))
+    dloss = w * ((dp * (1 + mag) + p * (E + 4 * u * (2 + mag))).sum(1, keepdim=True) + dpt * (lt + 1) + pt * (E + 4 * u) * (2 + lt))
+    A = p.sum(1, keepdim=True) + pt
+    excess = A * log_qt.exp() - pt
+    dexcess = A * log_qt.exp() * E * (1 + log_qt.abs().clamp(max=1e4) / 8) + dpt
+    far = (om - zz).abs().clamp(max=1e4)
+    dz = (w / tau * excess * share).scatter(1, at, w / tau * (A * logq.exp() - p))
+    ddz = (w / tau * (dexcess + excess.abs() * E * (1 + far / 8)) * share).scatter(
+        1, at, w / tau * (A * logq.exp() * E * (1 + logq.abs().clamp(max=1e4) / 8) + dpt * logq.exp() + dp))
+    return loss[:, 0], dz, dloss[:, 0], ddz
+
+
+# rows of each kernel: of a warp, of one CTA and of a cluster that stay, of a CTA for itself (many entries; not aligned), read twice
+EACH_KERNEL = [(5, 1000, 20, 0), (7, 5000, 20, 0), (3, 131072, 64, 0), (4, 5000, 300, 0), (3, 5000, 20, 1), (3, 700, 20, 1), (2, 150001, 20, 1)]
+
+
+@pytest.mark.parametrize("rows,V,K,shift", EACH_KERNEL)
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("where", ["row", "most", "named", "one named", "others"])
+@pytest.mark.parametrize("rest,tau", [(False, 1.0), (True, 1.0), (True, 4.0)])
+def test_lowest_finite_value(B, rows, V, K, shift, kind, where, rest, tau):
+    """torch.finfo.min as a mask is a logit like any other: a row of it alone is a flat one, beside others it has no mass, and
+    where the teacher has some the loss is as large as the formula makes it."""
+    z, T, I, t_lse = inputs(rows, V, K, kind, V + K, tau=tau, pad=shift or None, shift=shift)
+    low, at = torch.finfo(KINDS[kind]).min, I.long()
+    if where == "row":
+        z[:] = low
+    elif where == "most":
+        z[:, torch.arange(V, device="cuda") % 7 != 3] = low
+        z[:, at[0, 0]] = 1.0                                # some class has mass whatever V is
+    elif where == "named":
+        z.scatter_(1, at, low)
+    elif where == "one named":
+        z.scatter_(1, at[:, 1:2], low)
+    else:
+        keep = z.gather(1, at)
+        z[:] = low
+        z.scatter_(1, at, keep)
+    tl = t_lse + 0.05 if rest else None
+    weight = torch.rand(rows, generator=gen(V), device="cuda") * 0.5 + 0.25
+    d = desc(B, V, K, kind, tau=tau)
+    loss, loss2, dz = torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda"), matrix(rows, V, KINDS[kind], pad=shift or None, shift=shift)
+    B.fw_distill_forward(d, z, T, I, loss, t_lse=tl, weight=weight, dZ=dz)
+    B.fw_distill_forward(d, z, T, I, loss2, t_lse=tl, weight=weight)
+    want = by_logs(z, T, I, tau, tl, weight)
+    check(loss, want[0], want[2])
+    assert torch.equal(loss, loss2)
+    check(dz, want[1], want[3], HALF[KINDS[kind]])
+
+
+@pytest.mark.parametrize("rows,V,K,shift", EACH_KERNEL)
+def test_lowest_finite_value_of_the_teacher(B, rows, V, K, shift):
+    """A teacher whose named logits are all the lowest finite value is flat over them."""
+    z, T, I, _ = inputs(rows, V, K, "f32", V, pad=shift or None, shift=shift)
+    T[:] = torch.finfo(torch.float32).min
+    loss, dz = torch.empty(rows, device="cuda"), matrix(rows, V, torch.float32, pad=shift or None, shift=shift)
+    B.fw_distill_forward(desc(B, V, K, "f32"), z, T, I, loss, dZ=dz)
+    want = by_logs(z, torch.zeros_like(T), I, 1.0)
+    check(loss, want[0], want[2])
+    check(dz, want[1], want[3], HALF[torch.float32])
