@@ -413,7 +413,8 @@ fw_status fw_gated_sync_status(fw_gated* g);
  *           named (-inf for none); NULL in the forward call: not kept
  * forward: dZ NULL gives the loss alone; with dZ the gradient too, from the same pass over Z.
  * backward: the gradient from the forward call's stat (weight may be another, but a row that the
- * forward call left out has no stat to be read).
+ * forward call left out has no stat to be read).  fp32 holds a stat beyond 1024 too coarsely for exponentials, and of
+ * one at -3e38 nothing: such a row's sums are formed again from Z, without speed.
  * Logits of -inf have no mass (a mask): gradient 0, infinite loss where p_k > 0.  A row in which no
  * class has mass gives loss and gradient 0, and so does a row whose entries are all absent (t_lse
  * NULL).  The lowest finite value is a logit like any other: a row of it alone is flat.  A NaN in a

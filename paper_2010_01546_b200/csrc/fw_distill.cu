@@ -51,6 +51,8 @@ __global__ void __launch_bounds__(512, 2) distill_kernel(const Distill p) {
   const float wt = p.weight ? p.weight[row] : 1.f;
   const T* z = static_cast<const T*>(p.Z) + row * p.ldz;
   T* dz = MODE == DIST_LOSS ? nullptr : static_cast<T*>(p.dZ) + row * p.lddz;
+  // the row's sums are formed here, not taken from the forward call (the same decision in all CTAs of the row)
+  const bool sums = MODE != DIST_BACKWARD || (wt != 0.f && coarse(p.stat_in[2 * row], p.stat_in[2 * row + 1]));
   if (wt == 0.f) {                            // the row does not count: it is not read (the same decision in all CTAs of the row)
     if (MODE != DIST_LOSS) {
       const float zero[VEC] = {};
@@ -88,9 +90,9 @@ __global__ void __launch_bounds__(512, 2) distill_kernel(const Distill p) {
   __syncthreads();
   for (int k = tid; k < p.K; k += nt) {
     const int i = cls[k];
-    // the backward pass needs those of its slice alone, and dZ may be Z: another CTA's are being written over
+    // without sums those of its slice are enough, and dZ may be Z: another CTA's are being written over
     const bool here = i >= first && i < last;
-    zv[k] = (MODE == DIST_BACKWARD ? here : i >= 0) ? to_f(z[i]) : 0.f;
+    zv[k] = (sums ? i >= 0 : here) ? to_f(z[i]) : 0.f;
     if (here) atomicOr(&bits[(i - first) >> 5], 1u << ((i - first) & 31));
   }
   __syncthreads();
@@ -98,7 +100,7 @@ __global__ void __launch_bounds__(512, 2) distill_kernel(const Distill p) {
   // ---- the slice: largest logit and sum of exponentials of the classes that are not named ----
   float e[NV][VEC];
   MaxSum sum = {kLow, 0.f};
-  if (MODE != DIST_BACKWARD) {
+  if (sums) {
     for (int base = first; base < last; base += nt * NV * VEC) {
       MaxSum now = {kLow, 0.f};
 #pragma unroll
@@ -154,12 +156,12 @@ __global__ void __launch_bounds__(512, 2) distill_kernel(const Distill p) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) ts += __shfl_xor_sync(0xffffffffu, ts, o);
   if (lane == 0) red_p[warp] = ts;
-  if (MODE != DIST_BACKWARD && tid == 0) {
+  if (sums && tid == 0) {
     MaxSum s = {red_m[0], red_l[0]};
     for (int k = 1; k < nw; ++k) s = merge(s, {red_m[k], red_l[k]}, c2);
     cta_sum = s;
   }
-  if (MODE != DIST_BACKWARD) cluster.sync();
+  if (sums) cluster.sync();
   else __syncthreads();
   ts = 0.f;
   for (int k = 0; k < nw; ++k) ts += red_p[k];
@@ -172,10 +174,10 @@ __global__ void __launch_bounds__(512, 2) distill_kernel(const Distill p) {
 
   // ---- the student's normalisers: the others' over the cluster in order, then the named classes ----
   // q_j = exp((z_j - ref) / tau) inv, or, from what the forward call left, exp(z_j / tau - ref)
-  float ref, inv, qt, Q = 1.f;                // qt: the mass of the classes that are not named, Q: of those that are (forward)
+  float ref, inv, qt, Q = 1.f;                // qt: the mass of the classes that are not named, Q: of those that are (with sums)
   bool empty;                                 // no class has any
   MaxSum all = {kLow, 0.f}, others = {kLow, 0.f};
-  if (MODE != DIST_BACKWARD) {
+  if (sums) {
     others = *cluster.map_shared_rank(&cta_sum, 0);
     for (int r = 1; r < C; ++r) others = merge(others, *cluster.map_shared_rank(&cta_sum, r), c2);
     MaxSum n = {kLow, 0.f};
@@ -196,10 +198,10 @@ __global__ void __launch_bounds__(512, 2) distill_kernel(const Distill p) {
   } else {
     ref = p.stat_in[2 * row];
     inv = 1.f;
-    empty = ref == -INFINITY;
+    empty = false;
     qt = ex2((p.stat_in[2 * row + 1] - ref) * kLog2e);
   }
-  auto student = [&](float v) { return ex2(MODE == DIST_BACKWARD ? fmaf(v, p.inv_tau, -ref) * kLog2e : (v - ref) * c2) * inv; };
+  auto student = [&](float v) { return ex2(sums ? (v - ref) * c2 : fmaf(v, p.inv_tau, -ref) * kLog2e) * inv; };
 
   // ---- loss ----
   if (MODE != DIST_BACKWARD) {
@@ -232,8 +234,8 @@ __global__ void __launch_bounds__(512, 2) distill_kernel(const Distill p) {
     const float ws = empty ? 0.f : wt * p.inv_tau;
     // (A q_t - p_t) q_j / q_t of the others: the first factor, and q_j / q_t relative to the others' largest or their normaliser
     const float other = ws == 0.f ? 0.f : ws * excess_rest(A, pt, qt, whole, Q);
-    const float other_ref = MODE == DIST_BACKWARD ? p.stat_in[2 * row + 1] : others.m;
-    if (KEEP && MODE == DIST_BOTH) {
+    const float other_ref = sums ? others.m : p.stat_in[2 * row + 1];
+    if (KEEP && sums) {
       const float f = others.l == 0.f ? 0.f : other * ex2((sum.m - others.m) * c2) / others.l;
 #pragma unroll
       for (int k = 0; k < NV; ++k) {
@@ -243,7 +245,7 @@ __global__ void __launch_bounds__(512, 2) distill_kernel(const Distill p) {
         if (c < last) store<VEC>(dz + c, last - c, e[k]);
       }
     } else {
-      const float f = MODE == DIST_BACKWARD ? (other_ref == -INFINITY ? 0.f : other) : (others.l == 0.f ? 0.f : other / others.l);
+      const float f = !sums ? other : (others.l == 0.f ? 0.f : other / others.l);
       for (int base = first; base < last; base += nt * NV * VEC) {
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
@@ -255,7 +257,7 @@ __global__ void __launch_bounds__(512, 2) distill_kernel(const Distill p) {
           const int c = base + (k * nt + tid) * VEC;
 #pragma unroll
           for (int v = 0; v < VEC; ++v)
-            e[k][v] = f == 0.f ? 0.f : f * ex2(MODE == DIST_BACKWARD ? fmaf(e[k][v], p.inv_tau, -other_ref) * kLog2e : (e[k][v] - other_ref) * c2);
+            e[k][v] = f == 0.f ? 0.f : f * ex2(sums ? (e[k][v] - other_ref) * c2 : fmaf(e[k][v], p.inv_tau, -other_ref) * kLog2e);
           if (c < last) store<VEC>(dz + c, last - c, e[k]);
         }
       }
@@ -267,7 +269,7 @@ __global__ void __launch_bounds__(512, 2) distill_kernel(const Distill p) {
       put(dz + i, empty ? 0.f : ws * (A * student(zv[k]) - ex2(teacher2(tv[k])) * scale_p));
     }
   }
-  if (MODE != DIST_BACKWARD) cluster.sync();  // no CTA of the cluster leaves while its sum may still be read
+  if (sums) cluster.sync();                   // no CTA of the cluster leaves while its sum may still be read
 }
 
 fw_status desc_check(const fw_distill_desc* d) {

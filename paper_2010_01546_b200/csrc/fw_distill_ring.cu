@@ -47,7 +47,8 @@ __device__ __forceinline__ const void* word_of(const void* at) {
 }
 
 struct RingNumbers { float w, t_lse, s0, s1; };
-// What the sums' warp says of a row: to the classes that are not named, for the gradient of those that are, and for the loss
+// What the sums' warp says of a row: to the classes that are not named, for the gradient of those that are, and for the loss.  Without
+// sums of the row inv is 1, or 0 for a row that is left for the end.
 struct RingScale { float ref, other_ref, factor, ws, A, inv, scale_p; };
 // Of a row's entries: the teacher's exponentials and the named classes', each relative to its largest; with w the teacher's exponentials
 // and a their exponents (base 2), sum w a and sum w (z - named.m) kDown
@@ -66,6 +67,7 @@ __global__ void __launch_bounds__(kRingAll, 2) distill_ring_kernel(const Distill
   __shared__ float s_w[kRingWarps][kRingSlots + 2];
   __shared__ __align__(8) uint64_t bar_sums[2], bar_bits[2], bar_scale[2], bar_done[2], bar_clear[2];
   __shared__ int s_lost;                          // a wait gave up
+  __shared__ int s_coarse;                        // gradient alone: rows of this CTA are left for the end
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int rank = (int)blockIdx.x % C, row0 = (int)blockIdx.x / C, step = (int)gridDim.x / C;
   uint4* ring = reinterpret_cast<uint4*>(dyn8);                                             // [slot][k][thread]
@@ -91,7 +93,7 @@ __global__ void __launch_bounds__(kRingAll, 2) distill_ring_kernel(const Distill
   for (int i = tid; i < 2 * words; i += kRingAll) bits[i] = 0;
   for (int i = tid; i < kSeenBits / 32; i += kRingAll) s_seen[i] = 0;
   if (tid == 0) {
-    s_lost = 0;
+    s_lost = s_coarse = 0;
     for (int i = 0; i < 2; ++i) {
       sm100::mbar_init(bar(bar_sums[i]), 1);
       sm100::mbar_init(bar(bar_bits[i]), 1);
@@ -103,6 +105,12 @@ __global__ void __launch_bounds__(kRingAll, 2) distill_ring_kernel(const Distill
   }
   dep_wait();
   __syncthreads();
+  // Rows whose statistics are coarse are left out of the walk; of the cluster's rows a CTA does every C-th by itself at the end.  The
+  // choice rests on memory that no one writes, so all CTAs make the same one.
+  auto later = [&](int row) { return MODE == DIST_BACKWARD && coarse(p.stat_in[2 * (int64_t)row], p.stat_in[2 * (int64_t)row + 1]); };
+  if (MODE == DIST_BACKWARD)
+    for (int64_t row = row0 + (int64_t)(rank + tid * C) * step; row < rows; row += (int64_t)kRingAll * C * step)
+      if (later((int)row)) s_coarse = 1;
   // no CTA sends to another before that one has begun
   sm100::cluster_arrive();
   sm100::cluster_wait();
@@ -219,7 +227,8 @@ __global__ void __launch_bounds__(kRingAll, 2) distill_ring_kernel(const Distill
             } else {
               vscale<VEC>(e[k], f);
             }
-            store<VEC>(dz + (uint32_t)((k * kRingThreads + tid) * VEC), FILL == ROW_PART ? mine - k * kRingThreads * VEC : VEC, e[k]);
+            if (MODE != DIST_BACKWARD || sc.inv != 0.f)
+              store<VEC>(dz + (uint32_t)((k * kRingThreads + tid) * VEC), FILL == ROW_PART ? mine - k * kRingThreads * VEC : VEC, e[k]);
           }
         }
       } else if (MODE != DIST_LOSS) {
@@ -304,7 +313,7 @@ __global__ void __launch_bounds__(kRingAll, 2) distill_ring_kernel(const Distill
         const int i = c[k];
         if (i < first || i >= last) continue;
         bits[(it & 1) * words + ((i - first) >> 5)] = 0;
-        if (MODE != DIST_LOSS) {
+        if (MODE == DIST_BOTH || (MODE == DIST_BACKWARD && sc.inv != 0.f)) {
           const float z = __uint_as_float(values[kp + k]), pk = ex2(__uint_as_float(values[k])) * sc.scale_p;
           const float q = ex2(MODE == DIST_BACKWARD ? fmaf(z, p.inv_tau, -sc.ref) * kLog2e : (z - sc.ref) * c2) * sc.inv;
           put(dz + i, sc.ws == 0.f ? 0.f : sc.ws * (sc.A * q - pk));
@@ -481,15 +490,15 @@ __global__ void __launch_bounds__(kRingAll, 2) distill_ring_kernel(const Distill
             Q = n.l * ex2((n.m - all.m) * c2) * inv;
           } else {
             ref = s_num[slot_of(it)].s0;
-            inv = 1.f;
-            empty = ref == -INFINITY;
+            inv = coarse(ref, s_num[slot_of(it)].s1) ? 0.f : 1.f;
+            empty = false;
             qt = ex2((s_num[slot_of(it)].s1 - ref) * kLog2e);
           }
           const float ws = empty ? 0.f : w * p.inv_tau;
           // (A q_t - p_t) q_j / q_t of the others: the first factor, and q_j / q_t relative to the others' largest or their normaliser
           const float other = ws == 0.f ? 0.f : ws * excess_rest(A, pt, qt, whole, Q);
           const float other_ref = MODE == DIST_BACKWARD ? s_num[slot_of(it)].s1 : others.m;
-          const bool none = MODE == DIST_BACKWARD ? other_ref == -INFINITY : others.l == 0.f;
+          const bool none = MODE != DIST_BACKWARD && others.l == 0.f;
           if (lane == 0) {
             s_scale[it & 1] = {ref, other_ref, none ? 0.f : MODE == DIST_BACKWARD ? other : __fdividef(other, others.l), ws, A, inv, scale_p};
             sm100::mbar_arrive(bar(bar_scale[it & 1]));
@@ -523,6 +532,13 @@ __global__ void __launch_bounds__(kRingAll, 2) distill_ring_kernel(const Distill
           if (MODE != DIST_LOSS && first < last) put(static_cast<T*>(p.dZ) + (int64_t)r * p.lddz + first, NAN);
         }
     }
+  }
+  if (MODE == DIST_BACKWARD) {
+    __syncthreads();
+    if (s_coarse)
+      for (int64_t row = row0 + (int64_t)rank * step; row < rows; row += (int64_t)C * step)
+        if (later((int)row) && !(p.weight && p.weight[row] == 0.f))
+          coarse_row<T, VEC, true>(p, row, reinterpret_cast<uint32_t*>(dyn8), reinterpret_cast<float*>(s_seen));
   }
   dep_trigger();
   // no CTA leaves while its sums may still be written by another

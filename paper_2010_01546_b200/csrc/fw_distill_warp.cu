@@ -42,6 +42,11 @@ __global__ void __launch_bounds__(32 * kWarpRows) distill_warp_kernel(const Dist
     const int c = (k * 32 + lane) * VEC;
     load<VEC>(z + c, p.V - c, -INFINITY, e[k]);
   }
+  const float s0 = MODE == DIST_BACKWARD ? p.stat_in[2 * (int64_t)row] : 0.f, s1 = MODE == DIST_BACKWARD ? p.stat_in[2 * (int64_t)row + 1] : 0.f;
+  if (MODE == DIST_BACKWARD && coarse(s0, s1)) {
+    coarse_row<T, VEC, false>(p, row, bits, nullptr);
+    return;
+  }
   // ---- entries: a class named twice counts once, with its first logit: in the groups of 32 in order, in a group the lowest lane ----
   int cls[EPL];
   float tv[EPL], zv[EPL];
@@ -136,10 +141,10 @@ __global__ void __launch_bounds__(32 * kWarpRows) distill_warp_kernel(const Dist
     qt = others.l * ex2((others.m - all.m) * c2) * inv;
     Q = named.l * ex2((named.m - all.m) * c2) * inv;
   } else {
-    ref = p.stat_in[2 * (int64_t)row];
+    ref = s0;
     inv = 1.f;
-    empty = ref == -INFINITY;
-    qt = ex2((p.stat_in[2 * (int64_t)row + 1] - ref) * kLog2e);
+    empty = false;
+    qt = ex2((s1 - ref) * kLog2e);
   }
   auto student = [&](float v) { return ex2(MODE == DIST_BACKWARD ? fmaf(v, p.inv_tau, -ref) * kLog2e : (v - ref) * c2) * inv; };
   if (MODE != DIST_BACKWARD) {
@@ -165,14 +170,13 @@ __global__ void __launch_bounds__(32 * kWarpRows) distill_warp_kernel(const Dist
   if (MODE != DIST_LOSS) {
     const float ws = empty ? 0.f : wt * p.inv_tau;
     const float other = ws == 0.f ? 0.f : ws * excess_rest(A, pt, qt, whole, Q);
-    const float other_ref = MODE == DIST_BACKWARD ? p.stat_in[2 * (int64_t)row + 1] : others.m;
-    const float f = MODE == DIST_BACKWARD ? (other_ref == -INFINITY ? 0.f : other) : (others.l == 0.f ? 0.f : other / others.l);
+    const float f = MODE == DIST_BACKWARD ? other : (others.l == 0.f ? 0.f : other / others.l);
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
       const int c = (k * 32 + lane) * VEC;
       if (c >= p.V) continue;
 #pragma unroll
-      for (int v = 0; v < VEC; ++v) e[k][v] = MODE != DIST_BACKWARD ? e[k][v] * f : f == 0.f ? 0.f : f * ex2(fmaf(e[k][v], p.inv_tau, -other_ref) * kLog2e);
+      for (int v = 0; v < VEC; ++v) e[k][v] = MODE != DIST_BACKWARD ? e[k][v] * f : f == 0.f ? 0.f : f * ex2(fmaf(e[k][v], p.inv_tau, -s1) * kLog2e);
       store<VEC>(dz + c, p.V - c, e[k]);
     }
     __syncwarp();                             // the named classes are written over

@@ -492,3 +492,75 @@ def test_lowest_finite_value_of_the_teacher(B, rows, V, K, shift):
     want = by_logs(z, torch.zeros_like(T), I, 1.0)
     check(loss, want[0], want[2])
     check(dz, want[1], want[3], HALF[torch.float32])
+
+
+STAT = 1024.0                                              # statistics up to here are taken as they are (kFineStat)
+
+
+def gradient_alone(B, z, T, I, tau, tl, weight, kind, pad, shift):
+    """The backward call after a forward call that leaves the statistics: into a matrix of its own and over the logits."""
+    rows, V = z.shape
+    d = desc(B, V, T.shape[1], kind, tau=tau)
+    loss, stat = torch.empty(rows, device="cuda"), torch.empty(rows, 2, device="cuda")
+    B.fw_distill_forward(d, z, T, I, loss, stat=stat, t_lse=tl, weight=weight)
+    dz, zz = matrix(rows, V, KINDS[kind], pad=pad, shift=shift), put(z, KINDS[kind], pad=pad, shift=shift)
+    B.fw_distill_backward(d, z, T, I, stat, dz, t_lse=tl, weight=weight)
+    B.fw_distill_backward(d, zz, T, I, stat, zz, t_lse=tl, weight=weight)
+    assert surround_kept(dz) and surround_kept(zz)
+    assert torch.equal(dz.nan_to_num(nan=7.0), zz.nan_to_num(nan=7.0))
+    return dz, stat
+
+
+def check_alone(dz, want, tau, half):
+    """The forward call's bound and, where the statistics are used, their two roundings: 2 u 1024 of each exponential.  An exponential
+    below 2^-126 is 0 (fw_rows.cuh, ex2); it is multiplied by weight / tau, weight <= 1.5, and by masses and reciprocals of sums of at
+    most 1."""
+    relative = 2 * 2.0 ** -24 * STAT
+    check(dz, want[1], want[3] + relative * (want[1].abs() + want[3] * 2.0 ** 17) + 1.5 / tau * 2.0 ** -126, half)
+
+
+@pytest.mark.parametrize("rows,V,K,shift", EACH_KERNEL + [(1200, 9000, 20, 0), (300, 50021, 33, 0)])
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("rest", [False, True])
+@pytest.mark.parametrize("what", ["row", "others", "offset", "mask", "tau"])
+def test_gradient_alone_where_the_statistics_are_coarse(B, rows, V, K, shift, kind, rest, what):
+    """log sum exp(Z / tau) of -3e38 or 1e5 in fp32 says nothing of how many classes share the mass, or little: the gradient alone
+    is still the formula's.  Every third row is an ordinary one, every seventh has weight 0."""
+    tau = 2.0 ** -10 if what == "tau" else 1.0
+    z, T, I, t_lse = inputs(rows, V, K, kind, V + K, tau=tau, pad=shift or None, shift=shift)
+    if what == "tau":
+        T = (T * tau).contiguous()                          # a teacher of ordinary size beside a student scaled by 1000
+        t_lse = torch.logsumexp(T.to(F64) / tau, 1).float() + 0.5
+    coarse = torch.arange(rows, device="cuda") % 3 != 1
+    low, at = torch.finfo(KINDS[kind]).min, I.long()
+    new = z.clone()
+    if what == "row":
+        new[:] = low
+    elif what == "others":
+        new[:] = low
+        new.scatter_(1, at, z.gather(1, at))
+    elif what == "offset":
+        new = (z.float() - 1e5).to(z.dtype)
+    elif what == "mask":
+        new = (z.float() - 1e9).to(z.dtype)
+    z[coarse] = new[coarse]
+    weight = torch.rand(rows, generator=gen(V), device="cuda") + 0.5
+    weight[6::7] = 0
+    tl = t_lse + 0.05 if rest else None
+    pad = shift or None
+    dz, stat = gradient_alone(B, z, T, I, tau, tl, weight, kind, pad, shift)
+    assert not bool((dz[6::7] != 0).any())
+    for r0 in range(0, rows, 60):
+        r = slice(r0, r0 + 60)
+        check_alone(dz[r], by_logs(z[r], T[r], I[r], tau, None if tl is None else tl[r], weight[r]), tau, HALF[KINDS[kind]])
+
+
+def test_gradient_alone_where_the_statistics_pass_fp32(B):
+    """Logits of 1e38 over a tau of 1/16: the statistics are infinite, the gradient is not."""
+    for rows, V, K, shift in EACH_KERNEL:
+        z, T, I, _ = inputs(rows, V, K, "f32", V, pad=shift or None, shift=shift)
+        z[0], z[1, : V // 2] = -1e38, 1e38
+        dz, stat = gradient_alone(B, z, T, I, 0.0625, None, None, "f32", shift or None, shift)
+        assert bool(torch.isinf(stat[:2, 0]).all())
+        want = by_logs(z, T, I, 0.0625)
+        check_alone(dz, want, 0.0625, HALF[torch.float32])
