@@ -313,8 +313,9 @@ fw_status fw_cov_block_static(const float* X, int64_t rows, int64_t ldx, int32_t
  * sum and y may be x or res themselves (same address, type and ld); any other overlap
  * of outputs with inputs or with each other is FW_ERR_INVALID_ARG.
  * 1 <= M <= 16384.  A NaN or infinity in a row makes that row's y, rstd and
- * scale what the formulas give, and no other's.  The squares are fp32: a row with an
- * |s| beyond 1.8e19 has an infinite sum, so rstd and y are 0. */
+ * scale what the formulas give, and no other's.  The squares are added in fp32: where they pass
+ * 3.4e38 (an |s| of 1.8e19, or of 2.9e17 in each of 4096 places) the sum is infinite and rstd and y are 0.
+ * An e4m3 row is made from s w: where |s w| passes 3.4e38 its scale is infinite. */
 typedef struct {
   int32_t M;         /* features                                                 */
   int32_t dtype;     /* fw_dtype of x, res, sum: FW_F32 or FW_BF16                */

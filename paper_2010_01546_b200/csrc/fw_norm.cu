@@ -113,9 +113,10 @@ __global__ void __launch_bounds__(512) norm_forward_kernel(const NormFwd p) {
       top = over_group<MaxAbs>(top, width, buf[flip][1]);
       const float size = top * rstd;                         // max |y|; NaN where the row has a NaN or an infinity
       const bool tiny = size < kMinScale * kE4m3Max;
-      if (t == 0) p.y_scale[row] = top == 0.f ? 1.f : tiny ? kMinScale : size / kE4m3Max;
-      const bool by_size = tiny || top < 1e-36f;              // 448 / top may be beyond fp32
-      inv = tiny ? 1.f / kMinScale : size != size ? size : kE4m3Max * rcp(by_size ? size : top);
+      if (t == 0) p.y_scale[row] = size == 0.f ? 1.f : tiny ? kMinScale : size / kE4m3Max;
+      const bool by_size = tiny || top < 2e-36f;              // 448 / top may be beyond fp32 (below 1.32e-36)
+      // an exact quotient: its error moves every code of the row the same way
+      inv = tiny ? 1.f / kMinScale : size != size ? size : kE4m3Max / (by_size ? size : top);
       if (by_size) {
 #pragma unroll
         for (int k = 0; k < NV; ++k) vscale<VEC>(v[k], rstd);

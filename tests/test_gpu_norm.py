@@ -205,3 +205,66 @@ def test_other_stream_and_graph(B):
     torch.cuda.synchronize()
     for a, b in zip(got, (s, y, q.float(), scale, rstd, dx, dw)):
         assert torch.equal(a, b)
+
+
+def e4m3_of_row(s, w, eps):
+    """y / c and c in 64 bits."""
+    y = s.to(F64) * (s.to(F64).square().mean(1, keepdim=True) + eps).rsqrt() * w.to(F64)
+    c = y.abs().amax(1, keepdim=True) / 448
+    return y / c, c[:, 0]
+
+
+def nearest_within(q, ratio, rel):
+    """Each element of q is what some number within `rel` of `ratio` rounds to."""
+    low, high = ((ratio * (1 + k * rel)).float().to(torch.float8_e4m3fn).float() for k in (-1, 1))
+    q = q.float()
+    return (q >= torch.minimum(low, high)) & (q <= torch.maximum(low, high))
+
+
+@pytest.mark.parametrize("M", [520, 1537, 4096])
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+def test_e4m3_of_small_and_large_products(B, M, kind):
+    """Rows whose |s w| is near the lower end of fp32 while y is not (448 / 1.2e-36 is beyond it), and large ones.  Zeros stay zeros.
+    Squares of s below 1e-38 are 0 in fp32, as eps makes them in the definition.  What is rounded is within 7 u of y / c: s w, the largest
+    of them, below 2e-36 both times rstd, 448 over that, the product, and half a step of fp32 in this test."""
+    g, t = gen(M), KINDS[kind]
+    for size, wsize in ((1e-36, 1.0), (1.2e-30, 1e-6), (1e-26, 1e-10), (1e9, 1e-30), (1e9, 1e25)):
+        x = put(torch.rand(4, M, generator=g, device="cuda").mul_(2).sub_(1) * size, t, pad=None)
+        x[:, ::5] = 0
+        x[:, 1] = 1.2 * size
+        w = (0.5 + 0.5 * torch.rand(M, generator=g, device="cuda")) * wsize
+        y, scale = matrix(4, M, torch.float8_e4m3fn, pad=None), torch.empty(4, device="cuda")
+        B.fw_rmsnorm_forward(desc(B, M, kind, "e4m3", eps=1e-6), x, w, y, y_scale=scale)
+        ratio, c = e4m3_of_row(x, w, 1e-6)
+        assert bool(((scale.to(F64) - c).abs() <= (FWD + 4 * U) * c).all()), (size, wsize)
+        assert bool(nearest_within(y, ratio, 7 * U).all()), (size, wsize)
+        assert bool((y[:, ::5].float() == 0).all())
+
+
+def test_e4m3_codes(B):
+    """An ordinary matrix: every code is that of a number within 5 u of y / c (s w, the largest of them, 448 over that and the
+    product are rounded; one more half step in this test's own conversion)."""
+    rows, M = 4096, 4096
+    x, _, w = inputs(rows, M, "bf16", 1, pad=None)
+    y, scale = matrix(rows, M, torch.float8_e4m3fn, pad=None), torch.empty(rows, device="cuda")
+    B.fw_rmsnorm_forward(desc(B, M, "bf16", "e4m3"), x, w, y, y_scale=scale)
+    ratio, _ = e4m3_of_row(x, w, 1e-5)
+    assert bool(nearest_within(y, ratio, 5 * U).all())
+
+
+def test_e4m3_row_beyond_the_squares(B):
+    """|s| beyond 1.8e19: rstd and y are 0, a row of zeros with scale 1."""
+    x = torch.full((2, 64), 1e30, device="cuda")
+    y, scale, rstd = matrix(2, 64, torch.float8_e4m3fn), torch.empty(2, device="cuda"), torch.empty(2, device="cuda")
+    B.fw_rmsnorm_forward(desc(B, 64, "f32", "e4m3"), x, torch.ones(64, device="cuda"), y, y_scale=scale, rstd=rstd)
+    assert bool((rstd == 0).all()) and bool((y.float() == 0).all()) and bool((scale == 1).all())
+
+
+def test_e4m3_row_beyond_the_products(B):
+    """|s w| beyond 3.4e38 while y is not: an infinite scale says so; the other row is as ever."""
+    x = torch.ones(2, 64, device="cuda")
+    x[0] = 1e15
+    w = torch.full((64,), 1e25, device="cuda")
+    y, scale = matrix(2, 64, torch.float8_e4m3fn), torch.empty(2, device="cuda")
+    B.fw_rmsnorm_forward(desc(B, 64, "f32", "e4m3"), x, w, y, y_scale=scale)
+    assert float(scale[0]) == float("inf") and bool(torch.isfinite(scale[1])) and bool((y[1].float() == 448).all())
