@@ -412,12 +412,19 @@ def _vector(t, n, name, dev, dtype=FW_F32):
     return t.data_ptr()
 
 
+def _override(d, overrides):
+    """The description with some fields set; ctypes would take a misspelt one without a word."""
+    for k, v in overrides.items():
+        if not any(k == f[0] for f in d._fields_):
+            raise TypeError(f"{type(d).__name__} has no field {k}")
+        setattr(d, k, v)
+    return d
+
+
 def fw_norm_desc_default(M: int, **overrides) -> fw_norm_desc:
     d = fw_norm_desc()
     _lib().fw_norm_desc_default(C.byref(d), M)
-    for k, v in overrides.items():
-        setattr(d, k, v)
-    return d
+    return _override(d, overrides)
 
 
 def fw_rmsnorm_scratch_bytes(desc: fw_norm_desc) -> int:
@@ -453,9 +460,7 @@ def fw_rmsnorm_backward(desc: fw_norm_desc, dy, s, w, rstd, dx, dw=None, dsum=No
 def fw_distill_desc_default(V: int, K: int, **overrides) -> fw_distill_desc:
     d = fw_distill_desc()
     _lib().fw_distill_desc_default(C.byref(d), V, K)
-    for k, v in overrides.items():
-        setattr(d, k, v)
-    return d
+    return _override(d, overrides)
 
 
 def fw_distill_forward(desc: fw_distill_desc, Z, T, I, loss, stat=None, t_lse=None, weight=None, dZ=None, stream: int = 0) -> None:
@@ -553,8 +558,7 @@ class Gated:
         self.desc = fw_gated_desc()
         _lib().fw_gated_desc_default(C.byref(self.desc), M, N)
         self.desc.max_rows = max_rows
-        for k, v in desc_overrides.items():
-            setattr(self.desc, k, int(v))
+        _override(self.desc, {k: int(v) for k, v in desc_overrides.items()})
         self.M, self.N = M, N
         self.nbytes = int(_lib().fw_gated_workspace_bytes(C.byref(self.desc)))
         if self.nbytes == 0:

@@ -119,3 +119,14 @@ def test_gated_refusals(lib):
         assert f(None) == inv
     assert lib.fw_gated_forward(None, A, 1, 64, None, A, A, 64, None, None, None, None, A, 64, None, None, 0) == inv
     assert lib.fw_gated_backward(None, A, 1, 64, A, 64, A, A, 64, A, A, 64, A, 64, A, A, 0, A, A) == inv
+
+
+def test_unknown_options_are_refused():
+    """A description takes its own fields alone: a misspelt one would leave the default without a word."""
+    with pytest.raises(TypeError, match="epsilon"):
+        B.fw_norm_desc_default(64, epsilon=1e-3)
+    with pytest.raises(TypeError, match="temperature"):
+        B.fw_distill_desc_default(100, 10, temperature=2.0)
+    with pytest.raises(TypeError, match="activation"):
+        B.Gated(64, 32, activation=B.FW_ACT_RELU)
+    assert B.fw_norm_desc_default(64, eps=0.5).eps == 0.5
