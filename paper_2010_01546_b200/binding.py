@@ -449,6 +449,8 @@ def fw_rmsnorm_backward(desc: fw_norm_desc, dy, s, w, rstd, dx, dw=None, dsum=No
     pdx, lddx = _matrix(dx, rows, M, t, "dx", dev)
     n = 0
     if scratch is not None:
+        if not scratch.is_contiguous():
+            raise ValueError("scratch: its bytes have to be contiguous")
         if scratch.get_device() != dev:
             _refuse_device(scratch, dev, "scratch")
         n = scratch.numel() * scratch.element_size()
@@ -563,7 +565,10 @@ class Gated:
         self.nbytes = int(_lib().fw_gated_workspace_bytes(C.byref(self.desc)))
         if self.nbytes == 0:
             raise FwError(FW_ERR_INVALID_ARG, "fw_gated_workspace_bytes")
+        dev = _here()
         self.workspace = torch.empty(self.nbytes + 256, dtype=torch.uint8, device=device)
+        if not self.workspace.is_cuda or self.workspace.get_device() != dev:
+            _refuse_device(self.workspace, dev, "workspace")
         out = C.c_void_p()
         _check(_lib().fw_gated_create(C.byref(self.desc), (self.workspace.data_ptr() + 255) // 256 * 256, self.nbytes, stream,
                                       C.byref(out)), "fw_gated_create")

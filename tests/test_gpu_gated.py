@@ -301,3 +301,10 @@ def test_activations_at_the_ends(B, act):
     want = Zg[0].to(F64)
     assert bool(((dbg.to(F64) - (want > 0).to(F64)).abs() <= 4 * U).all()), dbg
     assert bool(((dbu.to(F64) - want.clamp(min=0)).abs() <= 4 * U * want.clamp(min=0)).all()), dbu
+
+
+def test_another_device_than_the_current_one(B, monkeypatch):
+    """The tensors are here and the current device is said to be another: nothing is launched."""
+    monkeypatch.setattr(B, "_here", lambda: 1)
+    with pytest.raises(ValueError, match="cuda:0, but the current device is cuda:1"):
+        B.Gated(64, 32)

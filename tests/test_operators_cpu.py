@@ -130,3 +130,14 @@ def test_unknown_options_are_refused():
     with pytest.raises(TypeError, match="activation"):
         B.Gated(64, 32, activation=B.FW_ACT_RELU)
     assert B.fw_norm_desc_default(64, eps=0.5).eps == 0.5
+
+
+def test_a_block_of_memory_elsewhere_is_refused():
+    """The workspace is on the device that the kernels are launched on."""
+    with pytest.raises(ValueError, match="CUDA"):
+        B.Gated(64, 32, device="cpu")
+    import torch
+    d = B.fw_norm_desc_default(8)
+    x = torch.zeros(2, 8, dtype=torch.bfloat16)
+    with pytest.raises(ValueError, match="contiguous"):         # its bytes are counted as if they lay next to each other
+        B.fw_rmsnorm_backward(d, x, x, torch.ones(8), torch.ones(2), x, dw=torch.zeros(8), scratch=torch.zeros(1 << 16, 2, dtype=torch.uint8)[:, 0])
