@@ -443,14 +443,14 @@ def fw_rmsnorm_forward(desc: fw_norm_desc, x, w, y, res=None, sum_out=None, y_sc
 
 def fw_rmsnorm_backward(desc: fw_norm_desc, dy, s, w, rstd, dx, dw=None, dsum=None, scratch=None, stream: int = 0) -> None:
     rows, M, t, dev = dy.shape[0], desc.M, desc.dtype, _here()
+    if scratch is not None and not scratch.is_contiguous():
+        raise ValueError("scratch: its bytes have to be contiguous")
     pdy, lddy = _matrix(dy, rows, M, t, "dy", dev)
     ps, lds = _matrix(s, rows, M, t, "s", dev)
     pds, ldds = _matrix(dsum, rows, M, t, "dsum", dev)
     pdx, lddx = _matrix(dx, rows, M, t, "dx", dev)
     n = 0
     if scratch is not None:
-        if not scratch.is_contiguous():
-            raise ValueError("scratch: its bytes have to be contiguous")
         if scratch.get_device() != dev:
             _refuse_device(scratch, dev, "scratch")
         n = scratch.numel() * scratch.element_size()
