@@ -553,7 +553,7 @@ class Layer:
 
 class Gated:
     """A gated feed-forward block over a workspace tensor of its own.  Methods take torch CUDA tensors, look at their sizes,
-    strides and types, and forward to the C entry points fw_gated_*."""
+    strides and types, and forward to the C entry points fw_gated_*.  The stream outlives the block."""
 
     def __init__(self, M: int, N: int, max_rows: int = 0, device="cuda", stream: int = 0, **desc_overrides):
         import torch
@@ -573,6 +573,8 @@ class Gated:
         _check(_lib().fw_gated_create(C.byref(self.desc), (self.workspace.data_ptr() + 255) // 256 * 256, self.nbytes, stream,
                                       C.byref(out)), "fw_gated_create")
         self.handle = out.value
+        # the memory is anybody's only when this stream is through with it too
+        self.workspace.record_stream(torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream())
 
     def close(self):
         if getattr(self, "handle", None):

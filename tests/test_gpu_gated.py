@@ -308,3 +308,23 @@ def test_another_device_than_the_current_one(B, monkeypatch):
     monkeypatch.setattr(B, "_here", lambda: 1)
     with pytest.raises(ValueError, match="cuda:0, but the current device is cuda:1"):
         B.Gated(64, 32)
+
+
+def test_workspace_outlives_the_work_on_its_stream(B):
+    """A block that goes while its work waits on a stream of its own: its memory is not given to anybody else before that."""
+    rows, M, N = 64, 64, 128
+    s = torch.cuda.Stream()
+    blk = B.Gated(M, N, rows, grad=1, stream=s.cuda_stream)
+    dH, Zg, Zu = (bf(rows, N, fill=1.0) for _ in range(3))
+    dbg, dbu = torch.empty(N, device="cuda"), torch.empty(N, device="cuda")
+    blk.backward(dH, None, None, None, Zg, Zu, dbg=dbg, dbu=dbu)     # the kernels are loaded
+    torch.cuda.synchronize()
+    at, n = blk.workspace.data_ptr(), blk.workspace.numel()
+    with torch.cuda.stream(s):
+        torch.cuda._sleep(200_000_000)
+    blk.backward(dH, None, None, None, Zg, Zu, dbg=dbg, dbu=dbu)
+    assert not s.query()
+    del blk
+    others = [torch.empty(n, dtype=torch.uint8, device="cuda") for _ in range(4)]
+    assert not s.query() and all(o.data_ptr() != at for o in others)
+    torch.cuda.synchronize()
