@@ -292,8 +292,10 @@ cudaError_t launch_mode(Distill p, int64_t rows, cudaStream_t s) {
   bool taken = false;
   cudaError_t e = launch_warp<T, VEC, MODE>(p, rows, s, &taken);
   if (taken) return e;
-  e = launch_ring<T, VEC, MODE>(p, rows, s, &taken);
-  if (taken) return e;
+  if constexpr (VEC > 1) {                                  // rows on 16 bytes
+    e = launch_ring<T, VEC, MODE>(p, rows, s, &taken);
+    if (taken) return e;
+  }
   constexpr int NV = VEC == 1 ? 16 : 32 / VEC;              // 32 classes of a thread in registers (16 single ones)
   constexpr int few = VEC == 1 ? 4 : 1;
   // threads and CTAs of a row: enough that the row is one trip, as far as 8 CTAs of 512 threads go

@@ -615,7 +615,7 @@ bool ring_shape(int V, int K, int vec, int* C, int* nv) {
 template <class T, int VEC, int MODE>
 cudaError_t launch_ring(const Distill& p0, int64_t rows, cudaStream_t s, bool* taken) {
   int C = 0, nv = 0;
-  *taken = VEC > 1 && ring_shape(p0.V, p0.K, VEC, &C, &nv);
+  *taken = ring_shape(p0.V, p0.K, VEC, &C, &nv);
   if (!*taken) return cudaSuccess;
   Distill p = p0;
   p.slice = ((p.V + C - 1) / C + 31) / 32 * 32;
@@ -628,15 +628,9 @@ cudaError_t launch_ring(const Distill& p0, int64_t rows, cudaStream_t s, bool* t
 template cudaError_t launch_ring<float, 4, DIST_LOSS>(const Distill&, int64_t, cudaStream_t, bool*);
 template cudaError_t launch_ring<float, 4, DIST_BOTH>(const Distill&, int64_t, cudaStream_t, bool*);
 template cudaError_t launch_ring<float, 4, DIST_BACKWARD>(const Distill&, int64_t, cudaStream_t, bool*);
-template cudaError_t launch_ring<float, 1, DIST_LOSS>(const Distill&, int64_t, cudaStream_t, bool*);
-template cudaError_t launch_ring<float, 1, DIST_BOTH>(const Distill&, int64_t, cudaStream_t, bool*);
-template cudaError_t launch_ring<float, 1, DIST_BACKWARD>(const Distill&, int64_t, cudaStream_t, bool*);
 template cudaError_t launch_ring<__nv_bfloat16, 8, DIST_LOSS>(const Distill&, int64_t, cudaStream_t, bool*);
 template cudaError_t launch_ring<__nv_bfloat16, 8, DIST_BOTH>(const Distill&, int64_t, cudaStream_t, bool*);
 template cudaError_t launch_ring<__nv_bfloat16, 8, DIST_BACKWARD>(const Distill&, int64_t, cudaStream_t, bool*);
-template cudaError_t launch_ring<__nv_bfloat16, 1, DIST_LOSS>(const Distill&, int64_t, cudaStream_t, bool*);
-template cudaError_t launch_ring<__nv_bfloat16, 1, DIST_BOTH>(const Distill&, int64_t, cudaStream_t, bool*);
-template cudaError_t launch_ring<__nv_bfloat16, 1, DIST_BACKWARD>(const Distill&, int64_t, cudaStream_t, bool*);
 
 }  // namespace distill
 }  // namespace fw

@@ -415,9 +415,11 @@ cudaError_t backward_launch(const NormBwd& p, cudaStream_t s, int* ctas) {
 template <class T, int VEC, int NV, bool DS>
 cudaError_t backward_launch(const NormBwd& p, cudaStream_t s, int* ctas) {
   constexpr int WHOLE = VEC > 1 ? ROW_WHOLE : ROW_PART, FULL = VEC > 1 ? ROW_FULL : ROW_PART;
-  if (p.width < 128)
-    return VEC > 1 && p.M % VEC == 0 ? backward_launch<T, VEC, NV, DS, WHOLE, false>(p, s, ctas)
-                                     : backward_launch<T, VEC, NV, DS, ROW_PART, false>(p, s, ctas);
+  if constexpr (NV <= 4) {                                   // more accesses a thread: 128 threads or more (see backward_nv)
+    if (p.width < 128)
+      return VEC > 1 && p.M % VEC == 0 ? backward_launch<T, VEC, NV, DS, WHOLE, false>(p, s, ctas)
+                                       : backward_launch<T, VEC, NV, DS, ROW_PART, false>(p, s, ctas);
+  }
   if (VEC > 1 && p.M == NV * VEC * p.width) return backward_launch<T, VEC, NV, DS, FULL, true>(p, s, ctas);
   if (VEC > 1 && p.M % VEC == 0) return backward_launch<T, VEC, NV, DS, WHOLE, true>(p, s, ctas);
   return backward_launch<T, VEC, NV, DS, ROW_PART, true>(p, s, ctas);
