@@ -162,3 +162,131 @@ def test_eight_bit_tokens(B, rows):
     n = s.to(F64)
     n = n * (n.square().mean(1, keepdim=True) + 1e-6).rsqrt()
     assert bool(((v - n).abs() <= 2.0 ** -4 * n.abs() * (1 + 2.0 ** -17) + 2.0 ** -10 * ys.to(F64)[:, None] + 2.0 ** -17 * n.abs()).all())
+
+
+def far_apart(rows, cols, dtype):
+    """Rows 2^30 elements apart: the third begins at 2^31."""
+    base = torch.empty((rows - 1) * 2 ** 30 + cols, dtype=dtype, device="cuda")
+    return torch.as_strided(base, (rows, cols), (2 ** 30, 1))
+
+
+def test_rows_beyond_32_bits(B):
+    """Offsets of 2^31 elements and more in every matrix that has a leading dimension: the bits of the same call on neighbouring rows."""
+    rows, M, N, V, K = 4, 264, 520, 9000, 20
+    g = gen(1)
+    r = lambda *s: torch.randn(*s, generator=g, device="cuda").to(BF16)  # noqa: E731
+    x, res, w = r(rows, M), r(rows, M), 1 + r(M).float() * 0.1
+    d = B.fw_norm_desc_default(M)
+
+    def norm(x, res, s, y, dx):
+        rstd = torch.empty(rows, device="cuda")
+        B.fw_rmsnorm_forward(d, x, w, y, res=res, sum_out=s, rstd=rstd)
+        B.fw_rmsnorm_backward(d, y, s, w, rstd, dx, dsum=x)
+        return s, y, dx
+
+    def gated(x, W, H, dX):
+        blk = B.Gated(M, N, rows, grad=1)
+        Zg, Zu = (torch.empty_strided((rows, N), (H.stride(0), 1), dtype=BF16, device="cuda") for _ in range(2)) if H.stride(0) == N else (far_apart(rows, N, BF16) for _ in range(2))
+        blk.forward(x, *W, H, Zg, Zu)
+        dWg, dWu = torch.empty(N, M, device="cuda"), torch.empty(N, M, device="cuda")
+        blk.backward(H, x, *W, Zg, Zu, dX=dX, dWg=dWg, dWu=dWu)
+        assert blk.sync_status() == B.FW_OK
+        return H, Zg, Zu, dX, dWg, dWu
+
+    def loss(z, dz, dz2):
+        ld, out, stat = B.fw_distill_desc_default(z.shape[1], K, t_dtype=B.FW_F32), torch.empty(rows, device="cuda"), torch.empty(rows, 2, device="cuda")
+        B.fw_distill_forward(ld, z, T, I[z.shape[1]], out, stat=stat, dZ=dz)
+        B.fw_distill_backward(ld, z, T, I[z.shape[1]], stat, dz2)
+        return out, dz, dz2
+
+    def same(near, far):
+        for a, b in zip(near, far):
+            assert torch.equal(a, b) and not bool(torch.isnan(a.float()).any())
+
+    e = lambda n: torch.empty(rows, n, dtype=BF16, device="cuda")  # noqa: E731
+    far = [far_apart(rows, V, BF16) for _ in range(5)]
+    put_far = lambda i, v: far[i][:, :v.shape[1]].copy_(v)  # noqa: E731
+    at = lambda i, n: far[i][:, :n]  # noqa: E731
+    same(norm(x, res, e(M), e(M), e(M)), norm(put_far(0, x), put_far(1, res), at(2, M), at(3, M), at(4, M)))
+    W = [r(N, M) * 0.1 for _ in range(2)]
+    same(gated(x, W, e(N), e(M)), gated(put_far(0, x), W, at(1, N), at(2, M)))
+    T = torch.randn(rows, K, generator=g, device="cuda")
+    I = {n: torch.stack([torch.randperm(n, generator=g, device="cuda")[:K] for _ in range(rows)]).to(torch.int32) for n in (1000, V)}
+    for n in (1000, V):
+        z = r(rows, n)
+        z[2] *= 2000                                             # statistics too coarse to be used
+        same(loss(z, e(n), e(n)), loss(put_far(0, z), at(1, n), at(2, n)))
+
+
+def test_a_small_block_between_layer_updates(B):
+    """Calls of a few rows in the stream of a bf16 layer's updates, whose products take all of the tensor memory of a SM: each waits for
+    the other, and both give what they give alone."""
+    g = gen(3)
+    r = lambda *s: torch.randn(*s, generator=g, device="cuda").to(BF16)  # noqa: E731
+    M, N, rows = 128, 1024, 16
+    X, W, H, H2 = r(rows, M), [r(N, M) * 0.1 for _ in range(2)], torch.empty(rows, N, dtype=BF16, device="cuda"), torch.empty(rows, N, dtype=BF16, device="cuda")
+    blk = B.Gated(M, N)
+    blk.forward(X, *W, H)
+    Y = r(4096, 576)
+    layers = [B.Layer(576, 64, x_dtype=B.FW_BF16, prec=B.FW_PREC_BF16) for _ in range(2)]
+    for _ in range(30):
+        layers[0].cov_update(Y)
+        layers[1].cov_update(Y)
+        for _ in range(3):
+            blk.forward(X, *W, H2)
+        layers[0].cov_update(Y)
+        layers[1].cov_update(Y)
+    assert torch.equal(H, H2) and blk.sync_status() == B.FW_OK
+    assert all(L.sync_status() == B.FW_OK for L in layers)
+    assert torch.equal(layers[0].get(B.FW_F_PHIX), layers[1].get(B.FW_F_PHIX))
+
+
+def test_two_streams_at_once(B):
+    """Norm, block and loss on two streams, one behind the other in each and captured in one of them: the bits of calls by themselves."""
+    M, N, rows, V, K = 512, 1024, 300, 20000, 40
+
+    def job(seed, stream):
+        g = gen(seed)
+        r = lambda *s: torch.randn(*s, generator=g, device="cuda").to(BF16)  # noqa: E731
+        x, res, w, W = r(rows, M), r(rows, M), 1 + r(M).float() * 0.1, [r(N, M) * 0.05 for _ in range(2)]
+        z, T, I = r(rows, V), r(rows, K), torch.stack([torch.randperm(V, generator=g, device="cuda")[:K] for _ in range(rows)]).to(torch.int32)
+        z[5::9] *= 2000
+        e = lambda *s, t=BF16: torch.empty(*s, dtype=t, device="cuda")  # noqa: E731
+        f = torch.float32
+        s, y, H, Zg, Zu, dX, dx, dz, dz2 = e(rows, M), e(rows, M), e(rows, N), e(rows, N), e(rows, N), e(rows, M), e(rows, M), e(rows, V), e(rows, V)
+        rstd, dw, out, stat, G = e(rows, t=f), e(M, t=f), e(rows, t=f), e(rows, 2, t=f), [e(N, M, t=f) for _ in range(2)]
+        d, ld = B.fw_norm_desc_default(M), B.fw_distill_desc_default(V, K)
+        scratch, blk = e(B.fw_rmsnorm_scratch_bytes(d), t=torch.uint8), B.Gated(M, N, rows, grad=1, stream=stream)
+
+        def call():
+            B.fw_rmsnorm_forward(d, x, w, y, res=res, sum_out=s, rstd=rstd, stream=stream)
+            blk.forward(y, *W, H, Zg, Zu)
+            B.fw_distill_forward(ld, z, T, I, out, stat=stat, dZ=dz, stream=stream)
+            B.fw_distill_backward(ld, z, T, I, stat, dz2, stream=stream)
+            blk.backward(H, y, *W, Zg, Zu, dX=dX, dWg=G[0], dWu=G[1])
+            B.fw_rmsnorm_backward(d, dX, s, w, rstd, dx, dw=dw, scratch=scratch, stream=stream)
+
+        return call, [s, y, H, Zg, Zu, dX, dx, dz, dz2, rstd, dw, out, stat, *G], blk
+
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    jobs = [job(k, s.cuda_stream) for k, s in enumerate(streams)]
+    torch.cuda.synchronize()
+    want = []
+    for call, outs, _ in jobs:
+        call()
+        torch.cuda.synchronize()
+        want.append([o.clone() for o in outs])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=streams[1]):
+        jobs[1][0]()
+    for _, outs, _ in jobs:
+        for o in outs:
+            o.fill_(float("nan"))
+    torch.cuda.synchronize()
+    for _ in range(10):
+        jobs[0][0]()
+        with torch.cuda.stream(streams[1]):
+            graph.replay()
+    torch.cuda.synchronize()
+    for (_, outs, blk), ref in zip(jobs, want):
+        assert all(torch.equal(a, b) for a, b in zip(outs, ref)) and blk.sync_status() == B.FW_OK
