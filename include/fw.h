@@ -298,7 +298,9 @@ fw_status fw_cov_block_static(const float* X, int64_t rows, int64_t ldx, int32_t
 /* ---- Operators around the layers: what makes a layer's input and its gradient.
  * They keep no state.  rows >= 1; ld* are leading dimensions in elements, at most
  * 2^30.  Any alignment to whole elements is taken; where every matrix starts on 16
- * bytes and its rows are a multiple of 16 bytes apart, 16 bytes move at a time.
+ * bytes and its rows are a multiple of 16 bytes apart, 16 bytes move at a time.  Of
+ * inputs the aligned word or 16 bytes that hold an element may be read whole: up to
+ * 15 bytes before a matrix and 2 behind it are read, never used.
  * Sums are fp32 in a fixed order: the same call gives the same bits. ---- */
 
 /* Residual addition and root-mean-square norm, a transform of layer inputs like
