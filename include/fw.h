@@ -440,6 +440,61 @@ fw_status fw_distill_backward(const fw_distill_desc* d, const void* Z, int64_t r
                               const void* I, const float* t_lse, const float* weight, const float* stat, void* dZ,
                               int64_t lddz, void* cuda_stream);
 
+/* AdamW over all tensors of a network in one launch (two with clipping): what fw_step and fw_step_momentum are to SGD.  Step t,
+ * with a gradient G times the clipping factor c:
+ *   m <- beta1 m + (1 - beta1) c G,  v <- beta2 v + (1 - beta2) (c G)^2
+ *   P <- P (1 - lr decay) - lr m / (1 - beta1^t) / (sqrt(v / (1 - beta2^t)) + eps)
+ * P is fp32; where copies are given each step also writes P rounded to bf16 there (weights of a gated block).  G is fp32 (G_t of
+ * fw_grad_transform, dw of the norms) or bf16, for each tensor as it comes.
+ * States: FW_F32, or FW_E4M3: for each 256 elements of a tensor (from its first) m is held as e4m3 codes times a power of
+ * two, v as the square of such a number; the update is made from m and v before they are rounded.  The scale is the least power of two
+ * (2^-100 at least) that takes the largest of the 256 to 448 or less.  Rounding is by chance, so that averages that move by less
+ * than a code in a step do move: of the two codes around m the upper one (in size) is taken where m's share of the way and
+ * chance1 / 2^16 reach 1, of the two around sqrt(v) the upper one where v's share of the way between their squares passes
+ * (chance2 + 1/2) / 2^16; a v > 0 is held as the smallest code at least.  chance1, chance2 are the lower and upper 16 bits of
+ * mix(i xor mix(seed xor t 0x9e3779b9)) for the i-th element of the state arrays (32-bit arithmetic), mix(x): x ^= x >> 16, x *= 0x7feb352d,
+ * x ^= x >> 15, x *= 0x846ca68b, x ^= x >> 16.
+ * Like a layer it is a host object over caller-supplied device memory with a stream of its own: the states, and the number of
+ * steps, live in the workspace (so that a replayed graph counts on).  Calls on one are not for several threads at once.  P and
+ * copies stay where they are as long as it lives, and overlap nothing.  A tensor of the same parameters twice is refused. */
+typedef struct fw_adamw fw_adamw;
+typedef struct {
+  int32_t n;            /* tensors, 1 ... 65536                                   */
+  int32_t state;        /* FW_F32 or FW_E4M3                                      */
+  double beta1, beta2;  /* 0 <= beta < 1 (1 - beta is rounded to fp32 as it is)   */
+  float eps;            /* > 0, finite                                            */
+  uint32_t seed;        /* of the chance in 8-bit states                          */
+} fw_adamw_desc;
+/* fp32 states, beta1 0.9, beta2 0.999, eps 1e-8, seed 0 */
+void fw_adamw_desc_default(fw_adamw_desc* d, int32_t n);
+/* sizes: elements of each tensor (HOST array), 1 ... 2^40; of all together, each rounded up to 256, 2^40 at most (2^32 with
+ * FW_E4M3).  0 if the description is invalid. */
+size_t fw_adamw_workspace_bytes(const fw_adamw_desc* d, const int64_t* sizes);
+/* HOST arrays of length n, read before the call returns: P device fp32; copies device bf16 (NULL, or NULL for some); decay the
+ * weight decay of each tensor (NULL: 0), >= 0.  Not to be captured.  States start at 0, as does the number of steps. */
+fw_status fw_adamw_create(const fw_adamw_desc* d, const int64_t* sizes, float* const* P, void* const* copies, const float* decay,
+                          void* dev_workspace, size_t bytes, void* cuda_stream, fw_adamw** out);
+fw_status fw_adamw_destroy(fw_adamw* a);
+/* One step.  G, g_dtype: HOST arrays of length n, the gradients (device) and their types (FW_F32 or FW_BF16; NULL: all fp32).
+ * lr >= 0; lr_factor: one device fp32 that multiplies lr (a schedule inside a captured graph), NULL: 1.
+ * max_norm > 0: c = min(1, max_norm / norm) with the norm of all gradients together; infinity: none are scaled, but the norm is
+ * looked at.  Where it is not finite (|G| beyond 1.8e19 counts as that) the whole step is left out (P, copies, states and number of steps stay as they
+ * are) and the next sync_status tells.  max_norm = 0: c = 1, and a NaN or infinity goes into P.
+ * norm_out: one device fp32, the norm before clipping; with max_norm > 0, NULL: not kept.  Gradients may not overlap P, copies
+ * or the workspace. */
+fw_status fw_adamw_step(fw_adamw* a, const void* const* G, const int32_t* g_dtype, float lr, const float* lr_factor,
+                        float max_norm, float* norm_out);
+/* Address and size of a part of the workspace, to be read or written between steps by work on the stream of `a` (checkpoints).
+ * Tensors follow one another, each from a multiple of 256 elements on, zeros behind its last. */
+typedef enum {
+  FW_A_M = 0, FW_A_V = 1,              /* fp32: m, v;  e4m3: codes of m and of sqrt(v)           */
+  FW_A_M_SCALE = 2, FW_A_V_SCALE = 3,  /* e4m3: scales, a byte b for each 256 elements: 2^(b - 127)  */
+  FW_A_STEP = 4                        /* int64: steps taken                                     */
+} fw_adamw_field;
+fw_status fw_adamw_state(fw_adamw* a, int32_t field, void** address, size_t* bytes);
+/* Waits for the stream; FW_WARN_NONFINITE if a step has been left out since the last call. */
+fw_status fw_adamw_sync_status(fw_adamw* a);
+
 /* State access (checkpointing, injecting a covariance, parity checks).
  * Matrices are M x M fp32 row-major, vectors M fp32, FW_F_LAMBDA_BAR one fp32.
  * Copies run on the layer's stream.  Setting FW_F_PHIX marks Phi_y stale, sets

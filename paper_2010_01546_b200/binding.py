@@ -39,9 +39,12 @@ EXPORTS = [
     "fw_distill_desc_default", "fw_distill_forward", "fw_distill_backward",
     "fw_gated_desc_default", "fw_gated_workspace_bytes", "fw_gated_create", "fw_gated_destroy", "fw_gated_forward",
     "fw_gated_backward", "fw_gated_sync_status",
+    "fw_adamw_desc_default", "fw_adamw_workspace_bytes", "fw_adamw_create", "fw_adamw_destroy", "fw_adamw_step", "fw_adamw_state",
+    "fw_adamw_sync_status",
 ]
 FW_STATIC_MAX_M = 256
 FW_ACT_SILU, FW_ACT_GELU, FW_ACT_GELU_TANH, FW_ACT_RELU = range(4)
+FW_A_M, FW_A_V, FW_A_M_SCALE, FW_A_V_SCALE, FW_A_STEP = range(5)
 FW_PROF_NAMES = ["pilot", "gram", "moments", "resync", "recur_mv", "recur_upd", "smooth", "gq", "misc", "recur_chip"]
 
 
@@ -70,6 +73,10 @@ class fw_distill_desc(C.Structure):
 class fw_gated_desc(C.Structure):
     _fields_ = [("M", C.c_int32), ("N", C.c_int32), ("x_dtype", C.c_int32), ("act", C.c_int32), ("grad", C.c_int32),
                 ("max_rows", C.c_int64)]
+
+
+class fw_adamw_desc(C.Structure):
+    _fields_ = [("n", C.c_int32), ("state", C.c_int32), ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_float), ("seed", C.c_uint32)]
 
 
 _LIB = None
@@ -145,6 +152,13 @@ def _lib():
     lib.fw_gated_backward.argtypes = [vp, vp, i64, i64, vp, i64, vp, vp, i64, vp, vp, i64, vp, i64, vp, vp, i32, vp, vp]
     lib.fw_gated_backward.restype = i32
     lib.fw_gated_sync_status.argtypes = [vp]; lib.fw_gated_sync_status.restype = i32
+    lib.fw_adamw_desc_default.argtypes = [P(fw_adamw_desc), i32]; lib.fw_adamw_desc_default.restype = None
+    lib.fw_adamw_workspace_bytes.argtypes = [P(fw_adamw_desc), P(i64)]; lib.fw_adamw_workspace_bytes.restype = sz
+    lib.fw_adamw_create.argtypes = [P(fw_adamw_desc), P(i64), P(vp), P(vp), P(f32), vp, sz, vp, P(vp)]; lib.fw_adamw_create.restype = i32
+    lib.fw_adamw_destroy.argtypes = [vp]; lib.fw_adamw_destroy.restype = i32
+    lib.fw_adamw_step.argtypes = [vp, P(vp), P(i32), f32, vp, f32, vp]; lib.fw_adamw_step.restype = i32
+    lib.fw_adamw_state.argtypes = [vp, i32, P(vp), P(sz)]; lib.fw_adamw_state.restype = i32
+    lib.fw_adamw_sync_status.argtypes = [vp]; lib.fw_adamw_sync_status.restype = i32
     _LIB = lib
     return lib
 
@@ -614,3 +628,99 @@ class Gated:
 
     def sync_status(self):
         return _check(_lib().fw_gated_sync_status(self.handle), "fw_gated_sync_status")
+
+
+class _Grads:
+    """Gradients that an AdamW has looked at: their addresses and types, and the tensors, which stay."""
+
+    def __init__(self, owner, tensors, pointers, kinds):
+        self.owner, self.tensors, self.pointers, self.kinds = owner, tensors, pointers, kinds
+
+
+class AdamW:
+    """AdamW over the fp32 tensors `params` of a network, over a workspace tensor of its own.  copies: None, or for each parameter
+    a bf16 tensor of its shape or None; decay: weight decay of each (one number: of all).  Methods look at their tensors and forward
+    to the C entry points fw_adamw_*.  Parameters and copies are kept; the stream outlives the object."""
+
+    def __init__(self, params, copies=None, decay=None, stream: int = 0, **desc_overrides):
+        import torch
+        params = list(params)
+        n = len(params)
+        copies = [None] * n if copies is None else list(copies)
+        decay = [float(decay or 0.0)] * n if decay is None or isinstance(decay, (int, float)) else [float(x) for x in decay]
+        if len(copies) != n or len(decay) != n:
+            raise ValueError(f"copies, decay: expected one for each of {n} parameters")
+        self.desc = fw_adamw_desc()
+        _lib().fw_adamw_desc_default(C.byref(self.desc), n)
+        _override(self.desc, desc_overrides)
+        if self.desc.n != n:
+            raise ValueError(f"n: {n} parameters are given")
+        dev = _here()
+        for i, (p, c) in enumerate(zip(params, copies)):
+            _vector(p, p.numel(), f"params[{i}]", dev)
+            if c is not None:
+                _vector(c, p.numel(), f"copies[{i}]", dev, FW_BF16)
+                if c.shape != p.shape:
+                    raise ValueError(f"copies[{i}]: expected {tuple(p.shape)}, got {tuple(c.shape)}")
+        self.params, self.copies = params, copies
+        sizes = (C.c_int64 * max(n, 1))(*[p.numel() for p in params])
+        self.nbytes = int(_lib().fw_adamw_workspace_bytes(C.byref(self.desc), sizes))
+        if self.nbytes == 0:
+            raise FwError(FW_ERR_INVALID_ARG, "fw_adamw_workspace_bytes")
+        self.workspace = torch.empty(self.nbytes + 256, dtype=torch.uint8, device="cuda")
+        out = C.c_void_p()
+        _check(_lib().fw_adamw_create(C.byref(self.desc), sizes, _vp_array(params), _vp_array(copies), (C.c_float * n)(*decay),
+                                      (self.workspace.data_ptr() + 255) // 256 * 256, self.nbytes, stream, C.byref(out)), "fw_adamw_create")
+        self.handle = out.value
+        # the memory is anybody's only when this stream is through with it too
+        self.workspace.record_stream(torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream())
+
+    def close(self):
+        if getattr(self, "handle", None):
+            _check(_lib().fw_adamw_destroy(self.handle), "fw_adamw_destroy")
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def grads(self, tensors):
+        """The gradients, one for each parameter, looked at once: buffers that are written again for every step need it once."""
+        tensors = list(tensors)
+        if len(tensors) != len(self.params):
+            raise ValueError(f"grads: expected {len(self.params)}, got {len(tensors)}")
+        dev, n = _here(), len(tensors)
+        pointers, kinds = (C.c_void_p * n)(), (C.c_int32 * n)()
+        half = _TYPES[FW_BF16]
+        for i, (t, p) in enumerate(zip(tensors, self.params)):
+            if t is None or t.shape != p.shape:
+                raise ValueError(f"grads[{i}]: expected {tuple(p.shape)}, got {None if t is None else tuple(t.shape)}")
+            kinds[i] = FW_BF16 if t.dtype is half else FW_F32
+            pointers[i] = _vector(t, p.numel(), f"grads[{i}]", dev, kinds[i])
+        return _Grads(self, tensors, pointers, kinds)
+
+    def step(self, grads, lr: float, lr_factor=None, max_norm: float = 0.0, norm_out=None):
+        """grads: a list of tensors, or what grads() gave for it."""
+        if not isinstance(grads, _Grads):
+            grads = self.grads(grads)
+        elif grads.owner is not self:
+            raise ValueError("grads: looked at by another AdamW")
+        dev = _here()
+        _check(_lib().fw_adamw_step(self.handle, grads.pointers, grads.kinds, lr, _vector(lr_factor, 1, "lr_factor", dev), max_norm,
+                                    _vector(norm_out, 1, "norm_out", dev)), "fw_adamw_step")
+
+    def state(self, field: int):
+        """A part of the workspace as a tensor (FW_A_*), for checkpoints: read or written between steps, on this object's stream."""
+        import torch
+        at, n = C.c_void_p(), C.c_size_t()
+        _check(_lib().fw_adamw_state(self.handle, field, C.byref(at), C.byref(n)), "fw_adamw_state")
+        first = at.value - self.workspace.data_ptr()
+        kind = (torch.int64 if field == FW_A_STEP else torch.float8_e8m0fnu if field in (FW_A_M_SCALE, FW_A_V_SCALE)
+                else torch.float32 if self.desc.state == FW_F32 else torch.float8_e4m3fn)
+        return self.workspace[first:first + n.value].view(kind)
+
+    def sync_status(self) -> int:
+        """FW_OK, or FW_WARN_NONFINITE where a step has been left out; raises on errors."""
+        return _check(_lib().fw_adamw_sync_status(self.handle), "fw_adamw_sync_status", allow=(FW_WARN_NONFINITE,))
