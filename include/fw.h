@@ -440,6 +440,75 @@ fw_status fw_distill_backward(const fw_distill_desc* d, const void* Z, int64_t r
                               const void* I, const float* t_lse, const float* weight, const float* stat, void* dZ,
                               int64_t lddz, void* cuda_stream);
 
+/* Log-probabilities of given classes (sampled tokens), and the gradient that comes back through them to the logits:
+ *   logp = Z_id / tau - log sum exp(Z / tau),  dZ_j = dlogp / tau ([j = id] - q_j),  q = softmax(Z / tau)
+ *   Z, dZ   rows x V, z_dtype; dZ may be Z (same address and ld), no other overlap
+ *   id      rows classes (index_bits 32 or 64, signed).  A class outside [0, V) marks a row that does not count (a prompt's
+ *           token, padding): it is not read, and its logp, stat and dZ are 0.
+ *   stat    rows x 2: the largest logit, and the sum of exp((Z - largest) / tau) over the classes other than id (so that a class
+ *           with almost all of the mass keeps what is left of it); NULL in the forward call: not kept
+ *   dlogp   rows; where it is 0 the row is not read and its dZ is 0
+ * Logits of -inf have no mass (a mask): gradient 0; the logp of such a class is -inf.  A row in which no class has mass gives
+ * logp, stat and gradient 0.  The lowest finite value is a logit like any other.  A NaN in a row, or +inf, makes that row's
+ * logp and gradient NaN.  Rows need not be aligned; where Z and dZ lie equally past a 16-byte boundary in each row, 16 bytes
+ * move at a time (16 bytes that hold an element may be read whole: up to 15 bytes before and behind a matrix are read, never used).
+ * 1 <= V <= 2^20, rows < 2^28. */
+typedef struct {
+  int32_t V;
+  int32_t z_dtype;      /* FW_F32 or FW_BF16                                      */
+  int32_t index_bits;   /* 32 or 64                                               */
+  float tau;            /* 1e-6 to 1e6                                            */
+} fw_logprob_desc;
+/* bf16 logits, 32-bit classes, tau 1 */
+void fw_logprob_desc_default(fw_logprob_desc* d, int32_t V);
+fw_status fw_logprob_forward(const fw_logprob_desc* d, const void* Z, int64_t rows, int64_t ldz, const void* id, float* logp,
+                             float* stat, void* cuda_stream);
+fw_status fw_logprob_backward(const fw_logprob_desc* d, const void* Z, int64_t rows, int64_t ldz, const void* id,
+                              const float* stat, const float* dlogp, void* dZ, int64_t lddz, void* cuda_stream);
+
+/* Clipped policy loss of sampled tokens with a KL term against a reference model: fw_logprob_forward with a loss over each
+ * row's logp,
+ *   r = exp(logp - logp_old),  k = logp_ref - logp
+ *   loss = weight [-min(r adv, clip(r, 1 - clip_low, 1 + clip_high) adv) + kl (exp(k) - 1 - k)]
+ *   dlogp = weight [-(r adv where the first of the two is the smaller or equal, else 0) - kl (exp(k) - 1)]
+ * and, with dZ, the gradient for the logits from the same pass over Z.  Without dZ it follows from fw_logprob_backward with
+ * the stat and dlogp of this call.
+ *   logp_old, adv, loss   rows;   logp_ref   rows, NULL: no KL term (kl has to be 0);   weight   rows, NULL: 1
+ *   logp, stat, dlogp     NULL: not kept
+ * A row in which no class has mass gives loss and dlogp 0.  A row of weight 0, like one whose class is outside [0, V), is not read: its loss, logp, stat, dlogp and dZ are 0. */
+typedef struct {
+  float clip_low;       /* 0 <= clip_low < 1                                      */
+  float clip_high;      /* >= 0; infinity: no bound                               */
+  float kl;             /* finite                                                 */
+} fw_policy_desc;
+/* clip_low = clip_high = 0.2, kl 0 */
+void fw_policy_desc_default(fw_policy_desc* p);
+fw_status fw_policy_forward(const fw_logprob_desc* d, const fw_policy_desc* p, const void* Z, int64_t rows, int64_t ldz,
+                            const void* id, const float* logp_old, const float* logp_ref, const float* adv, const float* weight,
+                            float* loss, float* logp, float* stat, float* dlogp, void* dZ, int64_t lddz, void* cuda_stream);
+
+/* Preference loss of pairs of answers from their tokens' log-probabilities (fw_logprob_forward; its gradient goes on through
+ * fw_logprob_backward).  Answer s has the rows seq[s] ... seq[s + 1] - 1; answer 2 i is the preferred one of pair i, 2 i + 1 the other.
+ *   sums_s = sum of logp over the answer's rows that count (id inside [0, V); id NULL: all), divided by their number with mean
+ *   h = beta ((sums_2i - ref_2i) - (sums_2i+1 - ref_2i+1)) - margin
+ *   loss_i = weight_i ((1 - smooth) log(1 + exp(-h)) + smooth log(1 + exp(h))),  dlogp = d loss / d logp
+ *   logp, dlogp  rows;  seq  2 pairs + 1 (32 bits), not decreasing, within [0, rows] (what lies outside is taken to the border; a device-side
+ *   value, no error);  ref  2 pairs (the same sums of a reference model), NULL: 0;  weight  pairs, NULL: 1
+ *   loss  pairs;  sums  2 pairs, NULL: not kept;  dlogp NULL: not wanted.  Rows that belong to no answer, or that do not count, get
+ *   dlogp 0.  An answer without rows that count has the sum 0.
+ * Of d the classes (V, index_bits) alone are looked at.  1 <= pairs <= 2^24, 1 <= rows < 2^28. */
+typedef struct {
+  float beta;           /* > 0, finite                                            */
+  float margin;         /* finite                                                 */
+  float smooth;         /* 0 <= smooth < 1                                        */
+  int32_t mean;         /* 1: sums by the number of rows                          */
+} fw_preference_desc;
+/* beta 0.1, margin 0, smooth 0, mean 0 */
+void fw_preference_desc_default(fw_preference_desc* p);
+fw_status fw_preference_loss(const fw_logprob_desc* d, const fw_preference_desc* p, const float* logp, int64_t rows,
+                             const void* id, const int32_t* seq, int32_t pairs, const float* ref, const float* weight,
+                             float* loss, float* sums, float* dlogp, void* cuda_stream);
+
 /* AdamW over all tensors of a network in one launch (two with clipping): what fw_step and fw_step_momentum are to SGD.  Step t,
  * with a gradient G times the clipping factor c:
  *   m <- beta1 m + (1 - beta1) c G,  v <- beta2 v + (1 - beta2) (c G)^2

@@ -39,6 +39,8 @@ EXPORTS = [
     "fw_distill_desc_default", "fw_distill_forward", "fw_distill_backward",
     "fw_gated_desc_default", "fw_gated_workspace_bytes", "fw_gated_create", "fw_gated_destroy", "fw_gated_forward",
     "fw_gated_backward", "fw_gated_sync_status",
+    "fw_logprob_desc_default", "fw_logprob_forward", "fw_logprob_backward", "fw_policy_desc_default", "fw_policy_forward",
+    "fw_preference_desc_default", "fw_preference_loss",
     "fw_adamw_desc_default", "fw_adamw_workspace_bytes", "fw_adamw_create", "fw_adamw_destroy", "fw_adamw_step", "fw_adamw_state",
     "fw_adamw_sync_status",
 ]
@@ -73,6 +75,18 @@ class fw_distill_desc(C.Structure):
 class fw_gated_desc(C.Structure):
     _fields_ = [("M", C.c_int32), ("N", C.c_int32), ("x_dtype", C.c_int32), ("act", C.c_int32), ("grad", C.c_int32),
                 ("max_rows", C.c_int64)]
+
+
+class fw_logprob_desc(C.Structure):
+    _fields_ = [("V", C.c_int32), ("z_dtype", C.c_int32), ("index_bits", C.c_int32), ("tau", C.c_float)]
+
+
+class fw_policy_desc(C.Structure):
+    _fields_ = [("clip_low", C.c_float), ("clip_high", C.c_float), ("kl", C.c_float)]
+
+
+class fw_preference_desc(C.Structure):
+    _fields_ = [("beta", C.c_float), ("margin", C.c_float), ("smooth", C.c_float), ("mean", C.c_int32)]
 
 
 class fw_adamw_desc(C.Structure):
@@ -152,6 +166,15 @@ def _lib():
     lib.fw_gated_backward.argtypes = [vp, vp, i64, i64, vp, i64, vp, vp, i64, vp, vp, i64, vp, i64, vp, vp, i32, vp, vp]
     lib.fw_gated_backward.restype = i32
     lib.fw_gated_sync_status.argtypes = [vp]; lib.fw_gated_sync_status.restype = i32
+    lib.fw_logprob_desc_default.argtypes = [P(fw_logprob_desc), i32]; lib.fw_logprob_desc_default.restype = None
+    lib.fw_logprob_forward.argtypes = [P(fw_logprob_desc), vp, i64, i64, vp, vp, vp, vp]; lib.fw_logprob_forward.restype = i32
+    lib.fw_logprob_backward.argtypes = [P(fw_logprob_desc), vp, i64, i64, vp, vp, vp, vp, i64, vp]; lib.fw_logprob_backward.restype = i32
+    lib.fw_policy_desc_default.argtypes = [P(fw_policy_desc)]; lib.fw_policy_desc_default.restype = None
+    lib.fw_policy_forward.argtypes = [P(fw_logprob_desc), P(fw_policy_desc), vp, i64, i64, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, i64, vp]
+    lib.fw_policy_forward.restype = i32
+    lib.fw_preference_desc_default.argtypes = [P(fw_preference_desc)]; lib.fw_preference_desc_default.restype = None
+    lib.fw_preference_loss.argtypes = [P(fw_logprob_desc), P(fw_preference_desc), vp, i64, vp, vp, i32, vp, vp, vp, vp, vp, vp]
+    lib.fw_preference_loss.restype = i32
     lib.fw_adamw_desc_default.argtypes = [P(fw_adamw_desc), i32]; lib.fw_adamw_desc_default.restype = None
     lib.fw_adamw_workspace_bytes.argtypes = [P(fw_adamw_desc), P(i64)]; lib.fw_adamw_workspace_bytes.restype = sz
     lib.fw_adamw_create.argtypes = [P(fw_adamw_desc), P(i64), P(vp), P(vp), P(f32), vp, sz, vp, P(vp)]; lib.fw_adamw_create.restype = i32
@@ -497,6 +520,64 @@ def fw_distill_backward(desc: fw_distill_desc, Z, T, I, stat, dZ, t_lse=None, we
                                       _vector(I, rows * K, "I", dev, "int64" if desc.index_bits == 64 else "int32"),
                                       _vector(t_lse, rows, "t_lse", dev), _vector(weight, rows, "weight", dev),
                                       _vector(stat, 2 * rows, "stat", dev), pd, lddz, stream), "fw_distill_backward")
+
+
+def fw_logprob_desc_default(V: int, **overrides) -> fw_logprob_desc:
+    d = fw_logprob_desc()
+    _lib().fw_logprob_desc_default(C.byref(d), V)
+    return _override(d, overrides)
+
+
+def _classes(desc, id, rows, dev):
+    return _vector(id, rows, "id", dev, "int64" if desc.index_bits == 64 else "int32")
+
+
+def fw_logprob_forward(desc: fw_logprob_desc, Z, id, logp, stat=None, stream: int = 0) -> None:
+    rows, dev = Z.shape[0], _here()
+    pz, ldz = _matrix(Z, rows, desc.V, desc.z_dtype, "Z", dev)
+    _check(_lib().fw_logprob_forward(C.byref(desc), pz, rows, ldz, _classes(desc, id, rows, dev), _vector(logp, rows, "logp", dev),
+                                     _vector(stat, 2 * rows, "stat", dev), stream), "fw_logprob_forward")
+
+
+def fw_logprob_backward(desc: fw_logprob_desc, Z, id, stat, dlogp, dZ, stream: int = 0) -> None:
+    rows, dev = Z.shape[0], _here()
+    pz, ldz = _matrix(Z, rows, desc.V, desc.z_dtype, "Z", dev)
+    pd, lddz = _matrix(dZ, rows, desc.V, desc.z_dtype, "dZ", dev)
+    _check(_lib().fw_logprob_backward(C.byref(desc), pz, rows, ldz, _classes(desc, id, rows, dev), _vector(stat, 2 * rows, "stat", dev),
+                                      _vector(dlogp, rows, "dlogp", dev), pd, lddz, stream), "fw_logprob_backward")
+
+
+def fw_policy_desc_default(**overrides) -> fw_policy_desc:
+    p = fw_policy_desc()
+    _lib().fw_policy_desc_default(C.byref(p))
+    return _override(p, overrides)
+
+
+def fw_policy_forward(desc: fw_logprob_desc, policy: fw_policy_desc, Z, id, logp_old, adv, loss, logp_ref=None, weight=None, logp=None,
+                      stat=None, dlogp=None, dZ=None, stream: int = 0) -> None:
+    rows, dev = Z.shape[0], _here()
+    pz, ldz = _matrix(Z, rows, desc.V, desc.z_dtype, "Z", dev)
+    pd, lddz = _matrix(dZ, rows, desc.V, desc.z_dtype, "dZ", dev)
+    v = lambda t, name: _vector(t, rows, name, dev)  # noqa: E731
+    _check(_lib().fw_policy_forward(C.byref(desc), C.byref(policy), pz, rows, ldz, _classes(desc, id, rows, dev), v(logp_old, "logp_old"),
+                                    v(logp_ref, "logp_ref"), v(adv, "adv"), v(weight, "weight"), v(loss, "loss"), v(logp, "logp"),
+                                    _vector(stat, 2 * rows, "stat", dev), v(dlogp, "dlogp"), pd, lddz, stream), "fw_policy_forward")
+
+
+def fw_preference_desc_default(**overrides) -> fw_preference_desc:
+    p = fw_preference_desc()
+    _lib().fw_preference_desc_default(C.byref(p))
+    return _override(p, overrides)
+
+
+def fw_preference_loss(desc: fw_logprob_desc, preference: fw_preference_desc, logp, id, seq, loss, ref=None, weight=None, sums=None,
+                       dlogp=None, stream: int = 0) -> None:
+    rows, pairs, dev = logp.numel(), loss.numel(), _here()
+    _check(_lib().fw_preference_loss(C.byref(desc), C.byref(preference), _vector(logp, rows, "logp", dev), rows,
+                                     _classes(desc, id, rows, dev), _vector(seq, 2 * pairs + 1, "seq", dev, "int32"), pairs,
+                                     _vector(ref, 2 * pairs, "ref", dev), _vector(weight, pairs, "weight", dev),
+                                     _vector(loss, pairs, "loss", dev), _vector(sums, 2 * pairs, "sums", dev),
+                                     _vector(dlogp, rows, "dlogp", dev), stream), "fw_preference_loss")
 
 
 # ---- convenience: a layer that owns its workspace tensor -------------------

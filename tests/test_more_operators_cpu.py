@@ -20,6 +20,85 @@ def table(kind, values):
     return (kind * len(values))(*values)
 
 
+def logprob(lib, d, what="fwd", rows=4, Z=A, ldz=104, id=2 * A, logp=3 * A, stat=4 * A, dlogp=5 * A, dZ=6 * A, lddz=104):
+    if what == "fwd":
+        return lib.fw_logprob_forward(C.byref(d), Z, rows, ldz, id, logp, stat, None)
+    return lib.fw_logprob_backward(C.byref(d), Z, rows, ldz, id, stat, dlogp, dZ, lddz, None)
+
+
+def policy(lib, d, p, rows=4, Z=A, ldz=104, id=2 * A, old=7 * A, ref=None, adv=8 * A, w=None, loss=9 * A, logp=3 * A, stat=4 * A, dlogp=5 * A,
+           dZ=6 * A, lddz=104):
+    return lib.fw_policy_forward(C.byref(d), C.byref(p) if p is not None else None, Z, rows, ldz, id, old, ref, adv, w, loss, logp, stat, dlogp,
+                                 dZ, lddz, None)
+
+
+def test_logprob_and_policy_refusals(lib):
+    inv, shape = B.FW_ERR_INVALID_ARG, B.FW_ERR_SHAPE
+    d, p = B.fw_logprob_desc_default(100), B.fw_policy_desc_default()
+    assert (d.z_dtype, d.index_bits, d.tau) == (B.FW_BF16, 32, 1.0) and (p.clip_low, p.clip_high, p.kl) == pytest.approx((0.2, 0.2, 0.0))
+    calls = (lambda d, **kw: logprob(lib, d, **kw), lambda d, **kw: logprob(lib, d, "bwd", **kw), lambda d, **kw: policy(lib, d, p, **kw))
+    for call in calls:
+        for kw in (dict(z_dtype=B.FW_E4M3), dict(index_bits=16), dict(tau=0.0), dict(tau=float("nan")), dict(tau=1e7)):
+            assert call(B.fw_logprob_desc_default(100, **kw)) == inv, kw
+        for V in (0, -1, (1 << 20) + 1):
+            assert call(B.fw_logprob_desc_default(V), ldz=1 << 21) == shape, V
+        for kw in (dict(Z=None), dict(id=None), dict(Z=A + 1), dict(id=2 * A + 2), dict(stat=4 * A + 2)):
+            assert call(d, **kw) == inv, kw
+        for kw in (dict(rows=0), dict(rows=-1), dict(rows=1 << 28), dict(ldz=99), dict(ldz=(1 << 30) + 1)):
+            assert call(d, **kw) == shape, kw
+        assert call(B.fw_logprob_desc_default(100, index_bits=64), id=2 * A + 4) == inv
+    assert lib.fw_logprob_forward(None, A, 4, 104, 2 * A, 3 * A, None, None) == inv
+    for kw in (dict(logp=None), dict(logp=A), dict(logp=2 * A + 8), dict(stat=3 * A + 8)):
+        assert logprob(lib, d, **kw) == inv, kw
+    for kw in (dict(stat=None), dict(dlogp=None), dict(dZ=None), dict(dZ=A + 208), dict(dZ=A, lddz=112), dict(dZ=2 * A), dict(dZ=5 * A), dict(dZ=4 * A)):
+        assert logprob(lib, d, "bwd", **kw) == inv, kw
+    assert logprob(lib, d, "bwd", lddz=99) == shape and policy(lib, d, p, lddz=99) == shape
+    for kw in (dict(old=None), dict(adv=None), dict(loss=None), dict(loss=7 * A), dict(w=5 * A), dict(logp=9 * A + 8), dict(dlogp=8 * A), dict(old=7 * A + 1),
+               dict(dZ=A, lddz=112), dict(dZ=8 * A), dict(ref=9 * A)):
+        assert policy(lib, d, p, **kw) == inv, kw
+    for kw in (dict(clip_low=-0.1), dict(clip_low=1.0), dict(clip_high=-0.1), dict(clip_high=float("nan")), dict(kl=float("inf")), dict(kl=0.1)):
+        assert policy(lib, d, B.fw_policy_desc_default(**kw)) == inv, kw                # (kl without logp_ref)
+    assert policy(lib, d, None) == inv
+
+
+def test_preference_refusals(lib):
+    inv, shape = B.FW_ERR_INVALID_ARG, B.FW_ERR_SHAPE
+
+    def call(d=None, p=None, logp=A, rows=100, id=2 * A, seq=3 * A, pairs=4, ref=None, w=None, loss=4 * A, sums=5 * A, dlogp=6 * A):
+        d, p = d or B.fw_logprob_desc_default(50), p or B.fw_preference_desc_default()
+        return lib.fw_preference_loss(C.byref(d), C.byref(p), logp, rows, id, seq, pairs, ref, w, loss, sums, dlogp, None)
+
+    p = B.fw_preference_desc_default()
+    assert (p.beta, p.margin, p.smooth, p.mean) == (pytest.approx(0.1), 0.0, 0.0, 0)
+    for kw in (dict(beta=0.0), dict(beta=float("inf")), dict(margin=float("nan")), dict(smooth=1.0), dict(smooth=-0.1), dict(mean=2)):
+        assert call(p=B.fw_preference_desc_default(**kw)) == inv, kw
+    for kw in (dict(logp=None), dict(seq=None), dict(loss=None), dict(seq=3 * A + 2), dict(loss=A), dict(dlogp=A), dict(sums=4 * A + 8), dict(ref=5 * A),
+               dict(w=4 * A), dict(dlogp=2 * A), dict(id=2 * A + 1), dict(loss=3 * A + 32)):
+        assert call(**kw) == inv, kw
+    for kw in (dict(rows=0), dict(rows=1 << 28), dict(pairs=0), dict(pairs=(1 << 24) + 1)):
+        assert call(**kw) == shape, kw
+    assert call(d=B.fw_logprob_desc_default(50, index_bits=8)) == inv and call(d=B.fw_logprob_desc_default(0)) == shape
+    assert lib.fw_preference_loss(None, C.byref(p), A, 4, None, A, 1, None, None, A, None, None, None) == inv
+
+
+def test_tensors_of_the_losses_are_looked_at():
+    import torch
+    d = B.fw_logprob_desc_default(8)
+    Z, id, v = torch.zeros(2, 8, dtype=torch.bfloat16), torch.zeros(2, dtype=torch.int32), torch.zeros(2)
+    with pytest.raises(ValueError, match="CUDA"):
+        B.fw_logprob_forward(d, Z, id, v)
+    with pytest.raises(TypeError):
+        B.fw_logprob_forward(d, Z.float(), id, v)
+    with pytest.raises(ValueError, match="expected"):
+        B.fw_logprob_forward(d, Z[:, :7], id, v)
+    with pytest.raises(TypeError, match="temperature"):
+        B.fw_logprob_desc_default(8, temperature=2.0)
+    with pytest.raises(TypeError, match="clip"):
+        B.fw_policy_desc_default(clip=0.2)
+    with pytest.raises(TypeError, match="gamma"):
+        B.fw_preference_desc_default(gamma=0.2)
+
+
 def test_adamw_refusals(lib):
     inv, shape, ws = B.FW_ERR_INVALID_ARG, B.FW_ERR_SHAPE, B.FW_ERR_WORKSPACE
     D = 1 << 40                          # of the workspace
