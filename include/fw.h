@@ -440,6 +440,44 @@ fw_status fw_distill_backward(const fw_distill_desc* d, const void* Z, int64_t r
                               const void* I, const float* t_lse, const float* weight, const float* stat, void* dZ,
                               int64_t lddz, void* cuda_stream);
 
+/* Norms around a block with its gate and the residual addition between them, in one pass: the norm behind a block's
+ * output o, the residual stream x, and the norm before the next block,
+ *   n1 = o rstd1, rstd1 = 1 / sqrt(mean(o^2) + eps)     (post = 0: n1 = o, rstd1 = 1)
+ *   h  = alpha x + gate w_post n1, rounded to `dtype`
+ *   y  = h rstd2 w_pre, rstd2 = 1 / sqrt(mean(h^2) + eps); of `dtype`, or e4m3 with a scale for each row as in
+ *        fw_rmsnorm_forward
+ * o, x, h: rows x M of `dtype`; w_post (NULL: 1; a layer scale goes here), w_pre: M fp32; gate: a number for each row (a
+ * router's weight), rows fp32, NULL: 1; rstd: rows x 2 fp32 (rstd1, rstd2), NULL: not kept; y_scale: rows, with e4m3 and only then.
+ * h and y may be o or x itself (same address, type and ld; not the same one); any other overlap of outputs with
+ * inputs or with each other is FW_ERR_INVALID_ARG.  What holds for the rows of fw_rmsnorm_forward holds here: NaN, infinity,
+ * squares that pass fp32, M <= 16384. */
+typedef struct {
+  int32_t M;
+  int32_t dtype;     /* fw_dtype of o, x, h: FW_F32 or FW_BF16                     */
+  int32_t y_dtype;   /* dtype, or FW_E4M3 (forward)                              */
+  int32_t post;      /* 1: o is normalised                                       */
+  float eps;         /* > 0                                                      */
+  float alpha;       /* finite                                                   */
+} fw_sandwich_desc;
+/* bf16 in and out, post 1, eps 1e-6, alpha 1 */
+void fw_sandwich_desc_default(fw_sandwich_desc* d, int32_t M);
+fw_status fw_sandwich_forward(const fw_sandwich_desc* d, int64_t rows, const void* o, int64_t ldo, const void* x, int64_t ldx,
+                              const float* w_post, const float* gate, const float* w_pre, void* h, int64_t ldh, void* y,
+                              int64_t ldy, float* y_scale, float* rstd, void* cuda_stream);
+/* From dy (the gradient of y), dh (the gradient that reaches h by itself; NULL: none) and the forward call's o, h, rstd:
+ *   u2 = dy w_pre, n2 = h rstd2, t = rstd2 (u2 - n2 mean(u2 n2)) + dh
+ *   dx = alpha t
+ *   u1 = t w_post, n1 = o rstd1, do = gate rstd1 (u1 - n1 mean(u1 n1))     (post = 0: do = gate u1)
+ *   dw_pre = sum over rows of dy n2, dw_post = sum over rows of gate t n1, dgate = sum over a row of u1 n1
+ * dy, dh, o, h, dx, do: rows x M of `dtype`.  dw_pre, dw_post: M fp32, dgate: rows fp32, overwritten; NULL: not wanted.
+ * scratch: with dw_pre or dw_post; caller-owned, 256-byte aligned, at least fw_sandwich_scratch_bytes(d) bytes, free again when
+ * the call's work is done.  dx may be dy, dh or h itself, d_o dy, dh, o or h (not the same one). */
+size_t fw_sandwich_scratch_bytes(const fw_sandwich_desc* d);
+fw_status fw_sandwich_backward(const fw_sandwich_desc* d, int64_t rows, const void* dy, int64_t lddy, const void* dh, int64_t lddh,
+                               const void* o, int64_t ldo, const void* h, int64_t ldh, const float* w_post, const float* gate,
+                               const float* w_pre, const float* rstd, void* dx, int64_t lddx, void* d_o, int64_t lddo,
+                               float* dw_post, float* dw_pre, float* dgate, void* scratch, size_t scratch_bytes, void* cuda_stream);
+
 /* Log-probabilities of given classes (sampled tokens), and the gradient that comes back through them to the logits:
  *   logp = Z_id / tau - log sum exp(Z / tau),  dZ_j = dlogp / tau ([j = id] - q_j),  q = softmax(Z / tau)
  *   Z, dZ   rows x V, z_dtype; dZ may be Z (same address and ld), no other overlap

@@ -39,6 +39,7 @@ EXPORTS = [
     "fw_distill_desc_default", "fw_distill_forward", "fw_distill_backward",
     "fw_gated_desc_default", "fw_gated_workspace_bytes", "fw_gated_create", "fw_gated_destroy", "fw_gated_forward",
     "fw_gated_backward", "fw_gated_sync_status",
+    "fw_sandwich_desc_default", "fw_sandwich_scratch_bytes", "fw_sandwich_forward", "fw_sandwich_backward",
     "fw_logprob_desc_default", "fw_logprob_forward", "fw_logprob_backward", "fw_policy_desc_default", "fw_policy_forward",
     "fw_preference_desc_default", "fw_preference_loss",
     "fw_adamw_desc_default", "fw_adamw_workspace_bytes", "fw_adamw_create", "fw_adamw_destroy", "fw_adamw_step", "fw_adamw_state",
@@ -75,6 +76,10 @@ class fw_distill_desc(C.Structure):
 class fw_gated_desc(C.Structure):
     _fields_ = [("M", C.c_int32), ("N", C.c_int32), ("x_dtype", C.c_int32), ("act", C.c_int32), ("grad", C.c_int32),
                 ("max_rows", C.c_int64)]
+
+
+class fw_sandwich_desc(C.Structure):
+    _fields_ = [("M", C.c_int32), ("dtype", C.c_int32), ("y_dtype", C.c_int32), ("post", C.c_int32), ("eps", C.c_float), ("alpha", C.c_float)]
 
 
 class fw_logprob_desc(C.Structure):
@@ -166,6 +171,13 @@ def _lib():
     lib.fw_gated_backward.argtypes = [vp, vp, i64, i64, vp, i64, vp, vp, i64, vp, vp, i64, vp, i64, vp, vp, i32, vp, vp]
     lib.fw_gated_backward.restype = i32
     lib.fw_gated_sync_status.argtypes = [vp]; lib.fw_gated_sync_status.restype = i32
+    lib.fw_sandwich_desc_default.argtypes = [P(fw_sandwich_desc), i32]; lib.fw_sandwich_desc_default.restype = None
+    lib.fw_sandwich_scratch_bytes.argtypes = [P(fw_sandwich_desc)]; lib.fw_sandwich_scratch_bytes.restype = sz
+    lib.fw_sandwich_forward.argtypes = [P(fw_sandwich_desc), i64, vp, i64, vp, i64, vp, vp, vp, vp, i64, vp, i64, vp, vp, vp]
+    lib.fw_sandwich_forward.restype = i32
+    lib.fw_sandwich_backward.argtypes = [P(fw_sandwich_desc), i64, vp, i64, vp, i64, vp, i64, vp, i64, vp, vp, vp, vp, vp, i64, vp, i64, vp, vp, vp,
+                                         vp, sz, vp]
+    lib.fw_sandwich_backward.restype = i32
     lib.fw_logprob_desc_default.argtypes = [P(fw_logprob_desc), i32]; lib.fw_logprob_desc_default.restype = None
     lib.fw_logprob_forward.argtypes = [P(fw_logprob_desc), vp, i64, i64, vp, vp, vp, vp]; lib.fw_logprob_forward.restype = i32
     lib.fw_logprob_backward.argtypes = [P(fw_logprob_desc), vp, i64, i64, vp, vp, vp, vp, i64, vp]; lib.fw_logprob_backward.restype = i32
@@ -520,6 +532,49 @@ def fw_distill_backward(desc: fw_distill_desc, Z, T, I, stat, dZ, t_lse=None, we
                                       _vector(I, rows * K, "I", dev, "int64" if desc.index_bits == 64 else "int32"),
                                       _vector(t_lse, rows, "t_lse", dev), _vector(weight, rows, "weight", dev),
                                       _vector(stat, 2 * rows, "stat", dev), pd, lddz, stream), "fw_distill_backward")
+
+
+def fw_sandwich_desc_default(M: int, **overrides) -> fw_sandwich_desc:
+    d = fw_sandwich_desc()
+    _lib().fw_sandwich_desc_default(C.byref(d), M)
+    return _override(d, overrides)
+
+
+def fw_sandwich_scratch_bytes(desc: fw_sandwich_desc) -> int:
+    return int(_lib().fw_sandwich_scratch_bytes(C.byref(desc)))
+
+
+def fw_sandwich_forward(desc: fw_sandwich_desc, o, x, w_pre, h, y, w_post=None, gate=None, y_scale=None, rstd=None, stream: int = 0) -> None:
+    rows, M, t, dev = o.shape[0], desc.M, desc.dtype, _here()
+    po, ldo = _matrix(o, rows, M, t, "o", dev)
+    px, ldx = _matrix(x, rows, M, t, "x", dev)
+    ph, ldh = _matrix(h, rows, M, t, "h", dev)
+    py, ldy = _matrix(y, rows, M, desc.y_dtype, "y", dev)
+    _check(_lib().fw_sandwich_forward(C.byref(desc), rows, po, ldo, px, ldx, _vector(w_post, M, "w_post", dev), _vector(gate, rows, "gate", dev),
+                                      _vector(w_pre, M, "w_pre", dev), ph, ldh, py, ldy, _vector(y_scale, rows, "y_scale", dev),
+                                      _vector(rstd, 2 * rows, "rstd", dev), stream), "fw_sandwich_forward")
+
+
+def fw_sandwich_backward(desc: fw_sandwich_desc, dy, o, h, w_pre, rstd, dx, d_o, w_post=None, gate=None, dh=None, dw_post=None, dw_pre=None,
+                         dgate=None, scratch=None, stream: int = 0) -> None:
+    rows, M, t, dev = dy.shape[0], desc.M, desc.dtype, _here()
+    if scratch is not None and not scratch.is_contiguous():
+        raise ValueError("scratch: its bytes have to be contiguous")
+    pdy, lddy = _matrix(dy, rows, M, t, "dy", dev)
+    pdh, lddh = _matrix(dh, rows, M, t, "dh", dev)
+    po, ldo = _matrix(o, rows, M, t, "o", dev)
+    ph, ldh = _matrix(h, rows, M, t, "h", dev)
+    pdx, lddx = _matrix(dx, rows, M, t, "dx", dev)
+    pdo, lddo = _matrix(d_o, rows, M, t, "d_o", dev)
+    n = 0
+    if scratch is not None:
+        if scratch.get_device() != dev:
+            _refuse_device(scratch, dev, "scratch")
+        n = scratch.numel() * scratch.element_size()
+    _check(_lib().fw_sandwich_backward(C.byref(desc), rows, pdy, lddy, pdh, lddh, po, ldo, ph, ldh, _vector(w_post, M, "w_post", dev),
+                                       _vector(gate, rows, "gate", dev), _vector(w_pre, M, "w_pre", dev), _vector(rstd, 2 * rows, "rstd", dev),
+                                       pdx, lddx, pdo, lddo, _vector(dw_post, M, "dw_post", dev), _vector(dw_pre, M, "dw_pre", dev),
+                                       _vector(dgate, rows, "dgate", dev), _ptr(scratch), n, stream), "fw_sandwich_backward")
 
 
 def fw_logprob_desc_default(V: int, **overrides) -> fw_logprob_desc:

@@ -1,0 +1,516 @@
+// The norms behind a block and before the next one with the gate and the residual addition between them, forward and backward, a
+// row at a time.
+//
+//   n1 = o rstd1 (or o)      h = alpha x + k w_post n1, kept in the type of x      n2 = h rstd2      y = n2 w_pre
+//   e4m3 y: c = max |y| / 448, y is held as e4m3(y / c) with c beside it
+//
+//   u2 = dy w_pre     t = rstd2 (u2 - n2 mean(u2 n2)) + dh     dx = alpha t     dw_pre = sum over the rows of dy n2
+//   u1 = t w_post     do = k rstd1 (u1 - n1 mean(u1 n1)) (or k u1)     dw_post = sum over the rows of k t n1     dk = sum of u1 n1
+//
+// Both directions read each element once and write each result once: HBM bandwidth bounds them.  A row stays on chip between its two
+// sums, which depend on one another, so a CTA has the next rows on their way meanwhile.
+#include "fw_norm.cuh"
+
+namespace fw {
+namespace {
+
+using namespace norm;
+
+struct SandwichFwd {
+  const void *o, *x;
+  const float *w1, *gate, *w2;   // w_post or null, a number a row or null, w_pre
+  void *h, *y;
+  float *y_scale, *rstd;
+  int64_t rows, ldo, ldx, ldh, ldy;
+  int32_t M, width, post;
+  float eps, inv_M, alpha;
+};
+
+// As norm_forward_kernel: T is the type of o, x and h, Y of y; VEC elements an access, NV accesses a thread, SLOTS rows of a CTA on
+// their way, a row at a time.
+template <class T, class Y, int VEC, int NV, int SLOTS, int FILL>
+__global__ void __launch_bounds__(512) sandwich_forward_kernel(const SandwichFwd p) {
+  typedef Ahead<T, VEC, NV, FILL> Ring;
+  extern __shared__ __align__(16) uint8_t room[];            // [slot][o, x]
+  __shared__ float buf[2][3][16];
+  const int t = threadIdx.x, width = blockDim.x;
+  const uint32_t row_bytes = Ring::row_bytes(p.M, width, width), slot_bytes = row_bytes * 2;
+  const uint32_t base = (uint32_t)__cvta_generic_to_shared(room);
+  auto o_row = [&](int64_t row) { return static_cast<const T*>(p.o) + row * p.ldo; };
+  auto x_row = [&](int64_t row) { return static_cast<const T*>(p.x) + row * p.ldx; };
+  auto fetch = [&](int64_t row, int i) {
+    if (row < p.rows) {
+      Ring::fetch(base + i * slot_bytes, o_row(row), p.M, t, width);
+      Ring::fetch(base + i * slot_bytes + row_bytes, x_row(row), p.M, t, width);
+    }
+    ahead_commit();
+  };
+  dep_wait();
+#pragma unroll
+  for (int i = 0; i < SLOTS; ++i) fetch((int64_t)blockIdx.x + (int64_t)i * gridDim.x, i);
+  int i = 0, flip = 0;
+  for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x, flip ^= 1) {
+    const uint8_t* slot = room + i * slot_bytes;
+    const float k1 = p.gate ? p.gate[row] : 1.f;
+    ahead_wait<SLOTS - 1>();
+    if (VEC == 1) __syncthreads();
+    float v[NV][VEC];
+    const T *o = o_row(row), *x = x_row(row);
+    T* h = static_cast<T*>(p.h) + row * p.ldh;
+    float sq[2] = {0.f, 0.f};
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      const uint32_t c = (uint32_t)(t + k * width) * VEC;
+      Ring::get(slot, o, p.M, width, k, c, p.M - (int)c, v[k]);
+      vdot<VEC>(sq, v[k], v[k]);
+    }
+    float r1 = 1.f;
+    if (p.post) r1 = rsqrtf(fmaf(over_group<Sum>(sq[0] + sq[1], width, buf[flip][0]), p.inv_M, p.eps));
+    const float f = k1 * r1;
+    sq[0] = sq[1] = 0.f;
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      const uint32_t c = (uint32_t)(t + k * width) * VEC;
+      const int n = p.M - (int)c;
+      float a[VEC];
+      if (p.w1) {
+        Ring::plain(p.w1 + c, n, a);
+        vmul<VEC>(v[k], a);
+      }
+      vscale<VEC>(v[k], f);
+      Ring::get(slot + row_bytes, x, p.M, width, k, c, n, a);
+      vfma<VEC>(v[k], a, p.alpha);
+      round_pairs(v[k], static_cast<const T*>(nullptr));
+      Ring::keep(h + c, n, v[k]);
+      vdot<VEC>(sq, v[k], v[k]);
+    }
+    const float r2 = rsqrtf(fmaf(over_group<Sum>(sq[0] + sq[1], width, buf[flip][1]), p.inv_M, p.eps));
+    fetch(row + (int64_t)SLOTS * gridDim.x, i);              // the slot has been read: the sum of its threads depends on it
+    if (t == 0 && p.rstd) { p.rstd[2 * row] = r1; p.rstd[2 * row + 1] = r2; }
+    float top = 0.f;
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      const uint32_t c = (uint32_t)(t + k * width) * VEC;
+      float w[VEC];
+      Ring::plain(p.w2 + c, p.M - (int)c, w);
+      if (sizeof(Y) != 1) vscale<VEC>(v[k], r2);             // the scale takes rstd out of an 8-bit y again: y / c = 448 h w / max |h w|
+      vmul<VEC>(v[k], w);
+      if (sizeof(Y) == 1) {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) top = max_keep_nan(top, fabsf(v[k][e]));
+      }
+    }
+    float inv = 1.f;
+    if (sizeof(Y) == 1) {
+      top = over_group<MaxAbs>(top, width, buf[flip][2]);
+      float scale;
+      inv = row_scale(top, r2, &scale);
+      if (t == 0) p.y_scale[row] = scale;
+      if (by_size(top, r2)) {
+#pragma unroll
+        for (int k = 0; k < NV; ++k) vscale<VEC>(v[k], r2);
+      }
+    }
+    Y* y = static_cast<Y*>(p.y) + row * p.ldy;
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      const uint32_t c = (uint32_t)(t + k * width) * VEC;
+      if (sizeof(Y) == 1) vscale<VEC>(v[k], inv);
+      Ring::keep(y + c, p.M - (int)c, v[k]);
+    }
+    if (++i == SLOTS) i = 0;
+  }
+  ahead_wait<0>();
+  dep_trigger();
+}
+
+struct SandwichBwd {
+  const void *dy, *dh, *o, *h;
+  const float *w1, *gate, *w2, *rstd;
+  void *dx, *d_o;
+  float *part, *dgate;           // part: two rows of M sums for each CTA (dw_pre, dw_post), or null
+  int64_t rows, lddy, lddh, ldo, ldh, lddx, lddo;
+  int32_t M, width, post;
+  float inv_M, alpha;
+};
+
+// As norm_backward_kernel: a CTA takes every gridDim-th group of rows, a row at a time (SOLO) or several, and keeps its columns' shares of
+// dw_pre and dw_post in registers.  DIRECT: dh is read where it is needed: four rows of 64 KB do not fit a SM.
+template <class T, int VEC, int NV, int SLOTS, bool DH, int FILL, bool SOLO>
+__global__ void __launch_bounds__(512) sandwich_backward_kernel(const SandwichBwd p) {
+  typedef Ahead<T, VEC, NV, FILL> Ring;
+  constexpr bool DIRECT = DH && (VEC == 1 || NV == 8);
+  constexpr int ROOMS = DH && !DIRECT ? 4 : 3;
+  extern __shared__ __align__(16) uint8_t room[];            // [slot][dy, h, o, dh], at the end the groups' sums
+  __shared__ float buf[2][2][16];
+  const int tid = threadIdx.x, nt = blockDim.x, width = SOLO ? nt : p.width, t = SOLO ? tid : tid & (width - 1);
+  const int per = SOLO ? 1 : nt / width, mine = SOLO ? 0 : tid / width;
+  const int64_t step = (int64_t)gridDim.x * per;
+  const uint32_t row_bytes = Ring::row_bytes(p.M, nt, width), slot_bytes = row_bytes * ROOMS;
+  const uint32_t base = (uint32_t)__cvta_generic_to_shared(room);
+  auto u_row = [&](int64_t row) { return static_cast<const T*>(p.dy) + row * p.lddy; };
+  auto h_row = [&](int64_t row) { return static_cast<const T*>(p.h) + row * p.ldh; };
+  auto o_row = [&](int64_t row) { return static_cast<const T*>(p.o) + row * p.ldo; };
+  auto d_row = [&](int64_t row) { return static_cast<const T*>(p.dh) + row * p.lddh; };
+  auto fetch = [&](int64_t row, int i) {
+    if (row < p.rows) {
+      const uint32_t at = base + i * slot_bytes;
+      Ring::fetch(at, u_row(row), p.M, t, width);
+      Ring::fetch(at + row_bytes, h_row(row), p.M, t, width);
+      Ring::fetch(at + 2 * row_bytes, o_row(row), p.M, t, width);
+      if (ROOMS == 4) Ring::fetch(at + 3 * row_bytes, d_row(row), p.M, t, width);
+    }
+    ahead_commit();
+  };
+  struct Head { float r1, r2, k; };
+  auto head = [&](int64_t row) {
+    Head a = {0.f, 0.f, 0.f};
+    if (row < p.rows) a = {p.post ? p.rstd[2 * row] : 1.f, p.rstd[2 * row + 1], p.gate ? p.gate[row] : 1.f};
+    return a;
+  };
+  dep_wait();
+  float dw1[NV][VEC], dw2[NV][VEC];
+#pragma unroll
+  for (int k = 0; k < NV; ++k)
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) dw1[k][e] = dw2[k][e] = 0.f;
+  const int64_t first = (int64_t)blockIdx.x * per;
+#pragma unroll
+  for (int i = 0; i < SLOTS; ++i) fetch(first + mine + i * step, i);
+  Head a = head(first + mine);
+  int i = 0, flip = 0;
+  for (int64_t row0 = first; row0 < p.rows; row0 += step, flip ^= 1) {
+    const int64_t row = row0 + mine;
+    const bool live = SOLO || row < p.rows;
+    const Head next = head(row + step);
+    const uint8_t* slot = room + i * slot_bytes;
+    ahead_wait<SLOTS - 1>();
+    if (VEC == 1) __syncthreads();
+    float u[NV][VEC];
+    const T *dy = u_row(row), *h = h_row(row), *o = o_row(row), *dh = DH ? d_row(row) : nullptr;
+    float dots[2] = {0.f, 0.f};
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      const uint32_t c = (uint32_t)(t + k * width) * VEC;
+      const int left = live ? p.M - (int)c : 0;
+      float n[VEC], w[VEC];
+      Ring::get(slot, dy, p.M, width, k, c, left, u[k]);
+      Ring::get(slot + row_bytes, h, p.M, width, k, c, left, n);
+      Ring::plain(p.w2 + c, p.M - (int)c, w);
+      vscale<VEC>(n, a.r2);
+      vfma<VEC>(dw2[k], u[k], n);
+      vmul<VEC>(u[k], w);
+      vdot<VEC>(dots, u[k], n);
+    }
+    const float f2 = over_group<Sum>(dots[0] + dots[1], width, buf[flip][0]) * -p.inv_M * a.r2;
+    T* dx = static_cast<T*>(p.dx) + row * p.lddx;
+    dots[0] = dots[1] = 0.f;
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      const uint32_t c = (uint32_t)(t + k * width) * VEC;
+      const int left = live ? p.M - (int)c : 0;
+      float n[VEC], w[VEC];
+      Ring::get(slot + row_bytes, h, p.M, width, k, c, left, n);
+      vfma<VEC>(u[k], n, f2);                                // u2 - n2 mean(u2 n2)
+      vscale<VEC>(u[k], a.r2);
+      if (DH) {
+        if (DIRECT) load<VEC>(dh + c, FILL == ROW_PART ? left : left > 0 ? VEC : 0, 0.f, n);
+        else Ring::get(slot + 3 * row_bytes, dh, p.M, width, k, c, left, n);
+        vadd<VEC>(u[k], n);
+      }
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) n[e] = u[k][e] * p.alpha;
+      if (live) Ring::keep(dx + c, p.M - (int)c, n);
+      Ring::get(slot + 2 * row_bytes, o, p.M, width, k, c, left, n);
+      vscale<VEC>(n, a.r1);
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) w[e] = n[e] * a.k;
+      vfma<VEC>(dw1[k], u[k], w);
+      if (p.w1) {
+        Ring::plain(p.w1 + c, p.M - (int)c, w);
+        vmul<VEC>(u[k], w);
+      }
+      vdot<VEC>(dots, u[k], n);
+    }
+    const float dot = over_group<Sum>(dots[0] + dots[1], width, buf[flip][1]);
+    if (p.dgate && t == 0 && live) p.dgate[row] = dot;
+    const float f1 = p.post ? -dot * p.inv_M * a.r1 : 0.f, scale = a.k * a.r1;      // (r1 = 1 without post)
+    T* d_o = static_cast<T*>(p.d_o) + row * p.lddo;
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      const uint32_t c = (uint32_t)(t + k * width) * VEC;
+      const int left = live ? p.M - (int)c : 0;
+      float n[VEC];
+      Ring::get(slot + 2 * row_bytes, o, p.M, width, k, c, left, n);
+      if (p.post) vfma<VEC>(u[k], n, f1);
+      vscale<VEC>(u[k], scale);
+      if (live) Ring::keep(d_o + c, p.M - (int)c, u[k]);
+    }
+    // the slot is given away when every thread that reads it has: itself, or (VEC = 1) the row's
+    if (VEC == 1) __syncthreads();
+    fetch(row + SLOTS * step, i);
+    a = next;
+    if (++i == SLOTS) i = 0;
+  }
+  ahead_wait<0>();
+  dep_trigger();
+  if (!p.part) return;
+  // the groups of the CTA in order, then the CTA's rows of sums
+  float* out = p.part + (int64_t)blockIdx.x * 2 * p.M;
+  float* shared = reinterpret_cast<float*>(room);
+  if (!SOLO) __syncthreads();
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+    const int c = (t + k * width) * VEC;
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) {
+      if (c + e >= p.M) continue;
+      float* to = SOLO ? out + c + e : shared + mine * 2 * p.M + c + e;
+      to[0] = dw2[k][e];
+      to[p.M] = dw1[k][e];
+    }
+  }
+  if (SOLO) return;
+  __syncthreads();
+  for (int c = threadIdx.x; c < 2 * p.M; c += blockDim.x) {
+    float s = 0.f;
+    for (int k = 0; k < per; ++k) s += shared[k * 2 * p.M + c];
+    out[c] = s;
+  }
+}
+
+// dw_pre and dw_post = sums of the CTAs' rows, 32 columns a CTA: 32 warps take every 32nd row, eight of them in flight, and are
+// added in pairs (as norm_weight_kernel).
+__global__ void __launch_bounds__(1024) sandwich_weight_kernel(const float* part, int n, int M, float* dw2, float* dw1) {
+  __shared__ float acc[32][33];
+  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, c = blockIdx.x * 32 + lane, cols = 2 * M;
+  dep_sync();
+  float a = 0.f;
+  if (c < cols) {
+    for (int k = w; k < n; k += 256) {
+      float b[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) b[j] = k + 32 * j < n ? part[(int64_t)(k + 32 * j) * cols + c] : 0.f;
+      a += ((b[0] + b[1]) + (b[2] + b[3])) + ((b[4] + b[5]) + (b[6] + b[7]));
+    }
+  }
+  acc[w][lane] = a;
+  __syncthreads();
+  // warp w: column w of the 32, a row of sums a lane
+  a = acc[lane][w];
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) a += __shfl_xor_sync(0xffffffffu, a, o);
+  const int at = blockIdx.x * 32 + w;
+  if (lane != 0 || at >= cols) return;
+  if (at < M) { if (dw2) dw2[at] = a; }
+  else if (dw1) dw1[at - M] = a;
+}
+
+fw_status desc_check(const fw_sandwich_desc* d) {
+  if (!d) return FW_ERR_INVALID_ARG;
+  if (d->M < 1 || d->M > kNormMaxM) return FW_ERR_SHAPE;
+  if (!type_ok(d->dtype) || (d->y_dtype != d->dtype && d->y_dtype != FW_E4M3) || (d->post != 0 && d->post != 1)) return FW_ERR_INVALID_ARG;
+  if (!(d->eps > 0.f && d->eps <= 3e38f) || !(d->alpha >= -3e38f && d->alpha <= 3e38f)) return FW_ERR_INVALID_ARG;
+  return FW_OK;
+}
+
+template <class T, class Y, int VEC, int NV, int FILL>
+cudaError_t forward_launch(const SandwichFwd& p, cudaStream_t s) {
+  constexpr int SLOTS = slots(VEC, NV, 2);
+  static FillCache cache;
+  auto kernel = sandwich_forward_kernel<T, Y, VEC, NV, SLOTS, FILL>;
+  const size_t smem = (size_t)SLOTS * 2 * Ahead<T, VEC, NV, FILL>::row_bytes(p.M, p.width, p.width);
+  int ctas = 0;
+  const cudaError_t e = fill(kernel, cache, p.width, smem, p.rows, 1 << 30, &ctas);
+  return e != cudaSuccess ? e : launch_dep(kernel, ctas, p.width, smem, s, p);
+}
+template <class T, class Y, int VEC, int NV>
+cudaError_t forward_launch(const SandwichFwd& p, cudaStream_t s) {
+  constexpr int WHOLE = VEC > 1 ? ROW_WHOLE : ROW_PART, FULL = VEC > 1 ? ROW_FULL : ROW_PART;
+  if (VEC > 1 && p.M == NV * VEC * p.width) return forward_launch<T, Y, VEC, NV, FULL>(p, s);
+  if (VEC > 1 && p.M % VEC == 0) return forward_launch<T, Y, VEC, NV, WHOLE>(p, s);
+  return forward_launch<T, Y, VEC, NV, ROW_PART>(p, s);
+}
+
+// Four accesses of 16 bytes a thread where there are rows for every SM, one where the chain of one row is all there is
+template <class T, class Y, int VEC>
+cudaError_t forward_nv(const SandwichFwd& p0, cudaStream_t s) {
+  SandwichFwd p = p0;
+  const int acc = (p.M + VEC - 1) / VEC;
+  p.width = row_width(acc, p.rows < 2 * sm_count() ? 1 : VEC > 1 ? 4 : 8, 512);
+  const int nv = (acc + p.width - 1) / p.width;
+  // 512 threads take kNormMaxM elements in four accesses of eight, eight of four or thirty-two of one
+  if (nv <= 1) return forward_launch<T, Y, VEC, 1>(p, s);
+  if (nv <= 2) return forward_launch<T, Y, VEC, 2>(p, s);
+  if (nv <= 4) return forward_launch<T, Y, VEC, 4>(p, s);
+  if (nv <= 8) return forward_launch<T, Y, VEC, VEC == 8 ? 4 : 8>(p, s);
+  if (nv <= 16) return forward_launch<T, Y, VEC, VEC == 8 ? 4 : VEC == 4 ? 8 : 16>(p, s);
+  return forward_launch<T, Y, VEC, VEC == 8 ? 4 : VEC == 4 ? 8 : 32>(p, s);
+}
+template <class T, class Y>
+cudaError_t forward_vec(const SandwichFwd& p, bool vec, cudaStream_t s) {
+  return vec ? forward_nv<T, Y, 16 / sizeof(T)>(p, s) : forward_nv<T, Y, 1>(p, s);
+}
+
+int backward_ctas() { return 4 * sm_count(); }
+
+template <class T, int VEC, int NV, bool DH, int FILL, bool SOLO>
+cudaError_t backward_launch(const SandwichBwd& p, cudaStream_t s, int* ctas) {
+  constexpr int ROOMS = DH && VEC > 1 && NV < 8 ? 4 : 3;
+  constexpr int SLOTS = slots(VEC, NV, ROOMS);
+  static FillCache cache;
+  auto kernel = sandwich_backward_kernel<T, VEC, NV, SLOTS, DH, FILL, SOLO>;
+  const int threads = SOLO ? p.width : 128, per = threads / p.width;
+  size_t smem = (size_t)SLOTS * ROOMS * Ahead<T, VEC, NV, FILL>::row_bytes(p.M, threads, p.width);
+  if (!SOLO && p.part && smem < (size_t)per * 2 * p.M * sizeof(float)) smem = (size_t)per * 2 * p.M * sizeof(float);
+  const cudaError_t e = fill(kernel, cache, threads, smem, (p.rows + per - 1) / per, backward_ctas(), ctas);
+  return e != cudaSuccess ? e : launch_dep(kernel, *ctas, threads, smem, s, p);
+}
+template <class T, int VEC, int NV, bool DH>
+cudaError_t backward_launch(const SandwichBwd& p, cudaStream_t s, int* ctas) {
+  constexpr int WHOLE = VEC > 1 ? ROW_WHOLE : ROW_PART, FULL = VEC > 1 ? ROW_FULL : ROW_PART;
+  if constexpr (NV <= 4) {                                   // more accesses a thread: 128 threads or more (see backward_nv)
+    if (p.width < 128)
+      return VEC > 1 && p.M % VEC == 0 ? backward_launch<T, VEC, NV, DH, WHOLE, false>(p, s, ctas)
+                                       : backward_launch<T, VEC, NV, DH, ROW_PART, false>(p, s, ctas);
+  }
+  if (VEC > 1 && p.M == NV * VEC * p.width) return backward_launch<T, VEC, NV, DH, FULL, true>(p, s, ctas);
+  if (VEC > 1 && p.M % VEC == 0) return backward_launch<T, VEC, NV, DH, WHOLE, true>(p, s, ctas);
+  return backward_launch<T, VEC, NV, DH, ROW_PART, true>(p, s, ctas);
+}
+template <class T, int VEC, int NV>
+cudaError_t backward_launch(const SandwichBwd& p, cudaStream_t s, int* ctas) {
+  return p.dh ? backward_launch<T, VEC, NV, true>(p, s, ctas) : backward_launch<T, VEC, NV, false>(p, s, ctas);
+}
+
+template <class T, int VEC>
+cudaError_t backward_nv(const SandwichBwd& p0, cudaStream_t s, int* ctas) {
+  SandwichBwd p = p0;
+  const int acc = (p.M + VEC - 1) / VEC;
+  p.width = row_width(acc, VEC == 1 || acc <= 128 ? 4 : 2, 512);
+  const int nv = (acc + p.width - 1) / p.width;
+  if (nv <= 1) return backward_launch<T, VEC, 1>(p, s, ctas);
+  if (nv <= 2) return backward_launch<T, VEC, 2>(p, s, ctas);
+  if (nv <= 4) return backward_launch<T, VEC, 4>(p, s, ctas);
+  if (nv <= 8) return backward_launch<T, VEC, VEC == 8 ? 4 : 8>(p, s, ctas);
+  if (nv <= 16) return backward_launch<T, VEC, VEC == 8 ? 4 : VEC == 4 ? 8 : 16>(p, s, ctas);
+  return backward_launch<T, VEC, VEC == 8 ? 4 : VEC == 4 ? 8 : 32>(p, s, ctas);
+}
+
+// A range of memory that a call reads or writes; ld, elem: of a matrix (0: a vector)
+struct Range { const void* p; uint64_t n; int64_t ld; int elem; };
+Range mat(const void* p, int64_t rows, int M, int64_t ld, int elem) { return {p, p ? matrix_span(rows, M, ld, elem) : 0, ld, elem}; }
+Range vec4(const void* p, uint64_t n) { return {p, 4 * n, 0, 4}; }
+bool meet(const Range& a, const Range& b) { return overlap(a.p, a.n, b.p, b.n); }
+bool same(const Range& a, const Range& b) { return a.ld && b.ld && a.p == b.p && a.ld == b.ld && a.elem == b.elem; }
+
+}  // namespace
+}  // namespace fw
+
+using namespace fw;
+
+extern "C" {
+
+void fw_sandwich_desc_default(fw_sandwich_desc* d, int32_t M) {
+  if (!d) return;
+  d->M = M; d->dtype = FW_BF16; d->y_dtype = FW_BF16; d->post = 1; d->eps = 1e-6f; d->alpha = 1.f;
+}
+
+size_t fw_sandwich_scratch_bytes(const fw_sandwich_desc* d) {
+  if (desc_check(d) != FW_OK) return 0;
+  return ((size_t)backward_ctas() * 2 * d->M * sizeof(float) + 255) / 256 * 256;
+}
+
+fw_status fw_sandwich_forward(const fw_sandwich_desc* d, int64_t rows, const void* o, int64_t ldo, const void* x, int64_t ldx,
+                              const float* w_post, const float* gate, const float* w_pre, void* h, int64_t ldh, void* y, int64_t ldy,
+                              float* y_scale, float* rstd, void* cuda_stream) {
+  fw_status st = desc_check(d);
+  if (st != FW_OK) return st;
+  const bool q8 = d->y_dtype == FW_E4M3;
+  if (!o || !x || !w_pre || !h || !y || (q8 != (y_scale != nullptr))) return FW_ERR_INVALID_ARG;
+  if ((st = rows_check(rows)) != FW_OK) return st;
+  const int M = d->M, es = type_bytes(d->dtype), ys = type_bytes(d->y_dtype), per16 = 16 / es;
+  bool vec = aligned_to(w_pre, 16) && aligned_to(w_post, 16);
+  const Mat mats[4] = {{o, ldo, es}, {x, ldx, es}, {h, ldh, es}, {y, ldy, ys}};
+  for (const Mat& m : mats)
+    if ((st = mat_check(m, M, per16, &vec)) != FW_OK) return st;
+  const Range in[5] = {mat(o, rows, M, ldo, es), mat(x, rows, M, ldx, es), vec4(w_post, M), vec4(gate, rows), vec4(w_pre, M)};
+  const Range out[4] = {mat(h, rows, M, ldh, es), mat(y, rows, M, ldy, ys), vec4(y_scale, rows), vec4(rstd, 2 * rows)};
+  for (int i = 2; i < 5; ++i)
+    if (!aligned_to(in[i].p, 4)) return FW_ERR_INVALID_ARG;
+  for (int i = 0; i < 4; ++i) {
+    if (!aligned_to(out[i].p, i < 2 ? 1 : 4)) return FW_ERR_INVALID_ARG;
+    // an output may be an input itself (a thread has read what it writes), any other overlap is refused
+    for (const Range& r : in)
+      if (meet(out[i], r) && !same(out[i], r)) return FW_ERR_INVALID_ARG;
+    for (int j = 0; j < i; ++j)
+      if (meet(out[i], out[j])) return FW_ERR_INVALID_ARG;
+  }
+  SandwichFwd p;
+  p.o = o; p.x = x; p.w1 = w_post; p.gate = gate; p.w2 = w_pre; p.h = h; p.y = y; p.y_scale = y_scale; p.rstd = rstd;
+  p.rows = rows; p.ldo = ldo; p.ldx = ldx; p.ldh = ldh; p.ldy = ldy; p.M = M; p.width = 0; p.post = d->post;
+  p.eps = d->eps; p.inv_M = 1.f / (float)M; p.alpha = d->alpha;
+  cudaStream_t s = (cudaStream_t)cuda_stream;
+  ProfScope ps(FW_PROF_MISC, s);
+  cudaError_t e;
+  if (d->dtype == FW_F32)
+    e = q8 ? forward_vec<float, __nv_fp8_storage_t>(p, vec, s) : forward_vec<float, float>(p, vec, s);
+  else
+    e = q8 ? forward_vec<__nv_bfloat16, __nv_fp8_storage_t>(p, vec, s) : forward_vec<__nv_bfloat16, __nv_bfloat16>(p, vec, s);
+  return failed(e, "fw_sandwich_forward");
+}
+
+fw_status fw_sandwich_backward(const fw_sandwich_desc* d, int64_t rows, const void* dy, int64_t lddy, const void* dh, int64_t lddh,
+                               const void* o, int64_t ldo, const void* h, int64_t ldh, const float* w_post, const float* gate,
+                               const float* w_pre, const float* rstd, void* dx, int64_t lddx, void* d_o, int64_t lddo, float* dw_post,
+                               float* dw_pre, float* dgate, void* scratch, size_t scratch_bytes, void* cuda_stream) {
+  fw_status st = desc_check(d);
+  if (st != FW_OK) return st;
+  if (!dy || !o || !h || !w_pre || !rstd || !dx || !d_o) return FW_ERR_INVALID_ARG;
+  if ((st = rows_check(rows)) != FW_OK) return st;
+  const bool sums = dw_post || dw_pre;
+  const size_t ns = fw_sandwich_scratch_bytes(d);
+  if (sums) {
+    if (!scratch) return FW_ERR_INVALID_ARG;
+    if (!aligned_to(scratch, 256) || scratch_bytes < ns) return FW_ERR_WORKSPACE;
+  }
+  const int M = d->M, es = type_bytes(d->dtype), per16 = 16 / es;
+  bool vec = aligned_to(w_pre, 16) && aligned_to(w_post, 16);
+  const Mat mats[6] = {{dy, lddy, es}, {dh, lddh, es}, {o, ldo, es}, {h, ldh, es}, {dx, lddx, es}, {d_o, lddo, es}};
+  for (const Mat& m : mats)
+    if (m.p && (st = mat_check(m, M, per16, &vec)) != FW_OK) return st;
+  const Range in[8] = {mat(dy, rows, M, lddy, es), mat(dh, rows, M, lddh, es), mat(o, rows, M, ldo, es), mat(h, rows, M, ldh, es),
+                       vec4(w_post, M), vec4(gate, rows), vec4(w_pre, M), vec4(rstd, 2 * rows)};
+  const Range out[6] = {mat(dx, rows, M, lddx, es), mat(d_o, rows, M, lddo, es), vec4(dw_post, M), vec4(dw_pre, M), vec4(dgate, rows),
+                        {sums ? scratch : nullptr, ns, 0, 4}};
+  for (int i = 4; i < 8; ++i)
+    if (!aligned_to(in[i].p, 4)) return FW_ERR_INVALID_ARG;
+  for (int i = 0; i < 6; ++i) {
+    if (i > 1 && !aligned_to(out[i].p, 4)) return FW_ERR_INVALID_ARG;
+    for (int j = 0; j < 8; ++j)
+      // o is read once more after dx has been written
+      if (meet(out[i], in[j]) && !(same(out[i], in[j]) && !(i == 0 && j == 2))) return FW_ERR_INVALID_ARG;
+    for (int j = 0; j < i; ++j)
+      if (meet(out[i], out[j])) return FW_ERR_INVALID_ARG;
+  }
+  SandwichBwd p;
+  p.dy = dy; p.dh = dh; p.o = o; p.h = h; p.w1 = w_post; p.gate = gate; p.w2 = w_pre; p.rstd = rstd; p.dx = dx; p.d_o = d_o;
+  p.part = sums ? static_cast<float*>(scratch) : nullptr; p.dgate = dgate;
+  p.rows = rows; p.lddy = lddy; p.lddh = lddh; p.ldo = ldo; p.ldh = ldh; p.lddx = lddx; p.lddo = lddo; p.M = M; p.width = 0;
+  p.post = d->post; p.inv_M = 1.f / (float)M; p.alpha = d->alpha;
+  cudaStream_t str = (cudaStream_t)cuda_stream;
+  int ctas = 0;
+  cudaError_t e;
+  {
+    ProfScope ps(FW_PROF_MISC, str);
+    if (d->dtype == FW_F32) e = vec ? backward_nv<float, 4>(p, str, &ctas) : backward_nv<float, 1>(p, str, &ctas);
+    else e = vec ? backward_nv<__nv_bfloat16, 8>(p, str, &ctas) : backward_nv<__nv_bfloat16, 1>(p, str, &ctas);
+  }
+  if (e == cudaSuccess && sums) {
+    ProfScope ps(FW_PROF_MISC, str);
+    e = launch_dep(sandwich_weight_kernel, (2 * M + 31) / 32, 1024, 0, str, p.part, ctas, M, dw_pre, dw_post);
+  }
+  return failed(e, "fw_sandwich_backward");
+}
+
+}  // extern "C"

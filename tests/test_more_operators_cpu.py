@@ -20,6 +20,45 @@ def table(kind, values):
     return (kind * len(values))(*values)
 
 
+def sandwich_forward(lib, d, rows=4, o=A, x=2 * A, w1=3 * A, gate=None, w2=4 * A, h=5 * A, y=6 * A, scale=None, rstd=7 * A, ld=64, ldh=64, ldy=64):
+    return lib.fw_sandwich_forward(C.byref(d) if d is not None else None, rows, o, ld, x, 64, w1, gate, w2, h, ldh, y, ldy, scale, rstd, None)
+
+
+def sandwich_backward(lib, d, rows=4, dy=A, dh=2 * A, o=3 * A, h=4 * A, w1=5 * A, gate=6 * A, w2=7 * A, rstd=8 * A, dx=9 * A, d_o=10 * A, dw1=11 * A,
+                      dw2=12 * A, dgate=13 * A, scratch=14 * A, n=1 << 24, lddx=64):
+    return lib.fw_sandwich_backward(C.byref(d), rows, dy, 64, dh, 64, o, 64, h, 64, w1, gate, w2, rstd, dx, lddx, d_o, 64, dw1, dw2, dgate, scratch, n, None)
+
+
+def test_sandwich_refusals(lib):
+    inv, shape, ws = B.FW_ERR_INVALID_ARG, B.FW_ERR_SHAPE, B.FW_ERR_WORKSPACE
+    ok = lambda **kw: B.fw_sandwich_desc_default(64, **kw)  # noqa: E731
+    d = ok()
+    assert (d.dtype, d.y_dtype, d.post, d.eps, d.alpha) == (B.FW_BF16, B.FW_BF16, 1, pytest.approx(1e-6), 1.0)
+    assert sandwich_forward(lib, None) == inv
+    for bad in (dict(dtype=2), dict(y_dtype=B.FW_F32), dict(post=2), dict(eps=0.0), dict(eps=float("nan")), dict(eps=float("inf")),
+                dict(alpha=float("nan")), dict(alpha=float("inf"))):
+        assert sandwich_forward(lib, ok(**bad)) == inv and sandwich_backward(lib, ok(**bad)) == inv, bad
+        assert B.fw_sandwich_scratch_bytes(ok(**bad)) == 0
+    for M in (0, -1, 16385):
+        assert sandwich_forward(lib, B.fw_sandwich_desc_default(M)) == shape
+    for kw in (dict(o=None), dict(x=None), dict(w2=None), dict(h=None), dict(y=None), dict(scale=8 * A), dict(o=A + 1), dict(w1=3 * A + 2), dict(gate=8 * A + 1),
+               dict(rstd=7 * A + 2), dict(h=6 * A + 64), dict(h=A + 64), dict(h=A, ldh=72), dict(y=2 * A + 128), dict(y=4 * A), dict(h=3 * A), dict(rstd=A),
+               dict(rstd=4 * A), dict(gate=5 * A), dict(rstd=6 * A)):
+        assert sandwich_forward(lib, d, **kw) == inv, kw
+    for kw in (dict(rows=0), dict(rows=1 << 31), dict(ld=63), dict(ldy=0), dict(ldh=(1 << 30) + 1)):
+        assert sandwich_forward(lib, d, **kw) == shape, kw
+    assert sandwich_forward(lib, ok(y_dtype=B.FW_E4M3)) == inv
+    assert sandwich_forward(lib, ok(y_dtype=B.FW_E4M3), y=A, scale=8 * A) == inv          # bytes over the bf16 rows they are made from
+    for kw in (dict(dy=None), dict(o=None), dict(h=None), dict(w2=None), dict(rstd=None), dict(dx=None), dict(d_o=None), dict(scratch=None), dict(dx=3 * A),
+               dict(dx=10 * A), dict(dx=A + 64), dict(dx=A, lddx=72), dict(dw1=A), dict(dw1=12 * A + 64), dict(dw2=14 * A + 512), dict(dgate=8 * A), dict(dgate=6 * A),
+               dict(scratch=4 * A), dict(scratch=9 * A), dict(d_o=7 * A)):
+        assert sandwich_backward(lib, d, **kw) == inv, kw
+    assert sandwich_backward(lib, d, rows=0) == shape and sandwich_backward(lib, d, lddx=60) == shape
+    assert sandwich_backward(lib, d, n=100) == ws and sandwich_backward(lib, d, scratch=14 * A + 8) == ws
+    with pytest.raises(TypeError, match="beta"):
+        ok(beta=1.0)
+
+
 def logprob(lib, d, what="fwd", rows=4, Z=A, ldz=104, id=2 * A, logp=3 * A, stat=4 * A, dlogp=5 * A, dZ=6 * A, lddz=104):
     if what == "fwd":
         return lib.fw_logprob_forward(C.byref(d), Z, rows, ldz, id, logp, stat, None)
