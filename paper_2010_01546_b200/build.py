@@ -10,7 +10,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libfw.so")
 
-SOURCES = ["fw_api.cu", "fw_gemm_ffma.cu", "fw_moments.cu", "fw_recursion.cu", "fw_recursion_cluster.cu", "fw_recursion_team.cu", "fw_recursion_apply.cu", "fw_umma.cu", "fw_umma_atb.cu", "fw_umma_pair.cu", "fw_umma_gq.cu", "fw_gq_small.cu", "fw_evd.cu", "fw_static.cu", "fw_norm.cu", "fw_distill.cu", "fw_distill_ring.cu", "fw_distill_warp.cu", "fw_gated.cu", "fw_gated_gemm.cu", "fw_gated_small.cu", "fw_sandwich.cu", "fw_logprob.cu", "fw_preference.cu", "fw_adamw.cu"]
+SOURCES = ["fw_api.cu", "fw_gemm_ffma.cu", "fw_moments.cu", "fw_recursion.cu", "fw_recursion_cluster.cu", "fw_recursion_team.cu", "fw_recursion_apply.cu", "fw_umma.cu", "fw_umma_atb.cu", "fw_umma_pair.cu", "fw_umma_gq.cu", "fw_gq_small.cu", "fw_evd.cu", "fw_static.cu", "fw_norm.cu", "fw_distill.cu", "fw_distill_ring.cu", "fw_distill_warp.cu", "fw_gated.cu", "fw_gated_gemm.cu", "fw_gated_small.cu", "fw_sandwich.cu", "fw_logprob.cu", "fw_logprob_resident.cu", "fw_preference.cu", "fw_adamw.cu"]
 
 
 def _stale() -> bool:

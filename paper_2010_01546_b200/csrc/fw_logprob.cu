@@ -9,6 +9,7 @@
 //
 // HBM bandwidth bounds it: a row is read once and its gradient written once.
 #include <cstdio>
+#include <type_traits>
 
 #include "fw_logprob.cuh"
 
@@ -17,174 +18,158 @@ namespace {
 
 using namespace logprob;
 
-// The 16 bytes of a row that begin `first` elements after its start (before it where rows are not aligned); elements that are not the
-// row's read as -inf
-template <class T> struct Group;
-template <> struct Group<float> {
-  static constexpr int VEC = 4;
-  static __device__ __forceinline__ uint4 none() { return make_uint4(0xff800000u, 0xff800000u, 0xff800000u, 0xff800000u); }
-  static __device__ __forceinline__ void open(uint4 q, float (&v)[4]) {
-    v[0] = __uint_as_float(q.x); v[1] = __uint_as_float(q.y); v[2] = __uint_as_float(q.z); v[3] = __uint_as_float(q.w);
-  }
-  static __device__ __forceinline__ uint4 close(const float (&v)[4]) {
-    return make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
-  }
-};
-template <> struct Group<__nv_bfloat16> {
-  static constexpr int VEC = 8;
-  static __device__ __forceinline__ uint4 none() { return make_uint4(0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u); }
-  static __device__ __forceinline__ void open(uint4 q, float (&v)[8]) {
-    v[0] = bf16_lo(q.x); v[1] = bf16_hi(q.x); v[2] = bf16_lo(q.y); v[3] = bf16_hi(q.y);
-    v[4] = bf16_lo(q.z); v[5] = bf16_hi(q.z); v[6] = bf16_lo(q.w); v[7] = bf16_hi(q.w);
-  }
-  static __device__ __forceinline__ uint4 close(const float (&v)[8]) {
-    return make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
-  }
-};
-
-// A row's place: its groups of 16 aligned bytes, of which the first and the last may be shared with other rows
-template <class T>
-struct Place {
-  static constexpr int VEC = Group<T>::VEC;
-  uintptr_t base;                                            // of the first group
-  int shift, groups;                                         // elements before the row in it
-  __device__ __forceinline__ Place(const void* matrix, int64_t row, int64_t ld, int V) {
-    const uintptr_t a = reinterpret_cast<uintptr_t>(matrix) + (uint64_t)row * (uint64_t)ld * sizeof(T);
-    base = a & ~(uintptr_t)15;
-    shift = (int)(a & 15) / (int)sizeof(T);
-    groups = (V + shift + VEC - 1) / VEC;
-  }
-  __device__ __forceinline__ const uint4* at(int g) const { return reinterpret_cast<const uint4*>(base) + g; }
-  __device__ __forceinline__ int first(int g) const { return g * VEC - shift; }        // the group's first element
-};
-
-// Group g's values, -inf in the place of elements that are not the row's
-template <class T, int VEC>
-__device__ __forceinline__ void values(const Place<T>& r, uint4 raw, int g, int V, float (&v)[VEC]) {
-  Group<T>::open(raw, v);
-  const int c = r.first(g);
-  if (c < 0 || c + VEC > V) {
+// Sums of the groups t, t + width ... of a row, U at a time
+template <class T, int U, bool LONG>
+__device__ __forceinline__ MaxSum sums_of(const Place<T>& z, int id, int t, int width, float c2) {
+  MaxSum s = {kLow, 0.f};
+  int g = t;
+  auto take = [&](auto whole) {
+    uint4 raw[U];
+    bool any = false;
 #pragma unroll
-    for (int e = 0; e < VEC; ++e)
-      if (c + e < 0 || c + e >= V) v[e] = -INFINITY;
+    for (int u = 0; u < U; ++u) {
+      raw[u] = make_uint4(Group<T>::kNone, Group<T>::kNone, Group<T>::kNone, Group<T>::kNone);
+      if (whole.value || g + u * width < z.groups) raw[u] = *z.at(g + u * width);
+      any |= z.special(g + u * width);
+    }
+    if (any) {
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (z.special(g + u * width)) raw[u] = z.others(raw[u], g + u * width, id);
+    }
+    s = add_groups<T, U>(s, raw, c2);
+    g += width * U;
+  };
+  if (LONG)
+    while (g - t + U * width <= z.groups) take(std::true_type());
+  while (g - t < z.groups) take(std::false_type());
+  return s;
+}
+// Their gradient
+template <class T, bool SAME, int U>
+__device__ __forceinline__ void gradient_of(const Logprob& p, const Place<T>& z, int64_t row, int id, int t, int width, float c2, const Scale& s) {
+  constexpr int VEC = Group<T>::VEC;
+  T* out = static_cast<T*>(p.dZ) + row * p.lddz;
+  uint4* d = reinterpret_cast<uint4*>(reinterpret_cast<uintptr_t>(out) & ~(uintptr_t)15);
+  if (s.zero) {
+    for (int g = t; g < z.groups; g += width) {
+      if (SAME && !z.edge(g)) d[g] = make_uint4(0, 0, 0, 0);
+      else put_singly<T>(z, g, make_uint4(0, 0, 0, 0), s, c2, out);
+    }
+    return;
   }
+  for (int g = t; g < z.groups; g += width * U) {
+    uint4 raw[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (g + u * width < z.groups) raw[u] = *z.at(g + u * width);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int at = g + u * width;
+      if (SAME) {
+        float v[VEC];
+        slopes<T, VEC>(raw[u], s, c2, v);
+        if (at < z.groups && !z.edge(at)) d[at] = Group<T>::close(v);
+      }
+    }
+    bool any = !SAME;
+#pragma unroll
+    for (int u = 0; u < U; ++u) any |= z.edge(g + u * width);
+    if (any) {
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (g + u * width < z.groups && (!SAME || z.edge(g + u * width))) put_singly<T>(z, g + u * width, raw[u], s, c2, out);
+    }
+  }
+  if (z.own % width == t) put(out + id, s.own);             // over what this thread has put there
 }
 
-// WARP: a warp takes a row, else a CTA.  SAME: Z and dZ lie equally past 16 bytes in every row.
-template <class T, int MODE, bool WARP, bool SAME>
-__global__ void __launch_bounds__(512) logprob_kernel(const Logprob p) {
-  constexpr int VEC = Group<T>::VEC, U = 4;
-  __shared__ MaxSum red[2][16];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, nw = blockDim.x >> 5;
-  const int width = WARP ? 32 : blockDim.x, t = WARP ? lane : threadIdx.x;
-  const int64_t first = WARP ? (int64_t)blockIdx.x * nw + warp : blockIdx.x, step = WARP ? (int64_t)gridDim.x * nw : gridDim.x;
+// A CTA takes a row, its last warp the row's numbers.  SAME: Z and dZ lie equally past 16 bytes in every row.
+template <class T, int MODE, bool SAME, int TH>
+__global__ void __launch_bounds__(TH, 1024 / TH) logprob_kernel(const Logprob p) {
+  constexpr int nw = TH / 32 - 1, width = TH - 32;
+  __shared__ MaxSum red[2 * 32];
+  __shared__ Scale scale[2];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, t = threadIdx.x, unit = blockIdx.x, units = gridDim.x;
   const float c2 = p.inv_tau * kLog2e;
   dep_wait();
-  Head next = head_of<T, MODE>(p, first);
-  int flip = 0;
-  for (int64_t row = first; row < p.rows; row += step) {
+  if (warp == nw) {
+    numbers<T, MODE>(p, unit, units, TH, nw, red, scale, true, [](MaxSum s, int) { return s; });
+  } else {
+    int64_t later = row_at(0, unit, units);
+    int next = id_of<MODE>(p, later), n = 0;
+    for (int it = 0; (int64_t)it * units < p.rows; ++it) {
+      const int id = next;
+      const int64_t row = later;
+      later = row_at(it + 1, unit, units);
+      next = id_of<MODE>(p, later);
+      if (row >= p.rows) continue;                           // (in the last turn)
+      const Place<T> z(p.Z, row, p.ldz, p.V, id);
+      Scale s = {0.f, 0.f, 0.f, 1};
+      if (id >= 0) {
+        if (MODE != LP_BACKWARD) {
+          const MaxSum sum = merge_lanes(sums_of<T, 4, true>(z, id, t, width, c2), c2);
+          if (MODE == LP_FORWARD && n >= 2) meet<BAR_READ>(n, TH);
+          if (lane == 0) red[(n & 1) * 32 + warp] = sum;
+          tell<BAR_SUMS>(n, TH);
+        }
+        if (MODE != LP_FORWARD) {
+          meet<BAR_SCALE>(n, TH);
+          s = scale[n & 1];
+          if (MODE == LP_BACKWARD) tell<BAR_READ>(n, TH);
+        }
+        ++n;
+      }
+      if (MODE != LP_FORWARD) gradient_of<T, SAME, 4>(p, z, row, id, t, width, c2, s);
+    }
+    if (MODE == LP_FORWARD)                                  // what the last warp has told is taken in
+      for (int k = n > 2 ? n - 2 : 0; k < n; ++k) meet<BAR_READ>(k, TH);
+  }
+  dep_trigger();
+}
+
+// A warp takes `batch` rows: their sums one after the other, their numbers a lane each, their gradients one after the other (the rows come
+// from L1 or L2 then).
+template <class T, int MODE, bool SAME>
+__global__ void __launch_bounds__(128, 8) logprob_warp_kernel(const Logprob p, int batch) {
+  const int lane = threadIdx.x & 31, unit = (int)blockIdx.x * 4 + (threadIdx.x >> 5), units = (int)gridDim.x * 4;
+  const float c2 = p.inv_tau * kLog2e;
+  dep_wait();
+  const int64_t none = p.rows;
+  auto mine = [&](int it) { return lane < batch ? row_at(it + lane, unit, units) : none; };
+  int64_t row = mine(0);
+  Head next = head_of<T, MODE>(p, row);
+  for (int it = 0; (int64_t)it * units < p.rows; it += batch) {
     const Head h = next;
-    next = head_of<T, MODE>(p, row + step);
-    // where dZ is Z: the logit of a row's class has been read by all before it is written over
-    if (MODE == LP_BACKWARD) { if (WARP) __syncwarp(); else __syncthreads(); }
-    const Place<T> z(p.Z, row, p.ldz, p.V);
+    const int64_t later = mine(it + batch);
+    next = head_of<T, MODE>(p, later);
     Row r = {0.f, 0.f, 0.f, 0.f, true};
+    if (MODE == LP_BACKWARD) {
+      if (h.id >= 0) r = row_of_stat(h, c2);
+    } else {
+      MaxSum s = {kLow, 0.f};
+      for (int i = 0; i < batch; ++i) {
+        const int id = __shfl_sync(0xffffffffu, h.id, i);
+        const int64_t at = __shfl_sync(0xffffffffu, row, i);
+        if (id < 0) continue;
+        const MaxSum sum = merge_lanes(sums_of<T, 4, false>(Place<T>(p.Z, at, p.ldz, p.V, id), id, lane, 32, c2), c2);
+        if (lane == i) s = sum;
+      }
+      if (h.id >= 0) r = row_of(s, h.z, c2, p.inv_tau);
+    }
     float dlogp = 0.f;
-    if (h.id >= 0) {
-      if (MODE == LP_BACKWARD) {
-        const float e = h.z == -INFINITY ? 0.f : ex2((h.z - h.b) * c2);
-        r = {h.b, h.c, h.c + e, 0.f, h.c + e == 0.f};
-        dlogp = h.a;
-      } else {
-        MaxSum s = {kLow, 0.f};
-        for (int g0 = t; g0 < z.groups; g0 += width * U) {
-          uint4 raw[U];
-#pragma unroll
-          for (int u = 0; u < U; ++u) raw[u] = g0 + u * width < z.groups ? *z.at(g0 + u * width) : Group<T>::none();
-          float v[U][VEC], m = s.m;
-#pragma unroll
-          for (int u = 0; u < U; ++u) {
-            values<T, VEC>(z, raw[u], g0 + u * width, p.V, v[u]);
-            const int k = h.id - z.first(g0 + u * width);
-            if ((unsigned)k < (unsigned)VEC) {
-#pragma unroll
-              for (int e = 0; e < VEC; ++e)
-                if (e == k) v[u][e] = -INFINITY;
-            }
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) m = fmaxf(m, v[u][e]);
-          }
-          float l[2] = {s.l * ex2((s.m - m) * c2), 0.f};
-#pragma unroll
-          for (int u = 0; u < U; ++u)
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) l[e & 1] += ex2((v[u][e] - m) * c2);
-          s = {m, l[0] + l[1]};
-        }
-        s = merge_lanes(s, c2);
-        if (!WARP) {
-          if (lane == 0) red[flip][warp] = s;
-          __syncthreads();
-          s = lane < nw ? red[flip][lane] : MaxSum{kLow, 0.f};
-          s = merge_lanes(s, c2);
-          flip ^= 1;                                         // (rows that do not count have no barrier)
-        }
-        r = row_of(s, h.z, c2, p.inv_tau);
-      }
-    }
-    if (MODE != LP_BACKWARD) {
-      Slope sl = {0.f, 0.f};
-      if (p.loss && !r.empty) sl = policy_of(p, h, r.logp);
-      dlogp = sl.dlogp;
-      if (t == 0) {
-        if (p.logp) p.logp[row] = r.empty ? 0.f : r.logp;
-        if (p.stat) {
-          p.stat[2 * row] = r.empty ? 0.f : r.m;
-          p.stat[2 * row + 1] = r.empty ? 0.f : r.others;
-        }
-        if (p.loss) p.loss[row] = sl.loss;
-        if (p.dlogp) p.dlogp[row] = sl.dlogp;
-      }
-    }
+    if (row < p.rows) dlogp = finish<MODE>(p, row, h, r, true);
     if (MODE != LP_FORWARD) {
-      const float coef = r.empty ? 0.f : dlogp * p.inv_tau, inv = 1.f / r.all, f = -coef * inv, own = coef * (r.others * inv);
-      const bool zero = r.empty || coef == 0.f;
-      T* out = static_cast<T*>(p.dZ) + row * p.lddz;
-      const Place<T> d(p.dZ, row, p.lddz, p.V);
-      for (int g0 = t; g0 < z.groups; g0 += width * U) {
-        uint4 raw[U];
-        if (!zero) {
-#pragma unroll
-          for (int u = 0; u < U; ++u) raw[u] = g0 + u * width < z.groups ? *z.at(g0 + u * width) : Group<T>::none();
-        }
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-          const int g = g0 + u * width, c = z.first(g), k = h.id - c;
-          if (g >= z.groups) break;
-          float v[VEC];
-          if (zero) {
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) v[e] = 0.f;
-          } else {
-            Group<T>::open(raw[u], v);
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) v[e] = f * ex2((v[e] - r.m) * c2);
-            if ((unsigned)k < (unsigned)VEC) {
-#pragma unroll
-              for (int e = 0; e < VEC; ++e)
-                if (e == k) v[e] = own;
-            }
-          }
-          if (SAME && c >= 0 && c + VEC <= p.V) {
-            *const_cast<uint4*>(d.at(g)) = Group<T>::close(v);
-          } else {
-#pragma unroll
-            for (int e = 0; e < VEC; ++e)
-              if (c + e >= 0 && c + e < p.V) put(out + c + e, v[e]);
-          }
-        }
+      const Scale s = scale_of(r, h.id >= 0 ? dlogp : 0.f, p.inv_tau);
+      for (int i = 0; i < batch; ++i) {
+        const int id = __shfl_sync(0xffffffffu, h.id, i);
+        const int64_t at = __shfl_sync(0xffffffffu, row, i);
+        const Scale si = {__shfl_sync(0xffffffffu, s.m, i), __shfl_sync(0xffffffffu, s.f, i), __shfl_sync(0xffffffffu, s.own, i),
+                          __shfl_sync(0xffffffffu, s.zero, i)};
+        if (at < p.rows) gradient_of<T, SAME, 4>(p, Place<T>(p.Z, at, p.ldz, p.V, id), at, id, lane, 32, c2, si);
       }
     }
+    row = later;
   }
   dep_trigger();
 }
@@ -198,19 +183,38 @@ fw_status desc_check(const fw_logprob_desc* d) {
   return FW_OK;
 }
 
-template <class T, int MODE, bool WARP, bool SAME>
+// Rows of up to 8 KB by a warp (8192 x 1000 bf16, loss and gradient, 11.4 us; by CTAs 55.9).
+constexpr int kWarpGroups = 512, kWarpRows = 8;
+
+template <class T, int MODE, bool SAME, int TH>
+cudaError_t launch_ctas(const Logprob& p, cudaStream_t s) {
+  const int64_t most = (int64_t)(1024 / TH) * sm_count();
+  return launch_dep(logprob_kernel<T, MODE, SAME, TH>, (unsigned)(p.rows < most ? p.rows : most), TH, 0, s, p);
+}
+template <class T, int MODE, bool SAME>
 cudaError_t launch(const Logprob& p, cudaStream_t s) {
-  const int threads = WARP ? 128 : 512, per = WARP ? threads / 32 : 1;
-  const int64_t want = (p.rows + per - 1) / per, most = (int64_t)(WARP ? 16 : 3) * sm_count();
-  return launch_dep(logprob_kernel<T, MODE, WARP, SAME>, (unsigned)(want < most ? want : most), threads, 0, s, p);
+  if (p.V <= kWarpGroups * Group<T>::VEC) {
+    const int64_t want = (p.rows + 3) / 4, most = 8 * (int64_t)sm_count(), ctas = want < most ? want : most;
+    const int64_t each = (p.rows + ctas * 4 - 1) / (ctas * 4);                // rows of a warp
+    return launch_dep(logprob_warp_kernel<T, MODE, SAME>, (unsigned)ctas, 128, 0, s, p, (int)(each < kWarpRows ? each : kWarpRows));
+  }
+  // the gradient alone: long rows by large CTAs (131072 bf16 329 us, by four of 256 threads a SM 353), others by small ones (8000 fp32 43
+  // against 58)
+  if (MODE == LP_BACKWARD && (int64_t)p.V * (int)sizeof(T) > 128 * 1024) return launch_ctas<T, MODE, SAME, 1024>(p, s);
+  return launch_ctas<T, MODE, SAME, 256>(p, s);
 }
 template <class T, int MODE>
 cudaError_t launch_mode(const Logprob& p, cudaStream_t s) {
   const bool same = MODE == LP_FORWARD || (((reinterpret_cast<uintptr_t>(p.Z) ^ reinterpret_cast<uintptr_t>(p.dZ)) & 15) == 0 &&
                                            ((p.ldz - p.lddz) * (int64_t)sizeof(T)) % 16 == 0);
-  const bool warp = p.V <= 4096;
-  if (MODE == LP_FORWARD || same) return warp ? launch<T, MODE, true, true>(p, s) : launch<T, MODE, false, true>(p, s);
-  return warp ? launch<T, MODE, true, false>(p, s) : launch<T, MODE, false, false>(p, s);
+  if constexpr (MODE == LP_BOTH) {
+    if (same && p.V > kWarpGroups * Group<T>::VEC) {
+      bool taken = false;
+      const cudaError_t e = launch_resident<T>(p, s, &taken);
+      if (taken) return e;
+    }
+  }
+  return MODE == LP_FORWARD || same ? launch<T, MODE, true>(p, s) : launch<T, MODE, false>(p, s);
 }
 template <class T>
 cudaError_t launch_type(const Logprob& p, int mode, cudaStream_t s) {

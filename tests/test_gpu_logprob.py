@@ -161,15 +161,22 @@ def test_policy(B, rows, V, kind, kl):
         s = out["dlogp"].to(F64)
         assert bool(((dZ.to(F64) - r.grad(s)).abs() <= r.grad_bound(s, torch.full_like(s, 8 * U), HALF[dZ.dtype])).all())
         assert surround_kept(dZ)
-        # without the gradient: the same numbers; and the gradient from what that call left
+        # without the gradient, where sums may be added in another order (each is within its bound of the formula); and the gradient from
+        # what that call left
         again, only, st2, d2 = (torch.empty_like(x) for x in (out["loss"], out["logp"], stat, dZ.contiguous()))
         slope2 = torch.empty_like(again)
         B.fw_policy_forward(d, p, Z, id, old, adv, again, logp_ref=ref if kl else None, weight=w, logp=only, stat=st2, dlogp=slope2)
-        assert torch.equal(again, out["loss"]) and torch.equal(only, out["logp"]) and torch.equal(st2, stat) and torch.equal(slope2, out["dlogp"])
+        assert bool(((only.to(F64) - r.logp).abs() <= logp_bound(r))[live].all()) and torch.equal(st2[:, 0], stat[:, 0])
+        assert bool(((st2 - stat)[:, 1].abs() <= 2 * SUM * stat[:, 1]).all())
+        assert bool(((again.to(F64) - loss).abs() <= (size + ssize) * (2 * e + 16 * U) + 2.0 ** -140)[~near].all())
+        assert bool(((slope2.to(F64) - slope).abs() <= b)[~near].all())
+        for x in (again, only, slope2, st2[:, 1]):
+            assert bool((x[~live] == 0).all())
+        s = slope2.to(F64)
         B.fw_logprob_backward(d, Z, id, st2, slope2, d2)
         assert bool(((d2.to(F64) - r.grad(s)).abs() <= r.grad_bound(s, torch.full_like(s, 8 * U), HALF[dZ.dtype])).all())
         # in place of the logits
-        B.fw_policy_forward(d, p, Z, id, old, adv, again, logp_ref=ref if kl else None, weight=w, dZ=Z)
+        B.fw_policy_forward(d, p, Z, id, old, adv, again, logp_ref=ref if kl else None, weight=w, dZ=Z)      # the same order
         assert torch.equal(again, out["loss"]) and torch.equal(Z, dZ)
 
 
