@@ -569,7 +569,7 @@ typedef struct {
   int32_t n;            /* tensors, 1 ... 65536                                   */
   int32_t state;        /* FW_F32 or FW_E4M3                                      */
   double beta1, beta2;  /* 0 <= beta < 1 (1 - beta is rounded to fp32 as it is)   */
-  float eps;            /* > 0, finite                                            */
+  float eps;            /* >= 1e-36, finite                                       */
   uint32_t seed;        /* of the chance in 8-bit states                          */
 } fw_adamw_desc;
 /* fp32 states, beta1 0.9, beta2 0.999, eps 1e-8, seed 0 */

@@ -18,28 +18,32 @@
 #include <new>
 #include <vector>
 
-#include "fw_internal.h"
-#include "fw_rows.cuh"
+#include "fw_norm.cuh"
 
 namespace fw {
 namespace {
 
-using namespace rows;
+using namespace norm;
 
 constexpr int kBlock = 256;              // elements of a warp's turn, and of a scale
 constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kMaxTensors = 65536;
 // Tensors of a launch: their gradients' addresses travel as parameters, which may be 4 KB in all
 constexpr int kPerLaunch = 440;
+// Blocks of a warp's turn at most.  Its tensor is looked up once for them, and in 8-bit states the scales come and go together: with a byte a
+// block 168M parameters took 550 us, with two 501, four 468, eight 457 and sixteen 461.
+__host__ __device__ constexpr int most_blocks(bool s8) { return s8 ? 8 : 4; }
 constexpr int kNormCtasPerSm = 8;
 
-struct Tensor {                          // in the workspace, from fw_adamw_create
+struct __align__(16) Tensor {             // in the workspace, from fw_adamw_create
   float* p;
   __nv_bfloat16* copy;                   // or null
   int64_t n;
   int64_t first, last;                   // its blocks among all
+  int64_t runs;                          // turns of the norm up to its end, among those of its launch
   float decay;
   int32_t aligned;                       // p and copy take whole accesses
+  int64_t pad;
 };
 
 struct Control {                         // in the workspace
@@ -52,7 +56,7 @@ struct Control {                         // in the workspace
 
 struct Grads {
   const void* g[kPerLaunch];
-  uint8_t kind[kPerLaunch];              // bit 0: bf16, bit 1: takes whole accesses
+  uint8_t kind[kPerLaunch];              // bit 0: bf16, bit 1: takes accesses of four elements, bit 2: of 16 bytes
 };
 
 struct Args {
@@ -61,7 +65,8 @@ struct Args {
   void *m, *v;
   uint8_t *m_scale, *v_scale;
   const float* lr_factor;
-  int64_t first, blocks;                 // this launch's
+  int64_t runs;                          // this launch's
+  int32_t each;                          // elements of a warp's turn
   int32_t n;
   int32_t last;                          // the step's last launch
   int32_t clipped;
@@ -75,7 +80,8 @@ struct NormArgs {
   Control* control;
   double* part;
   float* norm_out;
-  int64_t first, blocks;
+  int64_t runs;
+  int32_t each;                          // elements of a warp's turn
   int32_t n, part0, parts;               // parts: of all launches so far and this one
   int32_t last;
   float max_norm;
@@ -113,10 +119,10 @@ __device__ __forceinline__ void put4(float* p, const float* v) { __stcs(reinterp
 __device__ __forceinline__ void put4(__nv_bfloat16* p, const float* v) {
   __stcs(reinterpret_cast<uint2*>(p), make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])));
 }
-// The block at p, `left` elements of it there (0 in the place of the others); whole: 16 bytes (8 of bf16) at a time
-template <class T>
-__device__ __forceinline__ void get_block(const T* p, int64_t left, bool whole, int lane, float (&o)[8]) {
-  if (whole && left >= kBlock) {
+// The block at p, `left` elements of it there (0 in the place of the others); WHOLE: all, four elements at a time
+template <bool WHOLE, class T>
+__device__ __forceinline__ void get_block(const T* p, int64_t left, int lane, float (&o)[8]) {
+  if (WHOLE) {
     get4(p + 4 * lane, o);
     get4(p + 128 + 4 * lane, o + 4);
   } else {
@@ -124,32 +130,23 @@ __device__ __forceinline__ void get_block(const T* p, int64_t left, bool whole, 
     for (int e = 0; e < 8; ++e) o[e] = place(e, lane) < left ? to_f(p[place(e, lane)]) : 0.f;
   }
 }
-template <class T>
-__device__ __forceinline__ void put_block(T* p, int64_t left, bool whole, int lane, const float (&v)[8]) {
-  if (whole && left >= kBlock) {
-    put4(p + 4 * lane, v);
-    put4(p + 128 + 4 * lane, v + 4);
-  } else {
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-      if (place(e, lane) < left) put(p + place(e, lane), v[e]);
-  }
+// The launch's tensors in shared memory; the CTA meets behind it
+__device__ __forceinline__ const Tensor* table_of(const Tensor* from, int n, uint8_t* room) {
+  const uint4* q = reinterpret_cast<const uint4*>(from);
+  uint4* to = reinterpret_cast<uint4*>(room);
+  for (int i = threadIdx.x; i < n * (int)(sizeof(Tensor) / 16); i += kThreads) to[i] = q[i];
+  __syncthreads();
+  return reinterpret_cast<const Tensor*>(room);
 }
-__device__ __forceinline__ void get_grad(const Grads& g, int t, int64_t at, int64_t left, int lane, float (&o)[8]) {
-  const int kind = g.kind[t];
-  if (kind & 1) get_block(static_cast<const __nv_bfloat16*>(g.g[t]) + at, left, (kind & 2) != 0, lane, o);
-  else get_block(static_cast<const float*>(g.g[t]) + at, left, (kind & 2) != 0, lane, o);
-}
-
-// The tensor of block b: the last one that begins at b or before
-__device__ __forceinline__ int tensor_of(const Tensor* t, int n, int64_t b) {
-  int lo = 0, hi = n - 1;
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (t[mid].first <= b) lo = mid;
-    else hi = mid - 1;
-  }
-  return lo;
+// From tensor t on, the first that ends behind place b: 32 tensors looked at by the lanes of a warp
+template <class F>
+__device__ __forceinline__ int advance(int t, int n, int lane, F ended) {
+  uint32_t m;
+  do {
+    m = __ballot_sync(0xffffffffu, t + lane < n && ended(t + lane));
+    t += __popc(m);
+  } while (m == 0xffffffffu);
+  return t;
 }
 
 // Whether this CTA is the last of its grid; the others' writes before are then visible.  The count is back at 0 after it.
@@ -166,25 +163,53 @@ __device__ bool last_cta(uint32_t* done) {
   return last;
 }
 
-// Squares of all gradients: fp32 sums of a thread's elements, 64 bits beyond; the last CTA adds the CTAs' in order.
+// Sum of the squares of n neighbouring elements, of whole blocks four at a time
+template <class T>
+__device__ __forceinline__ void squares(const T* p, int n, bool aligned, int lane, float (&acc)[2]) {
+  constexpr int VEC = 16 / sizeof(T), N = kBlock / (32 * VEC);
+  const int blocks = aligned ? n / kBlock : 0;
+  for (int j = 0; j < blocks; j += 4) {
+    uint4 q[4 * N];
+#pragma unroll
+    for (int k = 0; k < 4 * N; ++k) {
+      q[k] = make_uint4(0, 0, 0, 0);
+      if (j + k / N < blocks) q[k] = __ldcs(reinterpret_cast<const uint4*>(p + j * kBlock) + k * 32 + lane);
+    }
+#pragma unroll
+    for (int k = 0; k < 4 * N; ++k) {
+      float x[VEC];
+      if (VEC == 8) {
+        x[0] = bf16_lo(q[k].x); x[1] = bf16_hi(q[k].x); x[2] = bf16_lo(q[k].y); x[3] = bf16_hi(q[k].y);
+        x[4 % VEC] = bf16_lo(q[k].z); x[5 % VEC] = bf16_hi(q[k].z); x[6 % VEC] = bf16_lo(q[k].w); x[7 % VEC] = bf16_hi(q[k].w);
+      } else {
+        x[0] = __uint_as_float(q[k].x); x[1] = __uint_as_float(q[k].y); x[2] = __uint_as_float(q[k].z); x[3] = __uint_as_float(q[k].w);
+      }
+      vdot<VEC>(acc, x, x);
+    }
+  }
+  for (int c = blocks * kBlock + lane; c < n; c += 32) {
+    const float x = to_f(p[c]);
+    acc[0] = fmaf(x, x, acc[0]);
+  }
+}
+
+// Squares of all gradients, a warp's turn at a time: fp32 sums of those, 64 bits beyond; the last CTA adds the CTAs' in order.
 __global__ void __launch_bounds__(kThreads) adamw_norm_kernel(const __grid_constant__ NormArgs a, const __grid_constant__ Grads g) {
+  extern __shared__ __align__(16) uint8_t room[];
   __shared__ double red[kWarps];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   dep_wait();
-  const int64_t b0 = a.first + a.blocks * blockIdx.x / gridDim.x, b1 = a.first + a.blocks * (blockIdx.x + 1) / gridDim.x;
+  const Tensor* tensors = table_of(a.tensors, a.n, room);
   double sum = 0.0;
-  if (b0 + warp < b1) {
-    int t = tensor_of(a.tensors, a.n, b0 + warp);
-    float acc[8] = {};
-    for (int64_t b = b0 + warp; b < b1; b += kWarps) {
-      while (b >= a.tensors[t].last) ++t;
-      const int64_t at = (b - a.tensors[t].first) * kBlock;
-      float x[8];
-      get_grad(g, t, at, a.tensors[t].n - at, lane, x);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) acc[e] = fmaf(x[e], x[e], acc[e]);
-    }
-    sum = (double)((acc[0] + acc[1]) + (acc[2] + acc[3])) + (double)((acc[4] + acc[5]) + (acc[6] + acc[7]));
+  int t = 0;
+  for (int64_t run = (int64_t)blockIdx.x * kWarps + warp; run < a.runs; run += (int64_t)gridDim.x * kWarps) {
+    t = advance(t, a.n, lane, [&](int i) { return run >= tensors[i].runs; });
+    const int64_t at = (run - (t > 0 ? tensors[t - 1].runs : 0)) * a.each, left = tensors[t].n - at;
+    float acc[2] = {0.f, 0.f};
+    const int kind = g.kind[t], n = left < a.each ? (int)left : a.each;
+    if (kind & 1) squares(static_cast<const __nv_bfloat16*>(g.g[t]) + at, n, (kind & 4) != 0, lane, acc);
+    else squares(static_cast<const float*>(g.g[t]) + at, n, (kind & 4) != 0, lane, acc);
+    sum += (double)(acc[0] + acc[1]);
   }
   sum = warp_sum(sum);
   if (lane == 0) red[warp] = sum;
@@ -214,7 +239,6 @@ __global__ void __launch_bounds__(kThreads) adamw_norm_kernel(const __grid_const
 }
 
 // ---- 8-bit states ----
-constexpr float kTiny = 0.015625f;       // 2^-6: below it codes are 2^-9 apart; above, three bits behind the leading one
 // The least power of two 2^(b - 127) that takes top to 448 = 1.75 2^8 or less, 2^-100 at least
 __device__ __forceinline__ uint32_t scale_byte(float top) {
   const uint32_t w = __float_as_uint(top);
@@ -223,21 +247,72 @@ __device__ __forceinline__ uint32_t scale_byte(float top) {
 }
 __device__ __forceinline__ float scale_of(uint32_t b) { return __uint_as_float(b << 23); }
 __device__ __forceinline__ float inverse_scale(uint32_t b) { return __uint_as_float((254u - b) << 23); }
-// a >= 0 up or down to a code, up where the share of the way and chance / 2^16 reach 1
-__device__ __forceinline__ float code_of(float a, uint32_t chance) {
-  const float shift = a < kTiny ? kTiny : 0.f;               // codes 2^-9 apart up to 2^-5
-  return __uint_as_float((__float_as_uint(a + shift) + (chance << 4)) & 0xfff00000u) - shift;
+// Codes of e4m3 are the upper bits of fp32 numbers times 2^-120: both have their least exponent there, and what lies below it is a
+// number of smallest codes in both.
+constexpr float kDown = 0x1p-120f, kUp = 0x1p120f;
+constexpr uint32_t kStep = 0x100000u;    // from one code to the next
+// The top bytes of four words
+__device__ __forceinline__ uint32_t top_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  return __byte_perm(__byte_perm(a, b, 0x0073), __byte_perm(c, d, 0x0073), 0x5410);
 }
-// r >= 0 up or down, up where the share of r^2 on the way between the codes' squares passes (chance + 1/2) / 2^16
-__device__ __forceinline__ float root_code_of(float r, uint32_t chance) {
-  const float shift = r < kTiny ? kTiny : 0.f;
-  const uint32_t w = __float_as_uint(r + shift) & 0xfff00000u;
-  const float low = __uint_as_float(w) - shift, high = __uint_as_float(w + 0x100000u) - shift;
-  const float c = fmaf((float)chance, 0x1p-16f, 0x1p-17f);
-  const float code = (r - low) * (r + low) > c * ((high - low) * (high + low)) ? high : low;
-  return r > 0.f ? fmaxf(code, 0x1p-9f) : code;
+// Four of m to codes, up where the share of the way and chance / 2^16 reach 1; down: 2^-120 over the scale; x: the elements' hashes, whose
+// lower halves are the chance
+__device__ __forceinline__ uint32_t mean_codes(float (&m)[4], float down, const uint32_t (&x)[4]) {
+  uint32_t w[4];
+  vscale<4>(m, down);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const uint32_t bits = __float_as_uint(m[e]), chance = __byte_perm(x[e] ^ (x[e] >> 16), 0, 0x4104);      // in bits 8 to 23
+    w[e] = (((bits << 4) + chance) & 0x7fffffffu) | (bits & 0x80000000u);
+  }
+  return top_bytes(w[0], w[1], w[2], w[3]);
 }
-__device__ __forceinline__ void from_e4m3(uint32_t w, float* o) {
+// Four roots r >= 0 over their scale to codes, up where the share of their squares between the codes' squares passes (chance + 1/2) / 2^16,
+// chance the hashes' upper halves; what is not 0 is not held as 0
+__device__ __forceinline__ uint32_t root_codes(const float (&r)[4], float inverse, const uint32_t (&x)[4]) {
+  uint32_t c[4], w[4];
+  float y[4], low[4], high[4], f[4], lhs[4], d[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) y[e] = r[e];
+  vscale<4>(y, inverse);
+  // from 2^-6 on, where almost all are, numbers and codes have their leading bits in common but for the exponent's origin
+  const bool plain = fminf(fminf(y[0], y[1]), fminf(y[2], y[3])) >= 0x1p-6f;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    f[e] = __uint_as_float(0x3f800000u | ((x[e] >> 9) & 0x7fff80u));      // 1 + chance / 2^16
+    lhs[e] = 0x1p-17f - 1.f;
+    low[e] = y[e];
+  }
+  vadd<4>(f, lhs);                                           // (chance + 1/2) / 2^16
+  if (!plain) vscale<4>(low, kDown);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    c[e] = __float_as_uint(low[e]) & 0xfff00000u;
+    low[e] = __uint_as_float(c[e]);
+    high[e] = __uint_as_float(c[e] + kStep);
+  }
+  if (!plain) {
+    vscale<4>(low, kUp);
+    vscale<4>(high, kUp);
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e) lhs[e] = -low[e];
+  vmul<4>(lhs, low);                                         // - low^2, exact
+#pragma unroll
+  for (int e = 0; e < 4; ++e) d[e] = lhs[e];
+  vfma<4>(d, high, high);                                    // high^2 - low^2, exact
+  vfma<4>(lhs, y, y);                                        // y^2 - low^2, rounded once
+  vmul<4>(f, d);
+  const uint32_t origin = plain ? 120u << 27 : 0u;           // of the exponent, four bits up
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    w[e] = lhs[e] > f[e] ? c[e] + kStep : c[e];
+    if (!plain) w[e] = max(w[e], min(__float_as_uint(r[e]), kStep));
+    w[e] = (w[e] << 4) - origin;
+  }
+  return top_bytes(w[0], w[1], w[2], w[3]);
+}
+__device__ __forceinline__ void from_e4m3(uint32_t w, float (&o)[4]) {
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
     const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w >> (16 * k)), __NV_E4M3);
@@ -258,87 +333,232 @@ __device__ __forceinline__ float root(float x) {
   return r;
 }
 
+// What a step's blocks share
+struct Step {
+  float lr, step, inv_root, beta1, beta2, c1, c2, eps;       // c1, c2: 1 - beta times the clipping factor, squared for c2
+  uint32_t key;
+};
+
+template <bool S8> struct StateBits;
+template <> struct StateBits<false> {
+  float m[8], v[8];
+  __device__ __forceinline__ void load(const Args& a, int64_t b, int lane) {
+    get_block<true>(static_cast<const float*>(a.m) + b * kBlock, kBlock, lane, m);
+    get_block<true>(static_cast<const float*>(a.v) + b * kBlock, kBlock, lane, v);
+  }
+};
+template <> struct StateBits<true> {
+  uint32_t m[2], v[2];
+  __device__ __forceinline__ void load(const Args& a, int64_t b, int lane) {
+    const uint32_t* mw = static_cast<const uint32_t*>(a.m) + b * (kBlock / 4) + lane;
+    const uint32_t* vw = static_cast<const uint32_t*>(a.v) + b * (kBlock / 4) + lane;
+    m[0] = __ldcs(mw); m[1] = __ldcs(mw + 32); v[0] = __ldcs(vw); v[1] = __ldcs(vw + 32);
+  }
+};
+// A block's place
+struct Where {
+  float* p;
+  __nv_bfloat16* copy;
+  const void* g;
+  int left;                              // elements there, 256 at most
+  float keep;
+  bool half, aligned;                    // gradients in bf16; all takes accesses of four elements
+  __device__ __forceinline__ bool whole() const { return aligned && left == kBlock; }
+};
+// A lane's part of a block as it is loaded
 template <bool S8>
-__global__ void __launch_bounds__(kThreads) adamw_step_kernel(const __grid_constant__ Args a, const __grid_constant__ Grads g) {
+struct Bits {
+  float p[8];
+  uint32_t g[8];                         // four words of them bf16
+  StateBits<S8> s;
+  __device__ __forceinline__ void load(const Args& a, const Where& w, int64_t b, int lane) {
+    s.load(a, b, lane);
+    if (w.whole()) {
+      get_block<true>(w.p, kBlock, lane, p);
+      if (w.half) {
+        const uint2 x = __ldcs(static_cast<const uint2*>(w.g) + lane), y = __ldcs(static_cast<const uint2*>(w.g) + 32 + lane);
+        g[0] = x.x; g[1] = x.y; g[2] = y.x; g[3] = y.y;
+      } else {
+        const uint4 x = __ldcs(static_cast<const uint4*>(w.g) + lane), y = __ldcs(static_cast<const uint4*>(w.g) + 32 + lane);
+        g[0] = x.x; g[1] = x.y; g[2] = x.z; g[3] = x.w; g[4] = y.x; g[5] = y.y; g[6] = y.z; g[7] = y.w;
+      }
+    } else {
+      get_block<false>(w.p, w.left, lane, p);
+      float v[8];
+      if (w.half) {
+        get_block<false>(static_cast<const __nv_bfloat16*>(w.g), w.left, lane, v);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) g[e] = pack_bf16(v[2 * e], v[2 * e + 1]);
+      } else {
+        get_block<false>(static_cast<const float*>(w.g), w.left, lane, v);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) g[e] = __float_as_uint(v[e]);
+      }
+    }
+  }
+  // the k-th four gradients
+  __device__ __forceinline__ void open(bool half, int k, float (&o)[4]) const {
+    if (half) {
+#pragma unroll
+      for (int e = 0; e < 2; ++e) { o[2 * e] = bf16_lo(g[2 * k + e]); o[2 * e + 1] = bf16_hi(g[2 * k + e]); }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] = __uint_as_float(g[4 * k + e]);
+    }
+  }
+};
+
+// Four elements at p, of which n are there (or all, at once)
+template <class T>
+__device__ __forceinline__ void put_four(T* p, int n, bool whole, const float (&v)[4]) {
+  if (whole) {
+    put4(p, v);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (e < n) put(p + e, v[e]);
+  }
+}
+
+// The step of block b, four elements of a lane at a time (all eight at once took 80 registers and more)
+template <bool S8>
+__device__ __forceinline__ void update(const Args& a, const Step& st, const Bits<S8>& in, const Where& at, int64_t b, int lane, uint32_t& scale_m, uint32_t& scale_v) {
+  float m[2][4], r[2][4];
+  const bool whole = at.whole();
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    float p[4], gr[4], v[4], q[4];
+    in.open(at.half, k, gr);
+    if constexpr (S8) {
+      from_e4m3(in.s.m[k], m[k]);
+      from_e4m3(in.s.v[k], v);
+      vscale<4>(m[k], scale_of(scale_m) * st.beta1);         // a power of two: no rounding but beta1's product
+      const float s = scale_of(scale_v);
+      if (scale_v >= 70) {                                   // its square is in range
+        vmul<4>(v, v);
+        vscale<4>(v, s * s * st.beta2);
+      } else {
+        vscale<4>(v, s);
+        vmul<4>(v, v);
+        vscale<4>(v, st.beta2);
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) { m[k][e] = in.s.m[4 * k + e]; v[e] = in.s.v[4 * k + e]; }
+      vscale<4>(m[k], st.beta1);
+      vscale<4>(v, st.beta2);
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) { p[e] = in.p[4 * k + e]; q[e] = gr[e]; }
+    vfma<4>(m[k], gr, st.c1);
+    vscale<4>(q, st.c2);
+    vfma<4>(v, q, gr);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      r[k][e] = root(v[e]);
+      q[e] = st.eps;
+    }
+    vfma<4>(q, r[k], st.inv_root);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) q[e] = rcp(q[e]);
+    vmul<4>(q, m[k]);
+    vscale<4>(p, at.keep);
+    vfma<4>(p, q, -st.step);
+    const int c = 128 * k + 4 * lane;
+    put_four(at.p + c, at.left - c, whole, p);
+    if (at.copy) put_four(at.copy + c, at.left - c, whole, p);
+    if (!S8) {
+      put4(static_cast<float*>(a.m) + b * kBlock + c, m[k]);
+      put4(static_cast<float*>(a.v) + b * kBlock + c, v);
+    }
+  }
+  if constexpr (S8) {
+    float tm = 0.f, tr = 0.f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      tm = fmaxf(tm, fmaxf(fabsf(m[0][e]), fabsf(m[1][e])));
+      tr = fmaxf(tr, fmaxf(r[0][e], r[1][e]));
+    }
+    uint32_t bm = scale_byte(warp_max(tm));
+    const uint32_t bv = scale_byte(warp_max(tr));
+    scale_m = bm;
+    scale_v = bv;
+    if (bm > 156) {                                          // 2^-120 over the scale is out of range
+      vscale<4>(m[0], 0x1p-100f);
+      vscale<4>(m[1], 0x1p-100f);
+      bm -= 100;
+    }
+    const float down = __uint_as_float(bm < 134 ? (134u - bm) << 23 : 0x400000u >> (bm - 134)), inverse = inverse_scale(bv);
+    // mix(i ^ key) of this lane's elements: its first step is the same for all but the lower 8 bits
+    uint32_t first = ((uint32_t)(b * kBlock) + 4u * lane) ^ st.key;
+    first ^= first >> 16;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      uint32_t hash[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        uint32_t h = (first ^ (uint32_t)(128 * k + e)) * 0x7feb352du;
+        h ^= h >> 15;
+        hash[e] = h * 0x846ca68bu;                           // its last step: the lower half by the upper one
+      }
+      const int64_t w = b * (kBlock / 4) + 32 * k + lane;
+      __stcs(static_cast<uint32_t*>(a.m) + w, mean_codes(m[k], down, hash));
+      __stcs(static_cast<uint32_t*>(a.v) + w, root_codes(r[k], inverse, hash));
+    }
+  }
+}
+
+template <bool S8>
+__global__ void __launch_bounds__(kThreads, S8 ? 3 : 2) adamw_step_kernel(const __grid_constant__ Args a, const __grid_constant__ Grads g) {
+  extern __shared__ __align__(16) uint8_t room[];            // table of the tensors
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   dep_wait();
+  const Tensor* tensors = table_of(a.tensors, a.n, room);
   const int64_t t1 = a.control->step + 1;
   const float clip = a.clipped ? a.control->clip : 1.f;
   const bool skip = a.clipped && a.control->skip;
-  const int64_t b0 = a.first + a.blocks * blockIdx.x / gridDim.x, b1 = a.first + a.blocks * (blockIdx.x + 1) / gridDim.x;
-  if (!skip && b0 + warp < b1) {
-    const float lr = a.lr_factor ? a.lr * *a.lr_factor : a.lr;
-    const float step = (float)((double)lr / one_minus_power(a.beta1, t1));
-    const float inv_root = (float)(1.0 / sqrt(one_minus_power(a.beta2, t1)));
-    const float beta1 = (float)a.beta1, beta2 = (float)a.beta2, c1 = (float)(1.0 - a.beta1), c2 = (float)(1.0 - a.beta2);
-    const uint32_t key = mix(a.seed ^ ((uint32_t)t1 * 0x9e3779b9u));
-    int t = tensor_of(a.tensors, a.n, b0 + warp);
-    Tensor x = a.tensors[t];
-    for (int64_t b = b0 + warp; b < b1; b += kWarps) {
-      while (b >= x.last) x = a.tensors[++t];
-      const int64_t at = (b - x.first) * kBlock, left = x.n - at;
-      float p[8], gr[8], m[8], v[8];
-      get_block(x.p + at, left, x.aligned, lane, p);
-      get_grad(g, t, at, left, lane, gr);
-      if (S8) {
-        const uint32_t* mw = static_cast<const uint32_t*>(a.m) + b * (kBlock / 4) + lane;
-        const uint32_t* vw = static_cast<const uint32_t*>(a.v) + b * (kBlock / 4) + lane;
-        const uint32_t m0 = __ldcs(mw), m1 = __ldcs(mw + 32), v0 = __ldcs(vw), v1 = __ldcs(vw + 32);
-        const float sm = scale_of(a.m_scale[b]), sv = scale_of(a.v_scale[b]);
-        from_e4m3(m0, m); from_e4m3(m1, m + 4);
-        from_e4m3(v0, v); from_e4m3(v1, v + 4);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          m[e] *= sm;
-          v[e] *= sv;
-          v[e] *= v[e];
-        }
-      } else {
-        get_block(static_cast<const float*>(a.m) + b * kBlock, kBlock, true, lane, m);
-        get_block(static_cast<const float*>(a.v) + b * kBlock, kBlock, true, lane, v);
+  int64_t run = (int64_t)blockIdx.x * kWarps + warp;
+  if (!skip && run < a.runs) {
+    Step st;
+    st.lr = a.lr_factor ? a.lr * *a.lr_factor : a.lr;
+    st.step = (float)((double)st.lr / one_minus_power(a.beta1, t1));
+    st.inv_root = (float)(1.0 / sqrt(one_minus_power(a.beta2, t1)));
+    st.beta1 = (float)a.beta1; st.beta2 = (float)a.beta2; st.eps = a.eps;
+    st.c1 = (float)((1.0 - a.beta1) * clip); st.c2 = (float)((1.0 - a.beta2) * ((double)clip * clip));
+    st.key = mix(a.seed ^ ((uint32_t)t1 * 0x9e3779b9u));
+    int t = 0;
+    for (; run < a.runs; run += (int64_t)gridDim.x * kWarps) {
+      t = advance(t, a.n, lane, [&](int i) { return run >= tensors[i].runs; });
+      const Tensor x = tensors[t];
+      const int64_t at = (run - (t > 0 ? tensors[t - 1].runs : 0)) * a.each;
+      const int kind = g.kind[t];
+      int left = x.n - at < a.each ? (int)(x.n - at) : a.each;
+      int64_t b = x.first + at / kBlock;
+      Where w;
+      w.p = x.p + at;
+      w.copy = x.copy ? x.copy + at : nullptr;
+      w.half = kind & 1;
+      w.g = static_cast<const char*>(g.g[t]) + at * (w.half ? 2 : 4);
+      w.keep = fmaf(-st.lr, x.decay, 1.f);
+      w.aligned = x.aligned && (kind & 2);
+      // scales: a lane each, all of the turn at once (single bytes of scattered warps took a quarter of the time)
+      const int blocks = (left + kBlock - 1) / kBlock;
+      uint32_t bm = 0, bv = 0;
+      if (S8 && lane < blocks) { bm = a.m_scale[b + lane]; bv = a.v_scale[b + lane]; }
+      const int64_t b0 = b;
+#pragma unroll 1
+      for (int j = 0; j < blocks; ++j, ++b, left -= kBlock) {
+        w.left = left < kBlock ? left : kBlock;
+        uint32_t sm = S8 ? __shfl_sync(0xffffffffu, bm, j) : 0, sv = S8 ? __shfl_sync(0xffffffffu, bv, j) : 0;
+        Bits<S8> in;
+        in.load(a, w, b, lane);
+        update<S8>(a, st, in, w, b, lane, sm, sv);
+        if (lane == j) { bm = sm; bv = sv; }
+        w.p += kBlock;
+        if (w.copy) w.copy += kBlock;
+        w.g = static_cast<const char*>(w.g) + kBlock * (w.half ? 2 : 4);
       }
-      const float keep = (float)(1.0 - (double)lr * x.decay);
-      float r[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float gc = gr[e] * clip;
-        m[e] = fmaf(beta1, m[e], c1 * gc);
-        v[e] = fmaf(beta2, v[e], c2 * gc * gc);
-        r[e] = root(v[e]);
-        p[e] = fmaf(-step, __fdividef(m[e], fmaf(r[e], inv_root, a.eps)), p[e] * keep);
-      }
-      put_block(x.p + at, left, x.aligned, lane, p);
-      if (x.copy) put_block(x.copy + at, left, x.aligned, lane, p);
-      if (S8) {
-        float tm = 0.f, tr = 0.f;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          tm = fmaxf(tm, fabsf(m[e]));
-          tr = fmaxf(tr, r[e]);
-        }
-        const uint32_t bm = scale_byte(warp_max(tm)), bv = scale_byte(warp_max(tr));
-        const float im = inverse_scale(bm), iv = inverse_scale(bv);
-        const uint32_t i0 = (uint32_t)(b * kBlock);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const uint32_t chance = mix((i0 + place(e, lane)) ^ key);
-          m[e] = copysignf(code_of(fabsf(m[e]) * im, chance & 0xffffu), m[e]);
-          v[e] = root_code_of(r[e] * iv, chance >> 16);
-        }
-        uint32_t* mw = static_cast<uint32_t*>(a.m) + b * (kBlock / 4) + lane;
-        uint32_t* vw = static_cast<uint32_t*>(a.v) + b * (kBlock / 4) + lane;
-        __stcs(mw, pack_e4m3(m[0], m[1], m[2], m[3]));
-        __stcs(mw + 32, pack_e4m3(m[4], m[5], m[6], m[7]));
-        __stcs(vw, pack_e4m3(v[0], v[1], v[2], v[3]));
-        __stcs(vw + 32, pack_e4m3(v[4], v[5], v[6], v[7]));
-        if (lane == 0) {
-          a.m_scale[b] = (uint8_t)bm;
-          a.v_scale[b] = (uint8_t)bv;
-        }
-      } else {
-        put_block(static_cast<float*>(a.m) + b * kBlock, kBlock, true, lane, m);
-        put_block(static_cast<float*>(a.v) + b * kBlock, kBlock, true, lane, v);
-      }
+      if (S8 && lane < blocks) { a.m_scale[b0 + lane] = (uint8_t)bm; a.v_scale[b0 + lane] = (uint8_t)bv; }
     }
   }
   const bool last = last_cta(&a.control->done);
@@ -358,8 +578,9 @@ struct fw_adamw {
   cudaStream_t stream;
   int device;
   int64_t blocks;
+  int32_t each;
   std::vector<int64_t>* sizes;
-  std::vector<int64_t>* first;             // first block of each tensor, and the number of all
+  std::vector<int64_t>* runs;              // as in the table
   std::vector<fw::Span>* out;              // P, copies and the workspace, in order
   fw::Control* control;
   fw::Tensor* tensors;
@@ -374,7 +595,7 @@ namespace {
 fw_status desc_check(const fw_adamw_desc* d, const int64_t* sizes, int64_t* blocks) {
   if (!d || !sizes) return FW_ERR_INVALID_ARG;
   if (d->state != FW_F32 && d->state != FW_E4M3) return FW_ERR_INVALID_ARG;
-  if (!(d->beta1 >= 0.0 && d->beta1 < 1.0) || !(d->beta2 >= 0.0 && d->beta2 < 1.0) || !(d->eps > 0.f && d->eps <= 3e38f)) return FW_ERR_INVALID_ARG;
+  if (!(d->beta1 >= 0.0 && d->beta1 < 1.0) || !(d->beta2 >= 0.0 && d->beta2 < 1.0) || !(d->eps >= 1e-36f && d->eps <= 3e38f)) return FW_ERR_INVALID_ARG;
   if (d->n < 1 || d->n > kMaxTensors) return FW_ERR_SHAPE;
   const int64_t most = (int64_t)1 << (d->state == FW_E4M3 ? 32 : 40);      // the chance counts elements in 32 bits
   int64_t b = 0;
@@ -387,8 +608,8 @@ fw_status desc_check(const fw_adamw_desc* d, const int64_t* sizes, int64_t* bloc
   return FW_OK;
 }
 
-int norm_ctas(int64_t blocks) {
-  const int64_t most = (int64_t)kNormCtasPerSm * sm_count(), want = (blocks + kWarps - 1) / kWarps;
+int norm_ctas(int64_t runs) {
+  const int64_t most = (int64_t)kNormCtasPerSm * sm_count(), want = (runs + kWarps - 1) / kWarps;
   return (int)(want < most ? want : most);
 }
 int launches(int n) { return (n + kPerLaunch - 1) / kPerLaunch; }
@@ -420,33 +641,21 @@ bool meets(const std::vector<Span>& sorted, uintptr_t at, uintptr_t end) {
   return it != sorted.end() && it->at < end;
 }
 
-fw_status failed(cudaError_t e, const char* where) {
-  if (e == cudaSuccess) return FW_OK;
-  fprintf(stderr, "[fw] %s: %s\n", where, cudaGetErrorString(e));
-  return FW_ERR_CUDA;
-}
-
 void release(fw_adamw* a) {
   if (!a) return;
   delete a->sizes;
-  delete a->first;
+  delete a->runs;
   delete a->out;
   delete a;
 }
 
 template <bool S8>
-cudaError_t step_ctas(int* per_sm) {
-  static std::mutex mu;
-  static int known = 0;
-  std::lock_guard<std::mutex> lock(mu);
-  if (!known) {
-    int n = 0;
-    const cudaError_t e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, adamw_step_kernel<S8>, kThreads, 0);
-    if (e != cudaSuccess) return e;
-    known = n > 0 ? n : 1;
-  }
-  *per_sm = known;
-  return cudaSuccess;
+cudaError_t launch_step(const Args& q, const Grads& g, cudaStream_t s) {
+  static FillCache cache;
+  const size_t smem = (size_t)q.n * sizeof(Tensor);
+  int ctas = 0;
+  const cudaError_t e = fill(adamw_step_kernel<S8>, cache, kThreads, smem, (q.runs + kWarps - 1) / kWarps, 1 << 30, &ctas);
+  return e != cudaSuccess ? e : launch_dep(adamw_step_kernel<S8>, (unsigned)ctas, kThreads, smem, s, q, g);
 }
 
 }  // namespace
@@ -481,7 +690,7 @@ fw_status fw_adamw_create(const fw_adamw_desc* d, const int64_t* sizes, float* c
   try {
     a = new fw_adamw();
     a->sizes = new std::vector<int64_t>(sizes, sizes + d->n);
-    a->first = new std::vector<int64_t>(d->n + 1);
+    a->runs = new std::vector<int64_t>(d->n);
     a->out = new std::vector<Span>();
     a->out->reserve(2 * (size_t)d->n + 1);
     a->d = *d;
@@ -491,6 +700,10 @@ fw_status fw_adamw_create(const fw_adamw_desc* d, const int64_t* sizes, float* c
     std::vector<Tensor> table(d->n);
     auto add = [&](const void* p, uint64_t n) { a->out->push_back({(uintptr_t)p, (uintptr_t)p + n}); };
     add(dev_workspace, need);
+    // a turn for every warp of the chip first
+    const int64_t turn = blocks / ((int64_t)sm_count() * 3 * kWarps), most = most_blocks(d->state == FW_E4M3);
+    const int64_t each = (turn < 1 ? 1 : turn < most ? turn : most) * kBlock;
+    a->each = (int32_t)each;
     int64_t b = 0;
     for (int i = 0; i < d->n; ++i) {
       Tensor& t = table[i];
@@ -499,13 +712,14 @@ fw_status fw_adamw_create(const fw_adamw_desc* d, const int64_t* sizes, float* c
       if (!P[i] || !aligned_to(P[i], 4) || !aligned_to(c, 2) || !(wd >= 0.f && wd <= 3e38f)) { release(a); return FW_ERR_INVALID_ARG; }
       t.p = P[i]; t.copy = (__nv_bfloat16*)c; t.n = sizes[i]; t.decay = wd;
       t.aligned = aligned_to(P[i], 16) && aligned_to(c, 8);
-      t.first = (*a->first)[i] = b;
+      t.first = b;
       b += (sizes[i] + kBlock - 1) / kBlock;
       t.last = b;
+      t.runs = (i % kPerLaunch ? table[i - 1].runs : 0) + (sizes[i] + each - 1) / each;
+      (*a->runs)[i] = t.runs;
       add(P[i], (uint64_t)sizes[i] * 4);
       if (c) add(c, (uint64_t)sizes[i] * 2);
     }
-    (*a->first)[d->n] = b;
     std::sort(a->out->begin(), a->out->end(), [](const Span& x, const Span& y) { return x.at < y.at; });
     for (size_t i = 1; i < a->out->size(); ++i)
       if ((*a->out)[i].at < (*a->out)[i - 1].end) { release(a); return FW_ERR_INVALID_ARG; }
@@ -557,14 +771,13 @@ fw_status fw_adamw_step(fw_adamw* a, const void* const* G, const int32_t* g_dtyp
   if (cudaGetDevice(&dev) != cudaSuccess) { cudaGetLastError(); return FW_ERR_CUDA; }
   if (dev != a->device) return FW_ERR_INVALID_ARG;
   const bool s8 = a->d.state == FW_E4M3;
-  int per_sm = 0;
-  cudaError_t e = s8 ? step_ctas<true>(&per_sm) : step_ctas<false>(&per_sm);
+  cudaError_t e = cudaSuccess;
   Grads g;
   auto fill = [&](int i0, int i1) {
     for (int i = i0; i < i1; ++i) {
       const bool half = g_dtype && g_dtype[i] == FW_BF16;
       g.g[i - i0] = G[i];
-      g.kind[i - i0] = (uint8_t)((half ? 1 : 0) | (aligned_to(G[i], half ? 8 : 16) ? 2 : 0));
+      g.kind[i - i0] = (uint8_t)((half ? 1 : 0) | (aligned_to(G[i], half ? 8 : 16) ? 2 : 0) | (aligned_to(G[i], 16) ? 4 : 0));
     }
   };
   const bool clipped = max_norm > 0.f;
@@ -575,11 +788,11 @@ fw_status fw_adamw_step(fw_adamw* a, const void* const* G, const int32_t* g_dtyp
       fill(i0, i1);
       NormArgs q;
       q.tensors = a->tensors + i0; q.control = a->control; q.part = a->part; q.norm_out = norm_out;
-      q.first = (*a->first)[i0]; q.blocks = (*a->first)[i1] - q.first; q.n = i1 - i0;
-      const int ctas = norm_ctas(q.blocks);
+      q.runs = (*a->runs)[i1 - 1]; q.each = a->each; q.n = i1 - i0;
+      const int ctas = norm_ctas(q.runs);
       q.part0 = parts; parts += ctas; q.parts = parts; q.last = i1 == n; q.max_norm = max_norm;
       ProfScope ps(FW_PROF_MISC, a->stream);
-      e = launch_dep(adamw_norm_kernel, ctas, kThreads, 0, a->stream, q, g);
+      e = launch_dep(adamw_norm_kernel, ctas, kThreads, (size_t)q.n * sizeof(Tensor), a->stream, q, g);
     }
   }
   for (int i0 = 0; i0 < n && e == cudaSuccess; i0 += kPerLaunch) {
@@ -587,11 +800,10 @@ fw_status fw_adamw_step(fw_adamw* a, const void* const* G, const int32_t* g_dtyp
     if (n > kPerLaunch || !clipped) fill(i0, i1);
     Args q;
     q.tensors = a->tensors + i0; q.control = a->control; q.m = a->m; q.v = a->v; q.m_scale = a->m_scale; q.v_scale = a->v_scale;
-    q.lr_factor = lr_factor; q.first = (*a->first)[i0]; q.blocks = (*a->first)[i1] - q.first; q.n = i1 - i0; q.last = i1 == n;
+    q.lr_factor = lr_factor; q.runs = (*a->runs)[i1 - 1]; q.each = a->each; q.n = i1 - i0; q.last = i1 == n;
     q.clipped = clipped; q.seed = a->d.seed; q.lr = lr; q.beta1 = a->d.beta1; q.beta2 = a->d.beta2; q.eps = a->d.eps;
-    const int64_t want = (q.blocks + kWarps - 1) / kWarps, most = (int64_t)per_sm * sm_count();
     ProfScope ps(FW_PROF_MISC, a->stream);
-    e = launch_dep(s8 ? adamw_step_kernel<true> : adamw_step_kernel<false>, (unsigned)(want < most ? want : most), kThreads, 0, a->stream, q, g);
+    e = s8 ? launch_step<true>(q, g, a->stream) : launch_step<false>(q, g, a->stream);
   }
   return failed(e, "fw_adamw_step");
 }
