@@ -16,40 +16,109 @@ namespace {
 
 using namespace norm;
 
+// How aligned accesses of a thread meet its rows.  Rows whose matrices all lie equally past 16 bytes (SHIFT) are taken by such accesses too:
+// the first and the last of a row may hold other rows' elements.  How far a row lies past them repeats every 16 bytes / element rows, so a CTA
+// takes rows of one residue, and its columns stay its own; the weights wait in shared memory, moved as the row is.  (Element by element,
+// backward of 5003 x 1537 fp32: 82 us.)
+enum { ROW_SHIFT = 3 };
+template <class T, int VEC, int NV, int FILL>
+struct Way {
+  typedef Ahead<T, VEC, NV, FILL == ROW_SHIFT ? ROW_PART : FILL> Ring;
+  int M, t, width, shift;
+  __device__ __forceinline__ int column(int k) const { return (t + k * width) * VEC - (FILL == ROW_SHIFT ? shift : 0); }
+  __device__ __forceinline__ bool inside(int c) const { return c >= 0 && c + VEC <= M; }
+  __device__ __forceinline__ void fetch(uint32_t room, const T* row) const {
+    if (FILL != ROW_SHIFT) {
+      Ring::fetch(room, row, M, t, width);
+    } else {
+#pragma unroll
+      for (int k = 0; k < NV; ++k) {
+        const int c = column(k);
+        if (c > -VEC && c < M) ahead16(room + (uint32_t)(k * (int)blockDim.x + (int)threadIdx.x) * 16u, row + c);
+      }
+    }
+  }
+  __device__ __forceinline__ void get(const uint8_t* room, const T* row, int k, float (&v)[VEC]) const {
+    const int c = column(k);
+    if (FILL != ROW_SHIFT) {
+      Ring::get(room, row, M, width, k, c, M - c, v);
+    } else {
+      load<VEC>(reinterpret_cast<const T*>(room + (k * (int)blockDim.x + (int)threadIdx.x) * 16), VEC, 0.f, v);
+      if (!inside(c)) {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e)
+          if (c + e < 0 || c + e >= M) v[e] = 0.f;
+      }
+    }
+  }
+  template <class Y>
+  __device__ __forceinline__ void keep(Y* row, int k, const float (&v)[VEC]) const {
+    const int c = column(k);
+    if (FILL != ROW_SHIFT) {
+      Ring::keep(row + c, M - c, v);
+    } else if (inside(c)) {
+      store<VEC>(row + c, VEC, v);
+    } else {
+#pragma unroll
+      for (int e = 0; e < VEC; ++e)
+        if (c + e >= 0 && c + e < M) put(row + c + e, v[e]);
+    }
+  }
+  // a row of weights, or (SHIFT) its place in shared memory
+  __device__ __forceinline__ void weights(const float* w, const float* moved, int k, float (&v)[VEC]) const {
+    if (FILL != ROW_SHIFT) Ring::plain(w + column(k), M - column(k), v);
+    else load<VEC>(moved + (t + k * width) * VEC, VEC, 0.f, v);
+  }
+  __device__ __forceinline__ void move(const float* w, float* moved) const {
+    for (int i = t; i < NV * width * VEC; i += width) moved[i] = i - shift >= 0 && i - shift < M ? w[i - shift] : 0.f;
+  }
+};
+
 struct SandwichFwd {
   const void *o, *x;
   const float *w1, *gate, *w2;   // w_post or null, a number a row or null, w_pre
   void *h, *y;
   float *y_scale, *rstd;
   int64_t rows, ldo, ldx, ldh, ldy;
-  int32_t M, width, post;
+  int32_t M, width, post, classes;   // classes: of rows that lie unequally past 16 bytes, 0: by other ways
   float eps, inv_M, alpha;
 };
 
 // As norm_forward_kernel: T is the type of o, x and h, Y of y; VEC elements an access, NV accesses a thread, SLOTS rows of a CTA on
 // their way, a row at a time.
 template <class T, class Y, int VEC, int NV, int SLOTS, int FILL>
-__global__ void __launch_bounds__(512) sandwich_forward_kernel(const SandwichFwd p) {
-  typedef Ahead<T, VEC, NV, FILL> Ring;
-  extern __shared__ __align__(16) uint8_t room[];            // [slot][o, x]
+__global__ void __maxnreg__(96) sandwich_forward_kernel(const SandwichFwd p) {
+  typedef Way<T, VEC, NV, FILL> Rows;
+  extern __shared__ __align__(16) uint8_t room[];            // [slot][o, x], with SHIFT w_post and w_pre
   __shared__ float buf[2][3][16];
   const int t = threadIdx.x, width = blockDim.x;
-  const uint32_t row_bytes = Ring::row_bytes(p.M, width, width), slot_bytes = row_bytes * 2;
+  const uint32_t row_bytes = Rows::Ring::row_bytes(p.M, width, width), slot_bytes = row_bytes * 2;
   const uint32_t base = (uint32_t)__cvta_generic_to_shared(room);
   auto o_row = [&](int64_t row) { return static_cast<const T*>(p.o) + row * p.ldo; };
   auto x_row = [&](int64_t row) { return static_cast<const T*>(p.x) + row * p.ldx; };
+  // the CTA's rows
+  const int first = FILL == ROW_SHIFT ? (int)blockIdx.x % p.classes : 0;
+  const int64_t step = FILL == ROW_SHIFT ? (int64_t)gridDim.x / p.classes * p.classes : gridDim.x, begin = blockIdx.x;
+  const Rows way = {p.M, t, width, FILL == ROW_SHIFT ? (int)((reinterpret_cast<uintptr_t>(o_row(first)) & 15) / sizeof(T)) : 0};
+  float* w1 = reinterpret_cast<float*>(room + SLOTS * slot_bytes);
+  float* w2 = w1 + NV * width * VEC;
   auto fetch = [&](int64_t row, int i) {
     if (row < p.rows) {
-      Ring::fetch(base + i * slot_bytes, o_row(row), p.M, t, width);
-      Ring::fetch(base + i * slot_bytes + row_bytes, x_row(row), p.M, t, width);
+      way.fetch(base + i * slot_bytes, o_row(row));
+      way.fetch(base + i * slot_bytes + row_bytes, x_row(row));
     }
     ahead_commit();
   };
   dep_wait();
 #pragma unroll
-  for (int i = 0; i < SLOTS; ++i) fetch((int64_t)blockIdx.x + (int64_t)i * gridDim.x, i);
+  for (int i = 0; i < SLOTS; ++i) fetch(begin + i * step, i);
+  if (FILL == ROW_SHIFT) {
+    if (p.w1) way.move(p.w1, w1);
+    way.move(p.w2, w2);
+    __syncthreads();
+  }
   int i = 0, flip = 0;
-  for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x, flip ^= 1) {
+  for (int64_t row = begin; row < p.rows; row += step, flip ^= 1) {
     const uint8_t* slot = room + i * slot_bytes;
     const float k1 = p.gate ? p.gate[row] : 1.f;
     ahead_wait<SLOTS - 1>();
@@ -60,8 +129,7 @@ __global__ void __launch_bounds__(512) sandwich_forward_kernel(const SandwichFwd
     float sq[2] = {0.f, 0.f};
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
-      const uint32_t c = (uint32_t)(t + k * width) * VEC;
-      Ring::get(slot, o, p.M, width, k, c, p.M - (int)c, v[k]);
+      way.get(slot, o, k, v[k]);
       vdot<VEC>(sq, v[k], v[k]);
     }
     float r1 = 1.f;
@@ -70,29 +138,26 @@ __global__ void __launch_bounds__(512) sandwich_forward_kernel(const SandwichFwd
     sq[0] = sq[1] = 0.f;
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
-      const uint32_t c = (uint32_t)(t + k * width) * VEC;
-      const int n = p.M - (int)c;
       float a[VEC];
       if (p.w1) {
-        Ring::plain(p.w1 + c, n, a);
+        way.weights(p.w1, w1, k, a);
         vmul<VEC>(v[k], a);
       }
       vscale<VEC>(v[k], f);
-      Ring::get(slot + row_bytes, x, p.M, width, k, c, n, a);
+      way.get(slot + row_bytes, x, k, a);
       vfma<VEC>(v[k], a, p.alpha);
       round_pairs(v[k], static_cast<const T*>(nullptr));
-      Ring::keep(h + c, n, v[k]);
+      way.keep(h, k, v[k]);
       vdot<VEC>(sq, v[k], v[k]);
     }
     const float r2 = rsqrtf(fmaf(over_group<Sum>(sq[0] + sq[1], width, buf[flip][1]), p.inv_M, p.eps));
-    fetch(row + (int64_t)SLOTS * gridDim.x, i);              // the slot has been read: the sum of its threads depends on it
+    fetch(row + SLOTS * step, i);              // the slot has been read: the sum of its threads depends on it
     if (t == 0 && p.rstd) { p.rstd[2 * row] = r1; p.rstd[2 * row + 1] = r2; }
     float top = 0.f;
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
-      const uint32_t c = (uint32_t)(t + k * width) * VEC;
       float w[VEC];
-      Ring::plain(p.w2 + c, p.M - (int)c, w);
+      way.weights(p.w2, w2, k, w);
       if (sizeof(Y) != 1) vscale<VEC>(v[k], r2);             // the scale takes rstd out of an 8-bit y again: y / c = 448 h w / max |h w|
       vmul<VEC>(v[k], w);
       if (sizeof(Y) == 1) {
@@ -114,9 +179,8 @@ __global__ void __launch_bounds__(512) sandwich_forward_kernel(const SandwichFwd
     Y* y = static_cast<Y*>(p.y) + row * p.ldy;
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
-      const uint32_t c = (uint32_t)(t + k * width) * VEC;
       if (sizeof(Y) == 1) vscale<VEC>(v[k], inv);
-      Ring::keep(y + c, p.M - (int)c, v[k]);
+      way.keep(y, k, v[k]);
     }
     if (++i == SLOTS) i = 0;
   }
@@ -130,7 +194,7 @@ struct SandwichBwd {
   void *dx, *d_o;
   float *part, *dgate;           // part: two rows of M sums for each CTA (dw_pre, dw_post), or null
   int64_t rows, lddy, lddh, ldo, ldh, lddx, lddo;
-  int32_t M, width, post;
+  int32_t M, width, post, classes;
   float inv_M, alpha;
 };
 
@@ -279,6 +343,195 @@ __global__ void __launch_bounds__(512) sandwich_backward_kernel(const SandwichBw
   }
 }
 
+// One sum over the CTA for each of R values, the same bits in every thread; buf: R floats for each warp, not used again before another
+// barrier of the CTA
+template <int R>
+__device__ __forceinline__ void over_cta(float (&v)[R], float* buf) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1)
+#pragma unroll
+    for (int r = 0; r < R; ++r) v[r] += __shfl_xor_sync(0xffffffffu, v[r], o);
+  const int warps = blockDim.x >> 5, lane = threadIdx.x & 31;
+  if (warps == 1) return;
+  if (lane == 0)
+#pragma unroll
+    for (int r = 0; r < R; ++r) buf[r * 16 + (threadIdx.x >> 5)] = v[r];
+  __syncthreads();
+#pragma unroll
+  for (int r = 0; r < R; ++r) v[r] = buf[r * 16 + (lane & (warps - 1))];
+  for (int o = warps >> 1; o > 0; o >>= 1)
+#pragma unroll
+    for (int r = 0; r < R; ++r) v[r] += __shfl_xor_sync(0xffffffffu, v[r], o);
+}
+
+// Aligned rows by CTAs of 128 threads and more: R rows of a CTA at a time, so that their chains of two sums run beside each other and the
+// weights are read once for them (a row at a time: 8192 x 4096 bf16 90 us).  A thread asks for the next rows' elements where it has
+// used up its own.
+template <class T, int VEC, int NV, int R, bool DH, int FILL>
+__global__ void __launch_bounds__(512) sandwich_backward_rows_kernel(const SandwichBwd p) {
+  typedef Way<T, VEC, NV, FILL> Rows;
+  constexpr bool DIRECT = DH && NV == 8;
+  constexpr int ROOMS = DH && !DIRECT ? 4 : 3;
+  extern __shared__ __align__(16) uint8_t room[];            // [row][dy, h, o, dh], with SHIFT w_pre and w_post
+  __shared__ float buf[2][R * 16];
+  const int t = threadIdx.x, width = blockDim.x;
+  const uint32_t row_bytes = Rows::Ring::row_bytes(p.M, width, width);
+  // rows that follow one another here are `apart` rows apart
+  const int apart = FILL == ROW_SHIFT ? p.classes : 1, first = FILL == ROW_SHIFT ? (int)blockIdx.x % p.classes : 0;
+  const int64_t step = (FILL == ROW_SHIFT ? (int64_t)gridDim.x / p.classes * p.classes : (int64_t)gridDim.x) * R;
+  const uint32_t base = (uint32_t)__cvta_generic_to_shared(room);
+  enum { DY, H, O, D };
+  auto row_of = [&](int which, int64_t row) {
+    return which == DY ? static_cast<const T*>(p.dy) + row * p.lddy : which == H ? static_cast<const T*>(p.h) + row * p.ldh :
+           which == O ? static_cast<const T*>(p.o) + row * p.ldo : static_cast<const T*>(p.dh) + row * p.lddh;
+  };
+  const Rows way = {p.M, t, width, FILL == ROW_SHIFT ? (int)((reinterpret_cast<uintptr_t>(row_of(DY, first)) & 15) / sizeof(T)) : 0};
+  float* w2 = reinterpret_cast<float*>(room + R * ROOMS * row_bytes);
+  float* w1 = w2 + NV * width * VEC;
+  auto fetch = [&](int which, int64_t row0) {
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+      if (row0 + r * apart < p.rows) way.fetch(base + (r * ROOMS + which) * row_bytes, row_of(which, row0 + r * apart));
+  };
+  auto get = [&](int which, int r, int64_t row0, int k, float (&v)[VEC]) {
+    way.get(room + (r * ROOMS + which) * row_bytes, row_of(which, row0 + r * apart), k, v);
+  };
+  struct Head { float r1, r2, k; };
+  auto head = [&](int64_t row) {
+    Head a = {0.f, 0.f, 0.f};
+    if (row < p.rows) a = {p.post ? p.rstd[2 * row] : 1.f, p.rstd[2 * row + 1], p.gate ? p.gate[row] : 1.f};
+    return a;
+  };
+  dep_wait();
+  float dw1[NV][VEC], dw2[NV][VEC];
+#pragma unroll
+  for (int k = 0; k < NV; ++k)
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) dw1[k][e] = dw2[k][e] = 0.f;
+  int64_t row0 = FILL == ROW_SHIFT ? first + (int64_t)(blockIdx.x / p.classes) * R * p.classes : (int64_t)blockIdx.x * R;
+  fetch(DY, row0);
+  fetch(H, row0);
+  fetch(O, row0);
+  if (ROOMS == 4) fetch(D, row0);
+  ahead_commit();
+  if (FILL == ROW_SHIFT) {
+    if (p.w1) way.move(p.w1, w1);
+    way.move(p.w2, w2);
+    __syncthreads();
+  }
+  Head a[R];
+#pragma unroll
+  for (int r = 0; r < R; ++r) a[r] = head(row0 + r * apart);
+  for (; row0 < p.rows; row0 += step) {
+    Head next[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) next[r] = head(row0 + step + r * apart);
+    ahead_wait<0>();
+    float u[R][NV][VEC], f[R];
+    {
+      float dots[R][2];
+#pragma unroll
+      for (int r = 0; r < R; ++r) dots[r][0] = dots[r][1] = 0.f;
+#pragma unroll
+      for (int k = 0; k < NV; ++k) {
+        float w[VEC];
+        way.weights(p.w2, w2, k, w);
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+          if (r > 0 && row0 + r * apart >= p.rows) continue;
+          float n[VEC];
+          get(DY, r, row0, k, u[r][k]);
+          get(H, r, row0, k, n);
+          vscale<VEC>(n, a[r].r2);
+          vfma<VEC>(dw2[k], u[r][k], n);
+          vmul<VEC>(u[r][k], w);
+          vdot<VEC>(dots[r], u[r][k], n);
+        }
+      }
+      fetch(DY, row0 + step);
+#pragma unroll
+      for (int r = 0; r < R; ++r) f[r] = dots[r][0] + dots[r][1];
+      over_cta<R>(f, buf[0]);
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        f[r] *= -p.inv_M * a[r].r2;
+        dots[r][0] = dots[r][1] = 0.f;
+      }
+#pragma unroll
+      for (int k = 0; k < NV; ++k) {
+        float w[VEC];
+        if (p.w1) way.weights(p.w1, w1, k, w);
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+          if (r > 0 && row0 + r * apart >= p.rows) continue;
+          float n[VEC];
+          get(H, r, row0, k, n);
+          vfma<VEC>(u[r][k], n, f[r]);                       // u2 - n2 mean(u2 n2)
+          vscale<VEC>(u[r][k], a[r].r2);
+          if (DH) {
+            if (DIRECT) load<VEC>(row_of(D, row0 + r * apart) + way.column(k), FILL == ROW_FULL ? VEC : FILL == ROW_WHOLE ? (p.M > way.column(k) ? VEC : 0) : p.M - way.column(k), 0.f, n);
+            else get(D, r, row0, k, n);
+            vadd<VEC>(u[r][k], n);
+          }
+#pragma unroll
+          for (int e = 0; e < VEC; ++e) n[e] = u[r][k][e];
+          vscale<VEC>(n, p.alpha);
+          way.keep(static_cast<T*>(p.dx) + (row0 + r * apart) * p.lddx, k, n);
+          get(O, r, row0, k, n);
+          vscale<VEC>(n, a[r].r1);
+          if (p.gate) {
+            float q[VEC];
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) q[e] = n[e];
+            vscale<VEC>(q, a[r].k);
+            vfma<VEC>(dw1[k], u[r][k], q);
+          } else {
+            vfma<VEC>(dw1[k], u[r][k], n);
+          }
+          if (p.w1) vmul<VEC>(u[r][k], w);
+          vdot<VEC>(dots[r], u[r][k], n);
+        }
+      }
+      fetch(H, row0 + step);
+      if (ROOMS == 4) fetch(D, row0 + step);
+#pragma unroll
+      for (int r = 0; r < R; ++r) f[r] = dots[r][0] + dots[r][1];
+      over_cta<R>(f, buf[1]);
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      if (r > 0 && row0 + r * apart >= p.rows) continue;
+      if (p.dgate && t == 0) p.dgate[row0 + r * apart] = f[r];
+      const float f1 = -f[r] * p.inv_M * a[r].r1, scale = a[r].k * a[r].r1;         // (r1 = 1 without post)
+#pragma unroll
+      for (int k = 0; k < NV; ++k) {
+        if (p.post) {
+          float n[VEC];
+          get(O, r, row0, k, n);
+          vfma<VEC>(u[r][k], n, f1);
+        }
+        vscale<VEC>(u[r][k], scale);
+        way.keep(static_cast<T*>(p.d_o) + (row0 + r * apart) * p.lddo, k, u[r][k]);
+      }
+    }
+    fetch(O, row0 + step);
+    ahead_commit();
+#pragma unroll
+    for (int r = 0; r < R; ++r) a[r] = next[r];
+  }
+  ahead_wait<0>();
+  dep_trigger();
+  if (!p.part) return;
+  float* out = p.part + (int64_t)blockIdx.x * 2 * p.M;
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+    const int c = way.column(k);
+#pragma unroll
+    for (int e = 0; e < VEC; ++e)
+      if (c + e >= 0 && c + e < p.M) { out[c + e] = dw2[k][e]; out[p.M + c + e] = dw1[k][e]; }
+  }
+}
+
 // dw_pre and dw_post = sums of the CTAs' rows, 32 columns a CTA: 32 warps take every 32nd row, eight of them in flight, and are
 // added in pairs (as norm_weight_kernel).
 __global__ void __launch_bounds__(1024) sandwich_weight_kernel(const float* part, int n, int M, float* dw2, float* dw1) {
@@ -314,18 +567,25 @@ fw_status desc_check(const fw_sandwich_desc* d) {
   return FW_OK;
 }
 
+// CTAs that take rows of each residue alike
+int whole_classes(int ctas, int classes) { return ctas < classes ? classes : ctas / classes * classes; }
+
 template <class T, class Y, int VEC, int NV, int FILL>
 cudaError_t forward_launch(const SandwichFwd& p, cudaStream_t s) {
   constexpr int SLOTS = slots(VEC, NV, 2);
   static FillCache cache;
   auto kernel = sandwich_forward_kernel<T, Y, VEC, NV, SLOTS, FILL>;
-  const size_t smem = (size_t)SLOTS * 2 * Ahead<T, VEC, NV, FILL>::row_bytes(p.M, p.width, p.width);
+  const size_t smem = (size_t)SLOTS * 2 * Way<T, VEC, NV, FILL>::Ring::row_bytes(p.M, p.width, p.width) +
+                      (FILL == ROW_SHIFT ? (size_t)2 * NV * p.width * VEC * sizeof(float) : 0);
   int ctas = 0;
   const cudaError_t e = fill(kernel, cache, p.width, smem, p.rows, 1 << 30, &ctas);
+  if (FILL == ROW_SHIFT && e == cudaSuccess) ctas = whole_classes(ctas, p.classes);
   return e != cudaSuccess ? e : launch_dep(kernel, ctas, p.width, smem, s, p);
 }
 template <class T, class Y, int VEC, int NV>
 cudaError_t forward_launch(const SandwichFwd& p, cudaStream_t s) {
+  if constexpr (VEC > 1 && sizeof(T) == sizeof(Y) && NV <= 4)
+    if (p.classes) return forward_launch<T, Y, VEC, NV, ROW_SHIFT>(p, s);
   constexpr int WHOLE = VEC > 1 ? ROW_WHOLE : ROW_PART, FULL = VEC > 1 ? ROW_FULL : ROW_PART;
   if (VEC > 1 && p.M == NV * VEC * p.width) return forward_launch<T, Y, VEC, NV, FULL>(p, s);
   if (VEC > 1 && p.M % VEC == 0) return forward_launch<T, Y, VEC, NV, WHOLE>(p, s);
@@ -336,7 +596,7 @@ cudaError_t forward_launch(const SandwichFwd& p, cudaStream_t s) {
 template <class T, class Y, int VEC>
 cudaError_t forward_nv(const SandwichFwd& p0, cudaStream_t s) {
   SandwichFwd p = p0;
-  const int acc = (p.M + VEC - 1) / VEC;
+  const int acc = (p.M + VEC - 1 + (p.classes ? VEC - 1 : 0)) / VEC;
   p.width = row_width(acc, p.rows < 2 * sm_count() ? 1 : VEC > 1 ? 4 : 8, 512);
   const int nv = (acc + p.width - 1) / p.width;
   // 512 threads take kNormMaxM elements in four accesses of eight, eight of four or thirty-two of one
@@ -349,7 +609,7 @@ cudaError_t forward_nv(const SandwichFwd& p0, cudaStream_t s) {
 }
 template <class T, class Y>
 cudaError_t forward_vec(const SandwichFwd& p, bool vec, cudaStream_t s) {
-  return vec ? forward_nv<T, Y, 16 / sizeof(T)>(p, s) : forward_nv<T, Y, 1>(p, s);
+  return vec || p.classes ? forward_nv<T, Y, 16 / sizeof(T)>(p, s) : forward_nv<T, Y, 1>(p, s);
 }
 
 int backward_ctas() { return 4 * sm_count(); }
@@ -360,23 +620,39 @@ cudaError_t backward_launch(const SandwichBwd& p, cudaStream_t s, int* ctas) {
   constexpr int SLOTS = slots(VEC, NV, ROOMS);
   static FillCache cache;
   auto kernel = sandwich_backward_kernel<T, VEC, NV, SLOTS, DH, FILL, SOLO>;
-  const int threads = SOLO ? p.width : 128, per = threads / p.width;
+  const int threads = SOLO ? p.width : 256, per = threads / p.width;
   size_t smem = (size_t)SLOTS * ROOMS * Ahead<T, VEC, NV, FILL>::row_bytes(p.M, threads, p.width);
   if (!SOLO && p.part && smem < (size_t)per * 2 * p.M * sizeof(float)) smem = (size_t)per * 2 * p.M * sizeof(float);
   const cudaError_t e = fill(kernel, cache, threads, smem, (p.rows + per - 1) / per, backward_ctas(), ctas);
   return e != cudaSuccess ? e : launch_dep(kernel, *ctas, threads, smem, s, p);
 }
+template <class T, int VEC, int NV, bool DH, int FILL>
+cudaError_t backward_rows_launch(const SandwichBwd& p, cudaStream_t s, int* ctas) {
+  constexpr int ROOMS = DH && NV < 8 ? 4 : 3, R = NV <= 2 ? 2 : 1;
+  static FillCache cache;
+  auto kernel = sandwich_backward_rows_kernel<T, VEC, NV, R, DH, FILL>;
+  const size_t smem = (size_t)R * ROOMS * Way<T, VEC, NV, FILL>::Ring::row_bytes(p.M, p.width, p.width) +
+                      (FILL == ROW_SHIFT ? (size_t)2 * NV * p.width * VEC * sizeof(float) : 0);
+  const cudaError_t e = fill(kernel, cache, p.width, smem, (p.rows + R - 1) / R, backward_ctas(), ctas);
+  if (FILL == ROW_SHIFT && e == cudaSuccess) *ctas = whole_classes(*ctas, p.classes);
+  return e != cudaSuccess ? e : launch_dep(kernel, *ctas, p.width, smem, s, p);
+}
 template <class T, int VEC, int NV, bool DH>
 cudaError_t backward_launch(const SandwichBwd& p, cudaStream_t s, int* ctas) {
-  constexpr int WHOLE = VEC > 1 ? ROW_WHOLE : ROW_PART, FULL = VEC > 1 ? ROW_FULL : ROW_PART;
+  if constexpr (VEC > 1 && NV <= 4)
+    if (p.classes) return backward_rows_launch<T, VEC, NV, DH, ROW_SHIFT>(p, s, ctas);
   if constexpr (NV <= 4) {                                   // more accesses a thread: 128 threads or more (see backward_nv)
     if (p.width < 128)
-      return VEC > 1 && p.M % VEC == 0 ? backward_launch<T, VEC, NV, DH, WHOLE, false>(p, s, ctas)
+      return VEC > 1 && p.M % VEC == 0 ? backward_launch<T, VEC, NV, DH, (VEC > 1 ? ROW_WHOLE : ROW_PART), false>(p, s, ctas)
                                        : backward_launch<T, VEC, NV, DH, ROW_PART, false>(p, s, ctas);
   }
-  if (VEC > 1 && p.M == NV * VEC * p.width) return backward_launch<T, VEC, NV, DH, FULL, true>(p, s, ctas);
-  if (VEC > 1 && p.M % VEC == 0) return backward_launch<T, VEC, NV, DH, WHOLE, true>(p, s, ctas);
-  return backward_launch<T, VEC, NV, DH, ROW_PART, true>(p, s, ctas);
+  if constexpr (VEC > 1) {
+    if (p.M == NV * VEC * p.width) return backward_rows_launch<T, VEC, NV, DH, ROW_FULL>(p, s, ctas);
+    if (p.M % VEC == 0) return backward_rows_launch<T, VEC, NV, DH, ROW_WHOLE>(p, s, ctas);
+    return backward_rows_launch<T, VEC, NV, DH, ROW_PART>(p, s, ctas);
+  } else {
+    return backward_launch<T, VEC, NV, DH, ROW_PART, true>(p, s, ctas);
+  }
 }
 template <class T, int VEC, int NV>
 cudaError_t backward_launch(const SandwichBwd& p, cudaStream_t s, int* ctas) {
@@ -386,7 +662,7 @@ cudaError_t backward_launch(const SandwichBwd& p, cudaStream_t s, int* ctas) {
 template <class T, int VEC>
 cudaError_t backward_nv(const SandwichBwd& p0, cudaStream_t s, int* ctas) {
   SandwichBwd p = p0;
-  const int acc = (p.M + VEC - 1) / VEC;
+  const int acc = (p.M + VEC - 1 + (p.classes ? VEC - 1 : 0)) / VEC;
   p.width = row_width(acc, VEC == 1 || acc <= 128 ? 4 : 2, 512);
   const int nv = (acc + p.width - 1) / p.width;
   if (nv <= 1) return backward_launch<T, VEC, 1>(p, s, ctas);
@@ -399,6 +675,14 @@ cudaError_t backward_nv(const SandwichBwd& p0, cudaStream_t s, int* ctas) {
 
 // A range of memory that a call reads or writes; ld, elem: of a matrix (0: a vector)
 struct Range { const void* p; uint64_t n; int64_t ld; int elem; };
+// Rows after which matrices that all lie equally past 16 bytes do so as at their beginning; 0 where they do not, where rows are so long that
+// they and the weights do not fit shared memory together, or so short that a few threads take several
+int classes_of(const Mat* m, int n, int M) {
+  uint64_t differ = 0;
+  for (int i = 0; i < n; ++i)
+    if (m[i].p) differ |= (reinterpret_cast<uintptr_t>(m[i].p) ^ reinterpret_cast<uintptr_t>(m[0].p)) | (uint64_t)((m[i].ld - m[0].ld) * m[0].elem);
+  return (differ & 15) == 0 && M <= 6144 && M * m[0].elem > 2048 ? 16 / m[0].elem : 0;
+}
 Range mat(const void* p, int64_t rows, int M, int64_t ld, int elem) { return {p, p ? matrix_span(rows, M, ld, elem) : 0, ld, elem}; }
 Range vec4(const void* p, uint64_t n) { return {p, 4 * n, 0, 4}; }
 bool meet(const Range& a, const Range& b) { return overlap(a.p, a.n, b.p, b.n); }
@@ -449,6 +733,7 @@ fw_status fw_sandwich_forward(const fw_sandwich_desc* d, int64_t rows, const voi
   SandwichFwd p;
   p.o = o; p.x = x; p.w1 = w_post; p.gate = gate; p.w2 = w_pre; p.h = h; p.y = y; p.y_scale = y_scale; p.rstd = rstd;
   p.rows = rows; p.ldo = ldo; p.ldx = ldx; p.ldh = ldh; p.ldy = ldy; p.M = M; p.width = 0; p.post = d->post;
+  p.classes = vec || q8 ? 0 : classes_of(mats, 4, M);
   p.eps = d->eps; p.inv_M = 1.f / (float)M; p.alpha = d->alpha;
   cudaStream_t s = (cudaStream_t)cuda_stream;
   ProfScope ps(FW_PROF_MISC, s);
@@ -497,14 +782,16 @@ fw_status fw_sandwich_backward(const fw_sandwich_desc* d, int64_t rows, const vo
   p.dy = dy; p.dh = dh; p.o = o; p.h = h; p.w1 = w_post; p.gate = gate; p.w2 = w_pre; p.rstd = rstd; p.dx = dx; p.d_o = d_o;
   p.part = sums ? static_cast<float*>(scratch) : nullptr; p.dgate = dgate;
   p.rows = rows; p.lddy = lddy; p.lddh = lddh; p.ldo = ldo; p.ldh = ldh; p.lddx = lddx; p.lddo = lddo; p.M = M; p.width = 0;
+  p.classes = vec ? 0 : classes_of(mats, 6, M);
   p.post = d->post; p.inv_M = 1.f / (float)M; p.alpha = d->alpha;
   cudaStream_t str = (cudaStream_t)cuda_stream;
   int ctas = 0;
   cudaError_t e;
   {
     ProfScope ps(FW_PROF_MISC, str);
-    if (d->dtype == FW_F32) e = vec ? backward_nv<float, 4>(p, str, &ctas) : backward_nv<float, 1>(p, str, &ctas);
-    else e = vec ? backward_nv<__nv_bfloat16, 8>(p, str, &ctas) : backward_nv<__nv_bfloat16, 1>(p, str, &ctas);
+    const bool wide = vec || p.classes;
+    if (d->dtype == FW_F32) e = wide ? backward_nv<float, 4>(p, str, &ctas) : backward_nv<float, 1>(p, str, &ctas);
+    else e = wide ? backward_nv<__nv_bfloat16, 8>(p, str, &ctas) : backward_nv<__nv_bfloat16, 1>(p, str, &ctas);
   }
   if (e == cudaSuccess && sums) {
     ProfScope ps(FW_PROF_MISC, str);
