@@ -108,7 +108,7 @@ __global__ void __launch_bounds__(TH, 1024 / TH) logprob_kernel(const Logprob p)
       Scale s = {0.f, 0.f, 0.f, 1};
       if (id >= 0) {
         if (MODE != LP_BACKWARD) {
-          const MaxSum sum = merge_lanes(sums_of<T, 4, true>(z, id, t, width, c2), c2);
+          const MaxSum sum = merge_lanes(sums_of<T, 6, true>(z, id, t, width, c2), c2);
           if (MODE == LP_FORWARD && n >= 2) meet<BAR_READ>(n, TH);
           if (lane == 0) red[(n & 1) * 32 + warp] = sum;
           tell<BAR_SUMS>(n, TH);
