@@ -378,6 +378,38 @@ def test_captured_and_on_a_stream(B):
     assert torch.equal(loss, want) and torch.equal(dZ, wantd)
 
 
+@pytest.mark.parametrize("pattern", ["none", "all", "tail", "power", "chance", "one"])
+def test_rows_that_do_not_count(B, pattern):
+    """Wherever they lie: their results are 0, the others' are what they are by themselves."""
+    for rows, V, kind in ((2500, 5003, "bf16"), (700, 50257, "bf16"), (3001, 2100, "f32"), (400, 140000, "bf16"), (300, 70000, "f32"), (9000, 600, "bf16")):
+        Z, id = inputs(rows, V, kind, V, pad=0)
+        n = torch.arange(rows, device="cuda")
+        out = {"none": n < 0, "all": n >= 0, "tail": n > rows // 3, "power": n % 16 != 5, "chance": torch.rand(rows, generator=gen(rows), device="cuda") < 0.4,
+               "one": n != rows - 2}[pattern]
+        w = torch.where(out & (n % 2 == 0), 0.0, 1.5)
+        use = torch.where(out & (n % 2 == 1), -7, id)
+        d = desc(B, V, kind, index_bits=64)
+        old, adv = -torch.rand(rows, device="cuda") * 9, torch.randn(rows, device="cuda")
+        got = [torch.full((rows,), 9.0, device="cuda") for _ in range(3)]
+        stat, dZ = torch.full((rows, 2), 9.0, device="cuda"), matrix(rows, V, KINDS[kind], pad=0)
+        B.fw_policy_forward(d, B.fw_policy_desc_default(), Z, use, old, adv, got[0], weight=w, logp=got[1], stat=stat, dlogp=got[2], dZ=dZ)
+        r = Ref(Z, id, 1.0)
+        live = ~out
+        assert bool(((got[1].to(F64) - r.logp).abs() <= logp_bound(r))[live].all())
+        s = got[2].to(F64)
+        assert bool(((dZ.to(F64) - r.grad(s)).abs() <= r.grad_bound(s, torch.full_like(s, 8 * U), HALF[dZ.dtype])).all()) and surround_kept(dZ)
+        for x in (*got, stat[:, 0], stat[:, 1]):
+            assert bool((x[out] == 0).all())
+        assert not bool(live.any()) or bool((got[0][live & (adv != 0)] != 0).any())
+        # the same rows by the two calls that follow one another
+        d2, lp, st2 = matrix(rows, V, KINDS[kind], pad=0), torch.full((rows,), 9.0, device="cuda"), torch.full((rows, 2), 9.0, device="cuda")
+        B.fw_logprob_forward(d, Z, torch.where(out, -1, id), lp, stat=st2)
+        assert bool(((lp.to(F64) - r.logp).abs() <= logp_bound(r))[live].all()) and bool((lp[out] == 0).all())
+        B.fw_logprob_backward(d, Z, id, st2, got[2], d2)
+        assert bool(((d2.to(F64) - r.grad(s)).abs() <= r.grad_bound(s, torch.full_like(s, 8 * U), HALF[dZ.dtype])).all()) and surround_kept(d2)
+        del r, d2, dZ
+
+
 def test_many_rows_and_far_offsets(B):
     """More rows than fit the chip at once; rows that begin beyond 2^31 elements."""
     for rows, V in ((30000, 70), (3000, 5001)):
