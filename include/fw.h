@@ -449,7 +449,8 @@ fw_status fw_distill_backward(const fw_distill_desc* d, const void* Z, int64_t r
  * o, x, h: rows x M of `dtype`; w_post (NULL: 1; a layer scale goes here), w_pre: M fp32; gate: a number for each row (a
  * router's weight), rows fp32, NULL: 1; rstd: rows x 2 fp32 (rstd1, rstd2), NULL: not kept; y_scale: rows, with e4m3 and only then.
  * h and y may be o or x itself (same address, type and ld; not the same one); any other overlap of outputs with
- * inputs or with each other is FW_ERR_INVALID_ARG.  What holds for the rows of fw_rmsnorm_forward holds here: NaN, infinity,
+ * inputs or with each other is FW_ERR_INVALID_ARG.  Matrices that all lie equally past a 16-byte boundary, and stay so from row to row
+ * together, move 16 bytes at a time too: up to 15 bytes behind an input are then read, never used.  What holds for the rows of fw_rmsnorm_forward holds here: NaN, infinity,
  * squares that pass fp32, M <= 16384. */
 typedef struct {
   int32_t M;
@@ -513,7 +514,8 @@ fw_status fw_logprob_backward(const fw_logprob_desc* d, const void* Z, int64_t r
  * the stat and dlogp of this call.
  *   logp_old, adv, loss   rows;   logp_ref   rows, NULL: no KL term (kl has to be 0);   weight   rows, NULL: 1
  *   logp, stat, dlogp     NULL: not kept
- * A row in which no class has mass gives loss and dlogp 0.  A row of weight 0, like one whose class is outside [0, V), is not read: its loss, logp, stat, dlogp and dZ are 0. */
+ * A row in which no class has mass gives loss and dlogp 0.  A row of weight 0, like one whose class is outside [0, V), is not read:
+ * its loss, logp, stat, dlogp and dZ are 0. */
 typedef struct {
   float clip_low;       /* 0 <= clip_low < 1                                      */
   float clip_high;      /* >= 0; infinity: no bound                               */
@@ -530,8 +532,8 @@ fw_status fw_policy_forward(const fw_logprob_desc* d, const fw_policy_desc* p, c
  *   sums_s = sum of logp over the answer's rows that count (id inside [0, V); id NULL: all), divided by their number with mean
  *   h = beta ((sums_2i - ref_2i) - (sums_2i+1 - ref_2i+1)) - margin
  *   loss_i = weight_i ((1 - smooth) log(1 + exp(-h)) + smooth log(1 + exp(h))),  dlogp = d loss / d logp
- *   logp, dlogp  rows;  seq  2 pairs + 1 (32 bits), not decreasing, within [0, rows] (what lies outside is taken to the border; a device-side
- *   value, no error);  ref  2 pairs (the same sums of a reference model), NULL: 0;  weight  pairs, NULL: 1
+ *   logp, dlogp  rows;  seq  2 pairs + 1 (32 bits), not decreasing, within [0, rows] (what lies outside is taken to the border; a
+ *   device-side value, no error);  ref  2 pairs (the same sums of a reference model), NULL: 0;  weight  pairs, NULL: 1
  *   loss  pairs;  sums  2 pairs, NULL: not kept;  dlogp NULL: not wanted.  Rows that belong to no answer, or that do not count, get
  *   dlogp 0.  An answer without rows that count has the sum 0.
  * Of d the classes (V, index_bits) alone are looked at.  1 <= pairs <= 2^24, 1 <= rows < 2^28. */
@@ -547,7 +549,7 @@ fw_status fw_preference_loss(const fw_logprob_desc* d, const fw_preference_desc*
                              const void* id, const int32_t* seq, int32_t pairs, const float* ref, const float* weight,
                              float* loss, float* sums, float* dlogp, void* cuda_stream);
 
-/* AdamW over all tensors of a network in one launch (two with clipping): what fw_step and fw_step_momentum are to SGD.  Step t,
+/* AdamW over all tensors of a network in one launch (two with clipping; as many again for each 440 tensors): what fw_step and fw_step_momentum are to SGD.  Step t,
  * with a gradient G times the clipping factor c:
  *   m <- beta1 m + (1 - beta1) c G,  v <- beta2 v + (1 - beta2) (c G)^2
  *   P <- P (1 - lr decay) - lr m / (1 - beta1^t) / (sqrt(v / (1 - beta2^t)) + eps)
@@ -585,8 +587,8 @@ fw_status fw_adamw_destroy(fw_adamw* a);
 /* One step.  G, g_dtype: HOST arrays of length n, the gradients (device) and their types (FW_F32 or FW_BF16; NULL: all fp32).
  * lr >= 0; lr_factor: one device fp32 that multiplies lr (a schedule inside a captured graph), NULL: 1.
  * max_norm > 0: c = min(1, max_norm / norm) with the norm of all gradients together; infinity: none are scaled, but the norm is
- * looked at.  Where it is not finite (|G| beyond 1.8e19 counts as that) the whole step is left out (P, copies, states and number of steps stay as they
- * are) and the next sync_status tells.  max_norm = 0: c = 1, and a NaN or infinity goes into P.
+ * looked at.  Where it is not finite (|G| beyond 1.8e19 counts as that) the whole step is left out (P, copies, states and number of
+ * steps stay as they are) and the next sync_status tells.  max_norm = 0: c = 1, and a NaN or infinity goes into P.
  * norm_out: one device fp32, the norm before clipping; with max_norm > 0, NULL: not kept.  Gradients may not overlap P, copies
  * or the workspace. */
 fw_status fw_adamw_step(fw_adamw* a, const void* const* G, const int32_t* g_dtype, float lr, const float* lr_factor,

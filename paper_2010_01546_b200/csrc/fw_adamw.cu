@@ -3,9 +3,10 @@
 //   m <- b1 m + (1 - b1) c g     v <- b2 v + (1 - b2) (c g)^2
 //   p <- p (1 - lr decay) - lr m / (1 - b1^t) / (sqrt(v / (1 - b2^t)) + eps)
 //
-// Every element is read once and written once (the gradient twice with clipping): HBM bandwidth bounds it.  A warp takes 256
-// neighbouring elements of one tensor at a time, which are what shares a scale in 8-bit states; CTAs take equal shares of all of them in
-// order, so that tensors of any size are one launch.
+// Every element is read once and written once (the gradient twice with clipping): HBM bandwidth bounds it, with 8-bit
+// states their arithmetic too.  A warp takes turns of a few blocks of 256 neighbouring elements, which are what shares a scale in 8-bit states;
+// the turns of all tensors follow one another and the warps of the grid take every n-th, so that tensors of any size are one launch.
+// 371M parameters with copies and clipping 1.82 ms (5.7 TB/s), without them 1.67; 168M with 8-bit states 0.58 ms (4.6 TB/s).
 //
 // 8-bit states.  An average that moves by 1 - beta a step stands still where it is rounded to the nearest code of three mantissa bits, so
 // codes are taken by chance: m's in proportion to its share of the way between two codes, sqrt(v)'s in proportion to v's share

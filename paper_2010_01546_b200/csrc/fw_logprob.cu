@@ -7,7 +7,8 @@
 // The classes other than id are summed by themselves: dZ_id = dlogp / tau (sum of the others) / (sum of all), not 1 - q_id, and logp
 // = -log(1 + others / own) where a class has most of the mass.
 //
-// HBM bandwidth bounds it: a row is read once and its gradient written once.
+// HBM bandwidth bounds it: a row is read once and its gradient written once.  4096 x 131072 bf16: log-probabilities 181 us (5.9 TB/s),
+// gradient from statistics 329 (6.5), loss and gradient in one pass 390 (5.5, the exponentials twice).
 #include <cstdio>
 #include <type_traits>
 
