@@ -587,7 +587,7 @@ fw_status fw_adamw_destroy(fw_adamw* a);
 /* One step.  G, g_dtype: HOST arrays of length n, the gradients (device) and their types (FW_F32 or FW_BF16; NULL: all fp32).
  * lr >= 0; lr_factor: one device fp32 that multiplies lr (a schedule inside a captured graph), NULL: 1.
  * max_norm > 0: c = min(1, max_norm / norm) with the norm of all gradients together; infinity: none are scaled, but the norm is
- * looked at.  Where it is not finite (|G| beyond 1.8e19 counts as that) the whole step is left out (P, copies, states and number of
+ * looked at.  Where it is not finite (|G| beyond 2e18 may count as that) the whole step is left out (P, copies, states and number of
  * steps stay as they are) and the next sync_status tells.  max_norm = 0: c = 1, and a NaN or infinity goes into P.
  * norm_out: one device fp32, the norm before clipping; with max_norm > 0, NULL: not kept.  Gradients may not overlap P, copies
  * or the workspace. */

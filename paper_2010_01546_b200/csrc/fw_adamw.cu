@@ -40,11 +40,10 @@ struct __align__(16) Tensor {             // in the workspace, from fw_adamw_cre
   float* p;
   __nv_bfloat16* copy;                   // or null
   int64_t n;
-  int64_t first, last;                   // its blocks among all
-  int64_t runs;                          // turns of the norm up to its end, among those of its launch
+  int64_t first;                         // its first block among all
+  int64_t runs;                          // turns up to its end, among those of its launch
   float decay;
   int32_t aligned;                       // p and copy take whole accesses
-  int64_t pad;
 };
 
 struct Control {                         // in the workspace
@@ -327,16 +326,16 @@ __device__ __forceinline__ float warp_max(float v) {
   asm("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
   return r;
 }
-// Within one unit in the last place
+// Relative error 2^-23, of subnormal numbers too: a v of gradients below 1e-18 is one, and eps may be less than its root
 __device__ __forceinline__ float root(float x) {
   float r;
-  asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
   return r;
 }
 
 // What a step's blocks share
 struct Step {
-  float lr, step, inv_root, beta1, beta2, c1, c2, eps;       // c1, c2: 1 - beta times the clipping factor, squared for c2
+  float lr, step, inv_root, beta1, beta2, c1, c2, eps;       // c1, c2: the clipping factor times 1 - beta1, root of 1 - beta2
   uint32_t key;
 };
 
@@ -453,7 +452,7 @@ __device__ __forceinline__ void update(const Args& a, const Step& st, const Bits
     for (int e = 0; e < 4; ++e) { p[e] = in.p[4 * k + e]; q[e] = gr[e]; }
     vfma<4>(m[k], gr, st.c1);
     vscale<4>(q, st.c2);
-    vfma<4>(v, q, gr);
+    vfma<4>(v, q, q);                                        // the square of a scaled gradient: a factor's own square may be out of range
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       r[k][e] = root(v[e]);
@@ -525,7 +524,7 @@ __global__ void __launch_bounds__(kThreads, S8 ? 3 : 2) adamw_step_kernel(const 
     st.step = (float)((double)st.lr / one_minus_power(a.beta1, t1));
     st.inv_root = (float)(1.0 / sqrt(one_minus_power(a.beta2, t1)));
     st.beta1 = (float)a.beta1; st.beta2 = (float)a.beta2; st.eps = a.eps;
-    st.c1 = (float)((1.0 - a.beta1) * clip); st.c2 = (float)((1.0 - a.beta2) * ((double)clip * clip));
+    st.c1 = (float)((1.0 - a.beta1) * clip); st.c2 = (float)(sqrt(1.0 - a.beta2) * clip);
     st.key = mix(a.seed ^ ((uint32_t)t1 * 0x9e3779b9u));
     int t = 0;
     for (; run < a.runs; run += (int64_t)gridDim.x * kWarps) {
@@ -715,7 +714,6 @@ fw_status fw_adamw_create(const fw_adamw_desc* d, const int64_t* sizes, float* c
       t.aligned = aligned_to(P[i], 16) && aligned_to(c, 8);
       t.first = b;
       b += (sizes[i] + kBlock - 1) / kBlock;
-      t.last = b;
       t.runs = (i % kPerLaunch ? table[i - 1].runs : 0) + (sizes[i] + each - 1) / each;
       (*a->runs)[i] = t.runs;
       add(P[i], (uint64_t)sizes[i] * 4);

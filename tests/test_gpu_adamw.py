@@ -330,3 +330,35 @@ def test_elements_beyond_31_bits(B):
     assert bool((P[:1000] == 0.5).all()) and bool((P[1 << 30:(1 << 30) + 1000] == 0.5).all())
     s = opt.state(B.FW_A_M_SCALE).float()
     assert float(s[:4].max()) == 2.0 ** -100 and float(s[-1]) > 2.0 ** -40
+
+
+@pytest.mark.parametrize("kind", ["f32", "e4m3"])
+def test_gradients_that_explode(B, kind):
+    """The clipping factor is 1e-21 and less, whose square is no fp32 number; the clipped gradients are ordinary ones."""
+    sizes = [1000, 300]
+    P, G = tensors(sizes, 41)
+    for x in G:
+        x.mul_(1e18)
+    opt = B.AdamW(P, state=B.FW_F32 if kind == "f32" else B.FW_E4M3)
+    norm = torch.empty(1, device="cuda")
+    want = torch.cat([x.to(F64) for x in G]).norm()
+    for t in (1, 2):
+        m0, v0 = states(B, opt, sizes)
+        before = ([p.clone() for p in P], m0, v0)
+        opt.step(G, 1e-2, max_norm=1e-4, norm_out=norm)
+        assert abs(float(norm) / float(want) - 1) <= 32 * U
+        check_step(B, opt, P, G, None, before, t, sizes, 1e-2, [0.0, 0.0], 1e-4 / float(want), 33 * U)
+    assert opt.sync_status() == B.FW_OK
+
+
+@pytest.mark.parametrize("kind", ["f32", "e4m3"])
+def test_gradients_whose_squares_are_subnormal(B, kind):
+    """v is a subnormal number (half a step of them is 2^-150), whose root still matters beside an eps of 1e-30."""
+    g = gen(42)
+    G = 1e-19 * (1 + torch.rand(3000, generator=g, device="cuda")) * (1 - 2 * torch.randint(0, 2, (3000,), generator=g, device="cuda"))
+    P = torch.zeros(3000, device="cuda")
+    opt = B.AdamW([P], state=B.FW_F32 if kind == "f32" else B.FW_E4M3, eps=1e-30)
+    opt.step([G], 1e-2)
+    zero = torch.zeros(3000, dtype=F64, device="cuda")
+    _, v1, p1, _, _ = formula(P * 0, G, zero, zero, 1, 1e-2, 0.0, 1.0, 0.9, 0.999, 1e-30)
+    assert bool(((P.to(F64) - p1).abs() <= p1.abs() * (0.5 * 2.0 ** -150 / v1 + 24 * U)).all())
