@@ -180,6 +180,13 @@ def test_policy(B, rows, V, kind, kl):
         assert torch.equal(again, out["loss"]) and torch.equal(Z, dZ)
 
 
+@pytest.mark.parametrize("rows,V", [(3, 25087), (3, 53761), (3, 111105), (2, 134906), (2, 222210), (2, 269825), (2, 444410), (2, 888830), (3, 1 << 20)])
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+def test_policy_of_long_rows(B, rows, V, kind):
+    """Rows about as long as one CTA, a cluster of two, four and eight hold, and longer than that."""
+    test_policy(B, rows, V, kind, 0.2)
+
+
 def test_policy_gradient_against_differences(B):
     """Central differences of the loss in 64 bits, step 1e-6: 1e-9 of the loss's terms; the kernel's slope is fp32."""
     rows, V, kl, tau = 12, 20, 0.3, 1.4
