@@ -8,7 +8,8 @@
 //
 // Both directions read each element once and write each result once: HBM bandwidth bounds them.  A row stays on chip between its two
 // sums, which depend on one another, so a CTA has the next rows on their way meanwhile, and backward forms two rows at once where they are
-// short enough.  8192 x 4096 bf16: forward 50 us (5.3 TB/s), backward 83 us (4.9 TB/s); 5003 x 1537 fp32 backward 46 us (4.0 TB/s).
+// short enough.  8192 x 4096 bf16: forward 50 us (5.4 TB/s), backward 75 us (5.3 TB/s), of which 7 are the
+// sum of the CTAs' shares of dw; 5003 x 1537 fp32 backward 45 us (4.1 TB/s).
 #include "fw_norm.cuh"
 
 namespace fw {
@@ -25,6 +26,10 @@ template <class T, int VEC, int NV, int FILL>
 struct Way {
   typedef Ahead<T, VEC, NV, FILL == ROW_SHIFT ? ROW_PART : FILL> Ring;
   int M, t, width, shift;
+  // bytes of a row of one tensor (not those of accesses that no thread has: 5003 x 1537 fp32 backward 46 us with them)
+  static __host__ __device__ __forceinline__ uint32_t row_bytes(int M, int width) {
+    return VEC > 1 ? (uint32_t)((M + (FILL == ROW_SHIFT ? 2 * VEC - 2 : VEC - 1)) / VEC * 16) : Ring::row_bytes(M, width, width);
+  }
   __device__ __forceinline__ int column(int k) const { return (t + k * width) * VEC - (FILL == ROW_SHIFT ? shift : 0); }
   __device__ __forceinline__ bool inside(int c) const { return c >= 0 && c + VEC <= M; }
   __device__ __forceinline__ void fetch(uint32_t room, const T* row) const {
@@ -43,6 +48,7 @@ struct Way {
     if (FILL != ROW_SHIFT) {
       Ring::get(room, row, M, width, k, c, M - c, v);
     } else {
+      // (of accesses behind the row's what comes next in shared memory, the weights at last)
       load<VEC>(reinterpret_cast<const T*>(room + (k * (int)blockDim.x + (int)threadIdx.x) * 16), VEC, 0.f, v);
       if (!inside(c)) {
 #pragma unroll
@@ -84,6 +90,26 @@ struct SandwichFwd {
   float eps, inv_M, alpha;
 };
 
+// Warps that a CTA's numbers are counted for when one warp joins them
+__device__ __forceinline__ int warp_span() {
+  const int warps = blockDim.x >> 5;
+  return warps <= 4 ? 4 : warps <= 8 ? 8 : 16;
+}
+// One value over the CTA, the same bits in every thread; 0 is nothing to Op.  buf: a float for each warp, not used again before another
+// barrier of the CTA
+template <class Op>
+__device__ __forceinline__ float over_row(float v, float* buf) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v = Op::of(v, __shfl_xor_sync(0xffffffffu, v, o));
+  const int warps = blockDim.x >> 5, lane = threadIdx.x & 31, span = warp_span(), at = lane & (span - 1);
+  if (warps == 1) return v;
+  if (lane == 0) buf[threadIdx.x >> 5] = v;
+  __syncthreads();
+  v = at < warps ? buf[at] : 0.f;
+  for (int o = span >> 1; o > 0; o >>= 1) v = Op::of(v, __shfl_xor_sync(0xffffffffu, v, o));
+  return v;
+}
+
 // As norm_forward_kernel: T is the type of o, x and h, Y of y; VEC elements an access, NV accesses a thread, SLOTS rows of a CTA on
 // their way, a row at a time.
 template <class T, class Y, int VEC, int NV, int SLOTS, int FILL>
@@ -92,7 +118,7 @@ __global__ void __maxnreg__(96) sandwich_forward_kernel(const SandwichFwd p) {
   extern __shared__ __align__(16) uint8_t room[];            // [slot][o, x], with SHIFT w_post and w_pre
   __shared__ float buf[2][3][16];
   const int t = threadIdx.x, width = blockDim.x;
-  const uint32_t row_bytes = Rows::Ring::row_bytes(p.M, width, width), slot_bytes = row_bytes * 2;
+  const uint32_t row_bytes = Rows::row_bytes(p.M, width), slot_bytes = row_bytes * 2;
   const uint32_t base = (uint32_t)__cvta_generic_to_shared(room);
   auto o_row = [&](int64_t row) { return static_cast<const T*>(p.o) + row * p.ldo; };
   auto x_row = [&](int64_t row) { return static_cast<const T*>(p.x) + row * p.ldx; };
@@ -133,7 +159,7 @@ __global__ void __maxnreg__(96) sandwich_forward_kernel(const SandwichFwd p) {
       vdot<VEC>(sq, v[k], v[k]);
     }
     float r1 = 1.f;
-    if (p.post) r1 = rsqrtf(fmaf(over_group<Sum>(sq[0] + sq[1], width, buf[flip][0]), p.inv_M, p.eps));
+    if (p.post) r1 = rsqrtf(fmaf(over_row<Sum>(sq[0] + sq[1], buf[flip][0]), p.inv_M, p.eps));
     const float f = k1 * r1;
     sq[0] = sq[1] = 0.f;
 #pragma unroll
@@ -150,7 +176,7 @@ __global__ void __maxnreg__(96) sandwich_forward_kernel(const SandwichFwd p) {
       way.keep(h, k, v[k]);
       vdot<VEC>(sq, v[k], v[k]);
     }
-    const float r2 = rsqrtf(fmaf(over_group<Sum>(sq[0] + sq[1], width, buf[flip][1]), p.inv_M, p.eps));
+    const float r2 = rsqrtf(fmaf(over_row<Sum>(sq[0] + sq[1], buf[flip][1]), p.inv_M, p.eps));
     fetch(row + SLOTS * step, i);              // the slot has been read: the sum of its threads depends on it
     if (t == 0 && p.rstd) { p.rstd[2 * row] = r1; p.rstd[2 * row + 1] = r2; }
     float top = 0.f;
@@ -167,7 +193,7 @@ __global__ void __maxnreg__(96) sandwich_forward_kernel(const SandwichFwd p) {
     }
     float inv = 1.f;
     if (sizeof(Y) == 1) {
-      top = over_group<MaxAbs>(top, width, buf[flip][2]);
+      top = over_row<MaxAbs>(top, buf[flip][2]);
       float scale;
       inv = row_scale(top, r2, &scale);
       if (t == 0) p.y_scale[row] = scale;
@@ -192,11 +218,13 @@ struct SandwichBwd {
   const void *dy, *dh, *o, *h;
   const float *w1, *gate, *w2, *rstd;
   void *dx, *d_o;
-  float *part, *dgate;           // part: two rows of M sums for each CTA (dw_pre, dw_post), or null
+  float *part, *dgate;           // part: two rows of sums for each CTA (dw_pre, dw_post), part_row(M) apart, or null
   int64_t rows, lddy, lddh, ldo, ldh, lddx, lddo;
   int32_t M, width, post, classes;
   float inv_M, alpha;
 };
+
+__host__ __device__ constexpr int part_row(int M) { return (M + 3) / 4 * 4; }
 
 // As norm_backward_kernel: a CTA takes every gridDim-th group of rows, a row at a time (SOLO) or several, and keeps its columns' shares of
 // dw_pre and dw_post in registers.  DIRECT: dh is read where it is needed: four rows of 64 KB do not fit a SM.
@@ -320,7 +348,8 @@ __global__ void __launch_bounds__(512) sandwich_backward_kernel(const SandwichBw
   dep_trigger();
   if (!p.part) return;
   // the groups of the CTA in order, then the CTA's rows of sums
-  float* out = p.part + (int64_t)blockIdx.x * 2 * p.M;
+  const int apart = part_row(p.M);
+  float* out = p.part + (int64_t)blockIdx.x * 2 * apart;
   float* shared = reinterpret_cast<float*>(room);
   if (!SOLO) __syncthreads();
 #pragma unroll
@@ -329,16 +358,16 @@ __global__ void __launch_bounds__(512) sandwich_backward_kernel(const SandwichBw
 #pragma unroll
     for (int e = 0; e < VEC; ++e) {
       if (c + e >= p.M) continue;
-      float* to = SOLO ? out + c + e : shared + mine * 2 * p.M + c + e;
+      float* to = SOLO ? out + c + e : shared + mine * 2 * apart + c + e;
       to[0] = dw2[k][e];
-      to[p.M] = dw1[k][e];
+      to[apart] = dw1[k][e];
     }
   }
   if (SOLO) return;
   __syncthreads();
-  for (int c = threadIdx.x; c < 2 * p.M; c += blockDim.x) {
+  for (int c = threadIdx.x; c < 2 * apart; c += blockDim.x) {
     float s = 0.f;
-    for (int k = 0; k < per; ++k) s += shared[k * 2 * p.M + c];
+    for (int k = 0; k < per; ++k) s += shared[k * 2 * apart + c];
     out[c] = s;
   }
 }
@@ -351,21 +380,20 @@ __device__ __forceinline__ void over_cta(float (&v)[R], float* buf) {
   for (int o = 16; o > 0; o >>= 1)
 #pragma unroll
     for (int r = 0; r < R; ++r) v[r] += __shfl_xor_sync(0xffffffffu, v[r], o);
-  const int warps = blockDim.x >> 5, lane = threadIdx.x & 31;
-  if (warps == 1) return;
+  const int warps = blockDim.x >> 5, lane = threadIdx.x & 31, span = warp_span(), at = lane & (span - 1);
   if (lane == 0)
 #pragma unroll
     for (int r = 0; r < R; ++r) buf[r * 16 + (threadIdx.x >> 5)] = v[r];
   __syncthreads();
 #pragma unroll
-  for (int r = 0; r < R; ++r) v[r] = buf[r * 16 + (lane & (warps - 1))];
-  for (int o = warps >> 1; o > 0; o >>= 1)
+  for (int r = 0; r < R; ++r) v[r] = at < warps ? buf[r * 16 + at] : 0.f;
+  for (int o = span >> 1; o > 0; o >>= 1)
 #pragma unroll
     for (int r = 0; r < R; ++r) v[r] += __shfl_xor_sync(0xffffffffu, v[r], o);
 }
 
 // Aligned rows by CTAs of 128 threads and more: R rows of a CTA at a time, so that their chains of two sums run beside each other and the
-// weights are read once for them (a row at a time: 8192 x 4096 bf16 90 us).  A thread asks for the next rows' elements where it has
+// weights are read once for them (a row at a time: 8192 x 4096 bf16 7 us more).  A thread asks for the next rows' elements where it has
 // used up its own.
 template <class T, int VEC, int NV, int R, bool DH, int FILL>
 __global__ void __launch_bounds__(512) sandwich_backward_rows_kernel(const SandwichBwd p) {
@@ -375,7 +403,7 @@ __global__ void __launch_bounds__(512) sandwich_backward_rows_kernel(const Sandw
   extern __shared__ __align__(16) uint8_t room[];            // [row][dy, h, o, dh], with SHIFT w_pre and w_post
   __shared__ float buf[2][R * 16];
   const int t = threadIdx.x, width = blockDim.x;
-  const uint32_t row_bytes = Rows::Ring::row_bytes(p.M, width, width);
+  const uint32_t row_bytes = Rows::row_bytes(p.M, width);
   // rows that follow one another here are `apart` rows apart
   const int apart = FILL == ROW_SHIFT ? p.classes : 1, first = FILL == ROW_SHIFT ? (int)blockIdx.x % p.classes : 0;
   const int64_t step = (FILL == ROW_SHIFT ? (int64_t)gridDim.x / p.classes * p.classes : (int64_t)gridDim.x) * R;
@@ -522,41 +550,68 @@ __global__ void __launch_bounds__(512) sandwich_backward_rows_kernel(const Sandw
   ahead_wait<0>();
   dep_trigger();
   if (!p.part) return;
-  float* out = p.part + (int64_t)blockIdx.x * 2 * p.M;
+  // four sums at a time, by way of shared memory where a thread's columns do not begin on four (8192 x 4096 bf16 with single stores here and
+  // single loads where they are added 82 us, so 75)
+  constexpr bool EVEN = FILL == ROW_FULL || FILL == ROW_WHOLE;
+  const int half = part_row(p.M);
+  float* out = p.part + (int64_t)blockIdx.x * 2 * half;
+  float* shared = reinterpret_cast<float*>(room);
+  if (!EVEN) __syncthreads();
 #pragma unroll
   for (int k = 0; k < NV; ++k) {
     const int c = way.column(k);
+    if (EVEN) {
 #pragma unroll
-    for (int e = 0; e < VEC; ++e)
-      if (c + e >= 0 && c + e < p.M) { out[c + e] = dw2[k][e]; out[p.M + c + e] = dw1[k][e]; }
-  }
-}
-
-// dw_pre and dw_post = sums of the CTAs' rows, 32 columns a CTA: 32 warps take every 32nd row, eight of them in flight, and are
-// added in pairs (as norm_weight_kernel).
-__global__ void __launch_bounds__(1024) sandwich_weight_kernel(const float* part, int n, int M, float* dw2, float* dw1) {
-  __shared__ float acc[32][33];
-  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, c = blockIdx.x * 32 + lane, cols = 2 * M;
-  dep_sync();
-  float a = 0.f;
-  if (c < cols) {
-    for (int k = w; k < n; k += 256) {
-      float b[8];
+      for (int e = 0; e < VEC; e += 4) {
+        if (FILL == ROW_WHOLE && c >= p.M) continue;
+        *reinterpret_cast<float4*>(out + c + e) = make_float4(dw2[k][e], dw2[k][e + 1], dw2[k][e + 2], dw2[k][e + 3]);
+        *reinterpret_cast<float4*>(out + half + c + e) = make_float4(dw1[k][e], dw1[k][e + 1], dw1[k][e + 2], dw1[k][e + 3]);
+      }
+    } else {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) b[j] = k + 32 * j < n ? part[(int64_t)(k + 32 * j) * cols + c] : 0.f;
-      a += ((b[0] + b[1]) + (b[2] + b[3])) + ((b[4] + b[5]) + (b[6] + b[7]));
+      for (int e = 0; e < VEC; ++e)
+        if (c + e >= 0 && c + e < p.M) { shared[c + e] = dw2[k][e]; shared[half + c + e] = dw1[k][e]; }
     }
   }
-  acc[w][lane] = a;
+  if (EVEN) return;
   __syncthreads();
-  // warp w: column w of the 32, a row of sums a lane
-  a = acc[lane][w];
+  for (int c = 4 * t; c < 2 * half; c += 4 * width) *reinterpret_cast<float4*>(out + c) = *reinterpret_cast<const float4*>(shared + c);
+}
+
+// dw_pre and dw_post = sums of the CTAs' rows, 32 columns a CTA: eight threads side by side take four columns each, of every 32nd row, eight
+// rows in flight; then in pairs.
+__global__ void __launch_bounds__(256) sandwich_weight_kernel(const float* part, int n, int M, float* dw2, float* dw1) {
+  __shared__ float4 acc[32][8];
+  const int t = threadIdx.x, x = t & 7, y = t >> 3, half = part_row(M), c = blockIdx.x * 32 + 4 * x;
+  dep_sync();
+  float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+  auto add = [](float4& s, const float4& v) { s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w; };
+  if (c < 2 * half) {
+    for (int k = y; k < n; k += 256) {
+      float4 b[8];
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) a += __shfl_xor_sync(0xffffffffu, a, o);
-  const int at = blockIdx.x * 32 + w;
-  if (lane != 0 || at >= cols) return;
-  if (at < M) { if (dw2) dw2[at] = a; }
-  else if (dw1) dw1[at - M] = a;
+      for (int j = 0; j < 8; ++j) {
+        b[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (k + 32 * j < n) b[j] = *reinterpret_cast<const float4*>(part + (int64_t)(k + 32 * j) * 2 * half + c);
+      }
+#pragma unroll
+      for (int j = 4; j > 0; j >>= 1)
+#pragma unroll
+        for (int i = 0; i < j; ++i) add(b[i], b[i + j]);
+      add(a, b[0]);
+    }
+  }
+  acc[y][x] = a;
+#pragma unroll
+  for (int j = 16; j > 0; j >>= 1) {
+    __syncthreads();
+    if (y < j) add(acc[y][x], acc[y + j][x]);
+  }
+  __syncthreads();
+  if (t >= 32) return;
+  const int at = blockIdx.x * 32 + t, col = at < half ? at : at - half;
+  float* dw = at < half ? dw2 : dw1;
+  if (dw && at < 2 * half && col < M) dw[col] = reinterpret_cast<const float*>(acc[0])[t];
 }
 
 fw_status desc_check(const fw_sandwich_desc* d) {
@@ -575,7 +630,7 @@ cudaError_t forward_launch(const SandwichFwd& p, cudaStream_t s) {
   constexpr int SLOTS = slots(VEC, NV, 2);
   static FillCache cache;
   auto kernel = sandwich_forward_kernel<T, Y, VEC, NV, SLOTS, FILL>;
-  const size_t smem = (size_t)SLOTS * 2 * Way<T, VEC, NV, FILL>::Ring::row_bytes(p.M, p.width, p.width) +
+  const size_t smem = (size_t)SLOTS * 2 * Way<T, VEC, NV, FILL>::row_bytes(p.M, p.width) +
                       (FILL == ROW_SHIFT ? (size_t)2 * NV * p.width * VEC * sizeof(float) : 0);
   int ctas = 0;
   const cudaError_t e = fill(kernel, cache, p.width, smem, p.rows, 1 << 30, &ctas);
@@ -592,6 +647,12 @@ cudaError_t forward_launch(const SandwichFwd& p, cudaStream_t s) {
   return forward_launch<T, Y, VEC, NV, ROW_PART>(p, s);
 }
 
+// Threads for a row of that many accesses, no more warps than have some (powers of two: 8192 x 5120 bf16 backward 146 us, so 115)
+int warps_for(int accesses, int each, int least) {
+  const int warps = (accesses + 32 * each - 1) / (32 * each);
+  return 32 * (warps < least ? least : warps);
+}
+
 // Four accesses of 16 bytes a thread where there are rows for every SM, one where the chain of one row is all there is
 template <class T, class Y, int VEC>
 cudaError_t forward_nv(const SandwichFwd& p0, cudaStream_t s) {
@@ -599,6 +660,7 @@ cudaError_t forward_nv(const SandwichFwd& p0, cudaStream_t s) {
   const int acc = (p.M + VEC - 1 + (p.classes ? VEC - 1 : 0)) / VEC;
   p.width = row_width(acc, p.rows < 2 * sm_count() ? 1 : VEC > 1 ? 4 : 8, 512);
   const int nv = (acc + p.width - 1) / p.width;
+  if (VEC > 1) p.width = warps_for(acc, nv <= 2 ? nv : nv <= 4 || VEC == 8 ? 4 : 8, 1);
   // 512 threads take kNormMaxM elements in four accesses of eight, eight of four or thirty-two of one
   if (nv <= 1) return forward_launch<T, Y, VEC, 1>(p, s);
   if (nv <= 2) return forward_launch<T, Y, VEC, 2>(p, s);
@@ -622,7 +684,8 @@ cudaError_t backward_launch(const SandwichBwd& p, cudaStream_t s, int* ctas) {
   auto kernel = sandwich_backward_kernel<T, VEC, NV, SLOTS, DH, FILL, SOLO>;
   const int threads = SOLO ? p.width : 256, per = threads / p.width;
   size_t smem = (size_t)SLOTS * ROOMS * Ahead<T, VEC, NV, FILL>::row_bytes(p.M, threads, p.width);
-  if (!SOLO && p.part && smem < (size_t)per * 2 * p.M * sizeof(float)) smem = (size_t)per * 2 * p.M * sizeof(float);
+  const size_t sums = (size_t)per * 2 * part_row(p.M) * sizeof(float);
+  if (!SOLO && p.part && smem < sums) smem = sums;
   const cudaError_t e = fill(kernel, cache, threads, smem, (p.rows + per - 1) / per, backward_ctas(), ctas);
   return e != cudaSuccess ? e : launch_dep(kernel, *ctas, threads, smem, s, p);
 }
@@ -631,8 +694,10 @@ cudaError_t backward_rows_launch(const SandwichBwd& p, cudaStream_t s, int* ctas
   constexpr int ROOMS = DH && NV < 8 ? 4 : 3, R = NV <= 2 ? 2 : 1;
   static FillCache cache;
   auto kernel = sandwich_backward_rows_kernel<T, VEC, NV, R, DH, FILL>;
-  const size_t smem = (size_t)R * ROOMS * Way<T, VEC, NV, FILL>::Ring::row_bytes(p.M, p.width, p.width) +
-                      (FILL == ROW_SHIFT ? (size_t)2 * NV * p.width * VEC * sizeof(float) : 0);
+  size_t smem = (size_t)R * ROOMS * Way<T, VEC, NV, FILL>::row_bytes(p.M, p.width) +
+                (FILL == ROW_SHIFT ? (size_t)2 * NV * p.width * VEC * sizeof(float) : 0);
+  const size_t sums = (size_t)2 * part_row(p.M) * sizeof(float);
+  if ((FILL == ROW_PART || FILL == ROW_SHIFT) && p.part && smem < sums) smem = sums;
   const cudaError_t e = fill(kernel, cache, p.width, smem, (p.rows + R - 1) / R, backward_ctas(), ctas);
   if (FILL == ROW_SHIFT && e == cudaSuccess) *ctas = whole_classes(*ctas, p.classes);
   return e != cudaSuccess ? e : launch_dep(kernel, *ctas, p.width, smem, s, p);
@@ -663,9 +728,11 @@ template <class T, int VEC>
 cudaError_t backward_nv(const SandwichBwd& p0, cudaStream_t s, int* ctas) {
   SandwichBwd p = p0;
   const int acc = (p.M + VEC - 1 + (p.classes ? VEC - 1 : 0)) / VEC;
-  // two accesses a thread; one where rows are short and many (30000 x 1000 bf16 90 us against 95, but 2000 x 1000 17.5 against 14.2)
-  p.width = row_width(acc, VEC == 1 ? 4 : acc <= 128 && p.rows > 32 * sm_count() ? 1 : 2, 512);
+  // two accesses a thread; one where rows are short and many (30000 x 1000 bf16 85 us against 95, but 2000 x 1000 17.5 against 14.2), and
+  // where 128 threads would take twice more than there are (8192 x 1536 bf16 39 us against 43, but 8192 x 2048 45.3 against 43.6)
+  p.width = row_width(acc, VEC == 1 ? 4 : (acc <= 128 && p.rows > 32 * sm_count()) || (acc > 128 && acc <= 192) ? 1 : 2, 512);
   const int nv = (acc + p.width - 1) / p.width;
+  if (VEC > 1 && p.width >= 128) p.width = warps_for(acc, nv <= 2 ? nv : nv <= 4 || VEC == 8 ? 4 : 8, 4);
   if (nv <= 1) return backward_launch<T, VEC, 1>(p, s, ctas);
   if (nv <= 2) return backward_launch<T, VEC, 2>(p, s, ctas);
   if (nv <= 4) return backward_launch<T, VEC, 4>(p, s, ctas);
@@ -703,7 +770,7 @@ void fw_sandwich_desc_default(fw_sandwich_desc* d, int32_t M) {
 
 size_t fw_sandwich_scratch_bytes(const fw_sandwich_desc* d) {
   if (desc_check(d) != FW_OK) return 0;
-  return ((size_t)backward_ctas() * 2 * d->M * sizeof(float) + 255) / 256 * 256;
+  return ((size_t)backward_ctas() * 2 * part_row(d->M) * sizeof(float) + 255) / 256 * 256;
 }
 
 fw_status fw_sandwich_forward(const fw_sandwich_desc* d, int64_t rows, const void* o, int64_t ldo, const void* x, int64_t ldx,
@@ -796,7 +863,7 @@ fw_status fw_sandwich_backward(const fw_sandwich_desc* d, int64_t rows, const vo
   }
   if (e == cudaSuccess && sums) {
     ProfScope ps(FW_PROF_MISC, str);
-    e = launch_dep(sandwich_weight_kernel, (2 * M + 31) / 32, 1024, 0, str, p.part, ctas, M, dw_pre, dw_post);
+    e = launch_dep(sandwich_weight_kernel, (2 * part_row(M) + 31) / 32, 256, 0, str, p.part, ctas, M, dw_pre, dw_post);
   }
   return failed(e, "fw_sandwich_backward");
 }

@@ -129,6 +129,15 @@ def test_backward(B, rows, M, kind):
             assert torch.equal(h, dx) and torch.equal(o, do) and surround_kept(h) and surround_kept(o)
 
 
+@pytest.mark.parametrize("M", [640, 1152, 1280, 1536, 1601, 1793, 2304, 3585, 5120, 5121, 6144, 7168, 9216, 10240, 11777, 12288, 14336])
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+def test_rows_of_any_number_of_warps(B, M, kind):
+    """Three to fifteen warps a row, with rows for one access of a thread and for several."""
+    for rows in (5, 310):
+        test_forward(B, rows, M, kind, "e4m3" if rows == 5 else "same")
+        test_backward(B, rows, M, kind)
+
+
 def test_gradient_against_differences(B):
     """Central differences of the definition in 64 bits, step 1e-6 (1e-9 of the loss's terms); the kernel's fp32 is bounded as 1e-4
     of the largest element."""
