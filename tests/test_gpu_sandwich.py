@@ -181,6 +181,35 @@ def test_in_place_and_repeated(B):
             assert torch.equal(a[h_in], h) and torch.equal(a["x" if h_in == "o" else "o"], y) and surround_kept(a["o"]) and surround_kept(a["x"])
 
 
+@pytest.mark.parametrize("kind,M,pad", [("f32", 1537, 0), ("bf16", 1537, 0), ("bf16", 4096, None), ("f32", 5120, None), ("bf16", 603, 1), ("f32", 96, None),
+                                        ("bf16", 16384, None), ("f32", 16381, 2)])
+def test_backward_in_place(B, kind, M, pad):
+    """Each gradient in the place of each input that the header allows: the bits of the call with outputs of their own."""
+    rows = 700
+    a, g = inputs(rows, M, kind, 6, pad=pad), inputs(rows, M, kind, 7, pad=pad)
+    keep = dict(dy=g["o"], dh=g["x"], o=a["o"], h=a["x"])
+    rstd = torch.rand(rows, 2, generator=gen(8), device="cuda") + 0.5
+    d = desc(B, M, kind)
+    scratch = torch.empty(B.fw_sandwich_scratch_bytes(d), dtype=torch.uint8, device="cuda")
+
+    def call(i, dx, do):
+        dw1, dw2, dgate = (torch.empty(n, device="cuda") for n in (M, M, rows))
+        B.fw_sandwich_backward(d, i["dy"], i["o"], i["h"], a["w2"], rstd, dx, do, w_post=a["w1"], gate=a["gate"], dh=i["dh"], dw_post=dw1,
+                               dw_pre=dw2, dgate=dgate, scratch=scratch)
+        return dx, do, dw1, dw2, dgate
+
+    want = call(keep, matrix(rows, M, KINDS[kind], pad=pad), matrix(rows, M, KINDS[kind], pad=pad))
+    for x in ("dy", "dh", "h"):
+        for o in ("dy", "dh", "o", "h"):
+            if x == o:
+                continue
+            i = {k: put(v, KINDS[kind], pad=pad) for k, v in keep.items()}
+            got = call(i, i[x], i[o])
+            assert all(torch.equal(p, q) for p, q in zip(got, want)), (x, o)
+            assert all(surround_kept(v) for v in i.values())
+            assert all(torch.equal(i[k], keep[k]) for k in i if k not in (x, o))
+
+
 def test_values_that_are_none(B):
     """A NaN or an infinity stays in its row; rows of zeros and squares that pass fp32 as in the norm."""
     M = 600
