@@ -189,8 +189,10 @@ constexpr int kWarpGroups = 512, kWarpRows = 8;
 
 template <class T, int MODE, bool SAME, int TH>
 cudaError_t launch_ctas(const Logprob& p, cudaStream_t s) {
-  const int64_t most = (int64_t)(1024 / TH) * sm_count();
-  return launch_dep(logprob_kernel<T, MODE, SAME, TH>, (unsigned)(p.rows < most ? p.rows : most), TH, 0, s, p);
+  const int64_t most = (int64_t)(1024 / TH) * sm_count(), turns = (p.rows + most - 1) / most;
+  // of the gradient alone no more CTAs than take equal turns (2451 x 50257 bf16 84.5 us against 87; the sums would be slower: 57 against 51)
+  const int64_t ctas = MODE == LP_BACKWARD ? (p.rows + turns - 1) / turns : most;
+  return launch_dep(logprob_kernel<T, MODE, SAME, TH>, (unsigned)(p.rows < ctas ? p.rows : ctas), TH, 0, s, p);
 }
 template <class T, int MODE, bool SAME>
 cudaError_t launch(const Logprob& p, cudaStream_t s) {
