@@ -21,36 +21,46 @@ using namespace norm;
 // the first and the last of a row may hold other rows' elements.  How far a row lies past them repeats every 16 bytes / element rows, so a CTA
 // takes rows of one residue, and its columns stay its own; the weights wait in shared memory, moved as the row is.  (Element by element,
 // backward of 5003 x 1537 fp32: 82 us.)
-enum { ROW_SHIFT = 3 };
+// Aligned rows that end inside an access (TAIL) are taken the same way, the copy filling what lies behind the row with zeros.  (Their last elements read one
+// by one where they are used, which all warps of the row waited for: 8192 x 4095 bf16 backward 134 us, so 98.)
+enum { ROW_SHIFT = 3, ROW_TAIL = 4 };
 template <class T, int VEC, int NV, int FILL>
 struct Way {
-  typedef Ahead<T, VEC, NV, FILL == ROW_SHIFT ? ROW_PART : FILL> Ring;
+  static constexpr bool MOVED = FILL == ROW_SHIFT || FILL == ROW_TAIL;
+  typedef Ahead<T, VEC, NV, MOVED ? ROW_PART : FILL> Ring;
   int M, t, width, shift;
-  // bytes of a row of one tensor (not those of accesses that no thread has: 5003 x 1537 fp32 backward 46 us with them)
+  // bytes of a row of one tensor
   static __host__ __device__ __forceinline__ uint32_t row_bytes(int M, int width) {
     return VEC > 1 ? (uint32_t)((M + (FILL == ROW_SHIFT ? 2 * VEC - 2 : VEC - 1)) / VEC * 16) : Ring::row_bytes(M, width, width);
   }
+  // bytes of a row of weights, where they wait in shared memory
+  static __host__ __device__ __forceinline__ uint32_t weight_bytes(int width) { return MOVED ? (uint32_t)(NV * width * VEC * sizeof(float)) : 0u; }
   __device__ __forceinline__ int column(int k) const { return (t + k * width) * VEC - (FILL == ROW_SHIFT ? shift : 0); }
   __device__ __forceinline__ bool inside(int c) const { return c >= 0 && c + VEC <= M; }
   __device__ __forceinline__ void fetch(uint32_t room, const T* row) const {
-    if (FILL != ROW_SHIFT) {
+    if (!MOVED) {
       Ring::fetch(room, row, M, t, width);
     } else {
 #pragma unroll
       for (int k = 0; k < NV; ++k) {
         const int c = column(k);
-        if (c > -VEC && c < M) ahead16(room + (uint32_t)(k * (int)blockDim.x + (int)threadIdx.x) * 16u, row + c);
+        const uint32_t to = room + (uint32_t)(k * (int)blockDim.x + (int)threadIdx.x) * 16u;
+        if (FILL == ROW_TAIL) {
+          if (c < M) ahead16(to, row + c, M - c < VEC ? (M - c) * (int)sizeof(T) : 16);
+        } else if (c > -VEC && c < M) {
+          ahead16(to, row + c);
+        }
       }
     }
   }
   __device__ __forceinline__ void get(const uint8_t* room, const T* row, int k, float (&v)[VEC]) const {
     const int c = column(k);
-    if (FILL != ROW_SHIFT) {
+    if (!MOVED) {
       Ring::get(room, row, M, width, k, c, M - c, v);
     } else {
-      // (of accesses behind the row's what comes next in shared memory, the weights at last)
-      load<VEC>(reinterpret_cast<const T*>(room + (k * (int)blockDim.x + (int)threadIdx.x) * 16), VEC, 0.f, v);
-      if (!inside(c)) {
+      // (SHIFT: of accesses behind the row's what comes next in shared memory, the weights at last)
+      load<VEC>(reinterpret_cast<const T*>(room + (k * (int)blockDim.x + (int)threadIdx.x) * 16), FILL == ROW_SHIFT || c < M ? VEC : 0, 0.f, v);
+      if (FILL == ROW_SHIFT && !inside(c)) {
 #pragma unroll
         for (int e = 0; e < VEC; ++e)
           if (c + e < 0 || c + e >= M) v[e] = 0.f;
@@ -60,7 +70,7 @@ struct Way {
   template <class Y>
   __device__ __forceinline__ void keep(Y* row, int k, const float (&v)[VEC]) const {
     const int c = column(k);
-    if (FILL != ROW_SHIFT) {
+    if (!MOVED) {
       Ring::keep(row + c, M - c, v);
     } else if (inside(c)) {
       store<VEC>(row + c, VEC, v);
@@ -70,9 +80,9 @@ struct Way {
         if (c + e >= 0 && c + e < M) put(row + c + e, v[e]);
     }
   }
-  // a row of weights, or (SHIFT) its place in shared memory
+  // a row of weights, or its place in shared memory
   __device__ __forceinline__ void weights(const float* w, const float* moved, int k, float (&v)[VEC]) const {
-    if (FILL != ROW_SHIFT) Ring::plain(w + column(k), M - column(k), v);
+    if (!MOVED) Ring::plain(w + column(k), M - column(k), v);
     else load<VEC>(moved + (t + k * width) * VEC, VEC, 0.f, v);
   }
   __device__ __forceinline__ void move(const float* w, float* moved) const {
@@ -138,7 +148,7 @@ __global__ void __maxnreg__(96) sandwich_forward_kernel(const SandwichFwd p) {
   dep_wait();
 #pragma unroll
   for (int i = 0; i < SLOTS; ++i) fetch(begin + i * step, i);
-  if (FILL == ROW_SHIFT) {
+  if (Rows::MOVED) {
     if (p.w1) way.move(p.w1, w1);
     way.move(p.w2, w2);
     __syncthreads();
@@ -442,7 +452,7 @@ __global__ void __launch_bounds__(512) sandwich_backward_rows_kernel(const Sandw
   fetch(O, row0);
   if (ROOMS == 4) fetch(D, row0);
   ahead_commit();
-  if (FILL == ROW_SHIFT) {
+  if (Rows::MOVED) {
     if (p.w1) way.move(p.w1, w1);
     way.move(p.w2, w2);
     __syncthreads();
@@ -630,8 +640,8 @@ cudaError_t forward_launch(const SandwichFwd& p, cudaStream_t s) {
   constexpr int SLOTS = slots(VEC, NV, 2);
   static FillCache cache;
   auto kernel = sandwich_forward_kernel<T, Y, VEC, NV, SLOTS, FILL>;
-  const size_t smem = (size_t)SLOTS * 2 * Way<T, VEC, NV, FILL>::row_bytes(p.M, p.width) +
-                      (FILL == ROW_SHIFT ? (size_t)2 * NV * p.width * VEC * sizeof(float) : 0);
+  typedef Way<T, VEC, NV, FILL> Rows;
+  const size_t smem = (size_t)SLOTS * 2 * Rows::row_bytes(p.M, p.width) + 2 * (size_t)Rows::weight_bytes(p.width);
   int ctas = 0;
   const cudaError_t e = fill(kernel, cache, p.width, smem, p.rows, 1 << 30, &ctas);
   if (FILL == ROW_SHIFT && e == cudaSuccess) ctas = whole_classes(ctas, p.classes);
@@ -640,7 +650,7 @@ cudaError_t forward_launch(const SandwichFwd& p, cudaStream_t s) {
 template <class T, class Y, int VEC, int NV>
 cudaError_t forward_launch(const SandwichFwd& p, cudaStream_t s) {
   if constexpr (VEC > 1 && sizeof(T) == sizeof(Y) && NV <= 4)
-    if (p.classes) return forward_launch<T, Y, VEC, NV, ROW_SHIFT>(p, s);
+    if (p.classes) return p.classes == 1 ? forward_launch<T, Y, VEC, NV, ROW_TAIL>(p, s) : forward_launch<T, Y, VEC, NV, ROW_SHIFT>(p, s);
   constexpr int WHOLE = VEC > 1 ? ROW_WHOLE : ROW_PART, FULL = VEC > 1 ? ROW_FULL : ROW_PART;
   if (VEC > 1 && p.M == NV * VEC * p.width) return forward_launch<T, Y, VEC, NV, FULL>(p, s);
   if (VEC > 1 && p.M % VEC == 0) return forward_launch<T, Y, VEC, NV, WHOLE>(p, s);
@@ -657,7 +667,7 @@ int warps_for(int accesses, int each, int least) {
 template <class T, class Y, int VEC>
 cudaError_t forward_nv(const SandwichFwd& p0, cudaStream_t s) {
   SandwichFwd p = p0;
-  const int acc = (p.M + VEC - 1 + (p.classes ? VEC - 1 : 0)) / VEC;
+  const int acc = (p.M + VEC - 1 + (p.classes > 1 ? VEC - 1 : 0)) / VEC;
   p.width = row_width(acc, p.rows < 2 * sm_count() ? 1 : VEC > 1 ? 4 : 8, 512);
   const int nv = (acc + p.width - 1) / p.width;
   if (VEC > 1) p.width = warps_for(acc, nv <= 2 ? nv : nv <= 4 || VEC == 8 ? 4 : 8, 1);
@@ -694,10 +704,10 @@ cudaError_t backward_rows_launch(const SandwichBwd& p, cudaStream_t s, int* ctas
   constexpr int ROOMS = DH && NV < 8 ? 4 : 3, R = NV <= 2 ? 2 : 1;
   static FillCache cache;
   auto kernel = sandwich_backward_rows_kernel<T, VEC, NV, R, DH, FILL>;
-  size_t smem = (size_t)R * ROOMS * Way<T, VEC, NV, FILL>::row_bytes(p.M, p.width) +
-                (FILL == ROW_SHIFT ? (size_t)2 * NV * p.width * VEC * sizeof(float) : 0);
+  typedef Way<T, VEC, NV, FILL> Rows;
+  size_t smem = (size_t)R * ROOMS * Rows::row_bytes(p.M, p.width) + 2 * (size_t)Rows::weight_bytes(p.width);
   const size_t sums = (size_t)2 * part_row(p.M) * sizeof(float);
-  if ((FILL == ROW_PART || FILL == ROW_SHIFT) && p.part && smem < sums) smem = sums;
+  if ((FILL == ROW_PART || Rows::MOVED) && p.part && smem < sums) smem = sums;
   const cudaError_t e = fill(kernel, cache, p.width, smem, (p.rows + R - 1) / R, backward_ctas(), ctas);
   if (FILL == ROW_SHIFT && e == cudaSuccess) *ctas = whole_classes(*ctas, p.classes);
   return e != cudaSuccess ? e : launch_dep(kernel, *ctas, p.width, smem, s, p);
@@ -705,7 +715,8 @@ cudaError_t backward_rows_launch(const SandwichBwd& p, cudaStream_t s, int* ctas
 template <class T, int VEC, int NV, bool DH>
 cudaError_t backward_launch(const SandwichBwd& p, cudaStream_t s, int* ctas) {
   if constexpr (VEC > 1 && NV <= 4)
-    if (p.classes) return backward_rows_launch<T, VEC, NV, DH, ROW_SHIFT>(p, s, ctas);
+    if (p.classes)
+      return p.classes == 1 ? backward_rows_launch<T, VEC, NV, DH, ROW_TAIL>(p, s, ctas) : backward_rows_launch<T, VEC, NV, DH, ROW_SHIFT>(p, s, ctas);
   if constexpr (NV <= 4) {                                   // more accesses a thread: 128 threads or more (see backward_nv)
     if (p.width < 128)
       return VEC > 1 && p.M % VEC == 0 ? backward_launch<T, VEC, NV, DH, (VEC > 1 ? ROW_WHOLE : ROW_PART), false>(p, s, ctas)
@@ -727,7 +738,7 @@ cudaError_t backward_launch(const SandwichBwd& p, cudaStream_t s, int* ctas) {
 template <class T, int VEC>
 cudaError_t backward_nv(const SandwichBwd& p0, cudaStream_t s, int* ctas) {
   SandwichBwd p = p0;
-  const int acc = (p.M + VEC - 1 + (p.classes ? VEC - 1 : 0)) / VEC;
+  const int acc = (p.M + VEC - 1 + (p.classes > 1 ? VEC - 1 : 0)) / VEC;
   // two accesses a thread; one where rows are short and many (30000 x 1000 bf16 85 us against 95, but 2000 x 1000 17.5 against 14.2), and
   // where 128 threads would take twice more than there are (8192 x 1536 bf16 39 us against 43, but 8192 x 2048 45.3 against 43.6)
   p.width = row_width(acc, VEC == 1 ? 4 : (acc <= 128 && p.rows > 32 * sm_count()) || (acc > 128 && acc <= 192) ? 1 : 2, 512);
@@ -743,13 +754,15 @@ cudaError_t backward_nv(const SandwichBwd& p0, cudaStream_t s, int* ctas) {
 
 // A range of memory that a call reads or writes; ld, elem: of a matrix (0: a vector)
 struct Range { const void* p; uint64_t n; int64_t ld; int elem; };
-// Rows after which matrices that all lie equally past 16 bytes do so as at their beginning; 0 where they do not, where rows are so long that
+// Rows after which matrices that all lie equally past 16 bytes do so as at their beginning (1: aligned rows that end inside 16 bytes); 0 where they do not, where rows are so long that
 // they and the weights do not fit shared memory together, or so short that a few threads take several
-int classes_of(const Mat* m, int n, int M) {
+int classes_of(const Mat* m, int n, int M, bool aligned) {
+  const bool fits = M <= 6144 && M * m[0].elem > 2048;
+  if (aligned) return fits && M * m[0].elem % 16 != 0 ? 1 : 0;
   uint64_t differ = 0;
   for (int i = 0; i < n; ++i)
     if (m[i].p) differ |= (reinterpret_cast<uintptr_t>(m[i].p) ^ reinterpret_cast<uintptr_t>(m[0].p)) | (uint64_t)((m[i].ld - m[0].ld) * m[0].elem);
-  return (differ & 15) == 0 && M <= 6144 && M * m[0].elem > 2048 ? 16 / m[0].elem : 0;
+  return (differ & 15) == 0 && fits ? 16 / m[0].elem : 0;
 }
 Range mat(const void* p, int64_t rows, int M, int64_t ld, int elem) { return {p, p ? matrix_span(rows, M, ld, elem) : 0, ld, elem}; }
 Range vec4(const void* p, uint64_t n) { return {p, 4 * n, 0, 4}; }
@@ -801,7 +814,7 @@ fw_status fw_sandwich_forward(const fw_sandwich_desc* d, int64_t rows, const voi
   SandwichFwd p;
   p.o = o; p.x = x; p.w1 = w_post; p.gate = gate; p.w2 = w_pre; p.h = h; p.y = y; p.y_scale = y_scale; p.rstd = rstd;
   p.rows = rows; p.ldo = ldo; p.ldx = ldx; p.ldh = ldh; p.ldy = ldy; p.M = M; p.width = 0; p.post = d->post;
-  p.classes = vec || q8 ? 0 : classes_of(mats, 4, M);
+  p.classes = q8 ? 0 : classes_of(mats, 4, M, vec);
   p.eps = d->eps; p.inv_M = 1.f / (float)M; p.alpha = d->alpha;
   cudaStream_t s = (cudaStream_t)cuda_stream;
   ProfScope ps(FW_PROF_MISC, s);
@@ -850,7 +863,7 @@ fw_status fw_sandwich_backward(const fw_sandwich_desc* d, int64_t rows, const vo
   p.dy = dy; p.dh = dh; p.o = o; p.h = h; p.w1 = w_post; p.gate = gate; p.w2 = w_pre; p.rstd = rstd; p.dx = dx; p.d_o = d_o;
   p.part = sums ? static_cast<float*>(scratch) : nullptr; p.dgate = dgate;
   p.rows = rows; p.lddy = lddy; p.lddh = lddh; p.ldo = ldo; p.ldh = ldh; p.lddx = lddx; p.lddo = lddo; p.M = M; p.width = 0;
-  p.classes = vec ? 0 : classes_of(mats, 6, M);
+  p.classes = classes_of(mats, 6, M, vec);
   p.post = d->post; p.inv_M = 1.f / (float)M; p.alpha = d->alpha;
   cudaStream_t str = (cudaStream_t)cuda_stream;
   int ctas = 0;
