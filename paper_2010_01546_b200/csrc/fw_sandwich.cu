@@ -22,16 +22,17 @@ using namespace norm;
 // takes rows of one residue, and its columns stay its own; the weights wait in shared memory, moved as the row is.  (Element by element,
 // backward of 5003 x 1537 fp32: 82 us.)
 // Aligned rows that end inside an access (TAIL) are taken the same way, the copy filling what lies behind the row with zeros.  (Their last elements read one
-// by one where they are used, which all warps of the row waited for: 8192 x 4095 bf16 backward 134 us, so 98.)
+// by one where they are used, which all warps of the row waited for: 8192 x 4095 bf16 backward 134 us, so 87.)
 enum { ROW_SHIFT = 3, ROW_TAIL = 4 };
 template <class T, int VEC, int NV, int FILL>
 struct Way {
   static constexpr bool MOVED = FILL == ROW_SHIFT || FILL == ROW_TAIL;
+  static constexpr bool ZEROS = VEC > 1 && (FILL == ROW_WHOLE || FILL == ROW_TAIL);      // in accesses behind the row, see zeros()
   typedef Ahead<T, VEC, NV, MOVED ? ROW_PART : FILL> Ring;
   int M, t, width, shift;
   // bytes of a row of one tensor
   static __host__ __device__ __forceinline__ uint32_t row_bytes(int M, int width) {
-    return VEC > 1 ? (uint32_t)((M + (FILL == ROW_SHIFT ? 2 * VEC - 2 : VEC - 1)) / VEC * 16) : Ring::row_bytes(M, width, width);
+    return VEC > 1 && !ZEROS ? (uint32_t)((M + (FILL == ROW_SHIFT ? 2 * VEC - 2 : VEC - 1)) / VEC * 16) : Ring::row_bytes(M, width, width);
   }
   // bytes of a row of weights, where they wait in shared memory
   static __host__ __device__ __forceinline__ uint32_t weight_bytes(int width) { return MOVED ? (uint32_t)(NV * width * VEC * sizeof(float)) : 0u; }
@@ -55,12 +56,14 @@ struct Way {
   }
   __device__ __forceinline__ void get(const uint8_t* room, const T* row, int k, float (&v)[VEC]) const {
     const int c = column(k);
-    if (!MOVED) {
+    if (ZEROS) {
+      load<VEC>(reinterpret_cast<const T*>(room + (k * (int)blockDim.x + (int)threadIdx.x) * 16), VEC, 0.f, v);
+    } else if (!MOVED) {
       Ring::get(room, row, M, width, k, c, M - c, v);
     } else {
-      // (SHIFT: of accesses behind the row's what comes next in shared memory, the weights at last)
-      load<VEC>(reinterpret_cast<const T*>(room + (k * (int)blockDim.x + (int)threadIdx.x) * 16), FILL == ROW_SHIFT || c < M ? VEC : 0, 0.f, v);
-      if (FILL == ROW_SHIFT && !inside(c)) {
+      // (of accesses behind the row's what comes next in shared memory, the weights at last)
+      load<VEC>(reinterpret_cast<const T*>(room + (k * (int)blockDim.x + (int)threadIdx.x) * 16), VEC, 0.f, v);
+      if (!inside(c)) {
 #pragma unroll
         for (int e = 0; e < VEC; ++e)
           if (c + e < 0 || c + e >= M) v[e] = 0.f;
@@ -79,6 +82,13 @@ struct Way {
       for (int e = 0; e < VEC; ++e)
         if (c + e >= 0 && c + e < M) put(row + c + e, v[e]);
     }
+  }
+  // Zeros in the accesses of n rows that lie behind a row's end: once, so that no reading of them asks (8192 x 4095 bf16 backward 98 us with that)
+  __device__ __forceinline__ void zeros(uint8_t* room, uint32_t stride, int n) const {
+    if (!ZEROS) return;
+    for (int k = 0; k < NV; ++k)
+      if (column(k) >= M)
+        for (int i = 0; i < n; ++i) *reinterpret_cast<uint4*>(room + i * stride + (k * (int)blockDim.x + (int)threadIdx.x) * 16) = make_uint4(0, 0, 0, 0);
   }
   // a row of weights, or its place in shared memory
   __device__ __forceinline__ void weights(const float* w, const float* moved, int k, float (&v)[VEC]) const {
@@ -153,6 +163,7 @@ __global__ void __maxnreg__(96) sandwich_forward_kernel(const SandwichFwd p) {
     way.move(p.w2, w2);
     __syncthreads();
   }
+  way.zeros(room, row_bytes, 2 * SLOTS);
   int i = 0, flip = 0;
   for (int64_t row = begin; row < p.rows; row += step, flip ^= 1) {
     const uint8_t* slot = room + i * slot_bytes;
@@ -457,6 +468,7 @@ __global__ void __launch_bounds__(512) sandwich_backward_rows_kernel(const Sandw
     way.move(p.w2, w2);
     __syncthreads();
   }
+  way.zeros(room, row_bytes, R * ROOMS);
   Head a[R];
 #pragma unroll
   for (int r = 0; r < R; ++r) a[r] = head(row0 + r * apart);
@@ -739,7 +751,7 @@ template <class T, int VEC>
 cudaError_t backward_nv(const SandwichBwd& p0, cudaStream_t s, int* ctas) {
   SandwichBwd p = p0;
   const int acc = (p.M + VEC - 1 + (p.classes > 1 ? VEC - 1 : 0)) / VEC;
-  // two accesses a thread; one where rows are short and many (30000 x 1000 bf16 85 us against 95, but 2000 x 1000 17.5 against 14.2), and
+  // two accesses a thread; one where rows are short and many (30000 x 1000 bf16 79 us against 95, but 2000 x 1000 17.5 against 14.2), and
   // where 128 threads would take twice more than there are (8192 x 1536 bf16 39 us against 43, but 8192 x 2048 45.3 against 43.6)
   p.width = row_width(acc, VEC == 1 ? 4 : (acc <= 128 && p.rows > 32 * sm_count()) || (acc > 128 && acc <= 192) ? 1 : 2, 512);
   const int nv = (acc + p.width - 1) / p.width;
