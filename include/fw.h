@@ -450,7 +450,7 @@ fw_status fw_distill_backward(const fw_distill_desc* d, const void* Z, int64_t r
  * router's weight), rows fp32, NULL: 1; rstd: rows x 2 fp32 (rstd1, rstd2), NULL: not kept; y_scale: rows, with e4m3 and only then.
  * h and y may be o or x itself (same address, type and ld; not the same one); any other overlap of outputs with
  * inputs or with each other is FW_ERR_INVALID_ARG.  Matrices that all lie equally past a 16-byte boundary, and stay so from row to row
- * together, move 16 bytes at a time too: up to 15 bytes behind an input are then read, never used.  What holds for the rows of fw_rmsnorm_forward holds here: NaN, infinity,
+ * together, move 16 bytes at a time too.  What holds for the rows of fw_rmsnorm_forward holds here: NaN, infinity,
  * squares that pass fp32, M <= 16384. */
 typedef struct {
   int32_t M;

@@ -18,21 +18,21 @@ namespace {
 using namespace norm;
 
 // How aligned accesses of a thread meet its rows.  Rows whose matrices all lie equally past 16 bytes (SHIFT) are taken by such accesses too:
-// the first and the last of a row may hold other rows' elements.  How far a row lies past them repeats every 16 bytes / element rows, so a CTA
+// the first of a row may hold the row before's elements, what lies behind the row the copy fills with zeros.  How far a row lies past them repeats every 16 bytes / element rows, so a CTA
 // takes rows of one residue, and its columns stay its own; the weights wait in shared memory, moved as the row is.  (Element by element,
 // backward of 5003 x 1537 fp32: 82 us.)
-// Aligned rows that end inside an access (TAIL) are taken the same way, the copy filling what lies behind the row with zeros.  (Their last elements read one
-// by one where they are used, which all warps of the row waited for: 8192 x 4095 bf16 backward 134 us, so 87.)
+// Aligned rows that end inside an access (TAIL) are taken the same way.  (Their last elements read one by one where
+// they are used, which all warps of the row waited for: 8192 x 4095 bf16 backward 134 us, so 87.)
 enum { ROW_SHIFT = 3, ROW_TAIL = 4 };
 template <class T, int VEC, int NV, int FILL>
 struct Way {
   static constexpr bool MOVED = FILL == ROW_SHIFT || FILL == ROW_TAIL;
-  static constexpr bool ZEROS = VEC > 1 && (FILL == ROW_WHOLE || FILL == ROW_TAIL);      // in accesses behind the row, see zeros()
+  static constexpr bool ZEROS = VEC > 1 && (FILL == ROW_WHOLE || MOVED);      // in accesses behind the row, see zeros()
   typedef Ahead<T, VEC, NV, MOVED ? ROW_PART : FILL> Ring;
   int M, t, width, shift;
   // bytes of a row of one tensor
   static __host__ __device__ __forceinline__ uint32_t row_bytes(int M, int width) {
-    return VEC > 1 && !ZEROS ? (uint32_t)((M + (FILL == ROW_SHIFT ? 2 * VEC - 2 : VEC - 1)) / VEC * 16) : Ring::row_bytes(M, width, width);
+    return VEC > 1 && !ZEROS ? (uint32_t)((M + VEC - 1) / VEC * 16) : Ring::row_bytes(M, width, width);
   }
   // bytes of a row of weights, where they wait in shared memory
   static __host__ __device__ __forceinline__ uint32_t weight_bytes(int width) { return MOVED ? (uint32_t)(NV * width * VEC * sizeof(float)) : 0u; }
@@ -46,11 +46,7 @@ struct Way {
       for (int k = 0; k < NV; ++k) {
         const int c = column(k);
         const uint32_t to = room + (uint32_t)(k * (int)blockDim.x + (int)threadIdx.x) * 16u;
-        if (FILL == ROW_TAIL) {
-          if (c < M) ahead16(to, row + c, M - c < VEC ? (M - c) * (int)sizeof(T) : 16);
-        } else if (c > -VEC && c < M) {
-          ahead16(to, row + c);
-        }
+        if (c < M) ahead16(to, row + c, M - c < VEC ? (M - c) * (int)sizeof(T) : 16);
       }
     }
   }
@@ -58,16 +54,13 @@ struct Way {
     const int c = column(k);
     if (ZEROS) {
       load<VEC>(reinterpret_cast<const T*>(room + (k * (int)blockDim.x + (int)threadIdx.x) * 16), VEC, 0.f, v);
-    } else if (!MOVED) {
-      Ring::get(room, row, M, width, k, c, M - c, v);
-    } else {
-      // (of accesses behind the row's what comes next in shared memory, the weights at last)
-      load<VEC>(reinterpret_cast<const T*>(room + (k * (int)blockDim.x + (int)threadIdx.x) * 16), VEC, 0.f, v);
-      if (!inside(c)) {
+      if (FILL == ROW_SHIFT && k == 0 && c < 0) {            // what the row before has there
 #pragma unroll
-        for (int e = 0; e < VEC; ++e)
-          if (c + e < 0 || c + e >= M) v[e] = 0.f;
+        for (int e = 0; e < VEC - 1; ++e)
+          if (c + e < 0) v[e] = 0.f;
       }
+    } else {
+      Ring::get(room, row, M, width, k, c, M - c, v);
     }
   }
   template <class Y>
@@ -661,8 +654,10 @@ cudaError_t forward_launch(const SandwichFwd& p, cudaStream_t s) {
 }
 template <class T, class Y, int VEC, int NV>
 cudaError_t forward_launch(const SandwichFwd& p, cudaStream_t s) {
-  if constexpr (VEC > 1 && sizeof(T) == sizeof(Y) && NV <= 4)
-    if (p.classes) return p.classes == 1 ? forward_launch<T, Y, VEC, NV, ROW_TAIL>(p, s) : forward_launch<T, Y, VEC, NV, ROW_SHIFT>(p, s);
+  if constexpr (VEC > 1 && NV <= 4)
+    if (p.classes == 1) return forward_launch<T, Y, VEC, NV, ROW_TAIL>(p, s);
+  if constexpr (VEC > 1 && NV <= 4 && sizeof(T) == sizeof(Y))
+    if (p.classes) return forward_launch<T, Y, VEC, NV, ROW_SHIFT>(p, s);
   constexpr int WHOLE = VEC > 1 ? ROW_WHOLE : ROW_PART, FULL = VEC > 1 ? ROW_FULL : ROW_PART;
   if (VEC > 1 && p.M == NV * VEC * p.width) return forward_launch<T, Y, VEC, NV, FULL>(p, s);
   if (VEC > 1 && p.M % VEC == 0) return forward_launch<T, Y, VEC, NV, WHOLE>(p, s);
@@ -826,7 +821,7 @@ fw_status fw_sandwich_forward(const fw_sandwich_desc* d, int64_t rows, const voi
   SandwichFwd p;
   p.o = o; p.x = x; p.w1 = w_post; p.gate = gate; p.w2 = w_pre; p.h = h; p.y = y; p.y_scale = y_scale; p.rstd = rstd;
   p.rows = rows; p.ldo = ldo; p.ldx = ldx; p.ldh = ldh; p.ldy = ldy; p.M = M; p.width = 0; p.post = d->post;
-  p.classes = q8 ? 0 : classes_of(mats, 4, M, vec);
+  p.classes = q8 && !vec ? 0 : classes_of(mats, q8 ? 3 : 4, M, vec);      // (a row of e4m3 lies otherwise past 16 bytes)
   p.eps = d->eps; p.inv_M = 1.f / (float)M; p.alpha = d->alpha;
   cudaStream_t s = (cudaStream_t)cuda_stream;
   ProfScope ps(FW_PROF_MISC, s);
