@@ -588,7 +588,10 @@ fw_status fw_adamw_destroy(fw_adamw* a);
  * lr >= 0; lr_factor: one device fp32 that multiplies lr (a schedule inside a captured graph), NULL: 1.
  * max_norm > 0: c = min(1, max_norm / norm) with the norm of all gradients together; infinity: none are scaled, but the norm is
  * looked at.  Where it is not finite (|G| beyond 2e18 may count as that) the whole step is left out (P, copies, states and number of
- * steps stay as they are) and the next sync_status tells.  max_norm = 0: c = 1, and a NaN or infinity goes into P.
+ * steps stay as they are) and the next sync_status tells.  max_norm = 0: c = 1, and a NaN or infinity goes into P.  An element whose v
+ * passes fp32 by a finite gradient (1.8e19 / sqrt(1 - beta2) and more) takes no step from then on, since v stays infinite.  In 8-bit states a v
+ * that is not finite is held as the NaN code, which is read as infinity, with the code 0 of m, and has no part in the scales: the other elements
+ * of its block go on as if it were not there.
  * norm_out: one device fp32, the norm before clipping; with max_norm > 0, NULL: not kept.  Gradients may not overlap P, copies
  * or the workspace. */
 fw_status fw_adamw_step(fw_adamw* a, const void* const* G, const int32_t* g_dtype, float lr, const float* lr_factor,

@@ -251,6 +251,7 @@ __device__ __forceinline__ float inverse_scale(uint32_t b) { return __uint_as_fl
 // number of smallest codes in both.
 constexpr float kDown = 0x1p-120f, kUp = 0x1p120f;
 constexpr uint32_t kStep = 0x100000u;    // from one code to the next
+constexpr float kMost = 3.402823466e38f; // the largest finite number
 // The top bytes of four words
 __device__ __forceinline__ uint32_t top_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
   return __byte_perm(__byte_perm(a, b, 0x0073), __byte_perm(c, d, 0x0073), 0x5410);
@@ -324,6 +325,11 @@ __device__ __forceinline__ void from_e4m3(uint32_t w, float (&o)[4]) {
 __device__ __forceinline__ float warp_max(float v) {
   float r;
   asm("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
+  return r;
+}
+__device__ __forceinline__ float warp_max_keep_nan(float v) {
+  float r;
+  asm("redux.sync.max.NaN.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
   return r;
 }
 // Relative error 2^-23, of subnormal numbers too: a v of gradients below 1e-18 is one, and eps may be less than its root
@@ -432,6 +438,10 @@ __device__ __forceinline__ void update(const Args& a, const Step& st, const Bits
     if constexpr (S8) {
       from_e4m3(in.s.m[k], m[k]);
       from_e4m3(in.s.v[k], v);
+      if ((in.s.v[k] + 0x01010101u) & 0x80808080u) {         // a NaN's code: infinity
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = fminf(v[e], INFINITY);
+      }
       vscale<4>(m[k], scale_of(scale_m) * st.beta1);         // a power of two: no rounding but beta1's product
       const float s = scale_of(scale_v);
       if (scale_v >= 70) {                                   // its square is in range
@@ -477,10 +487,31 @@ __device__ __forceinline__ void update(const Args& a, const Step& st, const Bits
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       tm = fmaxf(tm, fmaxf(fabsf(m[0][e]), fabsf(m[1][e])));
-      tr = fmaxf(tr, fmaxf(r[0][e], r[1][e]));
+      tr = max_keep_nan(tr, max_keep_nan(r[0][e], r[1][e]));
+    }
+    tr = warp_max_keep_nan(tr);
+    if (!(tr <= kMost)) {
+      // An element whose v is not finite takes no part in the scales, which would hold the others' as nothing: the code of its root is the
+      // NaN's, 480 = 1.875 2^8 in the codes' numbers, that of its m, which takes no step any more, 0.
+      tm = tr = 0.f;
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          if (r[k][e] <= kMost) tr = fmaxf(tr, r[k][e]);
+          else m[k][e] = 0.f;
+          tm = fmaxf(tm, fabsf(m[k][e]));
+        }
+      tr = warp_max(tr);
+      const float none = 480.f * scale_of(scale_byte(tr));
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (!(r[k][e] <= kMost)) r[k][e] = none;
     }
     uint32_t bm = scale_byte(warp_max(tm));
-    const uint32_t bv = scale_byte(warp_max(tr));
+    const uint32_t bv = scale_byte(tr);
     scale_m = bm;
     scale_v = bv;
     if (bm > 156) {                                          // 2^-120 over the scale is out of range

@@ -362,3 +362,46 @@ def test_gradients_whose_squares_are_subnormal(B, kind):
     zero = torch.zeros(3000, dtype=F64, device="cuda")
     _, v1, p1, _, _ = formula(P * 0, G, zero, zero, 1, 1e-2, 0.0, 1.0, 0.9, 0.999, 1e-30)
     assert bool(((P.to(F64) - p1).abs() <= p1.abs() * (0.5 * 2.0 ** -150 / v1 + 24 * U)).all())
+
+
+@pytest.mark.parametrize("kind", ["f32", "e4m3"])
+@pytest.mark.parametrize("bad", [1e21, 1e25, float("-inf"), float("nan")])
+def test_an_overflow_stays_in_its_element(B, kind, bad):
+    """Without clipping, a gradient whose scaled square passes fp32, an infinity, a NaN: the other elements of its block, those that never
+    had a gradient among them, go the way that they go where its gradients are 0.  P there: a v of infinity takes no step (m is finite), what is
+    not finite in m goes into P."""
+    n, at = 700, 300
+    P, G = tensors([n], 51)
+    G[0][256:400:3] = 0                                              # of the same block, v = 0
+    G[0][at] = 0
+    Q, p0 = [P[0].clone()], P[0].clone()
+    state = B.FW_F32 if kind == "f32" else B.FW_E4M3
+    a, b = B.AdamW(P, state=state, seed=9), B.AdamW(Q, state=state, seed=9)
+    others = torch.arange(n, device="cuda") != at
+    fields = (B.FW_A_M, B.FW_A_V) + ((B.FW_A_M_SCALE, B.FW_A_V_SCALE) if kind == "e4m3" else ())
+    for t in range(1, 6):
+        H = G[0].clone()
+        H[at] = 0.01 if t != 2 else bad                              # the step before it and those behind: an ordinary gradient
+        if t < 2:
+            H[at] = 0
+        before = P[0].clone()
+        a.step([H], 1e-2)
+        b.step(G, 1e-2)
+        assert torch.equal(P[0][others], Q[0][others]) and bool(P[0][others].isfinite().all()), t
+        for f in fields:
+            x, y = a.state(f).view(torch.uint8), b.state(f).view(torch.uint8)
+            if f in (B.FW_A_M, B.FW_A_V):
+                x, y = (v.view(-1, 4 if kind == "f32" else 1)[:n][others] for v in (x, y))
+            assert torch.equal(x, y), (t, f)
+        if t >= 2:
+            m, v = a.state(B.FW_A_M).float()[at], a.state(B.FW_A_V).float()[at]
+            if kind == "e4m3":
+                assert bool(v.isnan()) and float(m) == 0             # the codes of a v that is not finite
+            if abs(bad) < float("inf"):
+                assert torch.equal(P[0][at], before[at]) and torch.equal(P[0][at], p0[at])
+            else:
+                assert bool(P[0][at].isnan())
+    zero = (G[0] == 0) & others
+    moved = (G[0] != 0) & others
+    assert torch.equal(P[0][zero], p0[zero]) and bool((P[0][moved] != p0[moved]).all())
+    assert a.sync_status() == B.FW_OK
