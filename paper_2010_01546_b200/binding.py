@@ -637,19 +637,29 @@ def fw_preference_loss(desc: fw_logprob_desc, preference: fw_preference_desc, lo
                                      _vector(dlogp, rows, "dlogp", dev), stream), "fw_preference_loss")
 
 
+# ---- objects that own a workspace tensor ----
+def _workspace(n: int, device, stream: int):
+    """Memory for work on `stream`: taken from the allocator, and given back, as that stream's own.  Of the current stream's memory the
+    owner before may have work pending, which would write over what this stream puts there."""
+    import torch
+    if torch.device(device).type != "cuda":
+        return torch.empty(n, dtype=torch.uint8, device=device)
+    with torch.cuda.stream(torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream()):
+        return torch.empty(n, dtype=torch.uint8, device=device)
+
+
 # ---- convenience: a layer that owns its workspace tensor -------------------
 class Layer:
     """Holds the torch workspace tensor (device memory plumbing) and the handle.
     Methods forward to the C entry points of the same name."""
 
     def __init__(self, M: int, N: int, device="cuda", stream: int = 0, **desc_overrides):
-        import torch
         self.desc = fw_layer_desc_default(M, N, **desc_overrides)
         self.M, self.N = M, N
         self.nbytes = fw_layer_workspace_bytes(self.desc)
         if self.nbytes == 0:
             raise FwError(FW_ERR_INVALID_ARG, "fw_layer_workspace_bytes")
-        self.workspace = torch.empty(self.nbytes + 256, dtype=torch.uint8, device=device)
+        self.workspace = _workspace(self.nbytes + 256, device, stream)
         base = self.workspace.data_ptr()
         self._base = (base + 255) // 256 * 256
         self.handle = fw_layer_create(self.desc, self._base, self.nbytes, stream)
@@ -708,7 +718,6 @@ class Gated:
     strides and types, and forward to the C entry points fw_gated_*.  The stream outlives the block."""
 
     def __init__(self, M: int, N: int, max_rows: int = 0, device="cuda", stream: int = 0, **desc_overrides):
-        import torch
         self.desc = fw_gated_desc()
         _lib().fw_gated_desc_default(C.byref(self.desc), M, N)
         self.desc.max_rows = max_rows
@@ -718,15 +727,13 @@ class Gated:
         if self.nbytes == 0:
             raise FwError(FW_ERR_INVALID_ARG, "fw_gated_workspace_bytes")
         dev = _here()
-        self.workspace = torch.empty(self.nbytes + 256, dtype=torch.uint8, device=device)
+        self.workspace = _workspace(self.nbytes + 256, device, stream)
         if not self.workspace.is_cuda or self.workspace.get_device() != dev:
             _refuse_device(self.workspace, dev, "workspace")
         out = C.c_void_p()
         _check(_lib().fw_gated_create(C.byref(self.desc), (self.workspace.data_ptr() + 255) // 256 * 256, self.nbytes, stream,
                                       C.byref(out)), "fw_gated_create")
         self.handle = out.value
-        # the memory is anybody's only when this stream is through with it too
-        self.workspace.record_stream(torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream())
 
     def close(self):
         if getattr(self, "handle", None):
@@ -781,7 +788,6 @@ class AdamW:
     to the C entry points fw_adamw_*.  Parameters and copies are kept; the stream outlives the object."""
 
     def __init__(self, params, copies=None, decay=None, stream: int = 0, **desc_overrides):
-        import torch
         params = list(params)
         n = len(params)
         copies = [None] * n if copies is None else list(copies)
@@ -805,13 +811,11 @@ class AdamW:
         self.nbytes = int(_lib().fw_adamw_workspace_bytes(C.byref(self.desc), sizes))
         if self.nbytes == 0:
             raise FwError(FW_ERR_INVALID_ARG, "fw_adamw_workspace_bytes")
-        self.workspace = torch.empty(self.nbytes + 256, dtype=torch.uint8, device="cuda")
+        self.workspace = _workspace(self.nbytes + 256, "cuda", stream)
         out = C.c_void_p()
         _check(_lib().fw_adamw_create(C.byref(self.desc), sizes, _vp_array(params), _vp_array(copies), (C.c_float * n)(*decay),
                                       (self.workspace.data_ptr() + 255) // 256 * 256, self.nbytes, stream, C.byref(out)), "fw_adamw_create")
         self.handle = out.value
-        # the memory is anybody's only when this stream is through with it too
-        self.workspace.record_stream(torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream())
 
     def close(self):
         if getattr(self, "handle", None):

@@ -255,3 +255,38 @@ def test_eight_bit_tokens(B, rows):
     n = h.to(F64)
     n = n * (n.square().mean(1, keepdim=True) + 1e-6).rsqrt()
     assert bool(((v - n).abs() <= 2.0 ** -4 * n.abs() * (1 + 2.0 ** -17) + 2.0 ** -10 * ys.to(F64)[:, None] + 2.0 ** -17 * n.abs()).all())
+
+
+@pytest.mark.parametrize("kind", ["layer", "gated", "adamw"])
+def test_objects_on_a_stream_beside_pending_work(B, kind):
+    """Memory that the current stream has given up while its work on it is pending: an object on another stream is not given it, so what that work
+    writes in the end is in none of its states."""
+    s = torch.cuda.Stream()
+    P = torch.randn(5000, device="cuda")
+    p0, grad = P.clone(), torch.ones(5000, device="cuda")
+
+    def make():
+        if kind == "layer":
+            return B.Layer(200, 64, stream=s.cuda_stream)
+        return B.Gated(256, 512, 64, grad=1, stream=s.cuda_stream) if kind == "gated" else B.AdamW([P], stream=s.cuda_stream)
+
+    torch.cuda.empty_cache()
+    n = make().nbytes + 256                                          # (the kernels of its beginning are loaded)
+    before = torch.empty(n, dtype=torch.uint8, device="cuda")
+    at = before.data_ptr()
+    before.fill_(0)                                                  # (as is this kernel)
+    torch.cuda.synchronize()
+    torch.cuda._sleep(200_000_000)
+    before.fill_(0x7F)
+    del before
+    x = make()
+    s.synchronize()
+    assert not torch.cuda.current_stream().query()                   # the sleep's length: else nothing was pending
+    assert not at <= x.workspace.data_ptr() < at + n
+    torch.cuda.synchronize()
+    assert x.sync_status() == B.FW_OK
+    if kind == "adamw":
+        assert int(x.state(B.FW_A_STEP)) == 0 and not bool(x.state(B.FW_A_M).any()) and not bool(x.state(B.FW_A_V).any())
+        x.step([grad], 1e-2)
+        torch.cuda.synchronize()
+        assert bool(((P - p0) + 1e-2).abs().max() < 1e-6 + 4 * 2.0 ** -24 * float(p0.abs().max()))

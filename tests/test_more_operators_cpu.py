@@ -192,3 +192,55 @@ def test_adamw_looks_at_its_tensors():
         B.AdamW([torch.zeros(8)], betas=(0.9, 0.99))
     with pytest.raises(ValueError, match="expected one for each"):
         B.AdamW([torch.zeros(8)], decay=[0.1, 0.2])
+
+
+@pytest.mark.parametrize("kind", ["layer", "gated", "adamw"])
+@pytest.mark.parametrize("stream", [0, 0x5000])
+def test_workspaces_are_of_the_stream_they_are_used_on(monkeypatch, kind, stream):
+    """The memory comes from the allocator while the object's own stream is the current one: of another stream's memory the owner before
+    may have work pending, which would write over states and addresses that this stream has put there."""
+    import contextlib
+
+    import torch
+
+    class Memory:
+        is_cuda = True
+
+        def data_ptr(self):
+            return 1 << 40
+
+        def get_device(self):
+            return -1
+
+        def record_stream(self, s):
+            pass
+
+    current, taken = ["current"], []
+
+    @contextlib.contextmanager
+    def entered(s):
+        current.append(s)
+        yield
+        current.pop()
+
+    monkeypatch.setattr(torch, "empty", lambda *a, **kw: taken.append(current[-1]) or Memory())
+    monkeypatch.setattr(torch.cuda, "stream", entered)
+    monkeypatch.setattr(torch.cuda, "ExternalStream", lambda s: s)
+    monkeypatch.setattr(torch.cuda, "default_stream", lambda: 0)
+    monkeypatch.setattr(B, "_here", lambda: -1)
+
+    class Lib:
+        def __getattr__(self, name):
+            real = getattr(B_lib, name)
+            return (lambda *a: 0) if name.endswith(("_create", "_destroy")) else real
+
+    B_lib = B._lib()
+    monkeypatch.setattr(B, "_lib", Lib)
+    if kind == "layer":
+        monkeypatch.setattr(B, "fw_layer_create", lambda *a: 0)
+        B.Layer(64, 32, stream=stream)
+    elif kind == "gated":
+        B.Gated(64, 32, stream=stream)
+    else:
+        B.AdamW([torch.zeros(8)], stream=stream)
+    assert taken == [stream]
