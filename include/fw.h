@@ -512,7 +512,7 @@ fw_status fw_logprob_backward(const fw_logprob_desc* d, const void* Z, int64_t r
  *   dlogp = weight [-(r adv where the first of the two is the smaller or equal, else 0) - kl (exp(k) - 1)]
  * and, with dZ, the gradient for the logits from the same pass over Z.  Without dZ it follows from fw_logprob_backward with
  * the stat and dlogp of this call.
- *   logp_old, adv, loss   rows;   logp_ref   rows, NULL: no KL term (kl has to be 0);   weight   rows, NULL: 1
+ *   logp_old, adv, loss   rows;   logp_ref   rows, NULL: no KL term (kl has to be 0; with kl 0 it is not read);   weight   rows, NULL: 1
  *   logp, stat, dlogp     NULL: not kept
  * A row in which no class has mass gives loss and dlogp 0.  A row of weight 0, like one whose class is outside [0, V), is not read:
  * its loss, logp, stat, dlogp and dZ are 0. */

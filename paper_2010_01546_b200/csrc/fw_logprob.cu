@@ -248,6 +248,7 @@ fw_status run(const fw_logprob_desc* d, Logprob p, int mode, cudaStream_t s, con
     for (int j = 0; j < i; ++j)
       if (overlap(out[i].p, out[i].n, out[j].p, out[j].n)) return FW_ERR_INVALID_ARG;
   }
+  if (p.kl == 0.f) p.logp_ref = nullptr;                     // the term is off: exp(k) may be infinite, and 0 times that is NaN
   p.V = d->V; p.i64 = d->index_bits == 64; p.inv_tau = 1.f / d->tau;
   ProfScope ps(FW_PROF_MISC, s);
   const cudaError_t e = d->z_dtype == FW_F32 ? launch_type<float>(p, mode, s) : launch_type<__nv_bfloat16>(p, mode, s);

@@ -445,3 +445,23 @@ def test_many_rows_and_far_offsets(B):
     assert bool(((logp.to(F64) - r.logp).abs() <= logp_bound(r)).all())
     s = -r.logp.exp()
     assert bool(((Z.to(F64) - r.grad(s)).abs() <= r.grad_bound(s, torch.full_like(s, 3e-4), 2.0 ** -8)).all())
+
+
+@pytest.mark.parametrize("V", [100, 6000])
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+def test_a_kl_term_that_is_off(B, V, kind):
+    """kl = 0 with a reference model's log-probabilities at hand (a schedule that begins at 0): the bits of the call without them, however
+    far off they are."""
+    Z, id = inputs(8, V, kind, 71)
+    Z[1, id[1]] = float("-inf")                            # the class itself is masked: logp = -inf
+    d, p = desc(B, V, kind, index_bits=64), B.fw_policy_desc_default(kl=0.0)
+    ref = torch.tensor([-1.0, -2.0, 120.0, float("inf"), float("-inf"), float("nan"), 0.0, -500.0], device="cuda")
+    old, adv, w = torch.full((8,), -3.0, device="cuda"), torch.linspace(-1, 1, 8, device="cuda"), torch.ones(8, device="cuda")
+    outs = []
+    for r in (None, ref):
+        loss, dl, dZ = torch.empty(8, device="cuda"), torch.empty(8, device="cuda"), matrix(8, V, KINDS[kind])
+        B.fw_policy_forward(d, p, Z, id, old, adv, loss, logp_ref=r, weight=w, dlogp=dl, dZ=dZ)
+        only = torch.empty(8, device="cuda")
+        B.fw_policy_forward(d, p, Z, id, old, adv, only, logp_ref=r, weight=w)
+        outs.append((loss, dl, dZ, only))
+    assert all(torch.equal(x, y) for x, y in zip(*outs)) and all(bool(x.isfinite().all()) for x in outs[1])
