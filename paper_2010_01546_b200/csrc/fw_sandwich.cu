@@ -240,12 +240,13 @@ struct SandwichBwd {
 
 __host__ __device__ constexpr int part_row(int M) { return (M + 3) / 4 * 4; }
 
-// As norm_backward_kernel: a CTA takes every gridDim-th group of rows, a row at a time (SOLO) or several, and keeps its columns' shares of
-// dw_pre and dw_post in registers.  DIRECT: dh is read where it is needed: four rows of 64 KB do not fit a SM.
+// As norm_backward_kernel, for rows element by element (VEC = 1) and for short ones, several to a CTA: a CTA takes every gridDim-th group
+// of rows, a row at a time (SOLO) or several, and keeps its columns' shares of dw_pre and dw_post in registers.  DIRECT: dh is read where it is
+// needed: four rows of 64 KB do not fit a SM.
 template <class T, int VEC, int NV, int SLOTS, bool DH, int FILL, bool SOLO>
 __global__ void __launch_bounds__(512) sandwich_backward_kernel(const SandwichBwd p) {
   typedef Ahead<T, VEC, NV, FILL> Ring;
-  constexpr bool DIRECT = DH && (VEC == 1 || NV == 8);
+  constexpr bool DIRECT = DH && VEC == 1;
   constexpr int ROOMS = DH && !DIRECT ? 4 : 3;
   extern __shared__ __align__(16) uint8_t room[];            // [slot][dy, h, o, dh], at the end the groups' sums
   __shared__ float buf[2][2][16];
@@ -320,7 +321,7 @@ __global__ void __launch_bounds__(512) sandwich_backward_kernel(const SandwichBw
       vfma<VEC>(u[k], n, f2);                                // u2 - n2 mean(u2 n2)
       vscale<VEC>(u[k], a.r2);
       if (DH) {
-        if (DIRECT) load<VEC>(dh + c, FILL == ROW_PART ? left : left > 0 ? VEC : 0, 0.f, n);
+        if (DIRECT) load<VEC>(dh + c, left, 0.f, n);
         else Ring::get(slot + 3 * row_bytes, dh, p.M, width, k, c, left, n);
         vadd<VEC>(u[k], n);
       }
@@ -695,7 +696,7 @@ int backward_ctas() { return 4 * sm_count(); }
 
 template <class T, int VEC, int NV, bool DH, int FILL, bool SOLO>
 cudaError_t backward_launch(const SandwichBwd& p, cudaStream_t s, int* ctas) {
-  constexpr int ROOMS = DH && VEC > 1 && NV < 8 ? 4 : 3;
+  constexpr int ROOMS = DH && VEC > 1 ? 4 : 3;
   constexpr int SLOTS = slots(VEC, NV, ROOMS);
   static FillCache cache;
   auto kernel = sandwich_backward_kernel<T, VEC, NV, SLOTS, DH, FILL, SOLO>;
@@ -719,23 +720,29 @@ cudaError_t backward_rows_launch(const SandwichBwd& p, cudaStream_t s, int* ctas
   if (FILL == ROW_SHIFT && e == cudaSuccess) *ctas = whole_classes(*ctas, p.classes);
   return e != cudaSuccess ? e : launch_dep(kernel, *ctas, p.width, smem, s, p);
 }
+// What backward_nv comes to, and no other shapes, are built.
 template <class T, int VEC, int NV, bool DH>
 cudaError_t backward_launch(const SandwichBwd& p, cudaStream_t s, int* ctas) {
-  if constexpr (VEC > 1 && NV <= 4)
-    if (p.classes)
-      return p.classes == 1 ? backward_rows_launch<T, VEC, NV, DH, ROW_TAIL>(p, s, ctas) : backward_rows_launch<T, VEC, NV, DH, ROW_SHIFT>(p, s, ctas);
-  if constexpr (NV <= 4) {                                   // more accesses a thread: 128 threads or more (see backward_nv)
-    if (p.width < 128)
-      return VEC > 1 && p.M % VEC == 0 ? backward_launch<T, VEC, NV, DH, (VEC > 1 ? ROW_WHOLE : ROW_PART), false>(p, s, ctas)
-                                       : backward_launch<T, VEC, NV, DH, ROW_PART, false>(p, s, ctas);
-  }
-  if constexpr (VEC > 1) {
+  if constexpr (VEC == 1) {
+    if constexpr (NV <= 4)                                   // up to 512 columns
+      if (p.width < 128) return backward_launch<T, VEC, NV, DH, ROW_PART, false>(p, s, ctas);
+    if constexpr (NV >= 4) return backward_launch<T, VEC, NV, DH, ROW_PART, true>(p, s, ctas);
+  } else {
+    if constexpr (NV <= (VEC == 8 ? 2 : 4)) {                // 6144 columns at most (see classes_of)
+      if (p.classes == 1) return backward_rows_launch<T, VEC, NV, DH, ROW_TAIL>(p, s, ctas);
+      if (p.classes) return backward_rows_launch<T, VEC, NV, DH, ROW_SHIFT>(p, s, ctas);
+    }
+    if constexpr (NV <= 2) {                                 // more accesses a thread: 128 threads or more
+      if (p.width < 128)
+        return p.M % VEC == 0 ? backward_launch<T, VEC, NV, DH, ROW_WHOLE, false>(p, s, ctas)
+                              : backward_launch<T, VEC, NV, DH, ROW_PART, false>(p, s, ctas);
+    }
     if (p.M == NV * VEC * p.width) return backward_rows_launch<T, VEC, NV, DH, ROW_FULL>(p, s, ctas);
     if (p.M % VEC == 0) return backward_rows_launch<T, VEC, NV, DH, ROW_WHOLE>(p, s, ctas);
-    return backward_rows_launch<T, VEC, NV, DH, ROW_PART>(p, s, ctas);
-  } else {
-    return backward_launch<T, VEC, NV, DH, ROW_PART, true>(p, s, ctas);
+    // rows without classes that end inside an access: up to 2 KB, of one access, or of more than 6144 columns
+    if constexpr (VEC == 8 || NV != 2) return backward_rows_launch<T, VEC, NV, DH, ROW_PART>(p, s, ctas);
   }
+  return cudaErrorInvalidConfiguration;
 }
 template <class T, int VEC, int NV>
 cudaError_t backward_launch(const SandwichBwd& p, cudaStream_t s, int* ctas) {
