@@ -203,21 +203,23 @@ cudaError_t launch(const Logprob& p, cudaStream_t s) {
   }
   // the gradient alone: long rows by large CTAs (131072 bf16 329 us, by four of 256 threads a SM 353), others by small ones (8000 fp32 43
   // against 58)
-  if (MODE == LP_BACKWARD && (int64_t)p.V * (int)sizeof(T) > 128 * 1024) return launch_ctas<T, MODE, SAME, 1024>(p, s);
+  if constexpr (MODE == LP_BACKWARD)
+    if ((int64_t)p.V * (int)sizeof(T) > 128 * 1024) return launch_ctas<T, MODE, SAME, 1024>(p, s);
   return launch_ctas<T, MODE, SAME, 256>(p, s);
 }
 template <class T, int MODE>
 cudaError_t launch_mode(const Logprob& p, cudaStream_t s) {
-  const bool same = MODE == LP_FORWARD || (((reinterpret_cast<uintptr_t>(p.Z) ^ reinterpret_cast<uintptr_t>(p.dZ)) & 15) == 0 &&
-                                           ((p.ldz - p.lddz) * (int64_t)sizeof(T)) % 16 == 0);
-  if constexpr (MODE == LP_BOTH) {
-    if (same && p.V > kWarpGroups * Group<T>::VEC) {
+  if constexpr (MODE == LP_FORWARD) {
+    return launch<T, MODE, true>(p, s);
+  } else {
+    const bool same = ((reinterpret_cast<uintptr_t>(p.Z) ^ reinterpret_cast<uintptr_t>(p.dZ)) & 15) == 0 && ((p.ldz - p.lddz) * (int64_t)sizeof(T)) % 16 == 0;
+    if (MODE == LP_BOTH && same && p.V > kWarpGroups * Group<T>::VEC) {
       bool taken = false;
       const cudaError_t e = launch_resident<T>(p, s, &taken);
       if (taken) return e;
     }
+    return same ? launch<T, MODE, true>(p, s) : launch<T, MODE, false>(p, s);
   }
-  return MODE == LP_FORWARD || same ? launch<T, MODE, true>(p, s) : launch<T, MODE, false>(p, s);
 }
 template <class T>
 cudaError_t launch_type(const Logprob& p, int mode, cudaStream_t s) {
