@@ -276,3 +276,28 @@ def test_rows_beyond_32_bits(B):
     o.copy_(a["o"])
     B.fw_sandwich_forward(d, o, a["x"], a["w2"], h, o, w_post=a["w1"])
     assert torch.equal(h, h2) and torch.equal(o, y2)
+
+
+@pytest.mark.parametrize("kind,M,pad", [("f32", 1537, 0), ("bf16", 1537, 0), ("bf16", 4095, 3), ("bf16", 4095, None), ("f32", 1537, None), ("f32", 603, 1),
+                                        ("bf16", 7001, None), ("f32", 7001, 2)])
+def test_forward_in_place(B, kind, M, pad):
+    """h and y in the place of o and x, rows by whole accesses though they begin or end inside one: the bits of the call with outputs of
+    their own."""
+    rows = 700
+    keep = inputs(rows, M, kind, 9, pad=pad)
+    d = desc(B, M, kind)
+    h, y = matrix(rows, M, KINDS[kind], pad=pad), matrix(rows, M, KINDS[kind], pad=pad)
+    B.fw_sandwich_forward(d, keep["o"], keep["x"], keep["w2"], h, y, w_post=keep["w1"], gate=keep["gate"])
+    for h_in, y_in in (("o", "x"), ("x", "o"), ("o", None), ("x", None), (None, "o"), (None, "x")):
+        a = {k: put(keep[k], KINDS[kind], pad=pad) for k in ("o", "x")}
+        out = {n: a[k] if k else matrix(rows, M, KINDS[kind], pad=pad) for n, k in (("h", h_in), ("y", y_in))}
+        B.fw_sandwich_forward(d, a["o"], a["x"], keep["w2"], out["h"], out["y"], w_post=keep["w1"], gate=keep["gate"])
+        assert torch.equal(out["h"], h) and torch.equal(out["y"], y), (h_in, y_in)
+        assert surround_kept(a["o"]) and surround_kept(a["x"]) and surround_kept(out["h"]) and surround_kept(out["y"])
+        assert all(torch.equal(a[k], keep[k]) for k in a if k not in (h_in, y_in))
+
+
+@pytest.mark.parametrize("rows,M", [(5, 6145), (310, 7001), (310, 8183)])
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+def test_e4m3_from_long_odd_rows(B, rows, M, kind):
+    test_forward(B, rows, M, kind, "e4m3")
