@@ -245,8 +245,15 @@ __device__ __forceinline__ uint32_t scale_byte(float top) {
   const int b = (int)(w >> 23) - 8 + ((w & 0x7fffffu) > 0x600000u ? 1 : 0);
   return b < 27 ? 27u : (uint32_t)b;
 }
+// The same for the root of top: 448^2 = 1.53125 2^17
+__device__ __forceinline__ uint32_t root_scale_byte(float top) {
+  const bool low = top < 0x1p-100f;                          // it may be subnormal
+  const uint32_t w = __float_as_uint(low ? top * 0x1p96f : top);
+  const int n = (int)(w >> 23) - (low ? 240 : 144) + ((w & 0x7fffffu) > 0x440000u ? 1 : 0), b = 127 + ((n + 1) >> 1);
+  return b < 27 ? 27u : (uint32_t)b;
+}
 __device__ __forceinline__ float scale_of(uint32_t b) { return __uint_as_float(b << 23); }
-__device__ __forceinline__ float inverse_scale(uint32_t b) { return __uint_as_float((254u - b) << 23); }
+__device__ __forceinline__ float inverse_square(uint32_t b) { return __uint_as_float((381u - 2u * b) << 23); }      // 64 <= b <= 190
 // Codes of e4m3 are the upper bits of fp32 numbers times 2^-120: both have their least exponent there, and what lies below it is a
 // number of smallest codes in both.
 constexpr float kDown = 0x1p-120f, kUp = 0x1p120f;
@@ -255,6 +262,17 @@ constexpr float kMost = 3.402823466e38f; // the largest finite number
 // The top bytes of four words
 __device__ __forceinline__ uint32_t top_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
   return __byte_perm(__byte_perm(a, b, 0x0073), __byte_perm(c, d, 0x0073), 0x5410);
+}
+// Relative error 2^-23, of subnormal numbers too: a v of gradients below 1e-18 is one, and eps may be less than its root
+__device__ __forceinline__ float root(float x) {
+  float r;
+  asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+__device__ __forceinline__ float root_ftz(float x) {
+  float r;
+  asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
 }
 // Four of m to codes, up where the share of the way and chance / 2^16 reach 1; down: 2^-120 over the scale; x: the elements' hashes, whose
 // lower halves are the chance
@@ -268,14 +286,14 @@ __device__ __forceinline__ uint32_t mean_codes(float (&m)[4], float down, const 
   }
   return top_bytes(w[0], w[1], w[2], w[3]);
 }
-// Four roots r >= 0 over their scale to codes, up where the share of their squares between the codes' squares passes (chance + 1/2) / 2^16,
-// chance the hashes' upper halves; what is not 0 is not held as 0
-__device__ __forceinline__ uint32_t root_codes(const float (&r)[4], float inverse, const uint32_t (&x)[4]) {
+// Four v >= 0 to the codes of their roots, up where v's share of the way between the codes' squares passes (chance + 1/2) / 2^16, chance the
+// hashes' upper halves; what is not 0 is not held as 0.  v: over the square of the scale, 448^2 at most (480^2: the NaN's code).  The share is
+// v's own: the root, which may be a step off, tells only which two codes, and beside a code either pair gives that one.
+__device__ __forceinline__ uint32_t root_codes(const float (&v)[4], const uint32_t (&x)[4]) {
   uint32_t c[4], w[4];
   float y[4], low[4], high[4], f[4], lhs[4], d[4];
 #pragma unroll
-  for (int e = 0; e < 4; ++e) y[e] = r[e];
-  vscale<4>(y, inverse);
+  for (int e = 0; e < 4; ++e) y[e] = root_ftz(v[e]);
   // from 2^-6 on, where almost all are, numbers and codes have their leading bits in common but for the exponent's origin
   const bool plain = fminf(fminf(y[0], y[1]), fminf(y[2], y[3])) >= 0x1p-6f;
 #pragma unroll
@@ -302,13 +320,13 @@ __device__ __forceinline__ uint32_t root_codes(const float (&r)[4], float invers
 #pragma unroll
   for (int e = 0; e < 4; ++e) d[e] = lhs[e];
   vfma<4>(d, high, high);                                    // high^2 - low^2, exact
-  vfma<4>(lhs, y, y);                                        // y^2 - low^2, rounded once
+  vadd<4>(lhs, v);                                           // v - low^2, rounded once
   vmul<4>(f, d);
   const uint32_t origin = plain ? 120u << 27 : 0u;           // of the exponent, four bits up
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
     w[e] = lhs[e] > f[e] ? c[e] + kStep : c[e];
-    if (!plain) w[e] = max(w[e], min(__float_as_uint(r[e]), kStep));
+    if (!plain) w[e] = max(w[e], v[e] > 0.f ? kStep : 0u);
     w[e] = (w[e] << 4) - origin;
   }
   return top_bytes(w[0], w[1], w[2], w[3]);
@@ -330,12 +348,6 @@ __device__ __forceinline__ float warp_max(float v) {
 __device__ __forceinline__ float warp_max_keep_nan(float v) {
   float r;
   asm("redux.sync.max.NaN.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
-  return r;
-}
-// Relative error 2^-23, of subnormal numbers too: a v of gradients below 1e-18 is one, and eps may be less than its root
-__device__ __forceinline__ float root(float x) {
-  float r;
-  asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
   return r;
 }
 
@@ -429,46 +441,47 @@ __device__ __forceinline__ void put_four(T* p, int n, bool whole, const float (&
 // The step of block b, four elements of a lane at a time (all eight at once took 80 registers and more)
 template <bool S8>
 __device__ __forceinline__ void update(const Args& a, const Step& st, const Bits<S8>& in, const Where& at, int64_t b, int lane, uint32_t& scale_m, uint32_t& scale_v) {
-  float m[2][4], r[2][4];
+  float m[2][4], v[2][4];
   const bool whole = at.whole();
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
-    float p[4], gr[4], v[4], q[4];
+    float p[4], gr[4], q[4];
     in.open(at.half, k, gr);
     if constexpr (S8) {
       from_e4m3(in.s.m[k], m[k]);
-      from_e4m3(in.s.v[k], v);
+      from_e4m3(in.s.v[k], v[k]);
       if ((in.s.v[k] + 0x01010101u) & 0x80808080u) {         // a NaN's code: infinity
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = fminf(v[e], INFINITY);
+        for (int e = 0; e < 4; ++e) v[k][e] = fminf(v[k][e], INFINITY);
       }
       vscale<4>(m[k], scale_of(scale_m) * st.beta1);         // a power of two: no rounding but beta1's product
       const float s = scale_of(scale_v);
       if (scale_v >= 70) {                                   // its square is in range
-        vmul<4>(v, v);
-        vscale<4>(v, s * s * st.beta2);
+        vmul<4>(v[k], v[k]);
+        vscale<4>(v[k], s * s * st.beta2);
       } else {
-        vscale<4>(v, s);
-        vmul<4>(v, v);
-        vscale<4>(v, st.beta2);
+        vscale<4>(v[k], s);
+        vmul<4>(v[k], v[k]);
+        vscale<4>(v[k], st.beta2);
       }
     } else {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) { m[k][e] = in.s.m[4 * k + e]; v[e] = in.s.v[4 * k + e]; }
+      for (int e = 0; e < 4; ++e) { m[k][e] = in.s.m[4 * k + e]; v[k][e] = in.s.v[4 * k + e]; }
       vscale<4>(m[k], st.beta1);
-      vscale<4>(v, st.beta2);
+      vscale<4>(v[k], st.beta2);
     }
 #pragma unroll
     for (int e = 0; e < 4; ++e) { p[e] = in.p[4 * k + e]; q[e] = gr[e]; }
     vfma<4>(m[k], gr, st.c1);
     vscale<4>(q, st.c2);
-    vfma<4>(v, q, q);                                        // the square of a scaled gradient: a factor's own square may be out of range
+    vfma<4>(v[k], q, q);                                     // the square of a scaled gradient: a factor's own square may be out of range
+    float r[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      r[k][e] = root(v[e]);
+      r[e] = root(v[k][e]);
       q[e] = st.eps;
     }
-    vfma<4>(q, r[k], st.inv_root);
+    vfma<4>(q, r, st.inv_root);
 #pragma unroll
     for (int e = 0; e < 4; ++e) q[e] = rcp(q[e]);
     vmul<4>(q, m[k]);
@@ -479,39 +492,33 @@ __device__ __forceinline__ void update(const Args& a, const Step& st, const Bits
     if (at.copy) put_four(at.copy + c, at.left - c, whole, p);
     if (!S8) {
       put4(static_cast<float*>(a.m) + b * kBlock + c, m[k]);
-      put4(static_cast<float*>(a.v) + b * kBlock + c, v);
+      put4(static_cast<float*>(a.v) + b * kBlock + c, v[k]);
     }
   }
   if constexpr (S8) {
-    float tm = 0.f, tr = 0.f;
+    float tm = 0.f, tv = 0.f;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       tm = fmaxf(tm, fmaxf(fabsf(m[0][e]), fabsf(m[1][e])));
-      tr = max_keep_nan(tr, max_keep_nan(r[0][e], r[1][e]));
+      tv = max_keep_nan(tv, max_keep_nan(v[0][e], v[1][e]));
     }
-    tr = warp_max_keep_nan(tr);
-    if (!(tr <= kMost)) {
+    tv = warp_max_keep_nan(tv);
+    const bool none = !(tv <= kMost);
+    if (none) {
       // An element whose v is not finite takes no part in the scales, which would hold the others' as nothing: the code of its root is the
-      // NaN's, 480 = 1.875 2^8 in the codes' numbers, that of its m, which takes no step any more, 0.
-      tm = tr = 0.f;
+      // NaN's, that of its m, which takes no step any more, 0.
+      tm = tv = 0.f;
 #pragma unroll
       for (int k = 0; k < 2; ++k)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          if (r[k][e] <= kMost) tr = fmaxf(tr, r[k][e]);
-          else m[k][e] = 0.f;
+          if (v[k][e] <= kMost) tv = fmaxf(tv, v[k][e]);
+          else { v[k][e] = INFINITY; m[k][e] = 0.f; }
           tm = fmaxf(tm, fabsf(m[k][e]));
         }
-      tr = warp_max(tr);
-      const float none = 480.f * scale_of(scale_byte(tr));
-#pragma unroll
-      for (int k = 0; k < 2; ++k)
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (!(r[k][e] <= kMost)) r[k][e] = none;
+      tv = warp_max(tv);
     }
-    uint32_t bm = scale_byte(warp_max(tm));
-    const uint32_t bv = scale_byte(tr);
+    uint32_t bm = scale_byte(warp_max(tm)), bv = root_scale_byte(tv);
     scale_m = bm;
     scale_v = bv;
     if (bm > 156) {                                          // 2^-120 over the scale is out of range
@@ -519,7 +526,18 @@ __device__ __forceinline__ void update(const Args& a, const Step& st, const Bits
       vscale<4>(m[1], 0x1p-100f);
       bm -= 100;
     }
-    const float down = __uint_as_float(bm < 134 ? (134u - bm) << 23 : 0x400000u >> (bm - 134)), inverse = inverse_scale(bv);
+    if (!none && bv - 64u < 64u) {
+      vscale<4>(v[0], inverse_square(bv));
+      vscale<4>(v[1], inverse_square(bv));
+    } else {
+      // 1 over the scale's square may be out of range; what is not 0 stays so, however far below the largest
+      const float first = bv < 64 ? 0x1p80f : 1.f, second = inverse_square(bv < 64 ? bv + 40 : bv);
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[k][e] = fminf(fmaxf(v[k][e] * first * second, fminf(v[k][e], 0x1p-100f)), 480.f * 480.f);
+    }
+    const float down = __uint_as_float(bm < 134 ? (134u - bm) << 23 : 0x400000u >> (bm - 134));
     // mix(i ^ key) of this lane's elements: its first step is the same for all but the lower 8 bits
     uint32_t first = ((uint32_t)(b * kBlock) + 4u * lane) ^ st.key;
     first ^= first >> 16;
@@ -534,7 +552,7 @@ __device__ __forceinline__ void update(const Args& a, const Step& st, const Bits
       }
       const int64_t w = b * (kBlock / 4) + 32 * k + lane;
       __stcs(static_cast<uint32_t*>(a.m) + w, mean_codes(m[k], down, hash));
-      __stcs(static_cast<uint32_t*>(a.v) + w, root_codes(r[k], inverse, hash));
+      __stcs(static_cast<uint32_t*>(a.v) + w, root_codes(v[k], hash));
     }
   }
 }

@@ -75,3 +75,34 @@ def test_turns_of_several_blocks(B, kind, turn, shift, clip):  # noqa: F811
             assert abs(float(norm) - want) <= 33 * U * want
         check_large(B, opt, P, G, copies, before, t, sizes, decay, c, 33 * U if c < 1 else 0.0)
         assert int(opt.state(B.FW_A_STEP)) == t
+
+
+@pytest.mark.parametrize("size", [1e-19, 1e-17, 1e-8, 1.0, 1e9, 1e18])
+def test_8_bit_states_of_any_size(B, size):  # noqa: F811
+    """First steps of gradients that differ by up to fourteen orders within a block, at sizes where v is subnormal, where its scale's square or the
+    inverse of it is beyond fp32, and where it is near the largest number: v within 8 u of itself and two steps of subnormal numbers."""
+    n = 20 * BLOCK - 7
+    g = torch.Generator(device="cuda")
+    g.manual_seed(17)
+    far = 10.0 ** (-14 * torch.rand(n, generator=g, device="cuda").square())
+    G = torch.randn(n, generator=g, device="cuda") * far * size
+    G[3 * BLOCK + 5] = 0
+    P = torch.zeros(n, device="cuda")
+    opt = B.AdamW([P], state=B.FW_E4M3, seed=SEED, eps=1e-36)
+    opt.step([G], LR)
+    gd = torch.nn.functional.pad(G.to(F64), (0, 7)).view(-1, BLOCK)
+    m1, v1 = (1 - BETA1) * gd, (1 - BETA2) * gd * gd
+    ev, em = 8 * U * v1 + 2.0 ** -148, 4 * U * m1.abs() + 2.0 ** -148
+    chance = mix(torch.arange(gd.numel(), device="cuda") ^ mix((SEED ^ 0x9E3779B9) & 0xFFFFFFFF)).view(-1, BLOCK)
+    for field, scales, low, high, ch, square in ((B.FW_A_V, B.FW_A_V_SCALE, (v1 - ev).clamp(min=0).sqrt(), (v1 + ev).sqrt() * (v1 > 0), chance >> 16, True),
+                                                 (B.FW_A_M, B.FW_A_M_SCALE, (m1.abs() - em).clamp(min=0), (m1.abs() + em) * (m1 != 0), chance & 0xFFFF, False)):
+        s, code = opt.state(scales).to(F64), opt.state(field).to(F64).view(-1, BLOCK).abs()
+        assert bool(((s >= scale_of(low.amax(1))) & (s <= scale_of(high.amax(1)))).all()), field
+        assert bool(((code >= choose(low, s[:, None], ch, square)) & (code <= choose(high, s[:, None], ch, square))).all()), field
+        if square:
+            held = v1 > 2.0 ** -148
+            assert bool((code[held] > 0).all()) and bool((code[gd == 0] == 0).all())      # what is not 0 is not held as 0
+    p1 = -LR * (m1 / (1 - BETA1)) / ((v1 / (1 - BETA2)).sqrt() + 1e-36)
+    err = 24 * U + 0.5 * 2.0 ** -149 / v1.clamp(min=1e-60)
+    ok = (torch.nn.functional.pad(P.to(F64), (0, 7)).view(-1, BLOCK) - p1).abs() <= err * p1.abs()
+    assert bool(ok[v1 > 2.0 ** -140].all())
