@@ -514,8 +514,8 @@ fw_status fw_logprob_backward(const fw_logprob_desc* d, const void* Z, int64_t r
  * the stat and dlogp of this call.
  *   logp_old, adv, loss   rows;   logp_ref   rows, NULL: no KL term (kl has to be 0; with kl 0 it is not read);   weight   rows, NULL: 1
  *   logp, stat, dlogp     NULL: not kept
- * A row in which no class has mass gives loss and dlogp 0.  A row of weight 0, like one whose class is outside [0, V), is not read:
- * its loss, logp, stat, dlogp and dZ are 0. */
+ * An adv of 0 gives 0 (and the KL term) however large r is.  A row in which no class has mass gives loss and dlogp 0.  A row of
+ * weight 0, like one whose class is outside [0, V), is not read: its loss, logp, stat, dlogp and dZ are 0. */
 typedef struct {
   float clip_low;       /* 0 <= clip_low < 1                                      */
   float clip_high;      /* >= 0; infinity: no bound                               */

@@ -92,7 +92,8 @@ __device__ __forceinline__ Row row_of(MaxSum o, float z, float c2, float inv_tau
 // Loss and d loss / d logp of one row
 struct Slope { float loss, dlogp; };
 __device__ __forceinline__ Slope policy_of(const Logprob& p, const Head& h, float logp) {
-  const float ratio = expf(logp - h.b), free = ratio * h.a, held = fminf(fmaxf(ratio, p.low), p.high) * h.a;
+  const float ratio = expf(logp - h.b), held = fminf(fmaxf(ratio, p.low), p.high) * h.a;
+  const float free = ratio == INFINITY && h.a == 0.f ? 0.f : ratio * h.a;      // the ratio is a number, though beyond fp32
   Slope s = {-fminf(free, held), free <= held ? -free : 0.f};
   if (ratio != ratio || free != free) s = {free + ratio, free + ratio};
   if (p.logp_ref) {

@@ -465,3 +465,21 @@ def test_a_kl_term_that_is_off(B, V, kind):
         B.fw_policy_forward(d, p, Z, id, old, adv, only, logp_ref=r, weight=w)
         outs.append((loss, dl, dZ, only))
     assert all(torch.equal(x, y) for x, y in zip(*outs)) and all(bool(x.isfinite().all()) for x in outs[1])
+
+
+@pytest.mark.parametrize("high", [0.2, float("inf")])
+def test_an_advantage_of_zero(B, high):
+    """A ratio beyond fp32 times an advantage of 0 is 0, as the ratio itself is a number; a NaN among the logits stays one."""
+    V = 50
+    Z, id = inputs(6, V, "f32", 81)
+    Z[4, 7] = float("nan")
+    old = torch.tensor([-200.0, -1e30, float("-inf"), -3.0, -200.0, -200.0], device="cuda")
+    adv = torch.tensor([0.0, 0.0, -0.0, 0.0, 0.0, 1.0], device="cuda")
+    loss, dl, dZ = torch.empty(6, device="cuda"), torch.empty(6, device="cuda"), matrix(6, V, torch.float32)
+    B.fw_policy_forward(desc(B, V, "f32", index_bits=64), B.fw_policy_desc_default(clip_high=high), Z, id, old, adv, loss, dlogp=dl, dZ=dZ)
+    assert bool((loss[:4] == 0).all()) and bool((dl[:4] == 0).all()) and bool((dZ[:4] == 0).all())
+    assert bool(loss[4].isnan()) and bool(dl[4].isnan()) and bool(dZ[4].isnan().all())
+    if high < 1:
+        assert float(loss[5]) == pytest.approx(-1.2) and float(dl[5]) == 0 and bool((dZ[5] == 0).all())
+    else:
+        assert float(loss[5]) == float("-inf") and float(dl[5]) == float("-inf")
