@@ -592,7 +592,8 @@ fw_status fw_adamw_destroy(fw_adamw* a);
  * passes fp32 by a finite gradient (1.8e19 / sqrt(1 - beta2) and more) takes no step from then on, since v stays infinite.  In 8-bit states a v
  * that is not finite is held as the NaN code, which is read as infinity, with the code 0 of m, and has no part in the scales: the other elements
  * of its block go on as if it were not there.
- * norm_out: one device fp32, the norm before clipping; with max_norm > 0, NULL: not kept.  Gradients may not overlap P, copies
+ * norm_out: one device fp32, the norm before clipping; with max_norm > 0, NULL: not kept.  (Squares are fp32: where all |G| are below 1e-19 the
+ * norm has fewer bits, below 1e-23 it is 0.)  Gradients may not overlap P, copies
  * or the workspace. */
 fw_status fw_adamw_step(fw_adamw* a, const void* const* G, const int32_t* g_dtype, float lr, const float* lr_factor,
                         float max_norm, float* norm_out);

@@ -6,7 +6,7 @@
 // Every element is read once and written once (the gradient twice with clipping): HBM bandwidth bounds it, with 8-bit
 // states their arithmetic too.  A warp takes turns of a few blocks of 256 neighbouring elements, which are what shares a scale in 8-bit states;
 // the turns of all tensors follow one another and the warps of the grid take every n-th, so that tensors of any size are one launch.
-// 371M parameters with copies and clipping 1.82 ms (5.7 TB/s), without them 1.67; 168M with 8-bit states 0.58 ms (4.6 TB/s).
+// 371M parameters with copies and clipping 1.82-1.87 ms (5.6-5.7 TB/s), without clipping 1.67-1.71; 168M with 8-bit states 0.59-0.63 ms (4.3-4.5 TB/s).
 //
 // 8-bit states.  An average that moves by 1 - beta a step stands still where it is rounded to the nearest code of three mantissa bits, so
 // codes are taken by chance: m's in proportion to its share of the way between two codes, sqrt(v)'s in proportion to v's share
@@ -97,6 +97,7 @@ __device__ double one_minus_power(double beta, int64_t n) {
   return 1.0 - r;
 }
 
+// A published integer hash of two multiplications (C. Wellons, 2018), with its constants
 __device__ __forceinline__ uint32_t mix(uint32_t x) {
   x ^= x >> 16; x *= 0x7feb352du;
   x ^= x >> 15; x *= 0x846ca68bu;

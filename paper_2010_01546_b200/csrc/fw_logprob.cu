@@ -7,8 +7,8 @@
 // The classes other than id are summed by themselves: dZ_id = dlogp / tau (sum of the others) / (sum of all), not 1 - q_id, and logp
 // = -log(1 + others / own) where a class has most of the mass.
 //
-// HBM bandwidth bounds it: a row is read once and its gradient written once.  4096 x 131072 bf16: log-probabilities 181 us (5.9 TB/s),
-// gradient from statistics 329 (6.5), loss and gradient in one pass 390 (5.5, the exponentials twice).
+// HBM bandwidth bounds it: a row is read once and its gradient written once.  4096 x 131072 bf16: log-probabilities 181-188 us (5.7-5.9 TB/s),
+// gradient from statistics 329 (6.5), loss and gradient in one pass, an eighth of the rows out, 383-417 (4.8-5.3, the exponentials twice).
 #include <cstdio>
 #include <type_traits>
 

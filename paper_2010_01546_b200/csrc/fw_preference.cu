@@ -5,7 +5,7 @@
 //   loss = w ((1 - e) log(1 + exp(-h)) + e log(1 + exp(h)))      d loss / d s_a = beta w (e - 1 / (1 + exp(h))) = -d loss / d s_b
 //
 // A CTA a pair; a few bytes a row beside the rows of logits that made them: latency bounds it (16 pairs
-// of up to 160 tokens 3.3 us).  Sums are in 64 bits in a fixed order.
+// of up to 160 tokens: 2.9 us in a row of them, 5 between the passes over the logits).  Sums are in 64 bits in a fixed order.
 #include <cstdio>
 
 #include "fw_internal.h"

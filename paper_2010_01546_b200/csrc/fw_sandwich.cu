@@ -8,7 +8,7 @@
 //
 // Both directions read each element once and write each result once: HBM bandwidth bounds them.  A row stays on chip between its two
 // sums, which depend on one another, so a CTA has the next rows on their way meanwhile, and backward forms two rows at once where they are
-// short enough.  8192 x 4096 bf16: forward 50 us (5.4 TB/s), backward 75 us (5.3 TB/s), of which 7 are the
+// short enough.  8192 x 4096 bf16: forward 49-52 us (5.2-5.5 TB/s), backward 74-79 us (5.1-5.4 TB/s), of which 7 are the
 // sum of the CTAs' shares of dw; 5003 x 1537 fp32 backward 45 us (4.1 TB/s).
 #include "fw_norm.cuh"
 
@@ -768,8 +768,10 @@ cudaError_t backward_nv(const SandwichBwd& p0, cudaStream_t s, int* ctas) {
 
 // A range of memory that a call reads or writes; ld, elem: of a matrix (0: a vector)
 struct Range { const void* p; uint64_t n; int64_t ld; int elem; };
-// Rows after which matrices that all lie equally past 16 bytes do so as at their beginning (1: aligned rows that end inside 16 bytes); 0 where they do not, where rows are so long that
-// they and the weights do not fit shared memory together, or so short that a few threads take several
+// Rows after which matrices that all lie equally past 16 bytes do so as at their beginning (1: aligned rows that end inside 16 bytes); 0 where
+// they do not, where a row is so short that a few threads take several, and beyond 6144 columns.  (At 16384 a row and its weights are more than
+// a SM holds; between, up to 8191 columns, they would fit, but nothing has been measured there this way: 4096 x 7001 bf16, aligned rows, forward 71 us and
+// backward 127 by the way that is taken, 57 and 83 for 7008 columns.)
 int classes_of(const Mat* m, int n, int M, bool aligned) {
   const bool fits = M <= 6144 && M * m[0].elem > 2048;
   if (aligned) return fits && M * m[0].elem % 16 != 0 ? 1 : 0;
